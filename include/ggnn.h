@@ -47,7 +47,7 @@
 extern "C" {
 #endif
 
-#define GGNN_ABI_VERSION 12
+#define GGNN_ABI_VERSION 13
 
 typedef enum {
   GGNN_OK = 0,
@@ -649,6 +649,92 @@ ggnn_status ggnn_super_propagate_bwd(ggnn_dtype dt, int32_t n_pad, int32_t H, in
                                      const void* rows, const void* rows_t, const void* cols_t, const void* X,
                                      const void* W, const void* da, float* dX, float* dW, float* dbias,
                                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- Tokens: node states in, dropout, node tokens out ----------------------
+ *
+ * What surrounds the propagation where nodes carry labels made of tokens of a
+ * vocabulary: the first states X_0 from a token table, dropout, and the loss of
+ * chosen nodes' tokens with its gradients (the table may serve both ends: both
+ * gradient calls add to its gradient).  Here the node counts need not be
+ * multiples of 32.  Device arrays of ids are not checked on the host; ids out
+ * of range are handled as stated and never read out of bounds.
+ *
+ * Dropout (device): Y[e] = 0 where element e is dropped, else X[e] / (1 - p).
+ * The mask is a function of (seed, offset, e) alone and is not stored: element
+ * e takes 16-bit word e % 8 of the 7-round Philox4x32 block at counter
+ * (e / 8, offset) under the key seed, and is dropped where that word is below
+ * round(p * 2^16) (at most 65535; 1 - p above means 1 - that / 2^16).  The
+ * reverse is the same call on the gradient, in the gradient's type.
+ *   count   elements, at most 2^34;  X, Y [count] dt (Y may be X; a dropped
+ *           element is 0 whatever X holds there)
+ *   p       in [0, 1); 0 copies
+ *   seed, offset   offset tells draws under one seed apart (e.g. step number) */
+ggnn_status ggnn_dropout(ggnn_dtype dt, int64_t count, const void* X, float p, uint64_t seed, uint64_t offset,
+                         void* Y, void* stream);
+
+/* Node states from a token table (device): X[i] = c_i * sum_k table[tok[k]]
+ * over the tokens of node i, then dropout by element number i * H + h (exactly
+ * ggnn_dropout's mask; p = 0: none).  Sums are float32, rounded to dt once.
+ *   tok_ptr  [n + 1] int32, non-decreasing: node i lists tok[tok_ptr[i]] ..
+ *            tok[tok_ptr[i+1] - 1] (none: a zero row).  NULL: one token per node,
+ *            node i's is tok[i]; nodes n_tok .. n - 1 have none.
+ *   tok      [n_tok] int32 token ids (n_tok <= 2^30); an id outside [0, V) adds nothing
+ *   scale, mean   c_i = scale, or scale / (length of the list) where mean is not 0
+ *   table    [V][H] dt;  X [n][H] dt (written whole; must not overlap the table) */
+ggnn_status ggnn_embed(ggnn_dtype dt, int32_t n, int32_t H, int32_t V, const void* table, const int32_t* tok_ptr,
+                       const int32_t* tok, int32_t n_tok, float scale, int32_t mean, float p, uint64_t seed,
+                       uint64_t offset, void* X, void* stream);
+
+/* Workspace bytes of ggnn_embed_bwd (0 for unsupported sizes or no tokens). */
+size_t ggnn_embed_bwd_workspace_bytes(int32_t n, int32_t H, int32_t V, int32_t n_tok);
+
+/* Reverse of ggnn_embed for the gradient dX of X (ggnn_backward's dL/dX_0):
+ *   dtable[v] += sum over the listings k of token v, of node i: c_i * keep(i, .) * dX[i]
+ * with the forward call's tokens, scale, mean, p, seed and offset.  The listings
+ * are sorted by token on the device (stable) and each token's are added in
+ * listing order over a fixed partition: same inputs, same bits.
+ *   dX [n][H] float;  dtable [V][H] float += (rows of tokens that are not listed stay as they are) */
+ggnn_status ggnn_embed_bwd(int32_t n, int32_t H, int32_t V, const int32_t* tok_ptr, const int32_t* tok,
+                           int32_t n_tok, float scale, int32_t mean, float p, uint64_t seed, uint64_t offset,
+                           const float* dX, float* dtable, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Workspace bytes of ggnn_vocab_loss (grad = 0) or ggnn_vocab_loss_grad
+ * (grad != 0); 0 for unsupported sizes or no rows. */
+size_t ggnn_vocab_workspace_bytes(ggnn_dtype dt, int32_t H, int32_t n_rows, int32_t V, int32_t grad);
+
+/* Cross entropy of chosen nodes over a vocabulary (device), without the
+ * [n_rows][V] logits in memory.  Row r is node i = node[r]:
+ *   z_v = X[i] . W[v] + bias[v];  lse[r] = log sum_v exp z_v;  loss[r] = lse[r] - z_target[r]
+ *   n_nodes  rows of X;  n_rows <= 2^24 chosen nodes;  V entries, V * H < 2^31
+ *   X [n_nodes][H] dt;  W [V][H] dt;  bias [V] float or NULL.  A bias of -1e30 or
+ *            less (-inf and the lowest float among them) takes its entry out.
+ *   node     [n_rows] int32, or NULL: row r is node r.  One outside [0, n_nodes)
+ *            counts as a zero state without a target.
+ *   target   [n_rows] int32, or NULL (no losses).  A negative one: the row has no
+ *            loss (0) and no gradient; one at or above V: loss NaN, no gradient.
+ *   loss     [n_rows] float (written; NULL allowed without targets)
+ *   lse      [n_rows] float (written; -inf where every entry is taken out, the
+ *            loss then +inf, without a gradient)
+ *   best     [n_rows] int32 (written: the entry with the largest logit, the lowest
+ *            one of equals, -1 where every entry is taken out), or NULL
+ * A NaN or +inf logit makes its row's lse and loss NaN. */
+ggnn_status ggnn_vocab_loss(ggnn_dtype dt, int32_t n_nodes, int32_t H, int32_t n_rows, int32_t V, const void* X,
+                            const void* W, const float* bias, const int32_t* node, const int32_t* target,
+                            float* loss, float* lse, int32_t* best, void* workspace, size_t workspace_bytes,
+                            void* stream);
+
+/* The same losses with the gradients of scale * sum_r weight[r] * loss[r]:
+ *   dz_v = scale * weight[r] * (exp(z_v - lse[r]) - [v = target[r]])
+ *   dX   [n_nodes][H] float (written whole: sum_v dz_v W[v] on the row of each
+ *        chosen node, zero elsewhere) -- the dL/dX_T that ggnn_backward takes.  A
+ *        node may be chosen once (otherwise its row holds one of the contributions).
+ *   dW   [V][H] float += sum_r dz_v X[node[r]];  dbias [V] float += sum_r dz_v, or NULL
+ *   weight [n_rows] float, or NULL for 1
+ * In bf16 a probability enters the two gradient products as a bf16 pair (hi + lo). */
+ggnn_status ggnn_vocab_loss_grad(ggnn_dtype dt, int32_t n_nodes, int32_t H, int32_t n_rows, int32_t V, const void* X,
+                                 const void* W, const float* bias, const int32_t* node, const int32_t* target,
+                                 const float* weight, float scale, float* loss, float* lse, float* dX, float* dW,
+                                 float* dbias, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

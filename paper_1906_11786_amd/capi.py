@@ -42,6 +42,8 @@ EXPORTS = [
     "ggnn_super_propagate_bwd", "ggnn_super_active", "ggnn_super_fusable", "ggnn_super_model_workspace_bytes",
     "ggnn_profile_start", "ggnn_profile_stop", "ggnn_profile_count", "ggnn_profile_read", "ggnn_profile_name",
     "ggnn_readout_loss_bwd_noalloc",
+    "ggnn_dropout", "ggnn_embed", "ggnn_embed_bwd_workspace_bytes", "ggnn_embed_bwd",
+    "ggnn_vocab_workspace_bytes", "ggnn_vocab_loss", "ggnn_vocab_loss_grad",
 ]
 
 
@@ -73,7 +75,7 @@ class ggnn_grads(C.Structure):
 
 
 _lib = None
-vp, i32, i64, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
+vp, i32, i64, u64, f32, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_uint64, C.c_float, C.c_size_t
 I32P = C.POINTER(C.c_int32)
 I64P = C.POINTER(C.c_int64)
 
@@ -130,6 +132,14 @@ _SIGS = {
     "ggnn_profile_read": (C.c_int, [i32, vp, vp]),
     "ggnn_profile_name": (C.c_char_p, [i32]),
     "ggnn_readout_loss_bwd_noalloc": (C.c_int, [C.c_int, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]),
+    "ggnn_dropout": (C.c_int, [C.c_int, i64, vp, f32, u64, u64, vp, vp]),
+    "ggnn_embed": (C.c_int, [C.c_int, i32, i32, i32, vp, vp, vp, i32, f32, i32, f32, u64, u64, vp, vp]),
+    "ggnn_embed_bwd_workspace_bytes": (sz, [i32, i32, i32, i32]),
+    "ggnn_embed_bwd": (C.c_int, [i32, i32, i32, vp, vp, i32, f32, i32, f32, u64, u64, vp, vp, vp, sz, vp]),
+    "ggnn_vocab_workspace_bytes": (sz, [C.c_int, i32, i32, i32, i32]),
+    "ggnn_vocab_loss": (C.c_int, [C.c_int, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
+    "ggnn_vocab_loss_grad": (C.c_int, [C.c_int, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, f32, vp, vp, vp, vp, vp,
+                                       vp, sz, vp]),
 }
 
 
@@ -184,7 +194,7 @@ def _i32(a) -> np.ndarray:
 
 # Interface version this binding is written against (GGNN_ABI_VERSION of
 # include/ggnn.h); the library must report the same number.
-ABI_VERSION = 12
+ABI_VERSION = 13
 
 
 def ggnn_abi_version() -> int:
@@ -427,6 +437,47 @@ def ggnn_sgd_momentum(count, param, velocity, grad, lr, momentum, weight_decay=0
     _check("ggnn_sgd_momentum", lib().ggnn_sgd_momentum(
         count, _ptr(param), _ptr(velocity), _ptr(grad), lr, momentum, weight_decay, 1 if nesterov else 0,
         _dt(copy_dtype), _ptr(param_copy), _stream(stream)))
+
+
+# ------------------------------------- tokens: states in, dropout, tokens out
+
+def ggnn_dropout(dt, count, X, p, seed, offset, Y, stream=None):
+    _check("ggnn_dropout", lib().ggnn_dropout(_dt(dt), count, _ptr(X), p, seed, offset, _ptr(Y), _stream(stream)))
+
+
+def ggnn_embed(dt, n, H, V, table, tok_ptr, tok, n_tok, scale, mean, p, seed, offset, X, stream=None):
+    _check("ggnn_embed", lib().ggnn_embed(
+        _dt(dt), n, H, V, _ptr(table), _ptr(tok_ptr), _ptr(tok), n_tok, scale, 1 if mean else 0, p, seed, offset,
+        _ptr(X), _stream(stream)))
+
+
+def ggnn_embed_bwd_workspace_bytes(n, H, V, n_tok) -> int:
+    return int(lib().ggnn_embed_bwd_workspace_bytes(n, H, V, n_tok))
+
+
+def ggnn_embed_bwd(n, H, V, tok_ptr, tok, n_tok, scale, mean, p, seed, offset, dX, dtable, workspace,
+                   workspace_bytes, stream=None):
+    _check("ggnn_embed_bwd", lib().ggnn_embed_bwd(
+        n, H, V, _ptr(tok_ptr), _ptr(tok), n_tok, scale, 1 if mean else 0, p, seed, offset, _ptr(dX), _ptr(dtable),
+        _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def ggnn_vocab_workspace_bytes(dt, H, n_rows, V, grad) -> int:
+    return int(lib().ggnn_vocab_workspace_bytes(_dt(dt), H, n_rows, V, 1 if grad else 0))
+
+
+def ggnn_vocab_loss(dt, n_nodes, H, n_rows, V, X, W, bias, node, target, loss, lse, best, workspace, workspace_bytes,
+                    stream=None):
+    _check("ggnn_vocab_loss", lib().ggnn_vocab_loss(
+        _dt(dt), n_nodes, H, n_rows, V, _ptr(X), _ptr(W), _ptr(bias), _ptr(node), _ptr(target), _ptr(loss),
+        _ptr(lse), _ptr(best), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def ggnn_vocab_loss_grad(dt, n_nodes, H, n_rows, V, X, W, bias, node, target, weight, scale, loss, lse, dX, dW, dbias,
+                         workspace, workspace_bytes, stream=None):
+    _check("ggnn_vocab_loss_grad", lib().ggnn_vocab_loss_grad(
+        _dt(dt), n_nodes, H, n_rows, V, _ptr(X), _ptr(W), _ptr(bias), _ptr(node), _ptr(target), _ptr(weight), scale,
+        _ptr(loss), _ptr(lse), _ptr(dX), _ptr(dW), _ptr(dbias), _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
 # ------------------------------------------------ evaluation on every edge

@@ -1,0 +1,54 @@
+// Dropout of a flat tensor (counter_rng.h): y = kept ? x / (1 - p) : 0.  The
+// reverse is the same call on the gradient.
+//
+// Bound by memory: each element is read and written once.  One lane takes
+// eight consecutive elements, 16 (bf16) or 32 (float32) bytes, one generator
+// block.
+#include "counter_rng.h"
+
+namespace ggnn {
+namespace dev {
+
+constexpr int kDropThreads = 256;
+
+template <typename S, bool DROP>
+__global__ __launch_bounds__(kDropThreads) void dropout_kernel(uint64_t count, const S* X, S* Y, Dropout d) {
+  const uint64_t b = (uint64_t)blockIdx.x * kDropThreads + threadIdx.x;
+  const uint64_t e = 8 * b;
+  if (e >= count) return;
+  float v[8];
+  if (e + 8 <= count) {
+    load8f<S>(X + e, v);
+    if constexpr (DROP) drop8(v, b, d);
+    store8f(Y + e, v);
+  } else {   // the last, incomplete block
+    const int n = (int)(count - e);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < n ? to_f<S>(X[e + i]) : 0.f;
+    if constexpr (DROP) drop8(v, b, d);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) Y[e + i] = from_f<S>(v[i]);
+  }
+}
+
+}  // namespace dev
+
+namespace GGNN_IMPL_NS {
+hipError_t launch_dropout(long count, const void* X, void* Y, const Dropout& d, hipStream_t st) {
+  using S = dev::dt_t;
+  if (count == 0) return hipSuccess;
+  const long blocks = (count + 8 * dev::kDropThreads - 1) / (8 * dev::kDropThreads);
+  if (d.cut == 0) {
+    if (X == Y) return hipSuccess;
+    hipLaunchKernelGGL((dev::dropout_kernel<S, false>), dim3((unsigned)blocks), dim3(dev::kDropThreads), 0, st,
+                       (uint64_t)count, static_cast<const S*>(X), static_cast<S*>(Y), d);
+  } else {
+    hipLaunchKernelGGL((dev::dropout_kernel<S, true>), dim3((unsigned)blocks), dim3(dev::kDropThreads), 0, st,
+                       (uint64_t)count, static_cast<const S*>(X), static_cast<S*>(Y), d);
+  }
+  return hipGetLastError();
+}
+}  // namespace GGNN_IMPL_NS
+
+}  // namespace ggnn

@@ -45,6 +45,27 @@ hipError_t launch_gru_wgrad256(int nsplit, int rows_per_split, long K, const flo
 hipError_t reduce_or_defer(const float* part, float* out, int nsplit, int count, long stride, ReduceList* defer,
                            hipStream_t st);
 
+// Dropout by element number (csrc/counter_rng.h): element e is dropped where its
+// 16-bit word is below `cut`, else multiplied by `scale`; cut = 0: none.
+struct Dropout {
+  uint32_t seed_lo, seed_hi, offset_lo, offset_hi, cut;
+  float scale;
+};
+
+// Arguments of the vocabulary loss (csrc/vocab.hip), as in include/ggnn.h.
+struct VocabArgs {
+  int n_nodes, R, V;
+  const void *X, *W;
+  const float* bias;
+  const int32_t *node, *target;
+  const float* weight;
+  float scale;
+  float *loss, *lse;
+  int32_t* best;
+  float *dX, *dW, *dbias;
+  void* ws;
+};
+
 // Supernode share of a fused bit-band step (the first 32 nodes are
 // supernodes): the slice bits of the step's direction, [E][n_pad][s/8] (the
 // column slice forward, the transposed row slice reverse), and the record
@@ -95,6 +116,11 @@ struct SnStep {
   hipError_t launch_super_bwd(int n_pad, int H, int E, int s, const void* rows, const void* rows_t,              \
                               const void* cols_t, const void* X, const void* W, const void* da, float* dX,       \
                               float* dW, float* dbias, void* ws, hipStream_t st);                                \
+  hipError_t launch_dropout(long count, const void* X, void* Y, const Dropout& d, hipStream_t st);                \
+  hipError_t launch_embed(int n, int H, int V, const void* table, const int32_t* tok_ptr, const int32_t* tok,     \
+                          int n_tok, float scale, int mean, const Dropout& d, void* X, hipStream_t st);           \
+  size_t vocab_workspace(int H, int R, int V, bool grad);                                                         \
+  hipError_t launch_vocab(int H, const VocabArgs& c, bool grad, hipStream_t st);                                  \
   bool step_wide_applies(int B, int H);                                                                           \
   hipError_t launch_step_wide(bool rev, int n_pad, int B, int H, int E, const void* bits, const void* V,          \
                               const void* Wsrc, const float* bias, float* out, const float* dX_in, void* dM,      \
@@ -406,6 +432,28 @@ inline hipError_t launch_super_bwd(int dt, int n_pad, int H, int E, int s, const
 // Momentum update of float32 master parameters (and their compute copy).
 hipError_t launch_sgd_momentum(long count, float* theta, float* vel, const float* grad, float lr, float mu, float wd,
                                int nesterov, int copy_dt, void* copy, hipStream_t st);
+
+// Dropout of a flat tensor, node states from a token table, and the cross
+// entropy over a vocabulary (grad: with its gradients) with its workspace.
+inline hipError_t launch_dropout(int dt, long count, const void* X, void* Y, const Dropout& d, hipStream_t st) {
+  return GGNN_DT_PICK(launch_dropout, count, X, Y, d, st);
+}
+inline hipError_t launch_embed(int dt, int n, int H, int V, const void* table, const int32_t* tok_ptr,
+                               const int32_t* tok, int n_tok, float scale, int mean, const Dropout& d, void* X,
+                               hipStream_t st) {
+  return GGNN_DT_PICK(launch_embed, n, H, V, table, tok_ptr, tok, n_tok, scale, mean, d, X, st);
+}
+inline size_t vocab_workspace(int dt, int H, int R, int V, bool grad) {
+  return GGNN_DT_PICK(vocab_workspace, H, R, V, grad);
+}
+inline hipError_t launch_vocab(int dt, int H, const VocabArgs& c, bool grad, hipStream_t st) {
+  return GGNN_DT_PICK(launch_vocab, H, c, grad, st);
+}
+// The table's gradient (float32 whatever the table's type), dtable +=; workspace
+// of embed_bwd_workspace bytes.
+size_t embed_bwd_workspace(int H, int n_tok);
+hipError_t launch_embed_bwd(int n, int H, int V, const int32_t* tok_ptr, const int32_t* tok, int n_tok, float scale,
+                            int mean, const Dropout& d, const float* dX, float* dtable, void* ws, hipStream_t st);
 
 #undef GGNN_DT_PICK
 

@@ -1,0 +1,650 @@
+// Cross entropy of chosen nodes over a vocabulary, and its gradients, without
+// the logits in memory.
+//
+//   z_iv = x_i . w_v + b_v;  lse_i = log sum_v exp z_iv;  loss_i = lse_i - z_it
+//   dz_iv = g_i (exp(z_iv - lse_i) - [v = t_i])
+//   dX_i = sum_v dz_iv w_v;  dW_v += sum_i dz_iv x_i;  db_v += sum_i dz_iv
+//
+// Rows pass: a workgroup holds 128 rows of X as matrix-core fragments and
+// walks a share of the vocabulary in tiles staged in LDS.  Logits are formed
+// transposed (S^T = W X^T), so that a lane holds one row's logits: running
+// maximum, sum and the weighted sum of vocabulary rows O_i = sum_v p_iv w_v
+// need no exchange between lanes, and the probabilities are already in the
+// fragment order of the second product.  The shares (m, l, O) of the
+// vocabulary's splits are joined per row, which gives loss, lse and dX.
+// Columns pass: the same with the roles of X and W exchanged, p from the known
+// lse, which gives dW and db.  Logits are formed twice, 2 RVH operations each,
+// and the two other products cost 2 RVH each (4 in bf16, see below).
+//
+// Precision: dX and dW are float32, so in bf16 a probability enters the
+// products as a bf16 pair (hi + lo, 16 bits); one bf16 would put the rounding
+// of every probability, 2^-9, into both gradients.  Logits, maxima, sums and
+// accumulators are float32.
+#include "device_common.h"
+#include "kernels.h"
+#include "lds_dma.h"
+
+namespace ggnn {
+namespace dev {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int kVocThreads = 256, kVocWaves = 4;
+constexpr int kVocRows = 128;              // rows (or vocabulary entries) of a workgroup, 32 per wave
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kMaskedBias = -1e30f;      // a bias at or below takes its entry out
+constexpr float kNoMax = -3e38f;           // running maximum before the first logit
+
+// Entries of an LDS tile: 64 in bf16, 32 in float32 (twice the bytes).
+template <typename S> constexpr int voc_tile() { return sizeof(S) == 2 ? 64 : 32; }
+
+__device__ __forceinline__ void mma32(f32x16& acc, const bf16x8& a, const bf16x8& b) {
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, acc, 0, 0, 0);
+}
+__device__ __forceinline__ void mma32(f32x16& acc, const f32x8& a, const f32x8& b) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], acc, 0, 0, 0);
+}
+
+// LDS tile of rows of H elements in 16-byte pieces; piece c of row r lies at
+// place c ^ swz(r) of its row.  Sixteen rows read at one piece (fragments along
+// H) and four rows times four pieces (fragments across rows) then both fall on
+// different banks, without padding, so that the copies into LDS stay linear.
+template <typename S, int H>
+__device__ __forceinline__ int swz(int r) {
+  constexpr int CPR = H * (int)sizeof(S) / 16;
+  if constexpr (CPR >= 16) return ((r & 3) << 2) | ((r >> 2) & 3);
+  if constexpr (CPR == 8) return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+  return (r >> 2) & 3;
+}
+
+// Copies tile rows row0 .. row0 + T - 1 (the last one's where beyond) to LDS.
+template <typename S, int H>
+__device__ __forceinline__ void stage_tile(const S* __restrict__ src, long row0, long last, uint32_t lds, int wave,
+                                           int lane) {
+  constexpr int CPR = H * (int)sizeof(S) / 16;
+  constexpr int PIECES = voc_tile<S>() * CPR / 64;   // 1 KB copies
+#pragma unroll
+  for (int p = 0; p < PIECES / kVocWaves; ++p) {
+    const int piece = p * kVocWaves + wave, q = piece * 64 + lane;
+    const int r = q / CPR, c = (q % CPR) ^ swz<S, H>(r);
+    const long row = row0 + r < last ? row0 + r : last;
+    dma16(reinterpret_cast<const char*>(src + row * H) + 16 * c,
+          __builtin_amdgcn_readfirstlane(lds + (uint32_t)piece * 1024u));
+  }
+}
+
+// Fragment along H: row r0 + lane % 32, elements 16 kk + 8 (lane / 32) .. + 7.
+template <typename S, int H>
+__device__ __forceinline__ frag_t<S> row_frag(const S* tile, int r0, int kk, int lane) {
+  constexpr int CPR = H * (int)sizeof(S) / 16;
+  const int r = r0 + lane % 32, g = lane / 32;
+  if constexpr (sizeof(S) == 2) {
+    return load8(tile + ((size_t)r * CPR + ((2 * kk + g) ^ swz<S, H>(r))) * 8);
+  } else {
+    const int c = 4 * kk + 2 * g, s = swz<S, H>(r);
+    return load4x2(tile + (r * CPR + (c ^ s)) * 4, tile + (r * CPR + ((c + 1) ^ s)) * 4);
+  }
+}
+
+// Fragment across rows: column 32 ht + lane % 32, rows r0 + {0, 8} + 4 (lane / 32) + 0 .. 3
+// (the order in which a lane holds the accumulators of a 32 x 32 tile).
+template <int H>
+__device__ __forceinline__ bf16x8 col_frag(const bf16s* tile, int r0, int ht, int lane) {
+  constexpr int CPR = H * 2 / 16;
+  const int p = lane % 16, g = lane / 32;
+  const int c = 4 * ht + 2 * ((lane / 16) & 1) + (p % 4) / 2;
+  typedef short v8i16 __attribute__((ext_vector_type(8)));
+  tr_v4i16 t[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int r = r0 + 8 * i + 4 * g + p / 4;
+    bf16s* a = const_cast<bf16s*>(tile) + (r * CPR + (c ^ swz<bf16s, H>(r))) * 8 + 4 * (p % 2);
+    t[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr_v4i16*)(a));
+  }
+  const v8i16 v = __builtin_shufflevector(t[0], t[1], 0, 1, 2, 3, 4, 5, 6, 7);
+  return __builtin_bit_cast(bf16x8, v);
+}
+template <int H>
+__device__ __forceinline__ f32x8 col_frag(const float* tile, int r0, int ht, int lane) {
+  constexpr int CPR = H * 4 / 16;
+  const int q = lane % 32, g = lane / 32;
+  f32x8 v;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int r = r0 + (e / 4) * 8 + 4 * g + e % 4;
+    v[e] = tile[(r * CPR + ((8 * ht + q / 4) ^ swz<float, H>(r))) * 4 + q % 4];
+  }
+  return v;
+}
+
+// acc[ht] += (rows r0 .. r0 + 31 of the tile)^T p for the 32 values p of a tile
+// (lane's column, rows in accumulator order).
+template <int H>
+__device__ __forceinline__ void add_product(f32x16 (&acc)[H / 32], const float (&p)[16], const bf16s* tile, int r0,
+                                            int lane) {
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks) {
+    bf16x8 hi, lo;
+    split8(p + 8 * ks, hi, lo);
+#pragma unroll
+    for (int ht = 0; ht < H / 32; ++ht) {
+      const bf16x8 a = col_frag<H>(tile, r0 + 16 * ks, ht, lane);
+      mma32(acc[ht], a, hi);
+      mma32(acc[ht], a, lo);
+    }
+  }
+}
+template <int H>
+__device__ __forceinline__ void add_product(f32x16 (&acc)[H / 32], const float (&p)[16], const float* tile, int r0,
+                                            int lane) {
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks) {
+    const f32x8 b = pack8<float>(p + 8 * ks);
+#pragma unroll
+    for (int ht = 0; ht < H / 32; ++ht) mma32(acc[ht], col_frag<H>(tile, r0 + 16 * ks, ht, lane), b);
+  }
+}
+
+__device__ __forceinline__ float entry_bias(const float* bias, int v, int V) {
+  if (v >= V) return -INFINITY;
+  const float b = bias != nullptr ? bias[v] : 0.f;
+  return b <= kMaskedBias ? -INFINITY : b;
+}
+
+// Accumulator start values: a[8 (j / 4) + 4 (lane / 32) + j % 4] of 32 floats in LDS.
+__device__ __forceinline__ void start32(f32x16& acc, const float* a, int lane) {
+#pragma unroll
+  for (int j4 = 0; j4 < 4; ++j4) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(a + 8 * j4 + 4 * (lane / 32));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[4 * j4 + i] = v[i];
+  }
+}
+
+// One 32 x 32 tile of S^T: logits of the wave's rows (lane's row = lane % 32).
+template <typename S, int H>
+__device__ __forceinline__ void tile_logits(f32x16& acc, const frag_t<S> (&xf)[H / 16], const S* tile, int r0,
+                                            int lane) {
+#pragma unroll
+  for (int kk = 0; kk < H / 16; ++kk) mma32(acc, row_frag<S, H>(tile, r0, kk, lane), xf[kk]);
+}
+
+struct RowBest {   // largest logit so far and the lowest entry that has it
+  float z;
+  int v;
+};
+__device__ __forceinline__ void take_best(RowBest& b, float z, int v) {
+  if (z > b.z || (z == b.z && v < b.v)) b = RowBest{z, v};
+}
+
+// The row a lane stands for: its node, or -1 (beyond R, or outside the graph).
+__device__ __forceinline__ int row_node(const int32_t* __restrict__ node, int r, int R, int n_nodes) {
+  if (r >= R) return -1;
+  const int i = node != nullptr ? node[r] : r;
+  return (unsigned)i < (unsigned)n_nodes ? i : -1;
+}
+template <typename S, int H>
+__device__ __forceinline__ void load_row_frags(frag_t<S> (&f)[H / 16], const S* __restrict__ X, long row, int lane) {
+#pragma unroll
+  for (int kk = 0; kk < H / 16; ++kk) {
+    if (row >= 0) f[kk] = load8(X + row * H + 16 * kk + 8 * (lane / 32));
+    else f[kk] = frag_t<S>{};
+  }
+}
+
+// Rows pass.  Workgroup: row tile blockIdx.x % row_tiles, vocabulary tiles
+// split * per .. + per - 1.  Writes each row's (m in units of log 2, l, O) of
+// its split; SUM: O too; BEST: the largest logit's entry too.
+template <typename S, int H, bool SUM, bool BEST>
+__global__ __launch_bounds__(kVocThreads) void vocab_rows_kernel(int n_nodes, int R, int V, int row_tiles, int per,
+                                                                 const S* __restrict__ X, const S* __restrict__ W,
+                                                                 const float* __restrict__ bias,
+                                                                 const int32_t* __restrict__ node,
+                                                                 float* __restrict__ pm, float* __restrict__ pl,
+                                                                 float* __restrict__ po, RowBest* __restrict__ pb) {
+  constexpr int T = voc_tile<S>();
+  __shared__ __attribute__((aligned(1024))) S tile[2][T * H];
+  __shared__ __attribute__((aligned(16))) float tb[2][T];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = lane / 32;
+  const int id = xcd_swizzle(blockIdx.x, gridDim.x), rt = id % row_tiles, split = id / row_tiles;
+  const int Rp = row_tiles * kVocRows;
+  const int r = rt * kVocRows + wave * 32 + lane % 32;
+  const int tiles = (V + T - 1) / T, t0 = split * per, t1 = min(tiles, t0 + per);
+  const uint32_t lds[2] = {(uint32_t)(uintptr_t)tile[0], (uint32_t)(uintptr_t)tile[1]};
+
+  frag_t<S> xf[H / 16];
+  load_row_frags<S, H>(xf, X, row_node(node, r, R, n_nodes), lane);
+  f32x16 o[H / 32];
+  if constexpr (SUM) {
+#pragma unroll
+    for (int ht = 0; ht < H / 32; ++ht) o[ht] = f32x16{};
+  }
+  float m = kNoMax, l = 0.f;
+  RowBest best{-INFINITY, INT_MAX};
+  float nb = 0.f;
+  if (t0 < t1) {
+    stage_tile<S, H>(W, (long)t0 * T, V - 1, lds[0], wave, lane);
+    if (threadIdx.x < T) nb = entry_bias(bias, t0 * T + threadIdx.x, V);
+  }
+  for (int t = t0; t < t1; ++t) {
+    const int buf = (t - t0) & 1, v0 = t * T;
+    if (threadIdx.x < T) tb[buf][threadIdx.x] = nb;
+    wait_copies<0>();
+    __syncthreads();   // this tile has landed, and every wave has left the other buffer
+    if (t + 1 < t1) {
+      stage_tile<S, H>(W, (long)v0 + T, V - 1, lds[buf ^ 1], wave, lane);
+      if (threadIdx.x < T) nb = entry_bias(bias, v0 + T + threadIdx.x, V);
+    }
+    const bool plain = bias == nullptr && v0 + T <= V;
+#pragma unroll
+    for (int r0 = 0; r0 < T; r0 += 32) {
+      f32x16 s = {};
+      if (!plain) start32(s, tb[buf] + r0, lane);
+      tile_logits<S, H>(s, xf, tile[buf], r0, lane);
+      float top = s[0];
+#pragma unroll
+      for (int j = 1; j < 16; ++j) top = fmaxf(top, s[j]);
+      top *= kLog2e;
+      // The maximum follows only where it would grow by more than 2^8: until
+      // then the terms stay below 2^8 and the sums lose nothing.
+      if (__ballot(top > m + 8.f)) {
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+        const float mn = fmaxf(m, fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])));
+        const float f = __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        l *= f;
+        if constexpr (SUM) {
+#pragma unroll
+          for (int ht = 0; ht < H / 32; ++ht)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) o[ht][j] *= f;
+        }
+      }
+      float p[16];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        if constexpr (BEST) {
+          if (s[j] > best.z) best = RowBest{s[j], v0 + r0 + 8 * (j / 4) + 4 * g + j % 4};
+        }
+        p[j] = __builtin_amdgcn_exp2f(fmaf(s[j], kLog2e, -m));
+        l += p[j];
+      }
+      if constexpr (SUM) add_product<H>(o, p, tile[buf], r0, lane);
+    }
+  }
+  l += __shfl_xor(l, 32);
+  const size_t at = (size_t)split * Rp + r;
+  if constexpr (BEST) {
+    take_best(best, __shfl_xor(best.z, 32), __shfl_xor(best.v, 32));
+    if (g == 0) pb[at] = best;
+  }
+  if (g == 0) {
+    pm[at] = m;
+    pl[at] = l;
+  }
+  if constexpr (SUM) {
+#pragma unroll
+    for (int ht = 0; ht < H / 32; ++ht)
+#pragma unroll
+      for (int j4 = 0; j4 < 4; ++j4)
+        *reinterpret_cast<f32x4*>(po + at * H + 32 * ht + 8 * j4 + 4 * g) =
+            f32x4{o[ht][4 * j4], o[ht][4 * j4 + 1], o[ht][4 * j4 + 2], o[ht][4 * j4 + 3]};
+  }
+}
+
+// Rows pass for at most 32 rows (loss only): every wave holds the same rows
+// and takes `per` tiles of 32 entries, read straight from memory, since no
+// other wave needs them.
+template <typename S, int H, bool BEST>
+__global__ __launch_bounds__(kVocThreads) void vocab_few_kernel(int n_nodes, int R, int V, int per,
+                                                                const S* __restrict__ X, const S* __restrict__ W,
+                                                                const float* __restrict__ bias,
+                                                                const int32_t* __restrict__ node,
+                                                                float* __restrict__ pm, float* __restrict__ pl,
+                                                                RowBest* __restrict__ pb) {
+  const int lane = threadIdx.x % kWave, g = lane / 32, r = lane % 32;
+  const int split = blockIdx.x * kVocWaves + threadIdx.x / kWave;
+  const int tiles = (V + 31) / 32, t0 = split * per, t1 = min(tiles, t0 + per);
+  frag_t<S> xf[H / 16];
+  load_row_frags<S, H>(xf, X, row_node(node, r, R, n_nodes), lane);
+  float m = kNoMax, l = 0.f;
+  RowBest best{-INFINITY, INT_MAX};
+  for (int t = t0; t < t1; ++t) {
+    frag_t<S> wf[H / 16];
+    load_row_frags<S, H>(wf, W, min(t * 32 + r, V - 1), lane);
+    f32x16 s;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) s[j] = entry_bias(bias, t * 32 + 8 * (j / 4) + 4 * g + j % 4, V);
+#pragma unroll
+    for (int kk = 0; kk < H / 16; ++kk) mma32(s, wf[kk], xf[kk]);
+    float top = s[0];
+#pragma unroll
+    for (int j = 1; j < 16; ++j) top = fmaxf(top, s[j]);
+    const float mn = fmaxf(m, top * kLog2e);
+    l *= __builtin_amdgcn_exp2f(m - mn);
+    m = mn;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      if constexpr (BEST) {
+        if (s[j] > best.z) best = RowBest{s[j], t * 32 + 8 * (j / 4) + 4 * g + j % 4};
+      }
+      l += __builtin_amdgcn_exp2f(fmaf(s[j], kLog2e, -m));
+    }
+  }
+  const float m2 = __shfl_xor(m, 32), l2 = __shfl_xor(l, 32), mn = fmaxf(m, m2);
+  l = l * __builtin_amdgcn_exp2f(m - mn) + l2 * __builtin_amdgcn_exp2f(m2 - mn);
+  const size_t at = (size_t)split * 32 + r;
+  if constexpr (BEST) {
+    take_best(best, __shfl_xor(best.z, 32), __shfl_xor(best.v, 32));
+    if (g == 0) pb[at] = best;
+  }
+  if (g == 0) {
+    pm[at] = mn;
+    pl[at] = l;
+  }
+}
+
+// Joins the splits' shares of a row: H / 4 lanes per row, four features each.
+// GRAD: writes dX's row, and what the columns pass reads: the row's state
+// (zero rows up to Rp), its lse (infinite for rows without a gradient, whose
+// probabilities then vanish), target (-1) and factor.
+template <typename S, int H, bool GRAD, bool BEST>
+__global__ __launch_bounds__(kVocThreads) void vocab_join_kernel(
+    int n_nodes, int R, int V, int Rp, int splits, const S* __restrict__ X, const S* __restrict__ W,
+    const float* __restrict__ bias, const int32_t* __restrict__ node, const int32_t* __restrict__ target,
+    const float* __restrict__ weight, float scale, const float* __restrict__ pm, const float* __restrict__ pl,
+    const float* __restrict__ po, const RowBest* __restrict__ pb, float* __restrict__ loss, float* __restrict__ lse,
+    int32_t* __restrict__ best, float* __restrict__ dX, S* __restrict__ xg, float* __restrict__ lse_w,
+    int32_t* __restrict__ tgt_w, float* __restrict__ fac_w) {
+  constexpr int L = H / 4;
+  const int r = (int)(((long)blockIdx.x * kVocThreads + threadIdx.x) / L);
+  const int q = threadIdx.x % L, h = 4 * q;
+  if (r >= (GRAD ? Rp : R)) return;   // whole groups of L lanes leave together
+  const int n = row_node(node, r, R, n_nodes);
+  const f32x4 x = n >= 0 ? load4f(X + (size_t)n * H + h) : f32x4{};
+  float M = kNoMax, sum = 0.f;
+  if (r < R) {
+    for (int s = q; s < splits; s += L) M = fmaxf(M, pm[(size_t)s * Rp + r]);
+#pragma unroll
+    for (int o = L / 2; o >= 1; o /= 2) M = fmaxf(M, __shfl_xor(M, o));
+    for (int s = q; s < splits; s += L)
+      sum += pl[(size_t)s * Rp + r] * __builtin_amdgcn_exp2f(pm[(size_t)s * Rp + r] - M);
+#pragma unroll
+    for (int o = L / 2; o >= 1; o /= 2) sum += __shfl_xor(sum, o);
+  }
+  int t = r < R && n >= 0 && target != nullptr ? target[r] : -1;
+  const bool bad = t >= V;
+  if (bad) t = -1;
+  f32x4 w = {};
+  float zt = 0.f;
+  if (t >= 0) {
+    w = load4f(W + (size_t)t * H + h);
+    zt = x[0] * w[0] + x[1] * w[1] + x[2] * w[2] + x[3] * w[3];
+  }
+#pragma unroll
+  for (int o = L / 2; o >= 1; o /= 2) zt += __shfl_xor(zt, o);
+  const float row_lse = sum == 0.f ? -INFINITY : (M + __log2f(sum)) * kLn2;   // every entry masked: -inf
+  if (r < R && q == 0) {
+    lse[r] = row_lse;
+    if (loss != nullptr) {
+      float v = 0.f;
+      if (t >= 0) v = sum == 0.f ? INFINITY : row_lse - (zt + entry_bias(bias, t, V));
+      loss[r] = bad ? NAN : v;
+    }
+  }
+  if constexpr (BEST) {
+    RowBest b{-INFINITY, INT_MAX};
+    for (int s = q; s < splits; s += L) take_best(b, pb[(size_t)s * Rp + r].z, pb[(size_t)s * Rp + r].v);
+#pragma unroll
+    for (int o = L / 2; o >= 1; o /= 2) take_best(b, __shfl_xor(b.z, o), __shfl_xor(b.v, o));
+    if (q == 0) best[r] = b.v == INT_MAX ? -1 : b.v;
+  }
+  if constexpr (GRAD) {
+    const float f = (weight != nullptr && r < R ? weight[r] : 1.f) * scale;
+    const bool live = t >= 0 && sum != 0.f;
+    store4(xg + (size_t)r * H + h, x[0], x[1], x[2], x[3]);
+    if (q == 0) {
+      lse_w[r] = live ? row_lse : INFINITY;
+      tgt_w[r] = live ? t : -1;
+      fac_w[r] = f;
+    }
+    if (live) {
+      f32x4 o = {};
+      for (int s = 0; s < splits; ++s) {
+        const size_t at = (size_t)s * Rp + r;
+        o += *reinterpret_cast<const f32x4*>(po + at * H + h) * __builtin_amdgcn_exp2f(pm[at] - M);
+      }
+      *reinterpret_cast<f32x4*>(dX + (size_t)n * H + h) = (o * (1.f / sum) - w) * f;
+    }
+  }
+}
+
+// Columns pass.  Workgroup: entries tile blockIdx.x % col_tiles (128 entries,
+// 32 per wave), row tiles split * per .. + per - 1 of the gathered states.
+// Writes its split's share of dW [V][H] and db [V] (db NULL: none).
+template <typename S, int H>
+__global__ __launch_bounds__(kVocThreads) void vocab_cols_kernel(int V, int Rp, int col_tiles, int per,
+                                                                 const S* __restrict__ xg,
+                                                                 const S* __restrict__ W,
+                                                                 const float* __restrict__ bias,
+                                                                 const float* __restrict__ lse_w,
+                                                                 const int32_t* __restrict__ tgt_w,
+                                                                 const float* __restrict__ fac_w,
+                                                                 float* __restrict__ pw, float* __restrict__ pdb) {
+  constexpr int T = voc_tile<S>();
+  __shared__ __attribute__((aligned(1024))) S tile[2][T * H];
+  __shared__ __attribute__((aligned(16))) float tl[2][T], tf[2][T];
+  __shared__ __attribute__((aligned(16))) int tt[2][T];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = lane / 32;
+  const int id = xcd_swizzle(blockIdx.x, gridDim.x), ct = id % col_tiles, split = id / col_tiles;
+  const int vw = ct * kVocRows + wave * 32, v = vw + lane % 32;
+  const int tiles = Rp / T, t0 = split * per, t1 = min(tiles, t0 + per);
+  const uint32_t lds[2] = {(uint32_t)(uintptr_t)tile[0], (uint32_t)(uintptr_t)tile[1]};
+
+  frag_t<S> wf[H / 16];
+  load_row_frags<S, H>(wf, W, min(v, V - 1), lane);
+  const float b2 = entry_bias(bias, v, V) * kLog2e;
+  f32x16 a[H / 32];
+#pragma unroll
+  for (int ht = 0; ht < H / 32; ++ht) a[ht] = f32x16{};
+  float db = 0.f, nl = 0.f, nf = 0.f;
+  int nt = -1;
+  if (t0 < t1) {
+    stage_tile<S, H>(xg, (long)t0 * T, Rp - 1, lds[0], wave, lane);
+    if (threadIdx.x < T) {
+      nl = lse_w[t0 * T + threadIdx.x];
+      nt = tgt_w[t0 * T + threadIdx.x];
+      nf = fac_w[t0 * T + threadIdx.x];
+    }
+  }
+  for (int t = t0; t < t1; ++t) {
+    const int buf = (t - t0) & 1;
+    if (threadIdx.x < T) {
+      tl[buf][threadIdx.x] = -nl;
+      tt[buf][threadIdx.x] = nt;
+      tf[buf][threadIdx.x] = nf;
+    }
+    wait_copies<0>();
+    __syncthreads();   // this tile has landed, and every wave has left the other buffer
+    if (t + 1 < t1) {
+      stage_tile<S, H>(xg, (long)(t + 1) * T, Rp - 1, lds[buf ^ 1], wave, lane);
+      if (threadIdx.x < T) {
+        nl = lse_w[(t + 1) * T + threadIdx.x];
+        nt = tgt_w[(t + 1) * T + threadIdx.x];
+        nf = fac_w[(t + 1) * T + threadIdx.x];
+      }
+    }
+#pragma unroll
+    for (int r0 = 0; r0 < T; r0 += 32) {
+      f32x16 s;
+      start32(s, tl[buf] + r0, lane);
+      tile_logits<S, H>(s, wf, tile[buf], r0, lane);
+      float p[16];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(s[j], kLog2e, b2));
+      // the rows' targets, where any falls on this wave's entries
+      if (__ballot((unsigned)(tt[buf][r0 + lane % 32] - vw) < 32u)) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          if (tt[buf][r0 + 8 * (j / 4) + 4 * g + j % 4] == v) p[j] -= 1.f;
+      }
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        p[j] *= tf[buf][r0 + 8 * (j / 4) + 4 * g + j % 4];
+        db += p[j];
+      }
+      add_product<H>(a, p, tile[buf], r0, lane);
+    }
+  }
+  db += __shfl_xor(db, 32);
+  if (v < V) {
+    if (pdb != nullptr && g == 0) pdb[(size_t)split * V + v] = db;
+    float* out = pw + ((size_t)split * V + v) * H;
+#pragma unroll
+    for (int ht = 0; ht < H / 32; ++ht)
+#pragma unroll
+      for (int j4 = 0; j4 < 4; ++j4)
+        *reinterpret_cast<f32x4*>(out + 32 * ht + 8 * j4 + 4 * g) =
+            f32x4{a[ht][4 * j4], a[ht][4 * j4 + 1], a[ht][4 * j4 + 2], a[ht][4 * j4 + 3]};
+  }
+}
+
+}  // namespace dev
+
+namespace {
+inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+inline int cdiv(long a, long b) { return (int)((a + b - 1) / b); }
+
+// How a call is cut, and where its shares lie in the workspace.
+struct VocabPlan {
+  bool few;
+  int row_tiles, Rp, splits, per;           // rows pass
+  int col_tiles, csplits, cper;             // columns pass
+  size_t pm, pl, pb, po, xg, lse, tgt, fac, pw, pdb, bytes;
+};
+template <typename S>
+VocabPlan vocab_plan(int H, int R, int V, bool grad) {
+  constexpr int T = dev::voc_tile<S>();
+  VocabPlan p{};
+  p.few = !grad && R <= 32;
+  if (p.few) {
+    const int tiles = cdiv(V, 32);
+    p.row_tiles = 1;
+    p.Rp = 32;
+    p.per = cdiv(tiles, 1024);
+    p.splits = cdiv(cdiv(tiles, p.per), dev::kVocWaves) * dev::kVocWaves;
+  } else {
+    const int tiles = cdiv(V, T);
+    p.row_tiles = cdiv(R, dev::kVocRows);
+    p.Rp = p.row_tiles * dev::kVocRows;
+    int want = 1024 / p.row_tiles;
+    if (want > tiles / 4) want = tiles / 4;
+    if (want < 1) want = 1;
+    p.per = cdiv(tiles, want);
+    p.splits = cdiv(tiles, p.per);
+  }
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at = up256(at + bytes);
+    return here;
+  };
+  const size_t shares = (size_t)p.splits * p.Rp;
+  p.pm = take(shares * 4);
+  p.pl = take(shares * 4);
+  if (!grad) p.pb = take(shares * sizeof(dev::RowBest));
+  if (grad) {
+    const int tiles = p.Rp / T;
+    p.col_tiles = cdiv(V, dev::kVocRows);
+    int want = 1024 / p.col_tiles;
+    if (want > tiles / 4) want = tiles / 4;
+    if (want < 1) want = 1;
+    p.cper = cdiv(tiles, want);
+    p.csplits = cdiv(tiles, p.cper);
+    p.po = take(shares * H * 4);
+    p.xg = take((size_t)p.Rp * H * sizeof(S));
+    p.lse = take((size_t)p.Rp * 4);
+    p.tgt = take((size_t)p.Rp * 4);
+    p.fac = take((size_t)p.Rp * 4);
+    p.pw = take((size_t)p.csplits * V * H * 4);
+    p.pdb = take((size_t)p.csplits * V * 4);
+  }
+  p.bytes = at;
+  return p;
+}
+
+template <typename S, int H, bool BEST>
+hipError_t vocab_loss_h(const VocabArgs& c, hipStream_t st) {
+  using namespace dev;
+  const VocabPlan p = vocab_plan<S>(H, c.R, c.V, false);
+  char* ws = static_cast<char*>(c.ws);
+  float *pm = reinterpret_cast<float*>(ws + p.pm), *pl = reinterpret_cast<float*>(ws + p.pl);
+  RowBest* pb = reinterpret_cast<RowBest*>(ws + p.pb);
+  const S *X = static_cast<const S*>(c.X), *W = static_cast<const S*>(c.W);
+  if (p.few) {
+    hipLaunchKernelGGL((vocab_few_kernel<S, H, BEST>), dim3(p.splits / kVocWaves), dim3(kVocThreads), 0, st,
+                       c.n_nodes, c.R, c.V, p.per, X, W, c.bias, c.node, pm, pl, pb);
+  } else {
+    hipLaunchKernelGGL((vocab_rows_kernel<S, H, false, BEST>), dim3(p.row_tiles * p.splits), dim3(kVocThreads), 0, st,
+                       c.n_nodes, c.R, c.V, p.row_tiles, p.per, X, W, c.bias, c.node, pm, pl, nullptr, pb);
+  }
+  hipLaunchKernelGGL((vocab_join_kernel<S, H, false, BEST>), dim3(cdiv((long)c.R * (H / 4), kVocThreads)),
+                     dim3(kVocThreads), 0, st, c.n_nodes, c.R, c.V, p.Rp, p.splits, X, W, c.bias, c.node, c.target,
+                     nullptr, 1.f, pm, pl, nullptr, pb, c.loss, c.lse, c.best, nullptr, nullptr, nullptr, nullptr,
+                     nullptr);
+  return hipGetLastError();
+}
+
+template <typename S, int H>
+hipError_t vocab_grad_h(const VocabArgs& c, hipStream_t st) {
+  using namespace dev;
+  const VocabPlan p = vocab_plan<S>(H, c.R, c.V, true);
+  char* ws = static_cast<char*>(c.ws);
+  float *pm = reinterpret_cast<float*>(ws + p.pm), *pl = reinterpret_cast<float*>(ws + p.pl);
+  float *po = reinterpret_cast<float*>(ws + p.po), *lse_w = reinterpret_cast<float*>(ws + p.lse);
+  float *fac_w = reinterpret_cast<float*>(ws + p.fac), *pw = reinterpret_cast<float*>(ws + p.pw);
+  float* pdb = c.dbias != nullptr ? reinterpret_cast<float*>(ws + p.pdb) : nullptr;
+  int32_t* tgt_w = reinterpret_cast<int32_t*>(ws + p.tgt);
+  S* xg = reinterpret_cast<S*>(ws + p.xg);
+  const S *X = static_cast<const S*>(c.X), *W = static_cast<const S*>(c.W);
+  hipError_t err = launch_fill_zero(c.dX, (size_t)c.n_nodes * H, st);
+  if (err != hipSuccess) return err;
+  hipLaunchKernelGGL((vocab_rows_kernel<S, H, true, false>), dim3(p.row_tiles * p.splits), dim3(kVocThreads), 0, st,
+                     c.n_nodes, c.R, c.V, p.row_tiles, p.per, X, W, c.bias, c.node, pm, pl, po, nullptr);
+  hipLaunchKernelGGL((vocab_join_kernel<S, H, true, false>), dim3(cdiv((long)p.Rp * (H / 4), kVocThreads)),
+                     dim3(kVocThreads), 0, st, c.n_nodes, c.R, c.V, p.Rp, p.splits, X, W, c.bias, c.node, c.target,
+                     c.weight, c.scale, pm, pl, po, nullptr, c.loss, c.lse, nullptr, c.dX, xg, lse_w, tgt_w, fac_w);
+  hipLaunchKernelGGL((vocab_cols_kernel<S, H>), dim3(p.col_tiles * p.csplits), dim3(kVocThreads), 0, st, c.V, p.Rp,
+                     p.col_tiles, p.cper, xg, W, c.bias, lse_w, tgt_w, fac_w, pw, pdb);
+  err = hipGetLastError();
+  if (err != hipSuccess) return err;
+  ReduceList red;
+  red.seg[red.n++] = ReduceSeg{pw, c.dW, p.csplits, c.V * H, (long)c.V * H};
+  if (pdb != nullptr) red.seg[red.n++] = ReduceSeg{pdb, c.dbias, p.csplits, c.V, c.V};
+  return launch_reduce_multi(red, st);
+}
+
+template <typename S, int H>
+hipError_t vocab_h(const VocabArgs& c, bool grad, hipStream_t st) {
+  if (grad) return vocab_grad_h<S, H>(c, st);
+  return c.best != nullptr ? vocab_loss_h<S, H, true>(c, st) : vocab_loss_h<S, H, false>(c, st);
+}
+}  // namespace
+
+namespace GGNN_IMPL_NS {
+size_t vocab_workspace(int H, int R, int V, bool grad) { return vocab_plan<dev::dt_t>(H, R, V, grad).bytes; }
+
+hipError_t launch_vocab(int H, const VocabArgs& c, bool grad, hipStream_t st) {
+  using S = dev::dt_t;
+  switch (H) {
+    case 32: return vocab_h<S, 32>(c, grad, st);
+    case 64: return vocab_h<S, 64>(c, grad, st);
+    case 128: return vocab_h<S, 128>(c, grad, st);
+    case 256: return vocab_h<S, 256>(c, grad, st);
+  }
+  return hipErrorInvalidValue;
+}
+}  // namespace GGNN_IMPL_NS
+
+}  // namespace ggnn
