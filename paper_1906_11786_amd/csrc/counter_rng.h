@@ -71,5 +71,16 @@ __device__ __forceinline__ void store8f(float* p, const float (&v)[8]) {
   *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
 }
 
+// The same for results that this kernel does not read again: past the caches
+// that hold what it does.
+__device__ __forceinline__ void store8f_once(bf16s* p, const float (&v)[8]) {
+  __builtin_nontemporal_store(u32x4{pk2(v[0], v[1]), pk2(v[2], v[3]), pk2(v[4], v[5]), pk2(v[6], v[7])},
+                              reinterpret_cast<u32x4*>(p));
+}
+__device__ __forceinline__ void store8f_once(float* p, const float (&v)[8]) {
+  __builtin_nontemporal_store(f32x4{v[0], v[1], v[2], v[3]}, reinterpret_cast<f32x4*>(p));
+  __builtin_nontemporal_store(f32x4{v[4], v[5], v[6], v[7]}, reinterpret_cast<f32x4*>(p + 4));
+}
+
 }  // namespace dev
 }  // namespace ggnn

@@ -20,7 +20,7 @@ __global__ __launch_bounds__(kDropThreads) void dropout_kernel(uint64_t count, c
   if (e + 8 <= count) {
     load8f<S>(X + e, v);
     if constexpr (DROP) drop8(v, b, d);
-    store8f(Y + e, v);
+    store8f_once(Y + e, v);
   } else {   // the last, incomplete block
     const int n = (int)(count - e);
 #pragma unroll

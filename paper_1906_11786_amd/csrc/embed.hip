@@ -18,39 +18,83 @@ constexpr int kEmbThreads = 256;
 
 __device__ __forceinline__ int clampi(int v, int lo, int hi) { return min(max(v, lo), hi); }
 
-template <typename S, int H, bool BAG, bool DROP>
-__global__ __launch_bounds__(kEmbThreads) void embed_kernel(int n, int V, const S* __restrict__ table,
-                                                            const int32_t* __restrict__ tok_ptr,
-                                                            const int32_t* __restrict__ tok, int n_tok, float scale,
-                                                            int mean, Dropout d, S* __restrict__ X) {
-  constexpr int L = H / 8;
-  const int row = (int)(((long)blockIdx.x * kEmbThreads + threadIdx.x) / L);
-  const int h = 8 * (threadIdx.x % L);
-  if (row >= n) return;
-  int lo, hi;
-  if constexpr (BAG) {
-    lo = clampi(tok_ptr[row], 0, n_tok);
-    hi = clampi(tok_ptr[row + 1], lo, n_tok);
-  } else {
-    lo = row;
-    hi = min(row + 1, n_tok);
-  }
-  float acc[8] = {};
-  for (int k = lo; k < hi; ++k) {
-    const int id = tok[k];
-    if ((unsigned)id < (unsigned)V) {
-      float v[8];
-      load8f<S>(table + (size_t)id * H + h, v);
+constexpr int kEmbRows = 4;   // rows of a lane group, one token per node
+
+template <typename S, int H, bool DROP>
+__device__ __forceinline__ void embed_store(S* __restrict__ X, int row, int h, float (&v)[8], float c,
+                                            const Dropout& d) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) acc[i] += v[i];
+  for (int i = 0; i < 8; ++i) v[i] *= c;
+  const uint64_t e = (uint64_t)row * H + h;
+  if constexpr (DROP) drop8(v, e / 8, d);
+  store8f_once(X + e, v);
+}
+
+// One token per node: a group takes kEmbRows rows, all loads issued before
+// the first use.
+template <typename S, int H, bool DROP>
+__global__ __launch_bounds__(kEmbThreads) void embed_rows_kernel(int n, int V, const S* __restrict__ table,
+                                                                 const int32_t* __restrict__ tok, int n_tok,
+                                                                 float scale, Dropout d, S* __restrict__ X) {
+  constexpr int L = H / 8, G = kEmbThreads / L;   // lanes per row, groups per workgroup
+  const long row0 = (long)blockIdx.x * (G * kEmbRows) + threadIdx.x / L;
+  const int h = 8 * (threadIdx.x % L);
+  int id[kEmbRows];
+#pragma unroll
+  for (int j = 0; j < kEmbRows; ++j) {
+    const long row = row0 + j * G;
+    id[j] = row < n_tok ? tok[row] : -1;
+  }
+  float v[kEmbRows][8];
+#pragma unroll
+  for (int j = 0; j < kEmbRows; ++j) {
+    if ((unsigned)id[j] < (unsigned)V) {
+      load8f<S>(table + (size_t)id[j] * H + h, v[j]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[j][i] = 0.f;
     }
   }
-  const float c = BAG && mean && hi > lo ? scale / (float)(hi - lo) : scale;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) acc[i] *= c;
-  const uint64_t e = (uint64_t)row * H + h;
-  if constexpr (DROP) drop8(acc, e / 8, d);
-  store8f(X + e, acc);
+  for (int j = 0; j < kEmbRows; ++j) {
+    const long row = row0 + j * G;
+    if (row < n) embed_store<S, H, DROP>(X, (int)row, h, v[j], scale, d);
+  }
+}
+
+// Lists: four tokens of a list in flight, added in list order.
+template <typename S, int H, bool DROP>
+__global__ __launch_bounds__(kEmbThreads) void embed_lists_kernel(int n, int V, const S* __restrict__ table,
+                                                                  const int32_t* __restrict__ tok_ptr,
+                                                                  const int32_t* __restrict__ tok, int n_tok,
+                                                                  float scale, int mean, Dropout d,
+                                                                  S* __restrict__ X) {
+  constexpr int L = H / 8, U = 4;
+  const long row = ((long)blockIdx.x * kEmbThreads + threadIdx.x) / L;
+  const int h = 8 * (threadIdx.x % L);
+  if (row >= n) return;
+  const int lo = clampi(tok_ptr[row], 0, n_tok), hi = clampi(tok_ptr[row + 1], lo, n_tok);
+  float acc[8] = {};
+  for (int k = lo; k < hi; k += U) {
+    int id[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) id[u] = k + u < hi ? tok[k + u] : -1;
+    float v[U][8];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if ((unsigned)id[u] < (unsigned)V) {
+        load8f<S>(table + (size_t)id[u] * H + h, v[u]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[u][i] = 0.f;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[i] += v[u][i];
+  }
+  embed_store<S, H, DROP>(X, (int)row, h, acc, mean && hi > lo ? scale / (float)(hi - lo) : scale, d);
 }
 
 }  // namespace dev
@@ -59,17 +103,26 @@ namespace {
 template <typename S, int H>
 hipError_t embed_h(int n, int V, const void* table, const int32_t* tok_ptr, const int32_t* tok, int n_tok,
                    float scale, int mean, const Dropout& d, void* X, hipStream_t st) {
-  const long threads = (long)n * (H / 8);
-  const dim3 grid((unsigned)((threads + dev::kEmbThreads - 1) / dev::kEmbThreads)), block(dev::kEmbThreads);
-#define EMBED(BAG, DROP)                                                                                       \
-  hipLaunchKernelGGL((dev::embed_kernel<S, H, BAG, DROP>), grid, block, 0, st, n, V, static_cast<const S*>(table), \
-                     tok_ptr, tok, n_tok, scale, mean, d, static_cast<S*>(X))
+  constexpr int G = dev::kEmbThreads / (H / 8);
+  const int per = tok_ptr != nullptr ? G : G * dev::kEmbRows;   // rows of a workgroup
+  const dim3 grid((unsigned)(((long)n + per - 1) / per)), block(dev::kEmbThreads);
+  const S* E = static_cast<const S*>(table);
+  S* out = static_cast<S*>(X);
   if (tok_ptr != nullptr) {
-    if (d.cut != 0) EMBED(true, true); else EMBED(true, false);
+    if (d.cut != 0)
+      hipLaunchKernelGGL((dev::embed_lists_kernel<S, H, true>), grid, block, 0, st, n, V, E, tok_ptr, tok, n_tok,
+                         scale, mean, d, out);
+    else
+      hipLaunchKernelGGL((dev::embed_lists_kernel<S, H, false>), grid, block, 0, st, n, V, E, tok_ptr, tok, n_tok,
+                         scale, mean, d, out);
   } else {
-    if (d.cut != 0) EMBED(false, true); else EMBED(false, false);
+    if (d.cut != 0)
+      hipLaunchKernelGGL((dev::embed_rows_kernel<S, H, true>), grid, block, 0, st, n, V, E, tok, n_tok, scale, d,
+                         out);
+    else
+      hipLaunchKernelGGL((dev::embed_rows_kernel<S, H, false>), grid, block, 0, st, n, V, E, tok, n_tok, scale, d,
+                         out);
   }
-#undef EMBED
   return hipGetLastError();
 }
 }  // namespace
@@ -102,58 +155,98 @@ constexpr int kSortThreads = 256, kSortWaves = kSortThreads / kWave;
 constexpr int kSortPer = 8;                              // items per thread
 constexpr int kSortTile = kSortThreads * kSortPer;       // items per tile
 constexpr int kDigits = 256;
+constexpr int kFewTiles = 64;   // the placement adds up the counts of as many tiles itself: one launch less a pass
 
-// Row whose list holds position k: the last i with ptr[i] <= k.
-__device__ __forceinline__ int row_of(const int32_t* __restrict__ ptr, int n, int k) {
-  int lo = 0, hi = n;   // ptr[lo] <= k < ptr[hi]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (ptr[mid] <= k) lo = mid; else hi = mid;
+// The last row i with ptr[i] <= k, of rows 0 .. n - 1 (0 where there is none),
+// by the whole workgroup: kSortThreads probes a round.
+__device__ __forceinline__ int find_row(const int32_t* __restrict__ ptr, int n, int k) {
+  int lo = 0, len = n;   // the answer lies in lo .. lo + len - 1
+  while (len > 1) {
+    const int step = (len + kSortThreads - 1) / kSortThreads;
+    const long i = lo + (long)(threadIdx.x + 1) * step;
+    const int below = __syncthreads_count(i < (long)lo + len && ptr[i] <= k);
+    lo += below * step;
+    len = min(step, n - lo);
   }
   return lo;
 }
 
-// Item k of the unsorted list: its key and row.
-__device__ __forceinline__ u32x2 first_item(int k, int n, int V, const int32_t* __restrict__ tok_ptr,
-                                            const int32_t* __restrict__ tok) {
-  const int id = tok[k];
-  uint32_t key = (unsigned)id < (unsigned)V ? (uint32_t)id : (uint32_t)V;
-  int row = k;
-  if (tok_ptr != nullptr) {
-    if (k < tok_ptr[0] || k >= tok_ptr[n]) key = (uint32_t)V;   // no row's list holds it
-    row = row_of(tok_ptr, n, k);
-  }
-  return u32x2{key, (uint32_t)row};
-}
-
 // Digit counts of each tile, count[digit * tiles + tile].  FIRST: the items
-// are made from the token list and written to `items`.
+// are made from the token list and written to `items`; the row of a position
+// is the greatest row whose (not empty) list begins at or before it, so the
+// rows mark the positions where their lists begin and a running maximum over
+// the tile fills the rest.
+// (count[tile * kDigits + digit] where few tiles need no scan kernel.)
 template <bool FIRST>
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(int n_tok, int n, int V,
                                                                   const int32_t* __restrict__ tok_ptr,
                                                                   const int32_t* __restrict__ tok, u32x2* items,
-                                                                  int shift, uint32_t mask, int tiles,
+                                                                  int shift, uint32_t mask, int tiles, int few,
                                                                   uint32_t* __restrict__ count) {
   __shared__ uint32_t c[kDigits];
   c[threadIdx.x] = 0;
-  __syncthreads();
   const int k0 = blockIdx.x * kSortTile;
+  if constexpr (FIRST) {
+    __shared__ int rows[kSortTile];
+    __shared__ int wm[kSortWaves];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    int listed0 = 0, listed1 = n_tok;   // positions that lists hold
+    if (tok_ptr != nullptr) {
+      listed0 = tok_ptr[0];
+      listed1 = tok_ptr[n];
+      const int first = find_row(tok_ptr, n, k0);
 #pragma unroll
-  for (int i = 0; i < kSortPer; ++i) {
-    const int k = k0 + i * kSortThreads + threadIdx.x;
-    if (k < n_tok) {
-      u32x2 it;
-      if constexpr (FIRST) {
-        it = first_item(k, n, V, tok_ptr, tok);
-        items[k] = it;
-      } else {
-        it = items[k];
+      for (int i = 0; i < kSortPer; ++i) rows[i * kSortThreads + threadIdx.x] = first;
+      __syncthreads();
+      for (long i0 = first; i0 < n; i0 += kSortThreads) {
+        const long i = i0 + threadIdx.x;
+        const int b = i < n ? tok_ptr[i] : INT_MAX;
+        if (i < n && b >= k0 && b < k0 + kSortTile && b < tok_ptr[i + 1]) rows[b - k0] = (int)i;
+        if (__syncthreads_or(b >= k0 + kSortTile)) break;   // lists begin in order: the rest begin later
       }
-      atomicAdd(&c[(it.x >> shift) & mask], 1u);   // integers: the order does not matter
+      __syncthreads();
+      int m[kSortPer], top = 0;
+#pragma unroll
+      for (int i = 0; i < kSortPer; ++i) {
+        top = max(top, rows[threadIdx.x * kSortPer + i]);
+        m[i] = top;
+      }
+      int run = top;
+#pragma unroll
+      for (int o = 1; o < kWave; o <<= 1) {
+        const int u = __shfl_up(run, o);
+        if (lane >= o) run = max(run, u);
+      }
+      if (lane == kWave - 1) wm[wave] = run;
+      int before = __shfl_up(run, 1);
+      if (lane == 0) before = 0;
+      __syncthreads();
+      for (int w = 0; w < wave; ++w) before = max(before, wm[w]);
+#pragma unroll
+      for (int i = 0; i < kSortPer; ++i) rows[threadIdx.x * kSortPer + i] = max(m[i], before);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kSortPer; ++i) {
+      const int k = k0 + i * kSortThreads + threadIdx.x;
+      if (k < n_tok) {
+        const int id = tok[k];
+        const bool ok = (unsigned)id < (unsigned)V && k >= listed0 && k < listed1;
+        const uint32_t key = ok ? (uint32_t)id : (uint32_t)V;
+        items[k] = u32x2{key, (uint32_t)(tok_ptr != nullptr ? rows[k - k0] : k)};
+        atomicAdd(&c[(key >> shift) & mask], 1u);   // integers: the order does not matter
+      }
+    }
+  } else {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kSortPer; ++i) {
+      const int k = k0 + i * kSortThreads + threadIdx.x;
+      if (k < n_tok) atomicAdd(&c[(items[k].x >> shift) & mask], 1u);
     }
   }
   __syncthreads();
-  count[(size_t)threadIdx.x * tiles + blockIdx.x] = c[threadIdx.x];
+  count[few ? (size_t)blockIdx.x * kDigits + threadIdx.x : (size_t)threadIdx.x * tiles + blockIdx.x] = c[threadIdx.x];
 }
 
 // Exclusive scan of one digit's counts over the tiles; its total to total[].
@@ -192,7 +285,8 @@ __global__ __launch_bounds__(kSortThreads) void sort_scan_kernel(int tiles, uint
 // in earlier rounds of its wave and in lower lanes of its round.
 __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(int n_tok, const u32x2* __restrict__ in,
                                                                   u32x2* __restrict__ out, int shift, uint32_t mask,
-                                                                  int tiles, const uint32_t* __restrict__ count,
+                                                                  int tiles, int few,
+                                                                  const uint32_t* __restrict__ count,
                                                                   const uint32_t* __restrict__ total) {
   __shared__ uint32_t cnt[kSortWaves][kDigits];
   __shared__ uint32_t ws[kSortWaves];
@@ -200,7 +294,22 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(int n_tok, con
 #pragma unroll
   for (int w = 0; w < kSortWaves; ++w) cnt[w][dig] = 0;
   // exclusive scan of the digit totals
-  const uint32_t tot = total[dig];
+  uint32_t tot = 0, before = 0;   // the digit's items in all tiles, and in the tiles before this one
+  if (few) {
+    for (int t0 = 0; t0 < tiles; t0 += 8) {
+      uint32_t c[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) c[u] = t0 + u < tiles ? count[(size_t)(t0 + u) * kDigits + dig] : 0u;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        tot += c[u];
+        if (t0 + u < (int)blockIdx.x) before += c[u];
+      }
+    }
+  } else {
+    tot = total[dig];
+    before = count[(size_t)dig * tiles + blockIdx.x];
+  }
   uint32_t s = tot;
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) {
@@ -209,7 +318,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(int n_tok, con
   }
   if (lane == kWave - 1) ws[wave] = s;
   __syncthreads();
-  uint32_t base = s - tot + count[(size_t)dig * tiles + blockIdx.x];
+  uint32_t base = s - tot + before;
   for (int w = 0; w < wave; ++w) base += ws[w];
 
   const int k0 = blockIdx.x * kSortTile + wave * (kSortTile / kSortWaves);
@@ -258,115 +367,258 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(int n_tok, con
 
 // ---- sums over runs of one token -----------------------------------------
 //
-// The sorted list is cut into chunks of `chunk` items, one group of H / 8
-// lanes each.  A run inside one chunk is added to its row of the gradient
-// directly.  Of a run that crosses chunks, each chunk writes its share to
-// part[chunk][0] (it began before) or part[chunk][1] (it begins here), and the
-// join kernel adds the shares in chunk order.
+// The sorted list is cut into chunks, one group of H / 8 lanes each, and a
+// workgroup's groups take neighbouring chunks (a block of the list).  A run
+// inside one chunk is added to its row of the gradient at once.  Of a run that
+// crosses chunks, the chunks after the first leave their shares in LDS and the
+// chunk where it begins (or the block's first) adds them in order; of a run that
+// crosses blocks, each block writes its share to part[block][0] (it began
+// before) or part[block][1] (it begins here), and the join kernel adds those
+// in block order.
 
-template <int H, bool DROP>
-__global__ __launch_bounds__(kEmbThreads) void embed_runs_kernel(int n_tok, int V, int chunk,
-                                                                 const u32x2* __restrict__ items,
-                                                                 const int32_t* __restrict__ tok_ptr, float scale,
-                                                                 int mean, Dropout d, const float* __restrict__ dX,
-                                                                 float* __restrict__ dtable,
-                                                                 float* __restrict__ part) {
-  constexpr int L = H / 8;
-  const int c = (int)(((long)blockIdx.x * kEmbThreads + threadIdx.x) / L);
-  const int h = 8 * (threadIdx.x % L);
-  const long lo = (long)c * chunk;
-  if (lo >= n_tok) return;
-  const int k0 = (int)lo, k1 = min(n_tok, k0 + chunk);
-  uint32_t cur = items[k0].x;
-  bool before = k0 > 0 && items[k0 - 1].x == cur;
-  float acc[8] = {};
-  auto flush = [&](bool after) {
-    if (cur >= (uint32_t)V) return;
-    if (before || after) {
-      store8f(part + ((size_t)2 * c + (before ? 0 : 1)) * H + h, acc);
-    } else {
-      float* o = dtable + (size_t)cur * H + h;
-      float v[8];
-      load8f<float>(o, v);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] += acc[i];
-      store8f(o, v);
-    }
-  };
-  for (int k = k0; k < k1; ++k) {
-    const u32x2 it = items[k];
-    if (it.x != cur) {
-      flush(false);
-      cur = it.x;
-      before = false;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) acc[i] = 0.f;
-    }
-    if (cur < (uint32_t)V) {
-      const int row = (int)it.y;
-      float f = scale;
-      if (tok_ptr != nullptr && mean) f = scale / (float)max(tok_ptr[row + 1] - tok_ptr[row], 1);
-      float v[8];
-      const uint64_t e = (uint64_t)row * H + h;
-      load8f<float>(dX + e, v);
-      if constexpr (DROP) drop8(v, e / 8, d);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) acc[i] += f * v[i];
-    }
-  }
-  flush(k1 < n_tok && items[k1].x == cur);
-}
-
-// One group of H / 8 lanes per chunk: adds up a run that begins in the chunk and
-// leaves it.
-template <int H>
-__global__ __launch_bounds__(kEmbThreads) void embed_join_kernel(int n_tok, int V, int chunk,
-                                                                 const u32x2* __restrict__ items,
-                                                                 const float* __restrict__ part,
-                                                                 float* __restrict__ dtable) {
-  constexpr int L = H / 8;
-  const int c = (int)(((long)blockIdx.x * kEmbThreads + threadIdx.x) / L);
-  const int h = 8 * (threadIdx.x % L);
-  const long lo = (long)c * chunk;
-  const long end = lo + chunk;
-  if (end >= n_tok) return;   // the last chunk's runs end in it
-  const uint32_t key = items[end - 1].x;
-  if (key >= (uint32_t)V || items[end].x != key) return;
-  if (items[lo].x == key && lo > 0 && items[lo - 1].x == key) return;   // begins before
-  float acc[8], v[8];
-  load8f<float>(part + ((size_t)2 * c + 1) * H + h, acc);
-  for (long k = end, j = c + 1; k < n_tok && items[k].x == key; k += chunk, ++j) {
-    load8f<float>(part + (size_t)2 * j * H + h, v);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) acc[i] += v[i];
-  }
-  float* o = dtable + (size_t)key * H + h;
+// One row of the gradient += acc.
+__device__ __forceinline__ void add_row(float* __restrict__ o, const float (&acc)[8]) {
+  float v[8];
   load8f<float>(o, v);
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] += acc[i];
   store8f(o, v);
 }
 
+template <int H, bool DROP>
+__global__ __launch_bounds__(kEmbThreads) void embed_runs_kernel(int n_tok, int n, int V, int chunk,
+                                                                 const u32x2* __restrict__ items,
+                                                                 const int32_t* __restrict__ tok_ptr, float scale,
+                                                                 int mean, Dropout d, const float* __restrict__ dX,
+                                                                 float* __restrict__ dtable,
+                                                                 float* __restrict__ part) {
+  constexpr int L = H / 8, G = kEmbThreads / L, U = 4;
+  __shared__ __attribute__((aligned(16))) float head[G][H];   // share of a run that began before the chunk
+  __shared__ uint32_t hkey[G];    // its token; V: none
+  __shared__ int hfull[G];        // whether it also leaves the chunk
+  const int grp = threadIdx.x / L, h = 8 * (threadIdx.x % L);
+  const long lo = ((long)blockIdx.x * G + grp) * chunk;
+  const uint32_t none = (uint32_t)V;
+  const bool lead = threadIdx.x % L == 0;
+  float acc[8] = {};
+  uint32_t cur = none;
+  bool before = false, after = false;
+  if (lead) {
+    hkey[grp] = none;
+    hfull[grp] = 0;
+  }
+  if (lo < n_tok) {
+    const int k0 = (int)lo, k1 = (int)min((long)n_tok, lo + chunk);
+    cur = items[k0].x;
+    before = k0 > 0 && items[k0 - 1].x == cur;
+    float old[8] = {};   // the gradient's row of the current token
+    if (!before && cur < none) load8f<float>(dtable + (size_t)cur * H + h, old);
+    for (int k = k0; k < k1; k += U) {
+      u32x2 it[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) it[u] = items[min(k + u, k1 - 1)];
+      // every load of the four items first: state rows, list lengths, gradient rows of the tokens that begin
+      float v[U][8], w[U][8], f[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int row = min((int)it[u].y, n - 1);
+        const bool ok = it[u].x < none && k + u < k1;
+        f[u] = scale;
+        if (ok) {
+          load8f<float>(dX + (size_t)row * H + h, v[u]);
+          if (tok_ptr != nullptr && mean) f[u] = scale / (float)max(tok_ptr[row + 1] - tok_ptr[row], 1);
+          if (it[u].x != (u > 0 ? it[u - 1].x : cur)) load8f<float>(dtable + (size_t)it[u].x * H + h, w[u]);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (k + u >= k1) break;
+        if (it[u].x != cur) {   // the run ends inside the chunk
+          if (cur < none) {
+            if (before) {
+              store8f(&head[grp][h], acc);
+              if (lead) hkey[grp] = cur;
+            } else {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) old[i] += acc[i];
+              store8f(dtable + (size_t)cur * H + h, old);
+            }
+          }
+          cur = it[u].x;
+          before = false;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            acc[i] = 0.f;
+            old[i] = w[u][i];
+          }
+        }
+        if (cur < none) {
+          if constexpr (DROP) drop8(v[u], ((uint64_t)it[u].y * H + h) / 8, d);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) acc[i] += f[u] * v[u][i];
+        }
+      }
+    }
+    after = k1 < n_tok && items[k1].x == cur;
+    if (cur < none) {
+      if (!before && !after) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) old[i] += acc[i];
+        store8f(dtable + (size_t)cur * H + h, old);
+      } else if (before && grp > 0) {
+        store8f(&head[grp][h], acc);
+        if (lead) {
+          hkey[grp] = cur;
+          hfull[grp] = after;
+        }
+      }
+    }
+  }
+  __syncthreads();
+  if (lo >= n_tok || cur >= none) {
+    // (group 0's head share of a run that ended in its chunk is written below)
+  } else if (after && (!before || grp == 0)) {   // a run that leaves this chunk and is this one's to add up
+    int j = grp + 1;
+    for (bool open = true; open && j < G; ++j) {
+      float v[8];
+      load8f<float>(&head[j][h], v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[i] += v[i];
+      open = hfull[j] != 0;
+      after = open;
+    }
+    if (before || after) store8f(part + ((size_t)2 * blockIdx.x + (before ? 0 : 1)) * H + h, acc);
+    else add_row(dtable + (size_t)cur * H + h, acc);
+  } else if (before && !after && grp == 0) {   // the chunk is all one run that ends with it
+    store8f(part + (size_t)2 * blockIdx.x * H + h, acc);
+  }
+  if (grp == 0 && hkey[0] < none) {
+    float v[8];
+    load8f<float>(&head[0][h], v);
+    store8f(part + (size_t)2 * blockIdx.x * H + h, v);
+  }
+}
+
+// Adds up the runs that cross blocks.  A workgroup looks at kJoinBlocks
+// blocks: a group adds up a run that begins in its block and ends within
+// kJoinShort more; a longer one is added by all groups, each a fixed share of
+// its blocks, joined in a fixed tree.
+constexpr int kJoinThreads = 1024, kJoinBlocks = 64, kJoinShort = 16;
+
+template <int H>
+__global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(int n_tok, int V, int block, int blocks,
+                                                                  const u32x2* __restrict__ items,
+                                                                  const float* __restrict__ part,
+                                                                  float* __restrict__ dtable) {
+  constexpr int L = H / 8, G = kJoinThreads / L;
+  __shared__ __attribute__((aligned(16))) float share[G][H];
+  __shared__ int is_long[kJoinBlocks];
+  const int grp = threadIdx.x / L, h = 8 * (threadIdx.x % L);
+  const int b0 = blockIdx.x * kJoinBlocks;
+  if (threadIdx.x < kJoinBlocks) is_long[threadIdx.x] = 0;
+  __syncthreads();
+  auto first = [&](long b) { return items[b * block].x; };   // token at the start of block b < blocks
+  for (int b = b0 + grp; b < min(b0 + kJoinBlocks, blocks - 1); b += G) {
+    // whether the run at the end of block b goes on and began in it
+    const long far = min((long)b + kJoinShort + 1, (long)blocks - 1);
+    const uint32_t key = first(b + 1), last = items[((long)b + 1) * block - 1].x, start = first(b),
+                   prev = items[max((long)b * block - 1, 0l)].x, farkey = first(far);
+    if (key >= (uint32_t)V || last != key || (start == key && b > 0 && prev == key)) continue;
+    if (b + kJoinShort + 1 < blocks && farkey == key) {
+      if (h == 0) is_long[b - b0] = 1;
+      continue;
+    }
+    float acc[8];
+    load8f<float>(part + ((size_t)2 * b + 1) * H + h, acc);
+    bool open = true;
+    for (long j = b + 1; open; j += 4) {   // four blocks' keys and shares in flight
+      float w[4][8];
+      uint32_t k[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const long ju = min(j + u, (long)blocks - 1);
+        k[u] = j + u < blocks ? first(ju) : ~0u;
+        load8f<float>(part + (size_t)2 * ju * H + h, w[u]);   // not of this run where the key differs: unused
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        open = open && k[u] == key;
+        if (open) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) acc[i] += w[u][i];
+        }
+      }
+    }
+    add_row(dtable + (size_t)key * H + h, acc);
+  }
+  __syncthreads();
+  for (int i = 0; i < kJoinBlocks; ++i) {   // at most one in kJoinShort blocks begins a long run
+    if (is_long[i] == 0) continue;
+    const int b = b0 + i;
+    const uint32_t key = first(b + 1);
+    int lo = b + kJoinShort + 1, len = blocks - lo;   // the run's last block lies in lo .. lo + len - 1
+    while (len > 1) {                                 // kJoinThreads probes a round
+      const int step = (len + kJoinThreads - 1) / kJoinThreads;
+      const long j = lo + (long)(threadIdx.x + 1) * step;
+      const int same = __syncthreads_count(j < (long)lo + len && first(j) == key);
+      lo += same * step;
+      len = min(step, blocks - lo);
+    }
+    float acc[8] = {}, v[8];
+    if (grp == 0) load8f<float>(part + ((size_t)2 * b + 1) * H + h, acc);
+#pragma unroll 4
+    for (long j = b + 1 + grp; j <= lo; j += G) {
+      load8f<float>(part + (size_t)2 * j * H + h, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[i] += v[i];
+    }
+    store8f(&share[grp][h], acc);
+    __syncthreads();
+    for (int half = G / 2; half >= 1; half /= 2) {
+      if (grp < half) {
+        load8f<float>(&share[grp][h], acc);
+        load8f<float>(&share[grp + half][h], v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[i] += v[i];
+        store8f(&share[grp][h], acc);
+      }
+      __syncthreads();
+    }
+    if (grp == 0) {
+      load8f<float>(&share[0][h], acc);
+      add_row(dtable + (size_t)key * H + h, acc);
+    }
+    __syncthreads();
+  }
+}
+
 }  // namespace dev
 
 namespace {
-constexpr int kRunChunk = 32;
+// Items of a chunk: enough workgroups first, then few shares to join.
+int run_chunk(int H, int n_tok) {
+  const int groups = dev::kEmbThreads / (H / 8);
+  const long c = ((long)n_tok + 1024L * groups - 1) / (1024L * groups);
+  return c < 4 ? 4 : c > 32 ? 32 : (int)((c + 3) / 4 * 4);
+}
 
 struct EmbedLayout {
   size_t a, b, count, total, part, bytes;
-  int tiles, chunks;
+  int tiles, chunk, block, blocks;   // sort tiles; items of a chunk and of a block of the runs kernel
 };
 EmbedLayout embed_layout(int H, int n_tok) {
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   EmbedLayout l;
   l.tiles = (int)(((long)n_tok + dev::kSortTile - 1) / dev::kSortTile);
-  l.chunks = (int)(((long)n_tok + kRunChunk - 1) / kRunChunk);
+  l.chunk = run_chunk(H, n_tok);
+  l.block = l.chunk * (dev::kEmbThreads / (H / 8));
+  l.blocks = (int)(((long)n_tok + l.block - 1) / l.block);
   l.a = 0;
   l.b = up((size_t)n_tok * 8);
   l.count = l.b + up((size_t)n_tok * 8);
   l.total = l.count + up((size_t)dev::kDigits * l.tiles * 4);
   l.part = l.total + up((size_t)dev::kDigits * 4);
-  l.bytes = l.part + up((size_t)2 * l.chunks * H * 4);
+  l.bytes = l.part + up((size_t)2 * l.blocks * H * 4);
   return l;
 }
 
@@ -381,34 +633,37 @@ hipError_t embed_bwd_h(int n, int V, const int32_t* tok_ptr, const int32_t* tok,
   int bits = 1;
   while (bits < 31 && (V >> bits) != 0) ++bits;   // keys 0 .. V
   const int passes = (bits + 7) / 8, per = (bits + passes - 1) / passes;
+  const int few = l.tiles <= kFewTiles;
   for (int p = 0; p < passes; ++p) {
     const int shift = p * per;
     const uint32_t mask = (1u << per) - 1;
     if (p == 0) {
       hipLaunchKernelGGL(sort_count_kernel<true>, dim3(l.tiles), dim3(kSortThreads), 0, st, n_tok, n, V, tok_ptr,
-                         tok, a, shift, mask, l.tiles, count);
+                         tok, a, shift, mask, l.tiles, few, count);
     } else {
       hipLaunchKernelGGL(sort_count_kernel<false>, dim3(l.tiles), dim3(kSortThreads), 0, st, n_tok, n, V, tok_ptr,
-                         tok, a, shift, mask, l.tiles, count);
+                         tok, a, shift, mask, l.tiles, few, count);
     }
-    hipLaunchKernelGGL(sort_scan_kernel, dim3(kDigits), dim3(kSortThreads), 0, st, l.tiles, count, total);
+    if (!few)
+      hipLaunchKernelGGL(sort_scan_kernel, dim3(kDigits), dim3(kSortThreads), 0, st, l.tiles, count, total);
     hipLaunchKernelGGL(sort_place_kernel, dim3(l.tiles), dim3(kSortThreads), 0, st, n_tok, a, b, shift, mask,
-                       l.tiles, count, total);
+                       l.tiles, few, count, total);
     u32x2* t = a;
     a = b;
     b = t;
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
   }
-  const dim3 grid((unsigned)(((long)l.chunks * (H / 8) + kEmbThreads - 1) / kEmbThreads));
   if (d.cut != 0) {
-    hipLaunchKernelGGL((embed_runs_kernel<H, true>), grid, dim3(kEmbThreads), 0, st, n_tok, V, kRunChunk, a,
-                       tok_ptr, scale, mean, d, dX, dtable, part);
+    hipLaunchKernelGGL((embed_runs_kernel<H, true>), dim3(l.blocks), dim3(kEmbThreads), 0, st, n_tok, n, V, l.chunk,
+                       a, tok_ptr, scale, mean, d, dX, dtable, part);
   } else {
-    hipLaunchKernelGGL((embed_runs_kernel<H, false>), grid, dim3(kEmbThreads), 0, st, n_tok, V, kRunChunk, a,
-                       tok_ptr, scale, mean, d, dX, dtable, part);
+    hipLaunchKernelGGL((embed_runs_kernel<H, false>), dim3(l.blocks), dim3(kEmbThreads), 0, st, n_tok, n, V, l.chunk,
+                       a, tok_ptr, scale, mean, d, dX, dtable, part);
   }
-  hipLaunchKernelGGL((embed_join_kernel<H>), grid, dim3(kEmbThreads), 0, st, n_tok, V, kRunChunk, a, part, dtable);
+  if (l.blocks > 1)
+    hipLaunchKernelGGL((embed_join_kernel<H>), dim3((l.blocks + kJoinBlocks - 1) / kJoinBlocks), dim3(kJoinThreads),
+                       0, st, n_tok, V, l.block, l.blocks, a, part, dtable);
   return hipGetLastError();
 }
 }  // namespace
