@@ -90,22 +90,6 @@ __device__ __forceinline__ frag_t<S> row_frag(const S* tile, int r0, int kk, int
 // Fragment across rows: column 32 ht + lane % 32, rows r0 + {0, 8} + 4 (lane / 32) + 0 .. 3
 // (the order in which a lane holds the accumulators of a 32 x 32 tile).
 template <int H>
-__device__ __forceinline__ bf16x8 col_frag(const bf16s* tile, int r0, int ht, int lane) {
-  constexpr int CPR = H * 2 / 16;
-  const int p = lane % 16, g = lane / 32;
-  const int c = 4 * ht + 2 * ((lane / 16) & 1) + (p % 4) / 2;
-  typedef short v8i16 __attribute__((ext_vector_type(8)));
-  tr_v4i16 t[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int r = r0 + 8 * i + 4 * g + p / 4;
-    bf16s* a = const_cast<bf16s*>(tile) + (r * CPR + (c ^ swz<bf16s, H>(r))) * 8 + 4 * (p % 2);
-    t[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr_v4i16*)(a));
-  }
-  const v8i16 v = __builtin_shufflevector(t[0], t[1], 0, 1, 2, 3, 4, 5, 6, 7);
-  return __builtin_bit_cast(bf16x8, v);
-}
-template <int H>
 __device__ __forceinline__ f32x8 col_frag(const float* tile, int r0, int ht, int lane) {
   constexpr int CPR = H * 4 / 16;
   const int q = lane % 32, g = lane / 32;
@@ -118,33 +102,132 @@ __device__ __forceinline__ f32x8 col_frag(const float* tile, int r0, int ht, int
   return v;
 }
 
-// acc[ht] += (rows r0 .. r0 + 31 of the tile)^T p for the 32 values p of a tile
-// (lane's column, rows in accumulator order).
+// ---- the two products of a 32 x 32 tile -----------------------------------
+//
+// One wave alone must keep its matrix core busy at H = 256, where a SIMD holds
+// one, and an LDS read takes the time of several products.  So a step is laid
+// out by hand: fragments are read kAhead before their product, and every
+// product is followed by a share of the step's vector work, with the
+// compiler's scheduler kept from moving anything between these slots (its own
+// order read one fragment ahead and left the rest of the latency open).
+//
+// A step on tile rows r0 .. r0 + 31: logits of the next tile (NS products),
+// then the second product of this one (NO fragments, each times the hi and the
+// lo part of p).
+
+#if GGNN_DT_BF16
+typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
+
 template <int H>
-__device__ __forceinline__ void add_product(f32x16 (&acc)[H / 32], const float (&p)[16], const bf16s* tile, int r0,
-                                            int lane) {
+struct VocStep {
+  static constexpr int NS = H / 16, NO = H / 16;
+  static constexpr int kAhead = NS < 8 ? NS : 8;
+  static constexpr int CPR = H * 2 / 16;
+  static constexpr uint32_t ROW = H * 2;                       // bytes of a tile row
+  static constexpr int VS = NS < 8 ? NS : 8, VO = H / 32 < 4 ? H / 32 : 4;
+  uint32_t as[VS], ao[2][VO];   // LDS addresses of the fragments; the other ones lie 256 bytes or whole rows on
+  bf16x8 f[NS + NO];            // at most kAhead are alive
+
+  __device__ __forceinline__ void init(uint32_t lds, int lane) {
+    const int r = lane % 32, g = lane / 32, p = lane % 16;
 #pragma unroll
-  for (int ks = 0; ks < 2; ++ks) {
-    bf16x8 hi, lo;
-    split8(p + 8 * ks, hi, lo);
+    for (int k = 0; k < VS; ++k) as[k] = lds + (uint32_t)r * ROW + 16u * ((2 * k + g) ^ swz<bf16s, H>(r));
 #pragma unroll
-    for (int ht = 0; ht < H / 32; ++ht) {
-      const bf16x8 a = col_frag<H>(tile, r0 + 16 * ks, ht, lane);
-      mma32(acc[ht], a, hi);
-      mma32(acc[ht], a, lo);
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int ht = 0; ht < VO; ++ht) {
+        const int row = 8 * i + 4 * g + p / 4, c = 4 * ht + 2 * ((lane / 16) & 1) + (p % 4) / 2;
+        ao[i][ht] = lds + (uint32_t)row * ROW + 16u * (c ^ swz<bf16s, H>(row)) + 8u * (p % 2);
+      }
+  }
+  __device__ __forceinline__ void move_s(uint32_t by) {
+#pragma unroll
+    for (int k = 0; k < VS; ++k) as[k] += by;
+  }
+  __device__ __forceinline__ void move_o(uint32_t by) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int ht = 0; ht < VO; ++ht) ao[i][ht] += by;
+  }
+  // Fragment n of a step: n < NS along H of the next tile (rows rs), else
+  // across the rows of this one (rows ro); see row_frag and col_frag.
+  __device__ __forceinline__ void read(int n, int rs, int ro) {
+    if (n < NS) {
+      f[n] = __builtin_bit_cast(bf16x8, *(lds_u32x4*)(as[n % VS] + 256u * (n / VS) + (uint32_t)rs * ROW));
+    } else {
+      const int ks = (n - NS) / (H / 32), ht = (n - NS) % (H / 32);
+      typedef short v8i16 __attribute__((ext_vector_type(8)));
+      const uint32_t off = 256u * (ht / VO) + (uint32_t)(ro + 16 * ks) * ROW;
+      const tr_v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr_v4i16*)(ao[0][ht % VO] + off));
+      const tr_v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr_v4i16*)(ao[1][ht % VO] + off));
+      f[n] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
   }
-}
-template <int H>
-__device__ __forceinline__ void add_product(f32x16 (&acc)[H / 32], const float (&p)[16], const float* tile, int r0,
-                                            int lane) {
+  // The step's first reads.  LAST: number of the last fragment that it uses.
+  template <int LAST>
+  __device__ __forceinline__ void begin(int rs, int ro) {
 #pragma unroll
-  for (int ks = 0; ks < 2; ++ks) {
-    const f32x8 b = pack8<float>(p + 8 * ks);
-#pragma unroll
-    for (int ht = 0; ht < H / 32; ++ht) mma32(acc[ht], col_frag<H>(tile, r0 + 16 * ks, ht, lane), b);
+    for (int n = 0; n < kAhead; ++n)
+      if (n <= LAST) read(n, rs, ro);
   }
+  // s += logits of the next tile; work(i), i < 16, is done alongside.
+  template <int LAST, typename Work>
+  __device__ __forceinline__ void logits(f32x16& s, const bf16x8 (&x)[NS], int rs, int ro, Work work) {
+#pragma unroll
+    for (int n = 0; n < NS; ++n) {
+      if (n + kAhead <= LAST) read(n + kAhead, rs, ro);
+      mma32(s, f[n], x[n]);
+#pragma unroll
+      for (int i = n * 16 / NS; i < (n + 1) * 16 / NS; ++i) work(i);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  // acc[ht] += (tile rows)^T p (lane's column, rows in accumulator order);
+  // work(i), i < 4, is done alongside the first half, which needs p[0 .. 7] only.
+  template <typename Work>
+  __device__ __forceinline__ void product(f32x16 (&acc)[H / 32], const u32x4 (&hi)[2], const u32x4 (&lo)[2], int rs,
+                                          int ro, Work work) {
+#pragma unroll
+    for (int n = 0; n < NO; ++n) {
+      const int ks = n / (H / 32), ht = n % (H / 32);
+      if (n + kAhead < NO) read(NS + n + kAhead, rs, ro);
+      mma32(acc[ht], f[NS + n], __builtin_bit_cast(bf16x8, hi[ks]));
+      if (ks == 0) {
+#pragma unroll
+        for (int i = ht * 4 / (H / 32); i < (ht + 1) * 4 / (H / 32); ++i) work(i);
+      }
+      mma32(acc[ht], f[NS + n], __builtin_bit_cast(bf16x8, lo[ks]));
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+};
+
+// Two values as the i-th words of a bf16 pair.
+__device__ __forceinline__ void split2(float a, float b, u32x4& hi, u32x4& lo, int i) {
+  const uint32_t h = pk2(a, b);
+  hi[i] = h;
+  lo[i] = pk2(a - lo_f(h), b - hi_f(h));
 }
+#else
+// float32: a product takes 64 times as long, so that plain code keeps the
+// matrix cores busy.
+template <int H>
+struct VocStep {
+  __device__ __forceinline__ void logits(f32x16& s, const f32x8 (&x)[H / 16], const float* tile, int r0, int lane) {
+#pragma unroll
+    for (int kk = 0; kk < H / 16; ++kk) mma32(s, row_frag<float, H>(tile, r0, kk, lane), x[kk]);
+  }
+  __device__ __forceinline__ void product(f32x16 (&acc)[H / 32], const float (&p)[16], const float* tile, int r0,
+                                          int lane) {
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int ht = 0; ht < H / 32; ++ht)
+        mma32(acc[ht], col_frag<H>(tile, r0 + 16 * ks, ht, lane), pack8<float>(p + 8 * ks));
+  }
+};
+#endif
 
 __device__ __forceinline__ float entry_bias(const float* bias, int v, int V) {
   if (v >= V) return -INFINITY;
@@ -160,14 +243,6 @@ __device__ __forceinline__ void start32(f32x16& acc, const float* a, int lane) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) acc[4 * j4 + i] = v[i];
   }
-}
-
-// One 32 x 32 tile of S^T: logits of the wave's rows (lane's row = lane % 32).
-template <typename S, int H>
-__device__ __forceinline__ void tile_logits(f32x16& acc, const frag_t<S> (&xf)[H / 16], const S* tile, int r0,
-                                            int lane) {
-#pragma unroll
-  for (int kk = 0; kk < H / 16; ++kk) mma32(acc, row_frag<S, H>(tile, r0, kk, lane), xf[kk]);
 }
 
 struct RowBest {   // largest logit so far and the lowest entry that has it
@@ -193,9 +268,18 @@ __device__ __forceinline__ void load_row_frags(frag_t<S> (&f)[H / 16], const S* 
   }
 }
 
-// Rows pass.  Workgroup: row tile blockIdx.x % row_tiles, vocabulary tiles
-// split * per .. + per - 1.  Writes each row's (m in units of log 2, l, O) of
-// its split; SUM: O too; BEST: the largest logit's entry too.
+// The tiles of a workgroup's share pass through three LDS buffers: while one
+// is used, the next one has landed or is landing, and the copies of the one
+// after it go to the buffer that every wave left before the last barrier.
+// Within a wave the logits of the next 32 entries are formed before the
+// current ones are turned into probabilities, so that the matrix cores have
+// work during the exponentials.
+constexpr int kVocBufs = 3;
+__device__ __forceinline__ int next_buf(int b) { return b == kVocBufs - 1 ? 0 : b + 1; }
+
+// Rows pass.  Workgroup: row tile id % row_tiles, vocabulary tiles split * per
+// .. + per - 1.  Writes each row's (m in units of log 2, l, O) of its split;
+// SUM: O too; BEST: the largest logit's entry too.
 template <typename S, int H, bool SUM, bool BEST>
 __global__ __launch_bounds__(kVocThreads) void vocab_rows_kernel(int n_nodes, int R, int V, int row_tiles, int per,
                                                                  const S* __restrict__ X, const S* __restrict__ W,
@@ -204,14 +288,14 @@ __global__ __launch_bounds__(kVocThreads) void vocab_rows_kernel(int n_nodes, in
                                                                  float* __restrict__ pm, float* __restrict__ pl,
                                                                  float* __restrict__ po, RowBest* __restrict__ pb) {
   constexpr int T = voc_tile<S>();
-  __shared__ __attribute__((aligned(1024))) S tile[2][T * H];
-  __shared__ __attribute__((aligned(16))) float tb[2][T];
+  __shared__ __attribute__((aligned(1024))) S tile[kVocBufs][T * H];
+  __shared__ __attribute__((aligned(16))) float tb[kVocBufs][T];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = lane / 32;
   const int id = xcd_swizzle(blockIdx.x, gridDim.x), rt = id % row_tiles, split = id / row_tiles;
   const int Rp = row_tiles * kVocRows;
   const int r = rt * kVocRows + wave * 32 + lane % 32;
   const int tiles = (V + T - 1) / T, t0 = split * per, t1 = min(tiles, t0 + per);
-  const uint32_t lds[2] = {(uint32_t)(uintptr_t)tile[0], (uint32_t)(uintptr_t)tile[1]};
+  const uint32_t lds0 = (uint32_t)(uintptr_t)tile[0];
 
   frag_t<S> xf[H / 16];
   load_row_frags<S, H>(xf, X, row_node(node, r, R, n_nodes), lane);
@@ -223,25 +307,51 @@ __global__ __launch_bounds__(kVocThreads) void vocab_rows_kernel(int n_nodes, in
   float m = kNoMax, l = 0.f;
   RowBest best{-INFINITY, INT_MAX};
   float nb = 0.f;
-  if (t0 < t1) {
-    stage_tile<S, H>(W, (long)t0 * T, V - 1, lds[0], wave, lane);
-    if (threadIdx.x < T) nb = entry_bias(bias, t0 * T + threadIdx.x, V);
-  }
-  for (int t = t0; t < t1; ++t) {
-    const int buf = (t - t0) & 1, v0 = t * T;
+  auto fetch = [&](int t, int buf) {   // start the copies of tile t < t1
+    stage_tile<S, H>(W, (long)t * T, V - 1, lds0 + (uint32_t)(buf * T * H * sizeof(S)), wave, lane);
+    if (threadIdx.x < T) nb = entry_bias(bias, t * T + threadIdx.x, V);
+  };
+  auto land = [&](int buf) {   // and wait for those started last
     if (threadIdx.x < T) tb[buf][threadIdx.x] = nb;
     wait_copies<0>();
-    __syncthreads();   // this tile has landed, and every wave has left the other buffer
-    if (t + 1 < t1) {
-      stage_tile<S, H>(W, (long)v0 + T, V - 1, lds[buf ^ 1], wave, lane);
-      if (threadIdx.x < T) nb = entry_bias(bias, v0 + T + threadIdx.x, V);
-    }
-    const bool plain = bias == nullptr && v0 + T <= V;
+    __syncthreads();
+  };
+  auto start = [&](f32x16& s, int t, int buf, int r0) {   // biases of tile t's entries
+    if (bias == nullptr && (t + 1) * T <= V) s = f32x16{};
+    else start32(s, tb[buf] + r0, lane);
+  };
+  VocStep<H> step;
+  f32x16 s;
+  int buf = 0;
+  if (t0 < t1) {
+    fetch(t0, 0);
+    land(0);
+    if (t0 + 1 < t1) fetch(t0 + 1, 1);
+    start(s, t0, 0, 0);
+#pragma unroll
+    for (int kk = 0; kk < H / 16; ++kk) mma32(s, row_frag<S, H>(tile[0], 0, kk, lane), xf[kk]);
+  }
+#if GGNN_DT_BF16
+  step.init(lds0, lane);
+#endif
+  for (int t = t0; t < t1; ++t) {
+    const int nbuf = next_buf(buf);
 #pragma unroll
     for (int r0 = 0; r0 < T; r0 += 32) {
-      f32x16 s = {};
-      if (!plain) start32(s, tb[buf] + r0, lane);
-      tile_logits<S, H>(s, xf, tile[buf], r0, lane);
+      const bool last = r0 + 32 >= T;
+      const int rs = last ? 0 : r0 + 32;   // of the next tile (after the last one: of what the buffer holds, not used)
+      if (last) {
+        land(nbuf);
+        if (t + 2 < t1) fetch(t + 2, next_buf(nbuf));
+      }
+#if GGNN_DT_BF16
+      constexpr int LAST = SUM ? 2 * (H / 16) - 1 : H / 16 - 1;
+      constexpr uint32_t kTile = T * H * sizeof(S);
+      if (last) step.move_s(nbuf == 0 ? 0u - (kVocBufs - 1) * kTile : kTile);
+      step.template begin<LAST>(rs, r0);
+#endif
+      f32x16 sn;
+      start(sn, last ? t + 1 : t, last ? nbuf : buf, rs);
       float top = s[0];
 #pragma unroll
       for (int j = 1; j < 16; ++j) top = fmaxf(top, s[j]);
@@ -262,16 +372,34 @@ __global__ __launch_bounds__(kVocThreads) void vocab_rows_kernel(int n_nodes, in
         }
       }
       float p[16];
-#pragma unroll
-      for (int j = 0; j < 16; ++j) {
+      auto prob = [&](int j) {
         if constexpr (BEST) {
-          if (s[j] > best.z) best = RowBest{s[j], v0 + r0 + 8 * (j / 4) + 4 * g + j % 4};
+          if (s[j] > best.z) best = RowBest{s[j], t * T + r0 + 8 * (j / 4) + 4 * g + j % 4};
         }
         p[j] = __builtin_amdgcn_exp2f(fmaf(s[j], kLog2e, -m));
         l += p[j];
-      }
-      if constexpr (SUM) add_product<H>(o, p, tile[buf], r0, lane);
+      };
+#if GGNN_DT_BF16
+      u32x4 hi[2], lo[2];
+      __builtin_amdgcn_sched_barrier(0);
+      step.template logits<LAST>(sn, xf, rs, r0, [&](int j) {
+        prob(j);
+        if (SUM && j >= 8 && j % 2 == 1) split2(p[j - 9], p[j - 8], hi[0], lo[0], (j - 9) / 2);
+      });
+      if constexpr (SUM)
+        step.product(o, hi, lo, rs, r0, [&](int i) { split2(p[8 + 2 * i], p[9 + 2 * i], hi[1], lo[1], i); });
+#else
+      step.logits(sn, xf, tile[last ? nbuf : buf], rs, lane);
+#pragma unroll
+      for (int j = 0; j < 16; ++j) prob(j);
+      if constexpr (SUM) step.product(o, p, tile[buf], r0, lane);
+#endif
+      s = sn;
     }
+#if GGNN_DT_BF16
+    if constexpr (SUM) step.move_o(nbuf == 0 ? 0u - (kVocBufs - 1) * (uint32_t)(T * H * sizeof(S)) : (uint32_t)(T * H * sizeof(S)));
+#endif
+    buf = nbuf;
   }
   l += __shfl_xor(l, 32);
   const size_t at = (size_t)split * Rp + r;
@@ -420,11 +548,12 @@ __global__ __launch_bounds__(kVocThreads) void vocab_join_kernel(
   }
 }
 
-// Columns pass.  Workgroup: entries tile blockIdx.x % col_tiles (128 entries,
-// 32 per wave), row tiles split * per .. + per - 1 of the gathered states.
-// Writes its split's share of dW [V][H] and db [V] (db NULL: none).
-template <typename S, int H>
-__global__ __launch_bounds__(kVocThreads) void vocab_cols_kernel(int V, int Rp, int col_tiles, int per,
+// Columns pass.  Workgroup: entries tile id % col_tiles (128 entries, 32 per
+// wave), row tiles split * per .. + per - 1 of the gathered states.  Writes
+// its split's share of dW [V][H] and db [V] (pdb NULL: none).  WEIGHT: each
+// row has a factor of its own; otherwise all have `scale`.
+template <typename S, int H, bool WEIGHT>
+__global__ __launch_bounds__(kVocThreads) void vocab_cols_kernel(int V, int Rp, int col_tiles, int per, float scale,
                                                                  const S* __restrict__ xg,
                                                                  const S* __restrict__ W,
                                                                  const float* __restrict__ bias,
@@ -433,14 +562,14 @@ __global__ __launch_bounds__(kVocThreads) void vocab_cols_kernel(int V, int Rp, 
                                                                  const float* __restrict__ fac_w,
                                                                  float* __restrict__ pw, float* __restrict__ pdb) {
   constexpr int T = voc_tile<S>();
-  __shared__ __attribute__((aligned(1024))) S tile[2][T * H];
-  __shared__ __attribute__((aligned(16))) float tl[2][T], tf[2][T];
-  __shared__ __attribute__((aligned(16))) int tt[2][T];
+  __shared__ __attribute__((aligned(1024))) S tile[kVocBufs][T * H];
+  __shared__ __attribute__((aligned(16))) float tl[kVocBufs][T], tf[kVocBufs][T];
+  __shared__ __attribute__((aligned(16))) int tt[kVocBufs][T];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = lane / 32;
   const int id = xcd_swizzle(blockIdx.x, gridDim.x), ct = id % col_tiles, split = id / col_tiles;
   const int vw = ct * kVocRows + wave * 32, v = vw + lane % 32;
   const int tiles = Rp / T, t0 = split * per, t1 = min(tiles, t0 + per);
-  const uint32_t lds[2] = {(uint32_t)(uintptr_t)tile[0], (uint32_t)(uintptr_t)tile[1]};
+  const uint32_t lds0 = (uint32_t)(uintptr_t)tile[0];
 
   frag_t<S> wf[H / 16];
   load_row_frags<S, H>(wf, W, min(v, V - 1), lane);
@@ -450,54 +579,98 @@ __global__ __launch_bounds__(kVocThreads) void vocab_cols_kernel(int V, int Rp, 
   for (int ht = 0; ht < H / 32; ++ht) a[ht] = f32x16{};
   float db = 0.f, nl = 0.f, nf = 0.f;
   int nt = -1;
-  if (t0 < t1) {
-    stage_tile<S, H>(xg, (long)t0 * T, Rp - 1, lds[0], wave, lane);
+  auto fetch = [&](int t, int buf) {   // start the copies of tile t < t1
+    stage_tile<S, H>(xg, (long)t * T, Rp - 1, lds0 + (uint32_t)(buf * T * H * sizeof(S)), wave, lane);
     if (threadIdx.x < T) {
-      nl = lse_w[t0 * T + threadIdx.x];
-      nt = tgt_w[t0 * T + threadIdx.x];
-      nf = fac_w[t0 * T + threadIdx.x];
+      nl = lse_w[t * T + threadIdx.x];
+      nt = tgt_w[t * T + threadIdx.x];
+      if constexpr (WEIGHT) nf = fac_w[t * T + threadIdx.x];
     }
-  }
-  for (int t = t0; t < t1; ++t) {
-    const int buf = (t - t0) & 1;
+  };
+  auto land = [&](int buf) {   // and wait for those started last
     if (threadIdx.x < T) {
       tl[buf][threadIdx.x] = -nl;
       tt[buf][threadIdx.x] = nt;
-      tf[buf][threadIdx.x] = nf;
+      if constexpr (WEIGHT) tf[buf][threadIdx.x] = nf;
     }
     wait_copies<0>();
-    __syncthreads();   // this tile has landed, and every wave has left the other buffer
-    if (t + 1 < t1) {
-      stage_tile<S, H>(xg, (long)(t + 1) * T, Rp - 1, lds[buf ^ 1], wave, lane);
-      if (threadIdx.x < T) {
-        nl = lse_w[(t + 1) * T + threadIdx.x];
-        nt = tgt_w[(t + 1) * T + threadIdx.x];
-        nf = fac_w[(t + 1) * T + threadIdx.x];
-      }
-    }
+    __syncthreads();
+  };
+  VocStep<H> step;
+  f32x16 s;
+  int buf = 0;
+  if (t0 < t1) {
+    fetch(t0, 0);
+    land(0);
+    if (t0 + 1 < t1) fetch(t0 + 1, 1);
+    start32(s, tl[0], lane);
+#pragma unroll
+    for (int kk = 0; kk < H / 16; ++kk) mma32(s, row_frag<S, H>(tile[0], 0, kk, lane), wf[kk]);
+  }
+#if GGNN_DT_BF16
+  step.init(lds0, lane);
+#endif
+  for (int t = t0; t < t1; ++t) {
+    const int nbuf = next_buf(buf);
 #pragma unroll
     for (int r0 = 0; r0 < T; r0 += 32) {
-      f32x16 s;
-      start32(s, tl[buf] + r0, lane);
-      tile_logits<S, H>(s, wf, tile[buf], r0, lane);
+      const bool last = r0 + 32 >= T;
+      const int rs = last ? 0 : r0 + 32;   // of the next tile (after the last one: of what the buffer holds, not used)
+      if (last) {
+        land(nbuf);
+        if (t + 2 < t1) fetch(t + 2, next_buf(nbuf));
+      }
+#if GGNN_DT_BF16
+      constexpr int LAST = 2 * (H / 16) - 1;
+      constexpr uint32_t kTile = T * H * sizeof(S);
+      if (last) step.move_s(nbuf == 0 ? 0u - (kVocBufs - 1) * kTile : kTile);
+      step.template begin<LAST>(rs, r0);
+#endif
+      f32x16 sn;
+      start32(sn, tl[last ? nbuf : buf] + rs, lane);
+      const int tj = tt[buf][r0 + lane % 32];
       float p[16];
+      auto prob = [&](int j) { p[j] = __builtin_amdgcn_exp2f(fmaf(s[j], kLog2e, b2)); };
+#if GGNN_DT_BF16
+      __builtin_amdgcn_sched_barrier(0);
+      step.template logits<LAST>(sn, wf, rs, r0, prob);
+#else
+      step.logits(sn, wf, tile[last ? nbuf : buf], rs, lane);
 #pragma unroll
-      for (int j = 0; j < 16; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(s[j], kLog2e, b2));
+      for (int j = 0; j < 16; ++j) prob(j);
+#endif
       // the rows' targets, where any falls on this wave's entries
-      if (__ballot((unsigned)(tt[buf][r0 + lane % 32] - vw) < 32u)) {
+      if (__ballot((unsigned)(tj - vw) < 32u)) {
 #pragma unroll
         for (int j = 0; j < 16; ++j)
           if (tt[buf][r0 + 8 * (j / 4) + 4 * g + j % 4] == v) p[j] -= 1.f;
       }
+      if constexpr (WEIGHT) {
 #pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        p[j] *= tf[buf][r0 + 8 * (j / 4) + 4 * g + j % 4];
-        db += p[j];
+        for (int j = 0; j < 16; ++j) p[j] *= tf[buf][r0 + 8 * (j / 4) + 4 * g + j % 4];
       }
-      add_product<H>(a, p, tile[buf], r0, lane);
+#if GGNN_DT_BF16
+      u32x4 hi[2], lo[2];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) split2(p[2 * i], p[2 * i + 1], hi[0], lo[0], i);
+      step.product(a, hi, lo, rs, r0, [&](int i) {
+        split2(p[8 + 2 * i], p[9 + 2 * i], hi[1], lo[1], i);
+        db += (p[4 * i] + p[4 * i + 1]) + (p[4 * i + 2] + p[4 * i + 3]);
+      });
+#else
+#pragma unroll
+      for (int j = 0; j < 16; ++j) db += p[j];
+      step.product(a, p, tile[buf], r0, lane);
+#endif
+      s = sn;
     }
+#if GGNN_DT_BF16
+    step.move_o(nbuf == 0 ? 0u - (kVocBufs - 1) * (uint32_t)(T * H * sizeof(S)) : (uint32_t)(T * H * sizeof(S)));
+#endif
+    buf = nbuf;
   }
-  db += __shfl_xor(db, 32);
+  const float f = WEIGHT ? 1.f : scale;
+  db = (db + __shfl_xor(db, 32)) * f;
   if (v < V) {
     if (pdb != nullptr && g == 0) pdb[(size_t)split * V + v] = db;
     float* out = pw + ((size_t)split * V + v) * H;
@@ -506,7 +679,7 @@ __global__ __launch_bounds__(kVocThreads) void vocab_cols_kernel(int V, int Rp, 
 #pragma unroll
       for (int j4 = 0; j4 < 4; ++j4)
         *reinterpret_cast<f32x4*>(out + 32 * ht + 8 * j4 + 4 * g) =
-            f32x4{a[ht][4 * j4], a[ht][4 * j4 + 1], a[ht][4 * j4 + 2], a[ht][4 * j4 + 3]};
+            f32x4{a[ht][4 * j4] * f, a[ht][4 * j4 + 1] * f, a[ht][4 * j4 + 2] * f, a[ht][4 * j4 + 3] * f};
   }
 }
 
@@ -615,8 +788,12 @@ hipError_t vocab_grad_h(const VocabArgs& c, hipStream_t st) {
   hipLaunchKernelGGL((vocab_join_kernel<S, H, true, false>), dim3(cdiv((long)p.Rp * (H / 4), kVocThreads)),
                      dim3(kVocThreads), 0, st, c.n_nodes, c.R, c.V, p.Rp, p.splits, X, W, c.bias, c.node, c.target,
                      c.weight, c.scale, pm, pl, po, nullptr, c.loss, c.lse, nullptr, c.dX, xg, lse_w, tgt_w, fac_w);
-  hipLaunchKernelGGL((vocab_cols_kernel<S, H>), dim3(p.col_tiles * p.csplits), dim3(kVocThreads), 0, st, c.V, p.Rp,
-                     p.col_tiles, p.cper, xg, W, c.bias, lse_w, tgt_w, fac_w, pw, pdb);
+  if (c.weight != nullptr)
+    hipLaunchKernelGGL((vocab_cols_kernel<S, H, true>), dim3(p.col_tiles * p.csplits), dim3(kVocThreads), 0, st, c.V,
+                       p.Rp, p.col_tiles, p.cper, c.scale, xg, W, c.bias, lse_w, tgt_w, fac_w, pw, pdb);
+  else
+    hipLaunchKernelGGL((vocab_cols_kernel<S, H, false>), dim3(p.col_tiles * p.csplits), dim3(kVocThreads), 0, st,
+                       c.V, p.Rp, p.col_tiles, p.cper, c.scale, xg, W, c.bias, lse_w, tgt_w, fac_w, pw, pdb);
   err = hipGetLastError();
   if (err != hipSuccess) return err;
   ReduceList red;
