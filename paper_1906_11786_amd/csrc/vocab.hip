@@ -274,14 +274,64 @@ __device__ __forceinline__ void load_row_frags(frag_t<S> (&f)[H / 16], const S* 
 // Within a wave the logits of the next 32 entries are formed before the
 // current ones are turned into probabilities, so that the matrix cores have
 // work during the exponentials.
+//
+// Work is dealt in units of one LDS tile against one tile of 128 rows (or, in
+// the columns pass, entries).  `workers` workgroups first take whole 128-tiles,
+// one each a round; the 128-tiles that are left over are laid end to end and
+// cut into equal runs of units, so that all workgroups end together.  A 128-tile
+// is thus one share, or a few neighbouring workers' shares, joined afterwards in
+// that order.
+struct Deal {
+  int workers, tiles;   // workgroups; LDS tiles against one 128-tile
+  int whole, rest;      // 128-tiles dealt whole (a multiple of workers), and cut up
+  int slots;            // shares of a 128-tile, at most
+  // First unit of worker w in the rest, and the worker that has unit u.
+  __host__ __device__ long begin(int w) const { return (long)w * ((long)rest * tiles) / workers; }
+  __host__ __device__ int owner(long u) const { return (int)(((u + 1) * workers - 1) / ((long)rest * tiles)); }
+  // Shares of 128-tile i; share s of it is written to slot i * slots + s.
+  __host__ __device__ int shares(int i) const {
+    if (i < whole) return 1;
+    const long u = (long)(i - whole) * tiles;
+    return owner(u + tiles - 1) - owner(u) + 1;
+  }
+};
+// The next run of worker w: 128-tile, LDS tiles t0 .. t1 - 1, its slot.  `step`
+// counts the runs, `u` the units of the rest (begin(w) at first).
+struct Run {
+  int i, t0, t1, slot;
+};
+__device__ __forceinline__ bool next_run(const Deal& d, int w, int step, long& u, Run* r) {
+  if (step < d.whole / d.workers) {
+    *r = Run{step * d.workers + w, 0, d.tiles, 0};
+    r->slot = r->i * d.slots;
+    return true;
+  }
+  const long end = d.rest > 0 ? d.begin(w + 1) : 0;
+  if (u >= end) return false;
+  const int k = (int)(u / d.tiles);
+  r->i = d.whole + k;
+  r->t0 = (int)(u - (long)k * d.tiles);
+  r->t1 = (int)min((long)d.tiles, r->t0 + (end - u));
+  r->slot = r->i * d.slots + w - d.owner((long)k * d.tiles);
+  u += r->t1 - r->t0;
+  return true;
+}
+
+// Workgroups of a pass that a compute unit holds (waves per SIMD): by the
+// accumulators and fragments that a wave keeps, and at H = 256 by the buffers.
+template <typename S>
+constexpr int voc_waves(int H, bool sum) {
+  if (sizeof(S) == 4) return H <= 64 ? 2 : 1;
+  return H >= 256 ? 1 : H == 128 ? (sum ? 2 : 3) : H == 64 ? 3 : 4;
+}
+
 constexpr int kVocBufs = 3;
 __device__ __forceinline__ int next_buf(int b) { return b == kVocBufs - 1 ? 0 : b + 1; }
 
-// Rows pass.  Workgroup: row tile id % row_tiles, vocabulary tiles split * per
-// .. + per - 1.  Writes each row's (m in units of log 2, l, O) of its split;
-// SUM: O too; BEST: the largest logit's entry too.
+// Rows pass.  Writes each row's (m in units of log 2, l) of a share to pm, pl
+// [slot][128]; SUM: O too; BEST: the largest logit's entry too.
 template <typename S, int H, bool SUM, bool BEST>
-__global__ __launch_bounds__(kVocThreads) void vocab_rows_kernel(int n_nodes, int R, int V, int row_tiles, int per,
+__global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_kernel(int n_nodes, int R, int V, Deal deal,
                                                                  const S* __restrict__ X, const S* __restrict__ W,
                                                                  const float* __restrict__ bias,
                                                                  const int32_t* __restrict__ node,
@@ -291,133 +341,135 @@ __global__ __launch_bounds__(kVocThreads) void vocab_rows_kernel(int n_nodes, in
   __shared__ __attribute__((aligned(1024))) S tile[kVocBufs][T * H];
   __shared__ __attribute__((aligned(16))) float tb[kVocBufs][T];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = lane / 32;
-  const int id = xcd_swizzle(blockIdx.x, gridDim.x), rt = id % row_tiles, split = id / row_tiles;
-  const int Rp = row_tiles * kVocRows;
-  const int r = rt * kVocRows + wave * 32 + lane % 32;
-  const int tiles = (V + T - 1) / T, t0 = split * per, t1 = min(tiles, t0 + per);
   const uint32_t lds0 = (uint32_t)(uintptr_t)tile[0];
 
-  frag_t<S> xf[H / 16];
-  load_row_frags<S, H>(xf, X, row_node(node, r, R, n_nodes), lane);
-  f32x16 o[H / 32];
-  if constexpr (SUM) {
-#pragma unroll
-    for (int ht = 0; ht < H / 32; ++ht) o[ht] = f32x16{};
-  }
-  float m = kNoMax, l = 0.f;
-  RowBest best{-INFINITY, INT_MAX};
   float nb = 0.f;
-  auto fetch = [&](int t, int buf) {   // start the copies of tile t < t1
-    stage_tile<S, H>(W, (long)t * T, V - 1, lds0 + (uint32_t)(buf * T * H * sizeof(S)), wave, lane);
-    if (threadIdx.x < T) nb = entry_bias(bias, t * T + threadIdx.x, V);
-  };
-  auto land = [&](int buf) {   // and wait for those started last
-    if (threadIdx.x < T) tb[buf][threadIdx.x] = nb;
-    wait_copies<0>();
-    __syncthreads();
-  };
-  auto start = [&](f32x16& s, int t, int buf, int r0) {   // biases of tile t's entries
-    if (bias == nullptr && (t + 1) * T <= V) s = f32x16{};
-    else start32(s, tb[buf] + r0, lane);
-  };
-  VocStep<H> step;
-  f32x16 s;
-  int buf = 0;
-  if (t0 < t1) {
-    fetch(t0, 0);
-    land(0);
-    if (t0 + 1 < t1) fetch(t0 + 1, 1);
-    start(s, t0, 0, 0);
+  long unit = deal.begin(blockIdx.x);
+  Run run;
+  for (int round = 0; next_run(deal, blockIdx.x, round, unit, &run); ++round) {
+    const int t0 = run.t0, t1 = run.t1;
+    frag_t<S> xf[H / 16];
+    load_row_frags<S, H>(xf, X, row_node(node, run.i * kVocRows + wave * 32 + lane % 32, R, n_nodes), lane);
+    f32x16 o[H / 32];
+    if constexpr (SUM) {
 #pragma unroll
-    for (int kk = 0; kk < H / 16; ++kk) mma32(s, row_frag<S, H>(tile[0], 0, kk, lane), xf[kk]);
-  }
-#if GGNN_DT_BF16
-  step.init(lds0, lane);
-#endif
-  for (int t = t0; t < t1; ++t) {
-    const int nbuf = next_buf(buf);
+      for (int ht = 0; ht < H / 32; ++ht) o[ht] = f32x16{};
+    }
+    float m = kNoMax, l = 0.f;
+    RowBest best{-INFINITY, INT_MAX};
+    auto fetch = [&](int t, int buf) {   // start the copies of tile t < t1
+      stage_tile<S, H>(W, (long)t * T, V - 1, lds0 + (uint32_t)(buf * T * H * sizeof(S)), wave, lane);
+      if (threadIdx.x < T) nb = entry_bias(bias, t * T + threadIdx.x, V);
+    };
+    auto land = [&](int buf) {   // and wait for those started last
+      if (threadIdx.x < T) tb[buf][threadIdx.x] = nb;
+      wait_copies<0>();
+      __syncthreads();
+    };
+    auto start = [&](f32x16& s, int t, int buf, int r0) {   // biases of tile t's entries
+      if (bias == nullptr && (t + 1) * T <= V) s = f32x16{};
+      else start32(s, tb[buf] + r0, lane);
+    };
+    VocStep<H> step;
+    f32x16 s;
+    int buf = 0;
+    if (round > 0) __syncthreads();   // every wave has left the buffers of the run before
+    {
+      fetch(t0, 0);
+      land(0);
+      if (t0 + 1 < t1) fetch(t0 + 1, 1);
+      start(s, t0, 0, 0);
 #pragma unroll
-    for (int r0 = 0; r0 < T; r0 += 32) {
-      const bool last = r0 + 32 >= T;
-      const int rs = last ? 0 : r0 + 32;   // of the next tile (after the last one: of what the buffer holds, not used)
-      if (last) {
-        land(nbuf);
-        if (t + 2 < t1) fetch(t + 2, next_buf(nbuf));
-      }
-#if GGNN_DT_BF16
-      constexpr int LAST = SUM ? 2 * (H / 16) - 1 : H / 16 - 1;
-      constexpr uint32_t kTile = T * H * sizeof(S);
-      if (last) step.move_s(nbuf == 0 ? 0u - (kVocBufs - 1) * kTile : kTile);
-      step.template begin<LAST>(rs, r0);
-#endif
-      f32x16 sn;
-      start(sn, last ? t + 1 : t, last ? nbuf : buf, rs);
-      float top = s[0];
-#pragma unroll
-      for (int j = 1; j < 16; ++j) top = fmaxf(top, s[j]);
-      top *= kLog2e;
-      // The maximum follows only where it would grow by more than 2^8: until
-      // then the terms stay below 2^8 and the sums lose nothing.
-      if (__ballot(top > m + 8.f)) {
-        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-        const float mn = fmaxf(m, fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])));
-        const float f = __builtin_amdgcn_exp2f(m - mn);
-        m = mn;
-        l *= f;
-        if constexpr (SUM) {
-#pragma unroll
-          for (int ht = 0; ht < H / 32; ++ht)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) o[ht][j] *= f;
-        }
-      }
-      float p[16];
-      auto prob = [&](int j) {
-        if constexpr (BEST) {
-          if (s[j] > best.z) best = RowBest{s[j], t * T + r0 + 8 * (j / 4) + 4 * g + j % 4};
-        }
-        p[j] = __builtin_amdgcn_exp2f(fmaf(s[j], kLog2e, -m));
-        l += p[j];
-      };
-#if GGNN_DT_BF16
-      u32x4 hi[2], lo[2];
-      __builtin_amdgcn_sched_barrier(0);
-      step.template logits<LAST>(sn, xf, rs, r0, [&](int j) {
-        prob(j);
-        if (SUM && j >= 8 && j % 2 == 1) split2(p[j - 9], p[j - 8], hi[0], lo[0], (j - 9) / 2);
-      });
-      if constexpr (SUM)
-        step.product(o, hi, lo, rs, r0, [&](int i) { split2(p[8 + 2 * i], p[9 + 2 * i], hi[1], lo[1], i); });
-#else
-      step.logits(sn, xf, tile[last ? nbuf : buf], rs, lane);
-#pragma unroll
-      for (int j = 0; j < 16; ++j) prob(j);
-      if constexpr (SUM) step.product(o, p, tile[buf], r0, lane);
-#endif
-      s = sn;
+      for (int kk = 0; kk < H / 16; ++kk) mma32(s, row_frag<S, H>(tile[0], 0, kk, lane), xf[kk]);
     }
 #if GGNN_DT_BF16
-    if constexpr (SUM) step.move_o(nbuf == 0 ? 0u - (kVocBufs - 1) * (uint32_t)(T * H * sizeof(S)) : (uint32_t)(T * H * sizeof(S)));
+    step.init(lds0, lane);
 #endif
-    buf = nbuf;
-  }
-  l += __shfl_xor(l, 32);
-  const size_t at = (size_t)split * Rp + r;
-  if constexpr (BEST) {
-    take_best(best, __shfl_xor(best.z, 32), __shfl_xor(best.v, 32));
-    if (g == 0) pb[at] = best;
-  }
-  if (g == 0) {
-    pm[at] = m;
-    pl[at] = l;
-  }
-  if constexpr (SUM) {
+    for (int t = t0; t < t1; ++t) {
+      const int nbuf = next_buf(buf);
 #pragma unroll
-    for (int ht = 0; ht < H / 32; ++ht)
+      for (int r0 = 0; r0 < T; r0 += 32) {
+        const bool last = r0 + 32 >= T;
+        const int rs = last ? 0 : r0 + 32;   // of the next tile (after the last one: of what the buffer holds, not used)
+        if (last) {
+          land(nbuf);
+          if (t + 2 < t1) fetch(t + 2, next_buf(nbuf));
+        }
+#if GGNN_DT_BF16
+        constexpr int LAST = SUM ? 2 * (H / 16) - 1 : H / 16 - 1;
+        constexpr uint32_t kTile = T * H * sizeof(S);
+        if (last) step.move_s(nbuf == 0 ? 0u - (kVocBufs - 1) * kTile : kTile);
+        step.template begin<LAST>(rs, r0);
+#endif
+        f32x16 sn;
+        start(sn, last ? t + 1 : t, last ? nbuf : buf, rs);
+        float top = s[0];
 #pragma unroll
-      for (int j4 = 0; j4 < 4; ++j4)
-        *reinterpret_cast<f32x4*>(po + at * H + 32 * ht + 8 * j4 + 4 * g) =
-            f32x4{o[ht][4 * j4], o[ht][4 * j4 + 1], o[ht][4 * j4 + 2], o[ht][4 * j4 + 3]};
+        for (int j = 1; j < 16; ++j) top = fmaxf(top, s[j]);
+        top *= kLog2e;
+        // The maximum follows only where it would grow by more than 2^8: until
+        // then the terms stay below 2^8 and the sums lose nothing.
+        if (__ballot(top > m + 8.f)) {
+          const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+          const float mn = fmaxf(m, fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])));
+          const float f = __builtin_amdgcn_exp2f(m - mn);
+          m = mn;
+          l *= f;
+          if constexpr (SUM) {
+#pragma unroll
+            for (int ht = 0; ht < H / 32; ++ht)
+#pragma unroll
+              for (int j = 0; j < 16; ++j) o[ht][j] *= f;
+          }
+        }
+        float p[16];
+        auto prob = [&](int j) {
+          if constexpr (BEST) {
+            if (s[j] > best.z) best = RowBest{s[j], t * T + r0 + 8 * (j / 4) + 4 * g + j % 4};
+          }
+          p[j] = __builtin_amdgcn_exp2f(fmaf(s[j], kLog2e, -m));
+          l += p[j];
+        };
+#if GGNN_DT_BF16
+        u32x4 hi[2], lo[2];
+        __builtin_amdgcn_sched_barrier(0);
+        step.template logits<LAST>(sn, xf, rs, r0, [&](int j) {
+          prob(j);
+          if (SUM && j >= 8 && j % 2 == 1) split2(p[j - 9], p[j - 8], hi[0], lo[0], (j - 9) / 2);
+        });
+        if constexpr (SUM)
+          step.product(o, hi, lo, rs, r0, [&](int i) { split2(p[8 + 2 * i], p[9 + 2 * i], hi[1], lo[1], i); });
+#else
+        step.logits(sn, xf, tile[last ? nbuf : buf], rs, lane);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) prob(j);
+        if constexpr (SUM) step.product(o, p, tile[buf], r0, lane);
+#endif
+        s = sn;
+      }
+#if GGNN_DT_BF16
+      if constexpr (SUM) step.move_o(nbuf == 0 ? 0u - (kVocBufs - 1) * (uint32_t)(T * H * sizeof(S)) : (uint32_t)(T * H * sizeof(S)));
+#endif
+      buf = nbuf;
+    }
+    l += __shfl_xor(l, 32);
+    const size_t at = (size_t)run.slot * kVocRows + wave * 32 + lane % 32;
+    if constexpr (BEST) {
+      take_best(best, __shfl_xor(best.z, 32), __shfl_xor(best.v, 32));
+      if (g == 0) pb[at] = best;
+    }
+    if (g == 0) {
+      pm[at] = m;
+      pl[at] = l;
+    }
+    if constexpr (SUM) {
+#pragma unroll
+      for (int ht = 0; ht < H / 32; ++ht)
+#pragma unroll
+        for (int j4 = 0; j4 < 4; ++j4)
+          *reinterpret_cast<f32x4*>(po + at * H + 32 * ht + 8 * j4 + 4 * g) =
+              f32x4{o[ht][4 * j4], o[ht][4 * j4 + 1], o[ht][4 * j4 + 2], o[ht][4 * j4 + 3]};
+    }
   }
 }
 
@@ -473,13 +525,102 @@ __global__ __launch_bounds__(kVocThreads) void vocab_few_kernel(int n_nodes, int
   }
 }
 
-// Joins the splits' shares of a row: H / 4 lanes per row, four features each.
-// GRAD: writes dX's row, and what the columns pass reads: the row's state
-// (zero rows up to Rp), its lse (infinite for rows without a gradient, whose
-// probabilities then vanish), target (-1) and factor.
+// One row's (m, l, best) from its shares, held by L neighbouring lanes (q: the
+// lane's place); share s lies at at0 + s * stride.
+template <int L, bool BEST>
+__device__ __forceinline__ void join_shares(int n, size_t at0, size_t stride, int q, const float* __restrict__ pm,
+                                            const float* __restrict__ pl, const RowBest* __restrict__ pb, float& M,
+                                            float& sum, RowBest& best) {
+  M = kNoMax;
+  sum = 0.f;
+  best = RowBest{-INFINITY, INT_MAX};
+  constexpr int U = 4;   // shares in flight per lane
+  for (int s0 = q; s0 < n; s0 += L * U) {
+    float m[U], l[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int s = s0 + u * L;
+      const size_t at = at0 + (size_t)(s < n ? s : s0) * stride;
+      m[u] = s < n ? pm[at] : kNoMax;
+      l[u] = s < n ? pl[at] : 0.f;
+      if (BEST && s < n) take_best(best, pb[at].z, pb[at].v);
+    }
+    float top = M;
+#pragma unroll
+    for (int u = 0; u < U; ++u) top = fmaxf(top, m[u]);
+    sum *= __builtin_amdgcn_exp2f(M - top);
+#pragma unroll
+    for (int u = 0; u < U; ++u) sum += l[u] * __builtin_amdgcn_exp2f(m[u] - top);
+    M = top;
+  }
+#pragma unroll
+  for (int o = L / 2; o >= 1; o /= 2) {
+    const float m2 = __shfl_xor(M, o), s2 = __shfl_xor(sum, o), top = fmaxf(M, m2);
+    sum = sum * __builtin_amdgcn_exp2f(M - top) + s2 * __builtin_amdgcn_exp2f(m2 - top);
+    M = top;
+    if (BEST) take_best(best, __shfl_xor(best.z, o), __shfl_xor(best.v, o));
+  }
+}
+// lse of a row: -inf where every entry is masked.
+__device__ __forceinline__ float row_lse(float M, float sum) {
+  return sum == 0.f ? -INFINITY : (M + __log2f(sum)) * kLn2;
+}
+__device__ __forceinline__ float row_loss(float lse, float zt, int t, bool bad) {
+  return bad ? NAN : t < 0 ? 0.f : lse == -INFINITY ? INFINITY : lse - zt;
+}
+
+// The loss of at most 32 rows from the many shares of vocab_few_kernel: one
+// workgroup per row.
+template <typename S, int H, bool BEST>
+__global__ __launch_bounds__(kVocThreads) void vocab_few_join_kernel(
+    int n_nodes, int R, int V, int splits, const S* __restrict__ X, const S* __restrict__ W,
+    const float* __restrict__ bias, const int32_t* __restrict__ node, const int32_t* __restrict__ target,
+    const float* __restrict__ pm, const float* __restrict__ pl, const RowBest* __restrict__ pb,
+    float* __restrict__ loss, float* __restrict__ lse, int32_t* __restrict__ best) {
+  __shared__ float wm[kVocWaves], wl[kVocWaves], wz[kVocWaves];
+  __shared__ RowBest wb[kVocWaves];
+  const int r = blockIdx.x, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int n = row_node(node, r, R, n_nodes);
+  int t = n >= 0 && target != nullptr ? target[r] : -1;
+  const bool bad = t >= V;
+  if (bad) t = -1;
+  float z = 0.f;
+  if (t >= 0 && threadIdx.x < H) z = to_f<S>(X[(size_t)n * H + threadIdx.x]) * to_f<S>(W[(size_t)t * H + threadIdx.x]);
+  // each wave takes every fourth share
+  float M, sum;
+  RowBest b;
+  join_shares<kWave, BEST>((splits - wave + kVocWaves - 1) / kVocWaves, (size_t)wave * 32 + r, (size_t)kVocWaves * 32,
+                           lane, pm, pl, pb, M, sum, b);
+#pragma unroll
+  for (int o = kWave / 2; o >= 1; o /= 2) z += __shfl_xor(z, o);
+  if (lane == 0) {
+    wm[wave] = M;
+    wl[wave] = sum;
+    wz[wave] = z;
+    wb[wave] = b;
+  }
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  for (int w = 1; w < kVocWaves; ++w) {
+    const float top = fmaxf(M, wm[w]);
+    sum = sum * __builtin_amdgcn_exp2f(M - top) + wl[w] * __builtin_amdgcn_exp2f(wm[w] - top);
+    M = top;
+    z += wz[w];
+    if (BEST) take_best(b, wb[w].z, wb[w].v);
+  }
+  const float v = row_lse(M, sum);
+  lse[r] = v;
+  if (loss != nullptr) loss[r] = row_loss(v, t >= 0 ? z + entry_bias(bias, t, V) : 0.f, t, bad);
+  if (BEST) best[r] = b.v == INT_MAX ? -1 : b.v;
+}
+
+// Joins the shares of a row: H / 4 lanes per row, four features each.  GRAD:
+// writes dX's row, and what the columns pass reads: the row's state (zero rows
+// up to the end of the last 128-tile), its lse (infinite for rows without a
+// gradient, whose probabilities then vanish), target (-1) and factor.
 template <typename S, int H, bool GRAD, bool BEST>
 __global__ __launch_bounds__(kVocThreads) void vocab_join_kernel(
-    int n_nodes, int R, int V, int Rp, int splits, const S* __restrict__ X, const S* __restrict__ W,
+    int n_nodes, int R, int V, int Rp, Deal deal, const S* __restrict__ X, const S* __restrict__ W,
     const float* __restrict__ bias, const int32_t* __restrict__ node, const int32_t* __restrict__ target,
     const float* __restrict__ weight, float scale, const float* __restrict__ pm, const float* __restrict__ pl,
     const float* __restrict__ po, const RowBest* __restrict__ pb, float* __restrict__ loss, float* __restrict__ lse,
@@ -491,56 +632,38 @@ __global__ __launch_bounds__(kVocThreads) void vocab_join_kernel(
   if (r >= (GRAD ? Rp : R)) return;   // whole groups of L lanes leave together
   const int n = row_node(node, r, R, n_nodes);
   const f32x4 x = n >= 0 ? load4f(X + (size_t)n * H + h) : f32x4{};
-  float M = kNoMax, sum = 0.f;
-  if (r < R) {
-    for (int s = q; s < splits; s += L) M = fmaxf(M, pm[(size_t)s * Rp + r]);
-#pragma unroll
-    for (int o = L / 2; o >= 1; o /= 2) M = fmaxf(M, __shfl_xor(M, o));
-    for (int s = q; s < splits; s += L)
-      sum += pl[(size_t)s * Rp + r] * __builtin_amdgcn_exp2f(pm[(size_t)s * Rp + r] - M);
-#pragma unroll
-    for (int o = L / 2; o >= 1; o /= 2) sum += __shfl_xor(sum, o);
-  }
-  int t = r < R && n >= 0 && target != nullptr ? target[r] : -1;
+  const int shares = r < R ? deal.shares(r / kVocRows) : 0;
+  const size_t at0 = (size_t)(r / kVocRows) * deal.slots * kVocRows + r % kVocRows;
+  int t = n >= 0 && target != nullptr ? target[r] : -1;
   const bool bad = t >= V;
   if (bad) t = -1;
-  f32x4 w = {};
-  float zt = 0.f;
-  if (t >= 0) {
-    w = load4f(W + (size_t)t * H + h);
-    zt = x[0] * w[0] + x[1] * w[1] + x[2] * w[2] + x[3] * w[3];
-  }
+  const f32x4 w = t >= 0 ? load4f(W + (size_t)t * H + h) : f32x4{};
+  float M, sum;
+  RowBest b;
+  join_shares<L, BEST>(shares, at0, kVocRows, q, pm, pl, pb, M, sum, b);
+  float zt = x[0] * w[0] + x[1] * w[1] + x[2] * w[2] + x[3] * w[3];
 #pragma unroll
   for (int o = L / 2; o >= 1; o /= 2) zt += __shfl_xor(zt, o);
-  const float row_lse = sum == 0.f ? -INFINITY : (M + __log2f(sum)) * kLn2;   // every entry masked: -inf
+  const float v = row_lse(M, sum);
   if (r < R && q == 0) {
-    lse[r] = row_lse;
-    if (loss != nullptr) {
-      float v = 0.f;
-      if (t >= 0) v = sum == 0.f ? INFINITY : row_lse - (zt + entry_bias(bias, t, V));
-      loss[r] = bad ? NAN : v;
-    }
-  }
-  if constexpr (BEST) {
-    RowBest b{-INFINITY, INT_MAX};
-    for (int s = q; s < splits; s += L) take_best(b, pb[(size_t)s * Rp + r].z, pb[(size_t)s * Rp + r].v);
-#pragma unroll
-    for (int o = L / 2; o >= 1; o /= 2) take_best(b, __shfl_xor(b.z, o), __shfl_xor(b.v, o));
-    if (q == 0) best[r] = b.v == INT_MAX ? -1 : b.v;
+    lse[r] = v;
+    if (loss != nullptr) loss[r] = row_loss(v, t >= 0 ? zt + entry_bias(bias, t, V) : 0.f, t, bad);
+    if (BEST) best[r] = b.v == INT_MAX ? -1 : b.v;
   }
   if constexpr (GRAD) {
     const float f = (weight != nullptr && r < R ? weight[r] : 1.f) * scale;
     const bool live = t >= 0 && sum != 0.f;
     store4(xg + (size_t)r * H + h, x[0], x[1], x[2], x[3]);
     if (q == 0) {
-      lse_w[r] = live ? row_lse : INFINITY;
+      lse_w[r] = live ? v : INFINITY;
       tgt_w[r] = live ? t : -1;
       fac_w[r] = f;
     }
     if (live) {
       f32x4 o = {};
-      for (int s = 0; s < splits; ++s) {
-        const size_t at = (size_t)s * Rp + r;
+#pragma unroll 8
+      for (int s = 0; s < shares; ++s) {
+        const size_t at = at0 + (size_t)s * kVocRows;
         o += *reinterpret_cast<const f32x4*>(po + at * H + h) * __builtin_amdgcn_exp2f(pm[at] - M);
       }
       *reinterpret_cast<f32x4*>(dX + (size_t)n * H + h) = (o * (1.f / sum) - w) * f;
@@ -548,138 +671,176 @@ __global__ __launch_bounds__(kVocThreads) void vocab_join_kernel(
   }
 }
 
-// Columns pass.  Workgroup: entries tile id % col_tiles (128 entries, 32 per
-// wave), row tiles split * per .. + per - 1 of the gathered states.  Writes
-// its split's share of dW [V][H] and db [V] (pdb NULL: none).  WEIGHT: each
-// row has a factor of its own; otherwise all have `scale`.
+// Columns pass: 128 entries of a workgroup (32 per wave) against the gathered states.  Adds to dW [V][H] and db [V] (dbias NULL:
+// none) where the 128-tile is one share, else writes its share to pw
+// [slot][128][H] and pdb [slot][128].  WEIGHT: each row has a factor of its
+// own; otherwise all have `scale`.
 template <typename S, int H, bool WEIGHT>
-__global__ __launch_bounds__(kVocThreads) void vocab_cols_kernel(int V, int Rp, int col_tiles, int per, float scale,
+__global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols_kernel(int V, int Rp, Deal deal, float scale,
                                                                  const S* __restrict__ xg,
                                                                  const S* __restrict__ W,
                                                                  const float* __restrict__ bias,
                                                                  const float* __restrict__ lse_w,
                                                                  const int32_t* __restrict__ tgt_w,
                                                                  const float* __restrict__ fac_w,
+                                                                 float* __restrict__ dW, float* __restrict__ dbias,
                                                                  float* __restrict__ pw, float* __restrict__ pdb) {
   constexpr int T = voc_tile<S>();
   __shared__ __attribute__((aligned(1024))) S tile[kVocBufs][T * H];
   __shared__ __attribute__((aligned(16))) float tl[kVocBufs][T], tf[kVocBufs][T];
   __shared__ __attribute__((aligned(16))) int tt[kVocBufs][T];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = lane / 32;
-  const int id = xcd_swizzle(blockIdx.x, gridDim.x), ct = id % col_tiles, split = id / col_tiles;
-  const int vw = ct * kVocRows + wave * 32, v = vw + lane % 32;
-  const int tiles = Rp / T, t0 = split * per, t1 = min(tiles, t0 + per);
   const uint32_t lds0 = (uint32_t)(uintptr_t)tile[0];
 
-  frag_t<S> wf[H / 16];
-  load_row_frags<S, H>(wf, W, min(v, V - 1), lane);
-  const float b2 = entry_bias(bias, v, V) * kLog2e;
-  f32x16 a[H / 32];
-#pragma unroll
-  for (int ht = 0; ht < H / 32; ++ht) a[ht] = f32x16{};
-  float db = 0.f, nl = 0.f, nf = 0.f;
+  float nl = 0.f, nf = 0.f;
   int nt = -1;
-  auto fetch = [&](int t, int buf) {   // start the copies of tile t < t1
-    stage_tile<S, H>(xg, (long)t * T, Rp - 1, lds0 + (uint32_t)(buf * T * H * sizeof(S)), wave, lane);
-    if (threadIdx.x < T) {
-      nl = lse_w[t * T + threadIdx.x];
-      nt = tgt_w[t * T + threadIdx.x];
-      if constexpr (WEIGHT) nf = fac_w[t * T + threadIdx.x];
-    }
-  };
-  auto land = [&](int buf) {   // and wait for those started last
-    if (threadIdx.x < T) {
-      tl[buf][threadIdx.x] = -nl;
-      tt[buf][threadIdx.x] = nt;
-      if constexpr (WEIGHT) tf[buf][threadIdx.x] = nf;
-    }
-    wait_copies<0>();
-    __syncthreads();
-  };
-  VocStep<H> step;
-  f32x16 s;
-  int buf = 0;
-  if (t0 < t1) {
-    fetch(t0, 0);
-    land(0);
-    if (t0 + 1 < t1) fetch(t0 + 1, 1);
-    start32(s, tl[0], lane);
+  long unit = deal.begin(blockIdx.x);
+  Run run;
+  for (int round = 0; next_run(deal, blockIdx.x, round, unit, &run); ++round) {
+    const int t0 = run.t0, t1 = run.t1, vw = run.i * kVocRows + wave * 32, v = vw + lane % 32;
+    frag_t<S> wf[H / 16];
+    load_row_frags<S, H>(wf, W, min(v, V - 1), lane);
+    const float b2 = entry_bias(bias, v, V) * kLog2e;
+    f32x16 a[H / 32];
 #pragma unroll
-    for (int kk = 0; kk < H / 16; ++kk) mma32(s, row_frag<S, H>(tile[0], 0, kk, lane), wf[kk]);
-  }
-#if GGNN_DT_BF16
-  step.init(lds0, lane);
-#endif
-  for (int t = t0; t < t1; ++t) {
-    const int nbuf = next_buf(buf);
-#pragma unroll
-    for (int r0 = 0; r0 < T; r0 += 32) {
-      const bool last = r0 + 32 >= T;
-      const int rs = last ? 0 : r0 + 32;   // of the next tile (after the last one: of what the buffer holds, not used)
-      if (last) {
-        land(nbuf);
-        if (t + 2 < t1) fetch(t + 2, next_buf(nbuf));
+    for (int ht = 0; ht < H / 32; ++ht) a[ht] = f32x16{};
+    float db = 0.f;
+    auto fetch = [&](int t, int buf) {   // start the copies of tile t < t1
+      stage_tile<S, H>(xg, (long)t * T, Rp - 1, lds0 + (uint32_t)(buf * T * H * sizeof(S)), wave, lane);
+      if (threadIdx.x < T) {
+        nl = lse_w[t * T + threadIdx.x];
+        nt = tgt_w[t * T + threadIdx.x];
+        if constexpr (WEIGHT) nf = fac_w[t * T + threadIdx.x];
       }
+    };
+    auto land = [&](int buf) {   // and wait for those started last
+      if (threadIdx.x < T) {
+        tl[buf][threadIdx.x] = -nl;
+        tt[buf][threadIdx.x] = nt;
+        if constexpr (WEIGHT) tf[buf][threadIdx.x] = nf;
+      }
+      wait_copies<0>();
+      __syncthreads();
+    };
+    VocStep<H> step;
+    f32x16 s;
+    int buf = 0;
+    if (round > 0) __syncthreads();   // every wave has left the buffers of the run before
+    {
+      fetch(t0, 0);
+      land(0);
+      if (t0 + 1 < t1) fetch(t0 + 1, 1);
+      start32(s, tl[0], lane);
+#pragma unroll
+      for (int kk = 0; kk < H / 16; ++kk) mma32(s, row_frag<S, H>(tile[0], 0, kk, lane), wf[kk]);
+    }
 #if GGNN_DT_BF16
-      constexpr int LAST = 2 * (H / 16) - 1;
-      constexpr uint32_t kTile = T * H * sizeof(S);
-      if (last) step.move_s(nbuf == 0 ? 0u - (kVocBufs - 1) * kTile : kTile);
-      step.template begin<LAST>(rs, r0);
+    step.init(lds0, lane);
 #endif
-      f32x16 sn;
-      start32(sn, tl[last ? nbuf : buf] + rs, lane);
-      const int tj = tt[buf][r0 + lane % 32];
-      float p[16];
-      auto prob = [&](int j) { p[j] = __builtin_amdgcn_exp2f(fmaf(s[j], kLog2e, b2)); };
+    for (int t = t0; t < t1; ++t) {
+      const int nbuf = next_buf(buf);
+#pragma unroll
+      for (int r0 = 0; r0 < T; r0 += 32) {
+        const bool last = r0 + 32 >= T;
+        const int rs = last ? 0 : r0 + 32;   // of the next tile (after the last one: of what the buffer holds, not used)
+        if (last) {
+          land(nbuf);
+          if (t + 2 < t1) fetch(t + 2, next_buf(nbuf));
+        }
 #if GGNN_DT_BF16
-      __builtin_amdgcn_sched_barrier(0);
-      step.template logits<LAST>(sn, wf, rs, r0, prob);
+        constexpr int LAST = 2 * (H / 16) - 1;
+        constexpr uint32_t kTile = T * H * sizeof(S);
+        if (last) step.move_s(nbuf == 0 ? 0u - (kVocBufs - 1) * kTile : kTile);
+        step.template begin<LAST>(rs, r0);
+#endif
+        f32x16 sn;
+        start32(sn, tl[last ? nbuf : buf] + rs, lane);
+        const int tj = tt[buf][r0 + lane % 32];
+        float p[16];
+        auto prob = [&](int j) { p[j] = __builtin_amdgcn_exp2f(fmaf(s[j], kLog2e, b2)); };
+#if GGNN_DT_BF16
+        __builtin_amdgcn_sched_barrier(0);
+        step.template logits<LAST>(sn, wf, rs, r0, prob);
 #else
-      step.logits(sn, wf, tile[last ? nbuf : buf], rs, lane);
+        step.logits(sn, wf, tile[last ? nbuf : buf], rs, lane);
 #pragma unroll
-      for (int j = 0; j < 16; ++j) prob(j);
+        for (int j = 0; j < 16; ++j) prob(j);
 #endif
-      // the rows' targets, where any falls on this wave's entries
-      if (__ballot((unsigned)(tj - vw) < 32u)) {
+        // the rows' targets, where any falls on this wave's entries
+        if (__ballot((unsigned)(tj - vw) < 32u)) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j)
-          if (tt[buf][r0 + 8 * (j / 4) + 4 * g + j % 4] == v) p[j] -= 1.f;
-      }
-      if constexpr (WEIGHT) {
+          for (int j = 0; j < 16; ++j)
+            if (tt[buf][r0 + 8 * (j / 4) + 4 * g + j % 4] == v) p[j] -= 1.f;
+        }
+        if constexpr (WEIGHT) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) p[j] *= tf[buf][r0 + 8 * (j / 4) + 4 * g + j % 4];
-      }
+          for (int j = 0; j < 16; ++j) p[j] *= tf[buf][r0 + 8 * (j / 4) + 4 * g + j % 4];
+        }
 #if GGNN_DT_BF16
-      u32x4 hi[2], lo[2];
+        u32x4 hi[2], lo[2];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) split2(p[2 * i], p[2 * i + 1], hi[0], lo[0], i);
-      step.product(a, hi, lo, rs, r0, [&](int i) {
-        split2(p[8 + 2 * i], p[9 + 2 * i], hi[1], lo[1], i);
-        db += (p[4 * i] + p[4 * i + 1]) + (p[4 * i + 2] + p[4 * i + 3]);
-      });
+        for (int i = 0; i < 4; ++i) split2(p[2 * i], p[2 * i + 1], hi[0], lo[0], i);
+        step.product(a, hi, lo, rs, r0, [&](int i) {
+          split2(p[8 + 2 * i], p[9 + 2 * i], hi[1], lo[1], i);
+          db += (p[4 * i] + p[4 * i + 1]) + (p[4 * i + 2] + p[4 * i + 3]);
+        });
 #else
 #pragma unroll
-      for (int j = 0; j < 16; ++j) db += p[j];
-      step.product(a, p, tile[buf], r0, lane);
+        for (int j = 0; j < 16; ++j) db += p[j];
+        step.product(a, p, tile[buf], r0, lane);
 #endif
-      s = sn;
-    }
+        s = sn;
+      }
 #if GGNN_DT_BF16
-    step.move_o(nbuf == 0 ? 0u - (kVocBufs - 1) * (uint32_t)(T * H * sizeof(S)) : (uint32_t)(T * H * sizeof(S)));
+      step.move_o(nbuf == 0 ? 0u - (kVocBufs - 1) * (uint32_t)(T * H * sizeof(S)) : (uint32_t)(T * H * sizeof(S)));
 #endif
-    buf = nbuf;
+      buf = nbuf;
+    }
+    const float f = WEIGHT ? 1.f : scale;
+    db = (db + __shfl_xor(db, 32)) * f;
+    if (v < V) {
+      const bool only = deal.shares(run.i) == 1;   // no one else adds to these rows
+      const size_t at = (size_t)run.slot * kVocRows + wave * 32 + lane % 32;
+      if (dbias != nullptr && g == 0) {
+        if (only) dbias[v] += db;
+        else pdb[at] = db;
+      }
+      float* out = only ? dW + (size_t)v * H : pw + at * H;
+#pragma unroll
+      for (int ht = 0; ht < H / 32; ++ht)
+#pragma unroll
+        for (int j4 = 0; j4 < 4; ++j4) {
+          f32x4* q = reinterpret_cast<f32x4*>(out + 32 * ht + 8 * j4 + 4 * g);
+          f32x4 w = f32x4{a[ht][4 * j4], a[ht][4 * j4 + 1], a[ht][4 * j4 + 2], a[ht][4 * j4 + 3]} * f;
+          if (only) w += *q;
+          *q = w;
+        }
+    }
   }
-  const float f = WEIGHT ? 1.f : scale;
-  db = (db + __shfl_xor(db, 32)) * f;
-  if (v < V) {
-    if (pdb != nullptr && g == 0) pdb[(size_t)split * V + v] = db;
-    float* out = pw + ((size_t)split * V + v) * H;
-#pragma unroll
-    for (int ht = 0; ht < H / 32; ++ht)
-#pragma unroll
-      for (int j4 = 0; j4 < 4; ++j4)
-        *reinterpret_cast<f32x4*>(out + 32 * ht + 8 * j4 + 4 * g) =
-            f32x4{a[ht][4 * j4] * f, a[ht][4 * j4 + 1] * f, a[ht][4 * j4 + 2] * f, a[ht][4 * j4 + 3] * f};
+}
+
+// dW and db of the 128-tiles that several shares make up: += their sum, in
+// share order.  H / 4 lanes per entry, four features each.
+template <int H>
+__global__ __launch_bounds__(kVocThreads) void vocab_wsum_kernel(int V, Deal deal, const float* __restrict__ pw,
+                                                                 const float* __restrict__ pdb,
+                                                                 float* __restrict__ dW, float* __restrict__ dbias) {
+  constexpr int L = H / 4;
+  const long v = (long)deal.whole * kVocRows + ((long)blockIdx.x * kVocThreads + threadIdx.x) / L;
+  const int q = threadIdx.x % L;
+  if (v >= V) return;
+  const int i = (int)(v / kVocRows), n = deal.shares(i);
+  if (n == 1) return;
+  const size_t at = (size_t)i * deal.slots * kVocRows + v % kVocRows;
+  f32x4 w = {};
+#pragma unroll 8
+  for (int s = 0; s < n; ++s) w += *reinterpret_cast<const f32x4*>(pw + (at + (size_t)s * kVocRows) * H + 4 * q);
+  *reinterpret_cast<f32x4*>(dW + v * H + 4 * q) += w;
+  if (dbias != nullptr && q == 0) {
+    float b = 0.f;
+#pragma unroll 8
+    for (int s = 0; s < n; ++s) b += pdb[at + (size_t)s * kVocRows];
+    dbias[v] += b;
   }
 }
 
@@ -689,11 +850,34 @@ namespace {
 inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 inline int cdiv(long a, long b) { return (int)((a + b - 1) / b); }
 
+// Workgroups that the chip's 256 compute units hold at once.
+template <typename S>
+int voc_workers(int H, bool sum) {
+  return 256 * dev::voc_waves<S>(H, sum);
+}
+constexpr int kMinUnits = 4;   // tiles of a worker, at least
+
+dev::Deal make_deal(int tiles128, int tiles, int workers) {
+  dev::Deal d{};
+  d.tiles = tiles;
+  const long most = ((long)tiles128 * tiles + kMinUnits - 1) / kMinUnits;
+  d.workers = most < workers ? (int)most : workers;
+  d.whole = tiles128 / d.workers * d.workers;
+  d.rest = tiles128 - d.whole;
+  d.slots = 1;
+  for (int i = d.whole; i < tiles128; ++i) {
+    const int n = d.shares(i);
+    if (n > d.slots) d.slots = n;
+  }
+  return d;
+}
+
 // How a call is cut, and where its shares lie in the workspace.
 struct VocabPlan {
   bool few;
-  int row_tiles, Rp, splits, per;           // rows pass
-  int col_tiles, csplits, cper;             // columns pass
+  int splits, per;     // few rows
+  int row_tiles, Rp, col_tiles;
+  dev::Deal rows, cols;
   size_t pm, pl, pb, po, xg, lse, tgt, fac, pw, pdb, bytes;
 };
 template <typename S>
@@ -701,21 +885,17 @@ VocabPlan vocab_plan(int H, int R, int V, bool grad) {
   constexpr int T = dev::voc_tile<S>();
   VocabPlan p{};
   p.few = !grad && R <= 32;
+  size_t shares;
   if (p.few) {
     const int tiles = cdiv(V, 32);
-    p.row_tiles = 1;
-    p.Rp = 32;
     p.per = cdiv(tiles, 1024);
     p.splits = cdiv(cdiv(tiles, p.per), dev::kVocWaves) * dev::kVocWaves;
+    shares = (size_t)p.splits * 32;
   } else {
-    const int tiles = cdiv(V, T);
     p.row_tiles = cdiv(R, dev::kVocRows);
     p.Rp = p.row_tiles * dev::kVocRows;
-    int want = 1024 / p.row_tiles;
-    if (want > tiles / 4) want = tiles / 4;
-    if (want < 1) want = 1;
-    p.per = cdiv(tiles, want);
-    p.splits = cdiv(tiles, p.per);
+    p.rows = make_deal(p.row_tiles, cdiv(V, T), voc_workers<S>(H, grad));
+    shares = (size_t)p.row_tiles * p.rows.slots * dev::kVocRows;
   }
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -723,25 +903,20 @@ VocabPlan vocab_plan(int H, int R, int V, bool grad) {
     at = up256(at + bytes);
     return here;
   };
-  const size_t shares = (size_t)p.splits * p.Rp;
   p.pm = take(shares * 4);
   p.pl = take(shares * 4);
   if (!grad) p.pb = take(shares * sizeof(dev::RowBest));
   if (grad) {
-    const int tiles = p.Rp / T;
     p.col_tiles = cdiv(V, dev::kVocRows);
-    int want = 1024 / p.col_tiles;
-    if (want > tiles / 4) want = tiles / 4;
-    if (want < 1) want = 1;
-    p.cper = cdiv(tiles, want);
-    p.csplits = cdiv(tiles, p.cper);
+    p.cols = make_deal(p.col_tiles, p.Rp / T, voc_workers<S>(H, true));
+    const size_t cshares = (size_t)p.col_tiles * p.cols.slots * dev::kVocRows;
     p.po = take(shares * H * 4);
     p.xg = take((size_t)p.Rp * H * sizeof(S));
     p.lse = take((size_t)p.Rp * 4);
     p.tgt = take((size_t)p.Rp * 4);
     p.fac = take((size_t)p.Rp * 4);
-    p.pw = take((size_t)p.csplits * V * H * 4);
-    p.pdb = take((size_t)p.csplits * V * 4);
+    p.pw = take(cshares * H * 4);
+    p.pdb = take(cshares * 4);
   }
   p.bytes = at;
   return p;
@@ -758,12 +933,14 @@ hipError_t vocab_loss_h(const VocabArgs& c, hipStream_t st) {
   if (p.few) {
     hipLaunchKernelGGL((vocab_few_kernel<S, H, BEST>), dim3(p.splits / kVocWaves), dim3(kVocThreads), 0, st,
                        c.n_nodes, c.R, c.V, p.per, X, W, c.bias, c.node, pm, pl, pb);
-  } else {
-    hipLaunchKernelGGL((vocab_rows_kernel<S, H, false, BEST>), dim3(p.row_tiles * p.splits), dim3(kVocThreads), 0, st,
-                       c.n_nodes, c.R, c.V, p.row_tiles, p.per, X, W, c.bias, c.node, pm, pl, nullptr, pb);
+    hipLaunchKernelGGL((vocab_few_join_kernel<S, H, BEST>), dim3(c.R), dim3(kVocThreads), 0, st, c.n_nodes, c.R, c.V,
+                       p.splits, X, W, c.bias, c.node, c.target, pm, pl, pb, c.loss, c.lse, c.best);
+    return hipGetLastError();
   }
+  hipLaunchKernelGGL((vocab_rows_kernel<S, H, false, BEST>), dim3(p.rows.workers), dim3(kVocThreads), 0, st,
+                     c.n_nodes, c.R, c.V, p.rows, X, W, c.bias, c.node, pm, pl, nullptr, pb);
   hipLaunchKernelGGL((vocab_join_kernel<S, H, false, BEST>), dim3(cdiv((long)c.R * (H / 4), kVocThreads)),
-                     dim3(kVocThreads), 0, st, c.n_nodes, c.R, c.V, p.Rp, p.splits, X, W, c.bias, c.node, c.target,
+                     dim3(kVocThreads), 0, st, c.n_nodes, c.R, c.V, p.Rp, p.rows, X, W, c.bias, c.node, c.target,
                      nullptr, 1.f, pm, pl, nullptr, pb, c.loss, c.lse, c.best, nullptr, nullptr, nullptr, nullptr,
                      nullptr);
   return hipGetLastError();
@@ -777,29 +954,28 @@ hipError_t vocab_grad_h(const VocabArgs& c, hipStream_t st) {
   float *pm = reinterpret_cast<float*>(ws + p.pm), *pl = reinterpret_cast<float*>(ws + p.pl);
   float *po = reinterpret_cast<float*>(ws + p.po), *lse_w = reinterpret_cast<float*>(ws + p.lse);
   float *fac_w = reinterpret_cast<float*>(ws + p.fac), *pw = reinterpret_cast<float*>(ws + p.pw);
-  float* pdb = c.dbias != nullptr ? reinterpret_cast<float*>(ws + p.pdb) : nullptr;
+  float* pdb = reinterpret_cast<float*>(ws + p.pdb);
   int32_t* tgt_w = reinterpret_cast<int32_t*>(ws + p.tgt);
   S* xg = reinterpret_cast<S*>(ws + p.xg);
   const S *X = static_cast<const S*>(c.X), *W = static_cast<const S*>(c.W);
   hipError_t err = launch_fill_zero(c.dX, (size_t)c.n_nodes * H, st);
   if (err != hipSuccess) return err;
-  hipLaunchKernelGGL((vocab_rows_kernel<S, H, true, false>), dim3(p.row_tiles * p.splits), dim3(kVocThreads), 0, st,
-                     c.n_nodes, c.R, c.V, p.row_tiles, p.per, X, W, c.bias, c.node, pm, pl, po, nullptr);
+  hipLaunchKernelGGL((vocab_rows_kernel<S, H, true, false>), dim3(p.rows.workers), dim3(kVocThreads), 0, st,
+                     c.n_nodes, c.R, c.V, p.rows, X, W, c.bias, c.node, pm, pl, po, nullptr);
   hipLaunchKernelGGL((vocab_join_kernel<S, H, true, false>), dim3(cdiv((long)p.Rp * (H / 4), kVocThreads)),
-                     dim3(kVocThreads), 0, st, c.n_nodes, c.R, c.V, p.Rp, p.splits, X, W, c.bias, c.node, c.target,
+                     dim3(kVocThreads), 0, st, c.n_nodes, c.R, c.V, p.Rp, p.rows, X, W, c.bias, c.node, c.target,
                      c.weight, c.scale, pm, pl, po, nullptr, c.loss, c.lse, nullptr, c.dX, xg, lse_w, tgt_w, fac_w);
   if (c.weight != nullptr)
-    hipLaunchKernelGGL((vocab_cols_kernel<S, H, true>), dim3(p.col_tiles * p.csplits), dim3(kVocThreads), 0, st, c.V,
-                       p.Rp, p.col_tiles, p.cper, c.scale, xg, W, c.bias, lse_w, tgt_w, fac_w, pw, pdb);
+    hipLaunchKernelGGL((vocab_cols_kernel<S, H, true>), dim3(p.cols.workers), dim3(kVocThreads), 0, st, c.V, p.Rp,
+                       p.cols, c.scale, xg, W, c.bias, lse_w, tgt_w, fac_w, c.dW, c.dbias, pw, pdb);
   else
-    hipLaunchKernelGGL((vocab_cols_kernel<S, H, false>), dim3(p.col_tiles * p.csplits), dim3(kVocThreads), 0, st,
-                       c.V, p.Rp, p.col_tiles, p.cper, c.scale, xg, W, c.bias, lse_w, tgt_w, fac_w, pw, pdb);
-  err = hipGetLastError();
-  if (err != hipSuccess) return err;
-  ReduceList red;
-  red.seg[red.n++] = ReduceSeg{pw, c.dW, p.csplits, c.V * H, (long)c.V * H};
-  if (pdb != nullptr) red.seg[red.n++] = ReduceSeg{pdb, c.dbias, p.csplits, c.V, c.V};
-  return launch_reduce_multi(red, st);
+    hipLaunchKernelGGL((vocab_cols_kernel<S, H, false>), dim3(p.cols.workers), dim3(kVocThreads), 0, st, c.V, p.Rp,
+                       p.cols, c.scale, xg, W, c.bias, lse_w, tgt_w, fac_w, c.dW, c.dbias, pw, pdb);
+  const long left = (long)c.V - (long)p.cols.whole * kVocRows;
+  if (left > 0 && p.cols.slots > 1)
+    hipLaunchKernelGGL((vocab_wsum_kernel<H>), dim3(cdiv(left * (H / 4), kVocThreads)), dim3(kVocThreads), 0, st, c.V,
+                       p.cols, pw, pdb, c.dW, c.dbias);
+  return hipGetLastError();
 }
 
 template <typename S, int H>
