@@ -359,10 +359,12 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
     RowBest best{-INFINITY, INT_MAX};
     auto fetch = [&](int t, int buf) {   // start the copies of tile t < t1
       stage_tile<S, H>(W, (long)t * T, V - 1, lds0 + (uint32_t)(buf * T * H * sizeof(S)), wave, lane);
-      if (threadIdx.x < T) nb = entry_bias(bias, t * T + threadIdx.x, V);
+      // (the raw value: a use here would wait for the copies too)
+      if (threadIdx.x < T && bias != nullptr) nb = bias[min(t * T + (int)threadIdx.x, V - 1)];
     };
-    auto land = [&](int buf) {   // and wait for those started last
-      if (threadIdx.x < T) tb[buf][threadIdx.x] = nb;
+    auto land = [&](int t, int buf) {   // and wait for those started last, of tile t
+      if (threadIdx.x < T)
+        tb[buf][threadIdx.x] = t * T + (int)threadIdx.x >= V || nb <= kMaskedBias ? -INFINITY : nb;
       wait_copies<0>();
       __syncthreads();
     };
@@ -376,7 +378,7 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
     if (round > 0) __syncthreads();   // every wave has left the buffers of the run before
     {
       fetch(t0, 0);
-      land(0);
+      land(t0, 0);
       if (t0 + 1 < t1) fetch(t0 + 1, 1);
       start(s, t0, 0, 0);
 #pragma unroll
@@ -392,7 +394,7 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
         const bool last = r0 + 32 >= T;
         const int rs = last ? 0 : r0 + 32;   // of the next tile (after the last one: of what the buffer holds, not used)
         if (last) {
-          land(nbuf);
+          land(t + 1, nbuf);
           if (t + 2 < t1) fetch(t + 2, next_buf(nbuf));
         }
 #if GGNN_DT_BF16
