@@ -20,6 +20,8 @@
 // products as a bf16 pair (hi + lo, 16 bits); one bf16 would put the rounding
 // of every probability, 2^-9, into both gradients.  Logits, maxima, sums and
 // accumulators are float32.
+#include <type_traits>
+
 #include "device_common.h"
 #include "kernels.h"
 #include "lds_dma.h"
@@ -183,31 +185,33 @@ struct VocStep {
       __builtin_amdgcn_sched_barrier(0);
     }
   }
-  // acc[ht] += (tile rows)^T p (lane's column, rows in accumulator order);
-  // work(i), i < 4, is done alongside the first half, which needs p[0 .. 7] only.
-  template <typename Work>
-  __device__ __forceinline__ void product(f32x16 (&acc)[H / 32], const u32x4 (&hi)[2], const u32x4 (&lo)[2], int rs,
-                                          int ro, Work work) {
+  // acc[ht] += (tile rows)^T p (lane's column, rows in accumulator order), p as
+  // PARTS bf16 each; work(i), i < 4, is done alongside the first half, which
+  // needs part[.][0] only.
+  template <int PARTS, typename Work>
+  __device__ __forceinline__ void product(f32x16 (&acc)[H / 32], const u32x4 (&part)[PARTS][2], int rs, int ro,
+                                          Work work) {
 #pragma unroll
     for (int n = 0; n < NO; ++n) {
       const int ks = n / (H / 32), ht = n % (H / 32);
       if (n + kAhead < NO) read(NS + n + kAhead, rs, ro);
-      mma32(acc[ht], f[NS + n], __builtin_bit_cast(bf16x8, hi[ks]));
+      mma32(acc[ht], f[NS + n], __builtin_bit_cast(bf16x8, part[0][ks]));
       if (ks == 0) {
 #pragma unroll
         for (int i = ht * 4 / (H / 32); i < (ht + 1) * 4 / (H / 32); ++i) work(i);
       }
-      mma32(acc[ht], f[NS + n], __builtin_bit_cast(bf16x8, lo[ks]));
+#pragma unroll
+      for (int q = 1; q < PARTS; ++q) mma32(acc[ht], f[NS + n], __builtin_bit_cast(bf16x8, part[q][ks]));
       __builtin_amdgcn_sched_barrier(0);
     }
   }
 };
 
 // Two values as the i-th words of a bf16 pair.
-__device__ __forceinline__ void split2(float a, float b, u32x4& hi, u32x4& lo, int i) {
+__device__ __forceinline__ void split2(float a, float b, u32x4 (&part)[2][2], int ks, int i) {
   const uint32_t h = pk2(a, b);
-  hi[i] = h;
-  lo[i] = pk2(a - lo_f(h), b - hi_f(h));
+  part[0][ks][i] = h;
+  part[1][ks][i] = pk2(a - lo_f(h), b - hi_f(h));
 }
 #else
 // float32: a product takes 64 times as long, so that plain code keeps the
@@ -279,43 +283,68 @@ __device__ __forceinline__ void load_row_frags(frag_t<S> (&f)[H / 16], const S* 
 // the columns pass, entries).  `workers` workgroups first take whole 128-tiles,
 // one each a round; the 128-tiles that are left over are laid end to end and
 // cut into equal runs of units, so that all workgroups end together.  A 128-tile
-// is thus one share, or a few neighbouring workers' shares, joined afterwards in
-// that order.
+// is thus one share, or a few neighbouring pieces' shares, joined afterwards in
+// that order, whoever formed them.
 struct Deal {
   int workers, tiles;   // workgroups; LDS tiles against one 128-tile
   int whole, rest;      // 128-tiles dealt whole (a multiple of workers), and cut up
   int slots;            // shares of a 128-tile, at most
-  // First unit of worker w in the rest, and the worker that has unit u.
-  __host__ __device__ long begin(int w) const { return (long)w * ((long)rest * tiles) / workers; }
-  __host__ __device__ int owner(long u) const { return (int)(((u + 1) * workers - 1) / ((long)rest * tiles)); }
+  int pieces;           // runs that the rest is cut into: one a worker, or more and drawn from a queue
+  uint32_t each, more;  // units of a piece; the first `more` pieces have one more
+  // First unit of piece w of the rest, and the piece that has unit u.
+  __host__ __device__ uint32_t begin(uint32_t w) const { return w * each + (w < more ? w : more); }
+  __host__ __device__ int owner(uint32_t u) const {
+    const uint32_t k = more * (each + 1);
+    return (int)(u < k ? u / (each + 1) : more + (u - k) / each);
+  }
   // Shares of 128-tile i; share s of it is written to slot i * slots + s.
   __host__ __device__ int shares(int i) const {
     if (i < whole) return 1;
-    const long u = (long)(i - whole) * tiles;
+    const uint32_t u = (uint32_t)(i - whole) * tiles;
     return owner(u + tiles - 1) - owner(u) + 1;
   }
 };
-// The next run of worker w: 128-tile, LDS tiles t0 .. t1 - 1, its slot.  `step`
-// counts the runs, `u` the units of the rest (begin(w) at first).
+// The next run of worker w: 128-tile, LDS tiles t0 .. t1 - 1, its slot.
 struct Run {
   int i, t0, t1, slot;
 };
-__device__ __forceinline__ bool next_run(const Deal& d, int w, int step, long& u, Run* r) {
-  if (step < d.whole / d.workers) {
-    *r = Run{step * d.workers + w, 0, d.tiles, 0};
-    r->slot = r->i * d.slots;
+struct Dealt {
+  int step = 0;         // 128-tiles dealt whole so far
+  int piece = -1;       // of the rest
+  uint32_t u = 0, end = 0;
+  // `queue`: counter of the pieces drawn so far, zero at the kernel's start
+  // (NULL: worker w has piece w); `drawn`: a word of LDS.  Every thread of the
+  // workgroup calls it; ends for each after finitely many pieces.
+  __device__ __forceinline__ bool next(const Deal& d, int w, uint32_t* queue, int* drawn, Run* r) {
+    if (step * d.workers < d.whole) {
+      const int i = step * d.workers + w;
+      *r = Run{i, 0, d.tiles, i * d.slots};
+      ++step;
+      return true;
+    }
+    if (u >= end) {
+      if (queue != nullptr) {
+        if (threadIdx.x == 0) *drawn = (int)atomicAdd(queue, 1u);
+        __syncthreads();
+        piece = __builtin_amdgcn_readfirstlane(*drawn);
+        __syncthreads();
+      } else {
+        piece = piece < 0 ? w : d.pieces;
+      }
+      if (piece >= d.pieces) return false;
+      u = d.begin(piece);
+      end = d.begin(piece + 1);
+      if (u >= end) return false;
+    }
+    const uint32_t k = u / (uint32_t)d.tiles;
+    r->i = d.whole + (int)k;
+    r->t0 = (int)(u - k * d.tiles);
+    r->t1 = min(d.tiles, r->t0 + (int)(end - u));
+    r->slot = r->i * d.slots + (r->t0 == 0 ? 0 : piece - d.owner(k * d.tiles));
+    u += r->t1 - r->t0;
     return true;
   }
-  const long end = d.rest > 0 ? d.begin(w + 1) : 0;
-  if (u >= end) return false;
-  const int k = (int)(u / d.tiles);
-  r->i = d.whole + k;
-  r->t0 = (int)(u - (long)k * d.tiles);
-  r->t1 = (int)min((long)d.tiles, r->t0 + (end - u));
-  r->slot = r->i * d.slots + w - d.owner((long)k * d.tiles);
-  u += r->t1 - r->t0;
-  return true;
-}
+};
 
 // Workgroups of a pass that a compute unit holds (waves per SIMD): by the
 // accumulators and fragments that a wave keeps, and at H = 256 by the buffers.
@@ -329,27 +358,35 @@ constexpr int kVocBufs = 3;
 __device__ __forceinline__ int next_buf(int b) { return b == kVocBufs - 1 ? 0 : b + 1; }
 
 // Rows pass.  Writes each row's (m in units of log 2, l) of a share to pm, pl
-// [slot][128]; SUM: O too; BEST: the largest logit's entry too.
+// [slot][128]; SUM: O too; BEST: the largest logit's entry too.  A small dX is
+// cleared here, `clear` 16-byte pieces per thread (0: elsewhere).
 template <typename S, int H, bool SUM, bool BEST>
 __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_kernel(int n_nodes, int R, int V, Deal deal,
                                                                  const S* __restrict__ X, const S* __restrict__ W,
                                                                  const float* __restrict__ bias,
                                                                  const int32_t* __restrict__ node,
                                                                  float* __restrict__ pm, float* __restrict__ pl,
-                                                                 float* __restrict__ po, RowBest* __restrict__ pb) {
+                                                                 float* __restrict__ po, RowBest* __restrict__ pb,
+                                                                 float* __restrict__ dX, int clear) {
   constexpr int T = voc_tile<S>();
   __shared__ __attribute__((aligned(1024))) S tile[kVocBufs][T * H];
   __shared__ __attribute__((aligned(16))) float tb[kVocBufs][T];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = lane / 32;
   const uint32_t lds0 = (uint32_t)(uintptr_t)tile[0];
 
+  if constexpr (SUM) {
+    const size_t all = (size_t)n_nodes * (H / 4), each = (size_t)clear * kVocThreads;
+    for (int k = 0; k < clear; ++k) {
+      const size_t at = blockIdx.x * each + (size_t)k * kVocThreads + threadIdx.x;
+      if (at < all) reinterpret_cast<f32x4*>(dX)[at] = f32x4{};
+    }
+  }
   float nb = 0.f;
-  long unit = deal.begin(blockIdx.x);
   Run run;
-  for (int round = 0; next_run(deal, blockIdx.x, round, unit, &run); ++round) {
+  Dealt dealt;
+  for (int round = 0; dealt.next(deal, blockIdx.x, nullptr, nullptr, &run); ++round) {
     const int t0 = run.t0, t1 = run.t1;
     frag_t<S> xf[H / 16];
-    load_row_frags<S, H>(xf, X, row_node(node, run.i * kVocRows + wave * 32 + lane % 32, R, n_nodes), lane);
     f32x16 o[H / 32];
     if constexpr (SUM) {
 #pragma unroll
@@ -378,6 +415,7 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
     if (round > 0) __syncthreads();   // every wave has left the buffers of the run before
     {
       fetch(t0, 0);
+      load_row_frags<S, H>(xf, X, row_node(node, run.i * kVocRows + wave * 32 + lane % 32, R, n_nodes), lane);
       land(t0, 0);
       if (t0 + 1 < t1) fetch(t0 + 1, 1);
       start(s, t0, 0, 0);
@@ -433,14 +471,14 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
           l += p[j];
         };
 #if GGNN_DT_BF16
-        u32x4 hi[2], lo[2];
+        u32x4 part[2][2];
         __builtin_amdgcn_sched_barrier(0);
         step.template logits<LAST>(sn, xf, rs, r0, [&](int j) {
           prob(j);
-          if (SUM && j >= 8 && j % 2 == 1) split2(p[j - 9], p[j - 8], hi[0], lo[0], (j - 9) / 2);
+          if (SUM && j >= 8 && j % 2 == 1) split2(p[j - 9], p[j - 8], part, 0, (j - 9) / 2);
         });
         if constexpr (SUM)
-          step.product(o, hi, lo, rs, r0, [&](int i) { split2(p[8 + 2 * i], p[9 + 2 * i], hi[1], lo[1], i); });
+          step.template product<2>(o, part, rs, r0, [&](int i) { split2(p[8 + 2 * i], p[9 + 2 * i], part, 1, i); });
 #else
         step.logits(sn, xf, tile[last ? nbuf : buf], rs, lane);
 #pragma unroll
@@ -627,8 +665,9 @@ __global__ __launch_bounds__(kVocThreads) void vocab_join_kernel(
     const float* __restrict__ weight, float scale, const float* __restrict__ pm, const float* __restrict__ pl,
     const float* __restrict__ po, const RowBest* __restrict__ pb, float* __restrict__ loss, float* __restrict__ lse,
     int32_t* __restrict__ best, float* __restrict__ dX, S* __restrict__ xg, float* __restrict__ lse_w,
-    int32_t* __restrict__ tgt_w, float* __restrict__ fac_w) {
+    int32_t* __restrict__ tgt_w, float* __restrict__ fac_w, uint32_t* __restrict__ queue) {
   constexpr int L = H / 4;
+  if (GRAD && blockIdx.x == 0 && threadIdx.x == 0) *queue = 0;
   const int r = (int)(((long)blockIdx.x * kVocThreads + threadIdx.x) / L);
   const int q = threadIdx.x % L, h = 4 * q;
   if (r >= (GRAD ? Rp : R)) return;   // whole groups of L lanes leave together
@@ -686,7 +725,8 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
                                                                  const int32_t* __restrict__ tgt_w,
                                                                  const float* __restrict__ fac_w,
                                                                  float* __restrict__ dW, float* __restrict__ dbias,
-                                                                 float* __restrict__ pw, float* __restrict__ pdb) {
+                                                                 float* __restrict__ pw, float* __restrict__ pdb,
+                                                                 uint32_t* __restrict__ queue) {
   constexpr int T = voc_tile<S>();
   __shared__ __attribute__((aligned(1024))) S tile[kVocBufs][T * H];
   __shared__ __attribute__((aligned(16))) float tl[kVocBufs][T], tf[kVocBufs][T];
@@ -696,13 +736,12 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
 
   float nl = 0.f, nf = 0.f;
   int nt = -1;
-  long unit = deal.begin(blockIdx.x);
+  __shared__ int drawn;
   Run run;
-  for (int round = 0; next_run(deal, blockIdx.x, round, unit, &run); ++round) {
+  Dealt dealt;
+  for (int round = 0; dealt.next(deal, blockIdx.x, queue, &drawn, &run); ++round) {
     const int t0 = run.t0, t1 = run.t1, vw = run.i * kVocRows + wave * 32, v = vw + lane % 32;
     frag_t<S> wf[H / 16];
-    load_row_frags<S, H>(wf, W, min(v, V - 1), lane);
-    const float b2 = entry_bias(bias, v, V) * kLog2e;
     f32x16 a[H / 32];
 #pragma unroll
     for (int ht = 0; ht < H / 32; ++ht) a[ht] = f32x16{};
@@ -728,8 +767,11 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
     f32x16 s;
     int buf = 0;
     if (round > 0) __syncthreads();   // every wave has left the buffers of the run before
+    float b2;
     {
       fetch(t0, 0);
+      load_row_frags<S, H>(wf, W, min(v, V - 1), lane);
+      b2 = entry_bias(bias, v, V) * kLog2e;
       land(0);
       if (t0 + 1 < t1) fetch(t0 + 1, 1);
       start32(s, tl[0], lane);
@@ -768,22 +810,16 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
 #pragma unroll
         for (int j = 0; j < 16; ++j) prob(j);
 #endif
-        // the rows' targets, where any falls on this wave's entries
-        if (__ballot((unsigned)(tj - vw) < 32u)) {
-#pragma unroll
-          for (int j = 0; j < 16; ++j)
-            if (tt[buf][r0 + 8 * (j / 4) + 4 * g + j % 4] == v) p[j] -= 1.f;
-        }
         if constexpr (WEIGHT) {
 #pragma unroll
           for (int j = 0; j < 16; ++j) p[j] *= tf[buf][r0 + 8 * (j / 4) + 4 * g + j % 4];
         }
 #if GGNN_DT_BF16
-        u32x4 hi[2], lo[2];
+        u32x4 part[2][2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) split2(p[2 * i], p[2 * i + 1], hi[0], lo[0], i);
-        step.product(a, hi, lo, rs, r0, [&](int i) {
-          split2(p[8 + 2 * i], p[9 + 2 * i], hi[1], lo[1], i);
+        for (int i = 0; i < 4; ++i) split2(p[2 * i], p[2 * i + 1], part, 0, i);
+        step.template product<2>(a, part, rs, r0, [&](int i) {
+          split2(p[8 + 2 * i], p[9 + 2 * i], part, 1, i);
           db += (p[4 * i] + p[4 * i + 1]) + (p[4 * i + 2] + p[4 * i + 3]);
         });
 #else
@@ -791,6 +827,35 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
         for (int j = 0; j < 16; ++j) db += p[j];
         step.product(a, p, tile[buf], r0, lane);
 #endif
+        // The rows' targets, where any falls on this wave's entries: a product of
+        // its own, since a bf16 pair of p - 1 would lose low bits of p to the 1.
+        if (__ballot((unsigned)(tj - vw) < 32u)) {
+          float q[16];
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const int i = r0 + 8 * (j / 4) + 4 * g + j % 4;
+            q[j] = tt[buf][i] != v ? 0.f : WEIGHT ? -tf[buf][i] : -1.f;
+            db += q[j];
+          }
+#if GGNN_DT_BF16
+#pragma unroll
+          for (int n = 0; n < (WEIGHT ? 3 : 1); ++n) {   // -1 is one bf16, any float32 three
+            u32x4 e[1][2];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const uint32_t h = pk2(q[2 * i], q[2 * i + 1]);
+              e[0][i / 4][i % 4] = h;
+              q[2 * i] -= lo_f(h);
+              q[2 * i + 1] -= hi_f(h);
+            }
+#pragma unroll
+            for (int k = 0; k < step.kAhead; ++k) step.read(H / 16 + k, 0, r0);
+            step.template product<1>(a, e, rs, r0, [](int) {});
+          }
+#else
+          step.product(a, q, tile[buf], r0, lane);
+#endif
+        }
         s = sn;
       }
 #if GGNN_DT_BF16
@@ -857,15 +922,22 @@ template <typename S>
 int voc_workers(int H, bool sum) {
   return 256 * dev::voc_waves<S>(H, sum);
 }
-constexpr int kMinUnits = 4;   // tiles of a worker, at least
 
-dev::Deal make_deal(int tiles128, int tiles, int workers) {
+dev::Deal make_deal(int tiles128, int tiles, int workers, bool queue) {
   dev::Deal d{};
   d.tiles = tiles;
-  const long most = ((long)tiles128 * tiles + kMinUnits - 1) / kMinUnits;
-  d.workers = most < workers ? (int)most : workers;
+  // Four tiles a worker pay for its start and its share; fewer where that
+  // would leave compute units empty.
+  const long all = (long)tiles128 * tiles, few = all < 256 ? all : 256, want = all / 4 > few ? all / 4 : few;
+  d.workers = want < workers ? (int)want : workers;
   d.whole = tiles128 / d.workers * d.workers;
   d.rest = tiles128 - d.whole;
+  const uint32_t units = (uint32_t)d.rest * (uint32_t)tiles;   // fewer than workers * tiles
+  // Entries that many rows have for a target make their tiles' runs longer: where
+  // workers have whole tiles, the rest evens that out in smaller pieces.
+  d.pieces = queue && d.whole > 0 ? 4 * d.workers : d.workers;
+  d.each = units / d.pieces;
+  d.more = units % d.pieces;
   d.slots = 1;
   for (int i = d.whole; i < tiles128; ++i) {
     const int n = d.shares(i);
@@ -880,7 +952,7 @@ struct VocabPlan {
   int splits, per;     // few rows
   int row_tiles, Rp, col_tiles;
   dev::Deal rows, cols;
-  size_t pm, pl, pb, po, xg, lse, tgt, fac, pw, pdb, bytes;
+  size_t pm, pl, pb, po, xg, lse, tgt, fac, pw, pdb, queue, bytes;
 };
 template <typename S>
 VocabPlan vocab_plan(int H, int R, int V, bool grad) {
@@ -896,7 +968,7 @@ VocabPlan vocab_plan(int H, int R, int V, bool grad) {
   } else {
     p.row_tiles = cdiv(R, dev::kVocRows);
     p.Rp = p.row_tiles * dev::kVocRows;
-    p.rows = make_deal(p.row_tiles, cdiv(V, T), voc_workers<S>(H, grad));
+    p.rows = make_deal(p.row_tiles, cdiv(V, T), voc_workers<S>(H, grad), false);
     shares = (size_t)p.row_tiles * p.rows.slots * dev::kVocRows;
   }
   size_t at = 0;
@@ -910,7 +982,7 @@ VocabPlan vocab_plan(int H, int R, int V, bool grad) {
   if (!grad) p.pb = take(shares * sizeof(dev::RowBest));
   if (grad) {
     p.col_tiles = cdiv(V, dev::kVocRows);
-    p.cols = make_deal(p.col_tiles, p.Rp / T, voc_workers<S>(H, true));
+    p.cols = make_deal(p.col_tiles, p.Rp / T, voc_workers<S>(H, true), true);
     const size_t cshares = (size_t)p.col_tiles * p.cols.slots * dev::kVocRows;
     p.po = take(shares * H * 4);
     p.xg = take((size_t)p.Rp * H * sizeof(S));
@@ -919,6 +991,7 @@ VocabPlan vocab_plan(int H, int R, int V, bool grad) {
     p.fac = take((size_t)p.Rp * 4);
     p.pw = take(cshares * H * 4);
     p.pdb = take(cshares * 4);
+    p.queue = take(4);
   }
   p.bytes = at;
   return p;
@@ -940,11 +1013,11 @@ hipError_t vocab_loss_h(const VocabArgs& c, hipStream_t st) {
     return hipGetLastError();
   }
   hipLaunchKernelGGL((vocab_rows_kernel<S, H, false, BEST>), dim3(p.rows.workers), dim3(kVocThreads), 0, st,
-                     c.n_nodes, c.R, c.V, p.rows, X, W, c.bias, c.node, pm, pl, nullptr, pb);
+                     c.n_nodes, c.R, c.V, p.rows, X, W, c.bias, c.node, pm, pl, nullptr, pb, nullptr, 0);
   hipLaunchKernelGGL((vocab_join_kernel<S, H, false, BEST>), dim3(cdiv((long)c.R * (H / 4), kVocThreads)),
                      dim3(kVocThreads), 0, st, c.n_nodes, c.R, c.V, p.Rp, p.rows, X, W, c.bias, c.node, c.target,
                      nullptr, 1.f, pm, pl, nullptr, pb, c.loss, c.lse, c.best, nullptr, nullptr, nullptr, nullptr,
-                     nullptr);
+                     nullptr, nullptr);
   return hipGetLastError();
 }
 
@@ -959,20 +1032,29 @@ hipError_t vocab_grad_h(const VocabArgs& c, hipStream_t st) {
   float* pdb = reinterpret_cast<float*>(ws + p.pdb);
   int32_t* tgt_w = reinterpret_cast<int32_t*>(ws + p.tgt);
   S* xg = reinterpret_cast<S*>(ws + p.xg);
+  uint32_t* counter = reinterpret_cast<uint32_t*>(ws + p.queue);   // cleared by the join
+  uint32_t* queue = p.cols.pieces > p.cols.workers ? counter : nullptr;
   const S *X = static_cast<const S*>(c.X), *W = static_cast<const S*>(c.W);
-  hipError_t err = launch_fill_zero(c.dX, (size_t)c.n_nodes * H, st);
-  if (err != hipSuccess) return err;
+  // A small dX is cleared by the rows pass, one launch less (5 us of the 70 at
+  // 3,001 rows); a large one, which would hold its products up, by its own.
+  const long pieces = (long)c.n_nodes * (H / 4), each = (long)p.rows.workers * kVocThreads;
+  const int clear = pieces <= 8 * each ? (int)((pieces + each - 1) / each) : 0;
+  if (clear == 0) {
+    const hipError_t err = launch_fill_zero(c.dX, (size_t)c.n_nodes * H, st);
+    if (err != hipSuccess) return err;
+  }
   hipLaunchKernelGGL((vocab_rows_kernel<S, H, true, false>), dim3(p.rows.workers), dim3(kVocThreads), 0, st,
-                     c.n_nodes, c.R, c.V, p.rows, X, W, c.bias, c.node, pm, pl, po, nullptr);
+                     c.n_nodes, c.R, c.V, p.rows, X, W, c.bias, c.node, pm, pl, po, nullptr, c.dX, clear);
   hipLaunchKernelGGL((vocab_join_kernel<S, H, true, false>), dim3(cdiv((long)p.Rp * (H / 4), kVocThreads)),
                      dim3(kVocThreads), 0, st, c.n_nodes, c.R, c.V, p.Rp, p.rows, X, W, c.bias, c.node, c.target,
-                     c.weight, c.scale, pm, pl, po, nullptr, c.loss, c.lse, nullptr, c.dX, xg, lse_w, tgt_w, fac_w);
+                     c.weight, c.scale, pm, pl, po, nullptr, c.loss, c.lse, nullptr, c.dX, xg, lse_w, tgt_w, fac_w,
+                     counter);
   if (c.weight != nullptr)
     hipLaunchKernelGGL((vocab_cols_kernel<S, H, true>), dim3(p.cols.workers), dim3(kVocThreads), 0, st, c.V, p.Rp,
-                       p.cols, c.scale, xg, W, c.bias, lse_w, tgt_w, fac_w, c.dW, c.dbias, pw, pdb);
+                       p.cols, c.scale, xg, W, c.bias, lse_w, tgt_w, fac_w, c.dW, c.dbias, pw, pdb, queue);
   else
     hipLaunchKernelGGL((vocab_cols_kernel<S, H, false>), dim3(p.cols.workers), dim3(kVocThreads), 0, st, c.V, p.Rp,
-                       p.cols, c.scale, xg, W, c.bias, lse_w, tgt_w, fac_w, c.dW, c.dbias, pw, pdb);
+                       p.cols, c.scale, xg, W, c.bias, lse_w, tgt_w, fac_w, c.dW, c.dbias, pw, pdb, queue);
   const long left = (long)c.V - (long)p.cols.whole * kVocRows;
   if (left > 0 && p.cols.slots > 1)
     hipLaunchKernelGGL((vocab_wsum_kernel<H>), dim3(cdiv(left * (H / 4), kVocThreads)), dim3(kVocThreads), 0, st, c.V,
