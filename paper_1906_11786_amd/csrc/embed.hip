@@ -385,11 +385,14 @@ __device__ __forceinline__ void add_row(float* __restrict__ o, const float (&acc
   store8f(o, v);
 }
 
-template <int H, bool DROP>
+// S: type of the summed rows.  Row r's factor is scale (over its list's length
+// for the mean), or -factor[r] where factor is given.
+template <typename S, int H, bool DROP>
 __global__ __launch_bounds__(kEmbThreads) void embed_runs_kernel(int n_tok, int n, int V, int chunk,
                                                                  const u32x2* __restrict__ items,
                                                                  const int32_t* __restrict__ tok_ptr, float scale,
-                                                                 int mean, Dropout d, const float* __restrict__ dX,
+                                                                 int mean, const float* __restrict__ factor, Dropout d,
+                                                                 const S* __restrict__ dX,
                                                                  float* __restrict__ dtable,
                                                                  float* __restrict__ part) {
   constexpr int L = H / 8, G = kEmbThreads / L, U = 4;
@@ -425,7 +428,8 @@ __global__ __launch_bounds__(kEmbThreads) void embed_runs_kernel(int n_tok, int 
         const bool ok = it[u].x < none && k + u < k1;
         f[u] = scale;
         if (ok) {
-          load8f<float>(dX + (size_t)row * H + h, v[u]);
+          load8f<S>(dX + (size_t)row * H + h, v[u]);
+          if (factor != nullptr) f[u] = -factor[row];
           if (tok_ptr != nullptr && mean) f[u] = scale / (float)max(tok_ptr[row + 1] - tok_ptr[row], 1);
           if (it[u].x != (u > 0 ? it[u - 1].x : cur)) load8f<float>(dtable + (size_t)it[u].x * H + h, w[u]);
         }
@@ -622,9 +626,11 @@ EmbedLayout embed_layout(int H, int n_tok) {
   return l;
 }
 
-template <int H>
+template <typename S, int H>
 hipError_t embed_bwd_h(int n, int V, const int32_t* tok_ptr, const int32_t* tok, int n_tok, float scale, int mean,
-                       const Dropout& d, const float* dX, float* dtable, char* ws, hipStream_t st) {
+                       const float* factor, const Dropout& d, const void* grad, float* dtable, char* ws,
+                       hipStream_t st) {
+  const S* dX = static_cast<const S*>(grad);
   using namespace dev;
   const EmbedLayout l = embed_layout(H, n_tok);
   u32x2 *a = reinterpret_cast<u32x2*>(ws + l.a), *b = reinterpret_cast<u32x2*>(ws + l.b);
@@ -655,11 +661,11 @@ hipError_t embed_bwd_h(int n, int V, const int32_t* tok_ptr, const int32_t* tok,
     if (err != hipSuccess) return err;
   }
   if (d.cut != 0) {
-    hipLaunchKernelGGL((embed_runs_kernel<H, true>), dim3(l.blocks), dim3(kEmbThreads), 0, st, n_tok, n, V, l.chunk,
-                       a, tok_ptr, scale, mean, d, dX, dtable, part);
+    hipLaunchKernelGGL((embed_runs_kernel<S, H, true>), dim3(l.blocks), dim3(kEmbThreads), 0, st, n_tok, n, V, l.chunk,
+                       a, tok_ptr, scale, mean, factor, d, dX, dtable, part);
   } else {
-    hipLaunchKernelGGL((embed_runs_kernel<H, false>), dim3(l.blocks), dim3(kEmbThreads), 0, st, n_tok, n, V, l.chunk,
-                       a, tok_ptr, scale, mean, d, dX, dtable, part);
+    hipLaunchKernelGGL((embed_runs_kernel<S, H, false>), dim3(l.blocks), dim3(kEmbThreads), 0, st, n_tok, n, V, l.chunk,
+                       a, tok_ptr, scale, mean, factor, d, dX, dtable, part);
   }
   if (l.blocks > 1)
     hipLaunchKernelGGL((embed_join_kernel<H>), dim3((l.blocks + kJoinBlocks - 1) / kJoinBlocks), dim3(kJoinThreads),
@@ -675,12 +681,36 @@ hipError_t launch_embed_bwd(int n, int H, int V, const int32_t* tok_ptr, const i
   if (n_tok == 0 || n == 0) return hipSuccess;
   char* w = static_cast<char*>(ws);
   switch (H) {
-    case 32: return embed_bwd_h<32>(n, V, tok_ptr, tok, n_tok, scale, mean, d, dX, dtable, w, st);
-    case 64: return embed_bwd_h<64>(n, V, tok_ptr, tok, n_tok, scale, mean, d, dX, dtable, w, st);
-    case 128: return embed_bwd_h<128>(n, V, tok_ptr, tok, n_tok, scale, mean, d, dX, dtable, w, st);
-    case 256: return embed_bwd_h<256>(n, V, tok_ptr, tok, n_tok, scale, mean, d, dX, dtable, w, st);
+    case 32: return embed_bwd_h<float, 32>(n, V, tok_ptr, tok, n_tok, scale, mean, nullptr, d, dX, dtable, w, st);
+    case 64: return embed_bwd_h<float, 64>(n, V, tok_ptr, tok, n_tok, scale, mean, nullptr, d, dX, dtable, w, st);
+    case 128: return embed_bwd_h<float, 128>(n, V, tok_ptr, tok, n_tok, scale, mean, nullptr, d, dX, dtable, w, st);
+    case 256: return embed_bwd_h<float, 256>(n, V, tok_ptr, tok, n_tok, scale, mean, nullptr, d, dX, dtable, w, st);
   }
   return hipErrorInvalidValue;
+}
+
+size_t target_rows_workspace(int H, int R) { return embed_layout(H, R).bytes; }
+
+namespace {
+template <typename S>
+hipError_t target_rows(int R, int H, int V, const int32_t* target, const void* x, float scale, const float* factor,
+                       float* dW, char* ws, hipStream_t st) {
+  const Dropout none{};
+  switch (H) {
+    case 32: return embed_bwd_h<S, 32>(R, V, nullptr, target, R, scale, 0, factor, none, x, dW, ws, st);
+    case 64: return embed_bwd_h<S, 64>(R, V, nullptr, target, R, scale, 0, factor, none, x, dW, ws, st);
+    case 128: return embed_bwd_h<S, 128>(R, V, nullptr, target, R, scale, 0, factor, none, x, dW, ws, st);
+    case 256: return embed_bwd_h<S, 256>(R, V, nullptr, target, R, scale, 0, factor, none, x, dW, ws, st);
+  }
+  return hipErrorInvalidValue;
+}
+}  // namespace
+
+hipError_t launch_target_rows(int dt, int R, int H, int V, const int32_t* target, const void* x, float scale,
+                              const float* factor, float* dW, void* ws, hipStream_t st) {
+  char* w = static_cast<char*>(ws);
+  return dt == GGNN_BF16 ? target_rows<dev::bf16s>(R, H, V, target, x, scale, factor, dW, w, st)
+                         : target_rows<float>(R, H, V, target, x, scale, factor, dW, w, st);
 }
 #endif
 

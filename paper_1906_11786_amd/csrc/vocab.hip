@@ -117,6 +117,9 @@ __device__ __forceinline__ f32x8 col_frag(const float* tile, int r0, int ht, int
 // then the second product of this one (NO fragments, each times the hi and the
 // lo part of p).
 
+// Keeps the compiler from moving what forms v past this point.
+__device__ __forceinline__ void keep_here(float& v) { asm volatile("" : "+v"(v)); }
+
 #if GGNN_DT_BF16
 typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
 
@@ -283,15 +286,14 @@ __device__ __forceinline__ void load_row_frags(frag_t<S> (&f)[H / 16], const S* 
 // the columns pass, entries).  `workers` workgroups first take whole 128-tiles,
 // one each a round; the 128-tiles that are left over are laid end to end and
 // cut into equal runs of units, so that all workgroups end together.  A 128-tile
-// is thus one share, or a few neighbouring pieces' shares, joined afterwards in
-// that order, whoever formed them.
+// is thus one share, or a few neighbouring workers' shares, joined afterwards in
+// that order.
 struct Deal {
   int workers, tiles;   // workgroups; LDS tiles against one 128-tile
   int whole, rest;      // 128-tiles dealt whole (a multiple of workers), and cut up
   int slots;            // shares of a 128-tile, at most
-  int pieces;           // runs that the rest is cut into: one a worker, or more and drawn from a queue
-  uint32_t each, more;  // units of a piece; the first `more` pieces have one more
-  // First unit of piece w of the rest, and the piece that has unit u.
+  uint32_t each, more;  // units of the rest for a worker; the first `more` workers have one more
+  // First unit of worker w in the rest, and the worker that has unit u.
   __host__ __device__ uint32_t begin(uint32_t w) const { return w * each + (w < more ? w : more); }
   __host__ __device__ int owner(uint32_t u) const {
     const uint32_t k = more * (each + 1);
@@ -310,37 +312,21 @@ struct Run {
 };
 struct Dealt {
   int step = 0;         // 128-tiles dealt whole so far
-  int piece = -1;       // of the rest
-  uint32_t u = 0, end = 0;
-  // `queue`: counter of the pieces drawn so far, zero at the kernel's start
-  // (NULL: worker w has piece w); `drawn`: a word of LDS.  Every thread of the
-  // workgroup calls it; ends for each after finitely many pieces.
-  __device__ __forceinline__ bool next(const Deal& d, int w, uint32_t* queue, int* drawn, Run* r) {
+  uint32_t u, end;      // units of the rest
+  __device__ __forceinline__ Dealt(const Deal& d, int w) : u(d.begin(w)), end(d.begin(w + 1)) {}
+  __device__ __forceinline__ bool next(const Deal& d, int w, Run* r) {
     if (step * d.workers < d.whole) {
       const int i = step * d.workers + w;
       *r = Run{i, 0, d.tiles, i * d.slots};
       ++step;
       return true;
     }
-    if (u >= end) {
-      if (queue != nullptr) {
-        if (threadIdx.x == 0) *drawn = (int)atomicAdd(queue, 1u);
-        __syncthreads();
-        piece = __builtin_amdgcn_readfirstlane(*drawn);
-        __syncthreads();
-      } else {
-        piece = piece < 0 ? w : d.pieces;
-      }
-      if (piece >= d.pieces) return false;
-      u = d.begin(piece);
-      end = d.begin(piece + 1);
-      if (u >= end) return false;
-    }
+    if (u >= end) return false;
     const uint32_t k = u / (uint32_t)d.tiles;
     r->i = d.whole + (int)k;
     r->t0 = (int)(u - k * d.tiles);
     r->t1 = min(d.tiles, r->t0 + (int)(end - u));
-    r->slot = r->i * d.slots + (r->t0 == 0 ? 0 : piece - d.owner(k * d.tiles));
+    r->slot = r->i * d.slots + (r->t0 == 0 ? 0 : w - d.owner(k * d.tiles));
     u += r->t1 - r->t0;
     return true;
   }
@@ -383,8 +369,8 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
   }
   float nb = 0.f;
   Run run;
-  Dealt dealt;
-  for (int round = 0; dealt.next(deal, blockIdx.x, nullptr, nullptr, &run); ++round) {
+  Dealt dealt(deal, blockIdx.x);
+  for (int round = 0; dealt.next(deal, blockIdx.x, &run); ++round) {
     const int t0 = run.t0, t1 = run.t1;
     frag_t<S> xf[H / 16];
     f32x16 o[H / 32];
@@ -665,9 +651,8 @@ __global__ __launch_bounds__(kVocThreads) void vocab_join_kernel(
     const float* __restrict__ weight, float scale, const float* __restrict__ pm, const float* __restrict__ pl,
     const float* __restrict__ po, const RowBest* __restrict__ pb, float* __restrict__ loss, float* __restrict__ lse,
     int32_t* __restrict__ best, float* __restrict__ dX, S* __restrict__ xg, float* __restrict__ lse_w,
-    int32_t* __restrict__ tgt_w, float* __restrict__ fac_w, uint32_t* __restrict__ queue) {
+    int32_t* __restrict__ tgt_w, float* __restrict__ fac_w) {
   constexpr int L = H / 4;
-  if (GRAD && blockIdx.x == 0 && threadIdx.x == 0) *queue = 0;
   const int r = (int)(((long)blockIdx.x * kVocThreads + threadIdx.x) / L);
   const int q = threadIdx.x % L, h = 4 * q;
   if (r >= (GRAD ? Rp : R)) return;   // whole groups of L lanes leave together
@@ -715,8 +700,8 @@ __global__ __launch_bounds__(kVocThreads) void vocab_join_kernel(
 // Columns pass: 128 entries of a workgroup (32 per wave) against the gathered states.  Adds to dW [V][H] and db [V] (dbias NULL:
 // none) where the 128-tile is one share, else writes its share to pw
 // [slot][128][H] and pdb [slot][128].  WEIGHT: each row has a factor of its
-// own; otherwise all have `scale`.
-template <typename S, int H, bool WEIGHT>
+// own; otherwise all have `scale`.  TARGETS: see below.
+template <typename S, int H, bool WEIGHT, bool TARGETS>
 __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols_kernel(int V, int Rp, Deal deal, float scale,
                                                                  const S* __restrict__ xg,
                                                                  const S* __restrict__ W,
@@ -725,8 +710,7 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
                                                                  const int32_t* __restrict__ tgt_w,
                                                                  const float* __restrict__ fac_w,
                                                                  float* __restrict__ dW, float* __restrict__ dbias,
-                                                                 float* __restrict__ pw, float* __restrict__ pdb,
-                                                                 uint32_t* __restrict__ queue) {
+                                                                 float* __restrict__ pw, float* __restrict__ pdb) {
   constexpr int T = voc_tile<S>();
   __shared__ __attribute__((aligned(1024))) S tile[kVocBufs][T * H];
   __shared__ __attribute__((aligned(16))) float tl[kVocBufs][T], tf[kVocBufs][T];
@@ -736,10 +720,9 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
 
   float nl = 0.f, nf = 0.f;
   int nt = -1;
-  __shared__ int drawn;
   Run run;
-  Dealt dealt;
-  for (int round = 0; dealt.next(deal, blockIdx.x, queue, &drawn, &run); ++round) {
+  Dealt dealt(deal, blockIdx.x);
+  for (int round = 0; dealt.next(deal, blockIdx.x, &run); ++round) {
     const int t0 = run.t0, t1 = run.t1, vw = run.i * kVocRows + wave * 32, v = vw + lane % 32;
     frag_t<S> wf[H / 16];
     f32x16 a[H / 32];
@@ -801,7 +784,10 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
         start32(sn, tl[last ? nbuf : buf] + rs, lane);
         const int tj = tt[buf][r0 + lane % 32];
         float p[16];
-        auto prob = [&](int j) { p[j] = __builtin_amdgcn_exp2f(fmaf(s[j], kLog2e, b2)); };
+        auto prob = [&](int j) {
+          p[j] = __builtin_amdgcn_exp2f(fmaf(s[j], kLog2e, b2));
+          keep_here(p[j]);
+        };
 #if GGNN_DT_BF16
         __builtin_amdgcn_sched_barrier(0);
         step.template logits<LAST>(sn, wf, rs, r0, prob);
@@ -810,6 +796,17 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
 #pragma unroll
         for (int j = 0; j < 16; ++j) prob(j);
 #endif
+        // Whether a row's target falls on this wave's entries; its share of db.  (The
+        // branch also keeps the compiler from moving the exponentials away from
+        // the logits' products.)
+        const bool hit = __ballot((unsigned)(tj - vw) < 32u) != 0;
+        if (hit) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const int i = r0 + 8 * (j / 4) + 4 * g + j % 4;
+            if (tt[buf][i] == v) db -= WEIGHT ? tf[buf][i] : 1.f;
+          }
+        }
         if constexpr (WEIGHT) {
 #pragma unroll
           for (int j = 0; j < 16; ++j) p[j] *= tf[buf][r0 + 8 * (j / 4) + 4 * g + j % 4];
@@ -827,15 +824,15 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
         for (int j = 0; j < 16; ++j) db += p[j];
         step.product(a, p, tile[buf], r0, lane);
 #endif
-        // The rows' targets, where any falls on this wave's entries: a product of
-        // its own, since a bf16 pair of p - 1 would lose low bits of p to the 1.
-        if (__ballot((unsigned)(tj - vw) < 32u)) {
+        // The target's share of dW is a product of its own, since a bf16 pair of
+        // p - 1 would lose low bits of p to the 1.  (Without TARGETS it comes from
+        // launch_target_rows.)
+        if (TARGETS && hit) {
           float q[16];
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
             const int i = r0 + 8 * (j / 4) + 4 * g + j % 4;
             q[j] = tt[buf][i] != v ? 0.f : WEIGHT ? -tf[buf][i] : -1.f;
-            db += q[j];
           }
 #if GGNN_DT_BF16
 #pragma unroll
@@ -923,7 +920,7 @@ int voc_workers(int H, bool sum) {
   return 256 * dev::voc_waves<S>(H, sum);
 }
 
-dev::Deal make_deal(int tiles128, int tiles, int workers, bool queue) {
+dev::Deal make_deal(int tiles128, int tiles, int workers) {
   dev::Deal d{};
   d.tiles = tiles;
   // Four tiles a worker pay for its start and its share; fewer where that
@@ -933,11 +930,8 @@ dev::Deal make_deal(int tiles128, int tiles, int workers, bool queue) {
   d.whole = tiles128 / d.workers * d.workers;
   d.rest = tiles128 - d.whole;
   const uint32_t units = (uint32_t)d.rest * (uint32_t)tiles;   // fewer than workers * tiles
-  // Entries that many rows have for a target make their tiles' runs longer: where
-  // workers have whole tiles, the rest evens that out in smaller pieces.
-  d.pieces = queue && d.whole > 0 ? 4 * d.workers : d.workers;
-  d.each = units / d.pieces;
-  d.more = units % d.pieces;
+  d.each = units / d.workers;
+  d.more = units % d.workers;
   d.slots = 1;
   for (int i = d.whole; i < tiles128; ++i) {
     const int n = d.shares(i);
@@ -946,13 +940,21 @@ dev::Deal make_deal(int tiles128, int tiles, int workers, bool queue) {
   return d;
 }
 
+// Where the targets' share of dW, -g x of each row on its target's row, comes
+// from: a product beside the probabilities in the columns pass, or the sum over
+// rows sorted by target (csrc/embed.hip).  The first makes the workgroups with
+// the most frequent targets late (by a fifth of the pass at 60,001 rows over
+// 50,021 entries, H = 256: 4,875 us against 3,810), the second takes five
+// launches (about 45 us).
+bool targets_sorted(int H, int R, int V) { return (double)R * V * H > 4e10; }
+
 // How a call is cut, and where its shares lie in the workspace.
 struct VocabPlan {
   bool few;
   int splits, per;     // few rows
   int row_tiles, Rp, col_tiles;
   dev::Deal rows, cols;
-  size_t pm, pl, pb, po, xg, lse, tgt, fac, pw, pdb, queue, bytes;
+  size_t pm, pl, pb, po, xg, lse, tgt, fac, pw, pdb, sort, bytes;
 };
 template <typename S>
 VocabPlan vocab_plan(int H, int R, int V, bool grad) {
@@ -968,7 +970,7 @@ VocabPlan vocab_plan(int H, int R, int V, bool grad) {
   } else {
     p.row_tiles = cdiv(R, dev::kVocRows);
     p.Rp = p.row_tiles * dev::kVocRows;
-    p.rows = make_deal(p.row_tiles, cdiv(V, T), voc_workers<S>(H, grad), false);
+    p.rows = make_deal(p.row_tiles, cdiv(V, T), voc_workers<S>(H, grad));
     shares = (size_t)p.row_tiles * p.rows.slots * dev::kVocRows;
   }
   size_t at = 0;
@@ -982,7 +984,7 @@ VocabPlan vocab_plan(int H, int R, int V, bool grad) {
   if (!grad) p.pb = take(shares * sizeof(dev::RowBest));
   if (grad) {
     p.col_tiles = cdiv(V, dev::kVocRows);
-    p.cols = make_deal(p.col_tiles, p.Rp / T, voc_workers<S>(H, true), true);
+    p.cols = make_deal(p.col_tiles, p.Rp / T, voc_workers<S>(H, true));
     const size_t cshares = (size_t)p.col_tiles * p.cols.slots * dev::kVocRows;
     p.po = take(shares * H * 4);
     p.xg = take((size_t)p.Rp * H * sizeof(S));
@@ -991,7 +993,7 @@ VocabPlan vocab_plan(int H, int R, int V, bool grad) {
     p.fac = take((size_t)p.Rp * 4);
     p.pw = take(cshares * H * 4);
     p.pdb = take(cshares * 4);
-    p.queue = take(4);
+    if (targets_sorted(H, R, V)) p.sort = take(target_rows_workspace(H, p.Rp));
   }
   p.bytes = at;
   return p;
@@ -1017,7 +1019,7 @@ hipError_t vocab_loss_h(const VocabArgs& c, hipStream_t st) {
   hipLaunchKernelGGL((vocab_join_kernel<S, H, false, BEST>), dim3(cdiv((long)c.R * (H / 4), kVocThreads)),
                      dim3(kVocThreads), 0, st, c.n_nodes, c.R, c.V, p.Rp, p.rows, X, W, c.bias, c.node, c.target,
                      nullptr, 1.f, pm, pl, nullptr, pb, c.loss, c.lse, c.best, nullptr, nullptr, nullptr, nullptr,
-                     nullptr, nullptr);
+                     nullptr);
   return hipGetLastError();
 }
 
@@ -1032,8 +1034,6 @@ hipError_t vocab_grad_h(const VocabArgs& c, hipStream_t st) {
   float* pdb = reinterpret_cast<float*>(ws + p.pdb);
   int32_t* tgt_w = reinterpret_cast<int32_t*>(ws + p.tgt);
   S* xg = reinterpret_cast<S*>(ws + p.xg);
-  uint32_t* counter = reinterpret_cast<uint32_t*>(ws + p.queue);   // cleared by the join
-  uint32_t* queue = p.cols.pieces > p.cols.workers ? counter : nullptr;
   const S *X = static_cast<const S*>(c.X), *W = static_cast<const S*>(c.W);
   // A small dX is cleared by the rows pass, one launch less (5 us of the 70 at
   // 3,001 rows); a large one, which would hold its products up, by its own.
@@ -1047,19 +1047,25 @@ hipError_t vocab_grad_h(const VocabArgs& c, hipStream_t st) {
                      c.n_nodes, c.R, c.V, p.rows, X, W, c.bias, c.node, pm, pl, po, nullptr, c.dX, clear);
   hipLaunchKernelGGL((vocab_join_kernel<S, H, true, false>), dim3(cdiv((long)p.Rp * (H / 4), kVocThreads)),
                      dim3(kVocThreads), 0, st, c.n_nodes, c.R, c.V, p.Rp, p.rows, X, W, c.bias, c.node, c.target,
-                     c.weight, c.scale, pm, pl, po, nullptr, c.loss, c.lse, nullptr, c.dX, xg, lse_w, tgt_w, fac_w,
-                     counter);
-  if (c.weight != nullptr)
-    hipLaunchKernelGGL((vocab_cols_kernel<S, H, true>), dim3(p.cols.workers), dim3(kVocThreads), 0, st, c.V, p.Rp,
-                       p.cols, c.scale, xg, W, c.bias, lse_w, tgt_w, fac_w, c.dW, c.dbias, pw, pdb, queue);
-  else
-    hipLaunchKernelGGL((vocab_cols_kernel<S, H, false>), dim3(p.cols.workers), dim3(kVocThreads), 0, st, c.V, p.Rp,
-                       p.cols, c.scale, xg, W, c.bias, lse_w, tgt_w, fac_w, c.dW, c.dbias, pw, pdb, queue);
+                     c.weight, c.scale, pm, pl, po, nullptr, c.loss, c.lse, nullptr, c.dX, xg, lse_w, tgt_w, fac_w);
+  const bool sorted = targets_sorted(H, c.R, c.V);
+#define COLS(WEIGHT, TARGETS)                                                                                       \
+  hipLaunchKernelGGL((vocab_cols_kernel<S, H, WEIGHT, TARGETS>), dim3(p.cols.workers), dim3(kVocThreads), 0, st, c.V, \
+                     p.Rp, p.cols, c.scale, xg, W, c.bias, lse_w, tgt_w, fac_w, c.dW, c.dbias, pw, pdb)
+  if (c.weight != nullptr) {
+    if (sorted) COLS(true, false); else COLS(true, true);
+  } else {
+    if (sorted) COLS(false, false); else COLS(false, true);
+  }
+#undef COLS
   const long left = (long)c.V - (long)p.cols.whole * kVocRows;
   if (left > 0 && p.cols.slots > 1)
     hipLaunchKernelGGL((vocab_wsum_kernel<H>), dim3(cdiv(left * (H / 4), kVocThreads)), dim3(kVocThreads), 0, st, c.V,
                        p.cols, pw, pdb, c.dW, c.dbias);
-  return hipGetLastError();
+  const hipError_t err = hipGetLastError();
+  if (err != hipSuccess || !sorted) return err;
+  return launch_target_rows(sizeof(S) == 2 ? GGNN_BF16 : GGNN_F32, p.Rp, H, c.V, tgt_w, xg, -c.scale,
+                            c.weight != nullptr ? fac_w : nullptr, c.dW, ws + p.sort, st);
 }
 
 template <typename S, int H>
