@@ -217,21 +217,43 @@ __device__ __forceinline__ void split2(float a, float b, u32x4 (&part)[2][2], in
   part[1][ks][i] = pk2(a - lo_f(h), b - hi_f(h));
 }
 #else
-// float32: a product takes 64 times as long, so that plain code keeps the
-// matrix cores busy.
+// float32: a fragment's product takes 16 times as long, so that two fragments
+// ahead are enough.
 template <int H>
 struct VocStep {
-  __device__ __forceinline__ void logits(f32x16& s, const f32x8 (&x)[H / 16], const float* tile, int r0, int lane) {
-#pragma unroll
-    for (int kk = 0; kk < H / 16; ++kk) mma32(s, row_frag<float, H>(tile, r0, kk, lane), x[kk]);
+  static constexpr int NS = H / 16, NO = H / 16, kAhead = 2;
+  const float *st, *ot;   // tiles of the logits and of the second product
+  int lane;
+  f32x8 f[NS + NO];       // at most kAhead are alive
+
+  __device__ __forceinline__ void read(int n, int rs, int ro) {
+    if (n < NS) f[n] = row_frag<float, H>(st, rs, n, lane);
+    else f[n] = col_frag<H>(ot, ro + 16 * ((n - NS) / (H / 32)), (n - NS) % (H / 32), lane);
   }
-  __device__ __forceinline__ void product(f32x16 (&acc)[H / 32], const float (&p)[16], const float* tile, int r0,
-                                          int lane) {
+  template <int LAST>
+  __device__ __forceinline__ void begin(int rs, int ro) {
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
+    for (int n = 0; n < kAhead; ++n)
+      if (n <= LAST) read(n, rs, ro);
+  }
+  template <int LAST, typename Work>
+  __device__ __forceinline__ void logits(f32x16& s, const f32x8 (&x)[NS], int rs, int ro, Work work) {
 #pragma unroll
-      for (int ht = 0; ht < H / 32; ++ht)
-        mma32(acc[ht], col_frag<H>(tile, r0 + 16 * ks, ht, lane), pack8<float>(p + 8 * ks));
+    for (int n = 0; n < NS; ++n) {
+      if (n + kAhead <= LAST) read(n + kAhead, rs, ro);
+      mma32(s, f[n], x[n]);
+#pragma unroll
+      for (int i = n * 16 / NS; i < (n + 1) * 16 / NS; ++i) work(i);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  __device__ __forceinline__ void product(f32x16 (&acc)[H / 32], const float (&p)[16], int ro) {
+#pragma unroll
+    for (int n = 0; n < NO; ++n) {
+      if (n + kAhead < NO) read(NS + n + kAhead, 0, ro);
+      mma32(acc[n % (H / 32)], f[NS + n], pack8<float>(p + 8 * (n / (H / 32))));
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
 };
 #endif
@@ -283,25 +305,26 @@ __device__ __forceinline__ void load_row_frags(frag_t<S> (&f)[H / 16], const S* 
 // work during the exponentials.
 //
 // Work is dealt in units of one LDS tile against one tile of 128 rows (or, in
-// the columns pass, entries).  `workers` workgroups first take whole 128-tiles,
-// one each a round; the 128-tiles that are left over are laid end to end and
-// cut into equal runs of units, so that all workgroups end together.  A 128-tile
-// is thus one share, or a few neighbouring workers' shares, joined afterwards in
-// that order.
+// the columns pass, entries).  Many 128-tiles: `workers` workgroups first take
+// whole ones, one each a round; those left over are laid end to end and cut into
+// equal runs of units, so that all workgroups end together.  Few: each is cut
+// into `parts` runs, one a worker, so that no worker starts twice.  A 128-tile is
+// thus one share, or several workers' shares, joined afterwards in their order.
 struct Deal {
   int workers, tiles;   // workgroups; LDS tiles against one 128-tile
   int whole, rest;      // 128-tiles dealt whole (a multiple of workers), and cut up
   int slots;            // shares of a 128-tile, at most
-  uint32_t each, more;  // units of the rest for a worker; the first `more` workers have one more
-  // First unit of worker w in the rest, and the worker that has unit u.
+  int parts;            // of each 128-tile of the rest, or 0: cut end to end
+  uint32_t each, more;  // units of a worker (or a part); the first `more` have one more
   __host__ __device__ uint32_t begin(uint32_t w) const { return w * each + (w < more ? w : more); }
-  __host__ __device__ int owner(uint32_t u) const {
+  __host__ __device__ int owner(uint32_t u) const {   // worker that has unit u of the rest (parts = 0)
     const uint32_t k = more * (each + 1);
     return (int)(u < k ? u / (each + 1) : more + (u - k) / each);
   }
   // Shares of 128-tile i; share s of it is written to slot i * slots + s.
   __host__ __device__ int shares(int i) const {
     if (i < whole) return 1;
+    if (parts > 0) return parts;
     const uint32_t u = (uint32_t)(i - whole) * tiles;
     return owner(u + tiles - 1) - owner(u) + 1;
   }
@@ -312,8 +335,9 @@ struct Run {
 };
 struct Dealt {
   int step = 0;         // 128-tiles dealt whole so far
-  uint32_t u, end;      // units of the rest
-  __device__ __forceinline__ Dealt(const Deal& d, int w) : u(d.begin(w)), end(d.begin(w + 1)) {}
+  uint32_t u, end;      // units of the rest (parts: the worker's run, once)
+  __device__ __forceinline__ Dealt(const Deal& d, int w)
+      : u(d.begin(d.parts > 0 ? w % d.parts : w)), end(d.begin((d.parts > 0 ? w % d.parts : w) + 1)) {}
   __device__ __forceinline__ bool next(const Deal& d, int w, Run* r) {
     if (step * d.workers < d.whole) {
       const int i = step * d.workers + w;
@@ -322,6 +346,11 @@ struct Dealt {
       return true;
     }
     if (u >= end) return false;
+    if (d.parts > 0) {
+      *r = Run{w / d.parts, (int)u, (int)end, w / d.parts * d.slots + w % d.parts};
+      u = end;
+      return true;
+    }
     const uint32_t k = u / (uint32_t)d.tiles;
     r->i = d.whole + (int)k;
     r->t0 = (int)(u - k * d.tiles);
@@ -342,6 +371,11 @@ constexpr int voc_waves(int H, bool sum) {
 
 constexpr int kVocBufs = 3;
 __device__ __forceinline__ int next_buf(int b) { return b == kVocBufs - 1 ? 0 : b + 1; }
+// Bytes from the buffer before `b` to buffer b.
+template <uint32_t BYTES>
+__device__ __forceinline__ uint32_t buf_step(int b) {
+  return b == 0 ? 0u - (kVocBufs - 1) * BYTES : BYTES;
+}
 
 // Rows pass.  Writes each row's (m in units of log 2, l) of a share to pm, pl
 // [slot][128]; SUM: O too; BEST: the largest logit's entry too.  A small dX is
@@ -410,6 +444,8 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
     }
 #if GGNN_DT_BF16
     step.init(lds0, lane);
+#else
+    step.lane = lane;
 #endif
     for (int t = t0; t < t1; ++t) {
       const int nbuf = next_buf(buf);
@@ -421,12 +457,14 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
           land(t + 1, nbuf);
           if (t + 2 < t1) fetch(t + 2, next_buf(nbuf));
         }
-#if GGNN_DT_BF16
         constexpr int LAST = SUM ? 2 * (H / 16) - 1 : H / 16 - 1;
-        constexpr uint32_t kTile = T * H * sizeof(S);
-        if (last) step.move_s(nbuf == 0 ? 0u - (kVocBufs - 1) * kTile : kTile);
-        step.template begin<LAST>(rs, r0);
+#if GGNN_DT_BF16
+        if (last) step.move_s(buf_step<T * H * 2>(nbuf));
+#else
+        step.st = tile[last ? nbuf : buf];
+        step.ot = tile[buf];
 #endif
+        step.template begin<LAST>(rs, r0);
         f32x16 sn;
         start(sn, last ? t + 1 : t, last ? nbuf : buf, rs);
         float top = s[0];
@@ -466,15 +504,14 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
         if constexpr (SUM)
           step.template product<2>(o, part, rs, r0, [&](int i) { split2(p[8 + 2 * i], p[9 + 2 * i], part, 1, i); });
 #else
-        step.logits(sn, xf, tile[last ? nbuf : buf], rs, lane);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) prob(j);
-        if constexpr (SUM) step.product(o, p, tile[buf], r0, lane);
+        __builtin_amdgcn_sched_barrier(0);
+        step.template logits<LAST>(sn, xf, rs, r0, prob);
+        if constexpr (SUM) step.product(o, p, r0);
 #endif
         s = sn;
       }
 #if GGNN_DT_BF16
-      if constexpr (SUM) step.move_o(nbuf == 0 ? 0u - (kVocBufs - 1) * (uint32_t)(T * H * sizeof(S)) : (uint32_t)(T * H * sizeof(S)));
+      if constexpr (SUM) step.move_o(buf_step<T * H * 2>(nbuf));
 #endif
       buf = nbuf;
     }
@@ -763,6 +800,8 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
     }
 #if GGNN_DT_BF16
     step.init(lds0, lane);
+#else
+    step.lane = lane;
 #endif
     for (int t = t0; t < t1; ++t) {
       const int nbuf = next_buf(buf);
@@ -774,12 +813,14 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
           land(nbuf);
           if (t + 2 < t1) fetch(t + 2, next_buf(nbuf));
         }
-#if GGNN_DT_BF16
         constexpr int LAST = 2 * (H / 16) - 1;
-        constexpr uint32_t kTile = T * H * sizeof(S);
-        if (last) step.move_s(nbuf == 0 ? 0u - (kVocBufs - 1) * kTile : kTile);
-        step.template begin<LAST>(rs, r0);
+#if GGNN_DT_BF16
+        if (last) step.move_s(buf_step<T * H * 2>(nbuf));
+#else
+        step.st = tile[last ? nbuf : buf];
+        step.ot = tile[buf];
 #endif
+        step.template begin<LAST>(rs, r0);
         f32x16 sn;
         start32(sn, tl[last ? nbuf : buf] + rs, lane);
         const int tj = tt[buf][r0 + lane % 32];
@@ -788,14 +829,8 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
           p[j] = __builtin_amdgcn_exp2f(fmaf(s[j], kLog2e, b2));
           keep_here(p[j]);
         };
-#if GGNN_DT_BF16
         __builtin_amdgcn_sched_barrier(0);
         step.template logits<LAST>(sn, wf, rs, r0, prob);
-#else
-        step.logits(sn, wf, tile[last ? nbuf : buf], rs, lane);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) prob(j);
-#endif
         // Whether a row's target falls on this wave's entries; its share of db.  (The
         // branch also keeps the compiler from moving the exponentials away from
         // the logits' products.)
@@ -804,7 +839,10 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
             const int i = r0 + 8 * (j / 4) + 4 * g + j % 4;
-            if (tt[buf][i] == v) db -= WEIGHT ? tf[buf][i] : 1.f;
+            if (tt[buf][i] == v) {
+              if (sizeof(S) == 4 && TARGETS) p[j] -= 1.f;   // float32 loses nothing
+              else db -= WEIGHT ? tf[buf][i] : 1.f;
+            }
           }
         }
         if constexpr (WEIGHT) {
@@ -822,8 +860,9 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
 #else
 #pragma unroll
         for (int j = 0; j < 16; ++j) db += p[j];
-        step.product(a, p, tile[buf], r0, lane);
+        step.product(a, p, r0);
 #endif
+#if GGNN_DT_BF16
         // The target's share of dW is a product of its own, since a bf16 pair of
         // p - 1 would lose low bits of p to the 1.  (Without TARGETS it comes from
         // launch_target_rows.)
@@ -834,7 +873,6 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
             const int i = r0 + 8 * (j / 4) + 4 * g + j % 4;
             q[j] = tt[buf][i] != v ? 0.f : WEIGHT ? -tf[buf][i] : -1.f;
           }
-#if GGNN_DT_BF16
 #pragma unroll
           for (int n = 0; n < (WEIGHT ? 3 : 1); ++n) {   // -1 is one bf16, any float32 three
             u32x4 e[1][2];
@@ -849,14 +887,12 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
             for (int k = 0; k < step.kAhead; ++k) step.read(H / 16 + k, 0, r0);
             step.template product<1>(a, e, rs, r0, [](int) {});
           }
-#else
-          step.product(a, q, tile[buf], r0, lane);
-#endif
         }
+#endif
         s = sn;
       }
 #if GGNN_DT_BF16
-      step.move_o(nbuf == 0 ? 0u - (kVocBufs - 1) * (uint32_t)(T * H * sizeof(S)) : (uint32_t)(T * H * sizeof(S)));
+      step.move_o(buf_step<T * H * 2>(nbuf));
 #endif
       buf = nbuf;
     }
@@ -927,6 +963,15 @@ dev::Deal make_deal(int tiles128, int tiles, int workers) {
   // would leave compute units empty.
   const long all = (long)tiles128 * tiles, few = all < 256 ? all : 256, want = all / 4 > few ? all / 4 : few;
   d.workers = want < workers ? (int)want : workers;
+  d.parts = d.workers / tiles128 >= 4 ? d.workers / tiles128 : 0;
+  if (d.parts > 0) {
+    d.workers = d.parts * tiles128;
+    d.rest = tiles128;
+    d.each = (uint32_t)tiles / d.parts;
+    d.more = (uint32_t)tiles % d.parts;
+    d.slots = d.parts;
+    return d;
+  }
   d.whole = tiles128 / d.workers * d.workers;
   d.rest = tiles128 - d.whole;
   const uint32_t units = (uint32_t)d.rest * (uint32_t)tiles;   // fewer than workers * tiles
