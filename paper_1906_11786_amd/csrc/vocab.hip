@@ -210,12 +210,27 @@ struct VocStep {
   }
 };
 
-// Two values as the i-th words of a bf16 pair.
-__device__ __forceinline__ void split2(float a, float b, u32x4 (&part)[2][2], int ks, int i) {
-  const uint32_t h = pk2(a, b);
-  part[0][ks][i] = h;
-  part[1][ks][i] = pk2(a - lo_f(h), b - hi_f(h));
-}
+// Two values as the i-th words of a bf16 pair: hi rounds each to nearest, lo
+// the rest, which a two-element dot product with (-1, 0) or (0, -1) forms
+// exactly, without unpacking hi.  (From registers: the hardware does not read
+// the compiler's inline -1 as the low element.)
+struct Split {
+  bf16x2_t neg_lo, neg_hi;
+  __device__ __forceinline__ Split() {
+    uint32_t l, h;
+    asm("s_mov_b32 %0, 0xbf80" : "=s"(l));
+    asm("s_mov_b32 %0, 0xbf800000" : "=s"(h));
+    neg_lo = __builtin_bit_cast(bf16x2_t, l);
+    neg_hi = __builtin_bit_cast(bf16x2_t, h);
+  }
+  __device__ __forceinline__ void operator()(float a, float b, u32x4 (&part)[2][2], int ks, int i) const {
+    const uint32_t h = pk2(a, b);
+    const bf16x2_t v = __builtin_bit_cast(bf16x2_t, h);
+    part[0][ks][i] = h;
+    part[1][ks][i] = pk2(__builtin_amdgcn_fdot2_f32_bf16(v, neg_lo, a, false),
+                         __builtin_amdgcn_fdot2_f32_bf16(v, neg_hi, b, false));
+  }
+};
 #else
 // float32: a fragment's product takes 16 times as long, so that two fragments
 // ahead are enough.
@@ -378,9 +393,11 @@ __device__ __forceinline__ uint32_t buf_step(int b) {
 }
 
 // Rows pass.  Writes each row's (m in units of log 2, l) of a share to pm, pl
-// [slot][128]; SUM: O too; BEST: the largest logit's entry too.  A small dX is
-// cleared here, `clear` 16-byte pieces per thread (0: elsewhere).
-template <typename S, int H, bool SUM, bool BEST>
+// [slot][128]; SUM: O too; BEST: the largest logit's entry too; BIAS: there is
+// one (without, the logits' products start from zero, 16 registers less to set
+// a step).  A small dX is cleared here, `clear` 16-byte pieces per thread (0:
+// elsewhere).
+template <typename S, int H, bool SUM, bool BEST, bool BIAS>
 __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_kernel(int n_nodes, int R, int V, Deal deal,
                                                                  const S* __restrict__ X, const S* __restrict__ W,
                                                                  const float* __restrict__ bias,
@@ -390,7 +407,7 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
                                                                  float* __restrict__ dX, int clear) {
   constexpr int T = voc_tile<S>();
   __shared__ __attribute__((aligned(1024))) S tile[kVocBufs][T * H];
-  __shared__ __attribute__((aligned(16))) float tb[kVocBufs][T];
+  __shared__ __attribute__((aligned(16))) float tb[BIAS ? kVocBufs : 1][T];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = lane / 32;
   const uint32_t lds0 = (uint32_t)(uintptr_t)tile[0];
 
@@ -417,17 +434,17 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
     auto fetch = [&](int t, int buf) {   // start the copies of tile t < t1
       stage_tile<S, H>(W, (long)t * T, V - 1, lds0 + (uint32_t)(buf * T * H * sizeof(S)), wave, lane);
       // (the raw value: a use here would wait for the copies too)
-      if (threadIdx.x < T && bias != nullptr) nb = bias[min(t * T + (int)threadIdx.x, V - 1)];
+      if (BIAS && threadIdx.x < T) nb = bias[min(t * T + (int)threadIdx.x, V - 1)];
     };
     auto land = [&](int t, int buf) {   // and wait for those started last, of tile t
-      if (threadIdx.x < T)
+      if (BIAS && threadIdx.x < T)
         tb[buf][threadIdx.x] = t * T + (int)threadIdx.x >= V || nb <= kMaskedBias ? -INFINITY : nb;
       wait_copies<0>();
       __syncthreads();
     };
-    auto start = [&](f32x16& s, int t, int buf, int r0) {   // biases of tile t's entries
-      if (bias == nullptr && (t + 1) * T <= V) s = f32x16{};
-      else start32(s, tb[buf] + r0, lane);
+    auto start = [&](f32x16& s, int buf, int r0) {   // biases of a tile's entries
+      if constexpr (BIAS) start32(s, tb[buf] + r0, lane);
+      else s = f32x16{};
     };
     VocStep<H> step;
     f32x16 s;
@@ -438,7 +455,7 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
       load_row_frags<S, H>(xf, X, row_node(node, run.i * kVocRows + wave * 32 + lane % 32, R, n_nodes), lane);
       land(t0, 0);
       if (t0 + 1 < t1) fetch(t0 + 1, 1);
-      start(s, t0, 0, 0);
+      start(s, 0, 0);
 #pragma unroll
       for (int kk = 0; kk < H / 16; ++kk) mma32(s, row_frag<S, H>(tile[0], 0, kk, lane), xf[kk]);
     }
@@ -466,7 +483,12 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
 #endif
         step.template begin<LAST>(rs, r0);
         f32x16 sn;
-        start(sn, last ? t + 1 : t, last ? nbuf : buf, rs);
+        start(sn, last ? nbuf : buf, rs);
+        if (!BIAS && (t + 1) * T > V) {   // the last tile: beyond V (with a bias, the bias is -inf there)
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            if (t * T + r0 + 8 * (j / 4) + 4 * g + j % 4 >= V) s[j] = -INFINITY;
+        }
         float top = s[0];
 #pragma unroll
         for (int j = 1; j < 16; ++j) top = fmaxf(top, s[j]);
@@ -496,6 +518,7 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
         };
 #if GGNN_DT_BF16
         u32x4 part[2][2];
+        const Split split2;
         __builtin_amdgcn_sched_barrier(0);
         step.template logits<LAST>(sn, xf, rs, r0, [&](int j) {
           prob(j);
@@ -851,6 +874,7 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
         }
 #if GGNN_DT_BF16
         u32x4 part[2][2];
+        const Split split2;
 #pragma unroll
         for (int i = 0; i < 4; ++i) split2(p[2 * i], p[2 * i + 1], part, 0, i);
         step.template product<2>(a, part, rs, r0, [&](int i) {
@@ -1059,8 +1083,12 @@ hipError_t vocab_loss_h(const VocabArgs& c, hipStream_t st) {
                        p.splits, X, W, c.bias, c.node, c.target, pm, pl, pb, c.loss, c.lse, c.best);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((vocab_rows_kernel<S, H, false, BEST>), dim3(p.rows.workers), dim3(kVocThreads), 0, st,
-                     c.n_nodes, c.R, c.V, p.rows, X, W, c.bias, c.node, pm, pl, nullptr, pb, nullptr, 0);
+  if (c.bias != nullptr)
+    hipLaunchKernelGGL((vocab_rows_kernel<S, H, false, BEST, true>), dim3(p.rows.workers), dim3(kVocThreads), 0, st,
+                       c.n_nodes, c.R, c.V, p.rows, X, W, c.bias, c.node, pm, pl, nullptr, pb, nullptr, 0);
+  else
+    hipLaunchKernelGGL((vocab_rows_kernel<S, H, false, BEST, false>), dim3(p.rows.workers), dim3(kVocThreads), 0, st,
+                       c.n_nodes, c.R, c.V, p.rows, X, W, nullptr, c.node, pm, pl, nullptr, pb, nullptr, 0);
   hipLaunchKernelGGL((vocab_join_kernel<S, H, false, BEST>), dim3(cdiv((long)c.R * (H / 4), kVocThreads)),
                      dim3(kVocThreads), 0, st, c.n_nodes, c.R, c.V, p.Rp, p.rows, X, W, c.bias, c.node, c.target,
                      nullptr, 1.f, pm, pl, nullptr, pb, c.loss, c.lse, c.best, nullptr, nullptr, nullptr, nullptr,
@@ -1088,8 +1116,12 @@ hipError_t vocab_grad_h(const VocabArgs& c, hipStream_t st) {
     const hipError_t err = launch_fill_zero(c.dX, (size_t)c.n_nodes * H, st);
     if (err != hipSuccess) return err;
   }
-  hipLaunchKernelGGL((vocab_rows_kernel<S, H, true, false>), dim3(p.rows.workers), dim3(kVocThreads), 0, st,
-                     c.n_nodes, c.R, c.V, p.rows, X, W, c.bias, c.node, pm, pl, po, nullptr, c.dX, clear);
+  if (c.bias != nullptr)
+    hipLaunchKernelGGL((vocab_rows_kernel<S, H, true, false, true>), dim3(p.rows.workers), dim3(kVocThreads), 0, st,
+                       c.n_nodes, c.R, c.V, p.rows, X, W, c.bias, c.node, pm, pl, po, nullptr, c.dX, clear);
+  else
+    hipLaunchKernelGGL((vocab_rows_kernel<S, H, true, false, false>), dim3(p.rows.workers), dim3(kVocThreads), 0, st,
+                       c.n_nodes, c.R, c.V, p.rows, X, W, nullptr, c.node, pm, pl, po, nullptr, c.dX, clear);
   hipLaunchKernelGGL((vocab_join_kernel<S, H, true, false>), dim3(cdiv((long)p.Rp * (H / 4), kVocThreads)),
                      dim3(kVocThreads), 0, st, c.n_nodes, c.R, c.V, p.Rp, p.rows, X, W, c.bias, c.node, c.target,
                      c.weight, c.scale, pm, pl, po, nullptr, c.loss, c.lse, nullptr, c.dX, xg, lse_w, tgt_w, fac_w);
