@@ -1,0 +1,121 @@
+"""NodeTokens: one training step's losses, gradients and update against the
+oracle's propagation with the 64-bit references of the token operators; the
+example learns; serving answers with the largest logit."""
+import os
+import sys
+
+import numpy as np
+import pytest
+
+import oracle as O
+import token_reference as R
+from ggnn_synth import backbone_graph, draw_params, scramble_graph
+from gpu_helpers import TOL, host, relerr, round_to, say
+
+capi = pytest.importorskip("paper_1906_11786_amd.capi")
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from paper_1906_11786_amd.driver import BandedGGNN, compile_graphs  # noqa: E402
+from paper_1906_11786_amd.tokens import NodeTokens, token_lists  # noqa: E402
+
+
+@pytest.fixture(autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+
+
+def setup(dt, H, n=400, B=64, E=3, T=2, V=173, p=0.25):
+    rng = np.random.default_rng(H)
+    g = scramble_graph(9, 0, backbone_graph(9, 0, n, E, span_mean=6.0, max_span=B))[0]
+    comp = compile_graphs([g], B, E, reorder=True)
+    params = draw_params(9, comp.n_real, comp.n_pad, H, E, dt, with_bias=True)
+    lists = [list(rng.integers(0, V, rng.integers(0, 5))) for _ in range(n)]
+    ptr, tok = token_lists(lists, comp.n_pad)
+    table = round_to(dt, rng.standard_normal((V, H)) / np.sqrt(H))
+    bias = round_to("f32", 0.3 * rng.standard_normal(V))
+    m = BandedGGNN(comp, H, T, dt, params)
+    t = NodeTokens(m, table, ptr, tok, bias=bias, scale=float(np.sqrt(H)), p_in=p, p_out=p, seed=2**40 + 3)
+    node = rng.permutation(n)[:60]
+    target = rng.integers(0, V, 60)
+    target[::7] = -1
+    return m, t, comp, params, ptr, tok, table, bias, node, target, (B, T, V, p)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("H", [64, 128])
+def test_training_step_against_the_oracle(dt, H):
+    say(f"node tokens dt={dt} H={H}")
+    m, t, comp, params, ptr, tok, table, bias, node, target, (B, T, V, p) = setup(dt, H)
+    n, sc, step = comp.n_pad, float(np.sqrt(H)), 3
+    t.setup_training(node, target, lr=0.125, momentum=0.5)
+    t.step = step
+    t.gradients(step)
+    got = dict(loss=host(t.loss), dtable=host(t.dtable), dbias=host(t.dbias), dW=host(m.dW), dWi=host(m.dWi),
+               dU=host(m.dU), db=host(m.db))
+    # the same step in 64 bits; the first states are the stored (rounded) ones
+    X0, _, _ = R.embed(table, n, ptr, tok, int(ptr[-1]), sc, True, p, t.seed, 2 * step)
+    X0 = host(m.X[0]) if dt == "bf16" else X0
+    out = O.propagate(n, B, comp.src, comp.dst, comp.etype, X0, params.W, params.Wi, params.U, params.b, T,
+                      bias=params.bias)
+    keep = R.keep_factor(0, n * H, p, t.seed, 2 * step + 1).reshape(n, H)
+    live = int((target >= 0).sum())
+    v = R.vocab(out["X"][-1] * keep, table, bias, node, target, None, 1.0 / live, dt)
+    out = O.propagate(n, B, comp.src, comp.dst, comp.etype, X0, params.W, params.Wi, params.U, params.b, T,
+                      G=v["dX"] * keep, bias=params.bias)
+    dT, _, _ = R.embed_grad(out["dX0"], V, ptr, tok, int(ptr[-1]), sc, True, p, t.seed, 2 * step)
+    want = dict(loss=v["loss"], dtable=v["dW"] + dT, dbias=v["db"], dW=out["dW"], dWi=out["dWi"], dU=out["dU"],
+                db=out["db"])
+    for k, w in want.items():
+        e = relerr(got[k], w)
+        say(f"  {k}: {e:.2e}")
+        assert e <= TOL[dt], k
+    # the update: velocities start at zero, so parameter -= lr * gradient
+    before = t.master.clone()
+    t.train_step()
+    assert t.step == step + 1
+    assert torch.equal(t.master, before - 0.125 * t.grad)
+    if dt == "bf16":
+        assert torch.equal(t.compute_copy, t.master.to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_serving_answers_with_the_largest_logit(dt):
+    m, t, comp, params, ptr, tok, table, bias, node, target, _ = setup(dt, 64)
+    out = t.evaluate(node[:5], target[:5])
+    x = host(m.X[m.T])[node[:5]]
+    z = x @ host(t.table).T + host(t.bias)
+    top = np.sort(z, 1)
+    assert np.all(top[:, -1] - top[:, -2] > 1e-3)    # no near ties in these five rows
+    assert np.array_equal(out["best"].cpu().numpy(), np.argmax(z, 1))
+    one = t.evaluate(node[:1])
+    assert torch.equal(one["best"], out["best"][:1]) and "loss" not in one
+    lse = np.log(np.exp(z).sum(1))
+    assert np.max(np.abs(host(out["lse"]) - lse)) <= 1e-4
+    want = np.where(target[:5] >= 0, lse - z[np.arange(5), np.maximum(target[:5], 0)], 0.0)
+    assert np.max(np.abs(host(out["loss"]) - want)) <= 1e-4
+
+
+def test_refusals():
+    m, t, comp, params, ptr, tok, table, bias, node, target, (_, _, V, _) = setup("f32", 64)
+    with pytest.raises(ValueError, match="table"):
+        NodeTokens(m, table[:, :32], ptr, tok)
+    with pytest.raises(ValueError, match="tok_ptr"):
+        NodeTokens(m, table, ptr[:-1], tok)
+    with pytest.raises(ValueError, match="more than once"):
+        t.setup_training([3, 3], [0, 1])
+    with pytest.raises(ValueError, match="node ids"):
+        t.evaluate([comp.n_pad])
+    with pytest.raises(ValueError, match="targets"):
+        t.setup_training([3, 4], [0, V])
+    with pytest.raises(RuntimeError, match="setup_training"):
+        t.train_step()
+
+
+def test_example_learns():
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import hidden_tokens
+    losses = hidden_tokens.main(steps=40)
+    assert losses[0] > 5.0                       # about log 500 at the start
+    assert np.mean(losses[-5:]) < 0.5 * losses[0]

@@ -135,3 +135,14 @@ def test_generator_words_are_spread_evenly():
                   R.philox7(np.arange(1 << 16, dtype=np.uint64), 5, 2**40 + 8)):
         bits = np.unpackbits((w ^ other).view(np.uint8)).mean()
         assert abs(bits - 0.5) < 6 * 0.5 / (w.size * 32) ** 0.5
+
+
+def test_token_lists_layout():
+    tokens = pytest.importorskip("paper_1906_11786_amd.tokens")
+    ptr, tok = tokens.token_lists([[3, 1], [], [2]], 5)
+    assert ptr.tolist() == [0, 2, 2, 3, 3, 3] and tok.tolist() == [3, 1, 2]
+    assert ptr.dtype == np.int32 and tok.dtype == np.int32
+    ptr, tok = tokens.token_lists([[], []], 4)
+    assert ptr.tolist() == [0, 0, 0, 0, 0] and len(tok) == 1
+    with pytest.raises(ValueError, match="3 token lists for 2 nodes"):
+        tokens.token_lists([[], [], []], 2)
