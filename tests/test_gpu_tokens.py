@@ -431,3 +431,65 @@ def test_token_calls_in_a_captured_graph_on_a_side_stream():
         torch.cuda.synchronize()
         for t, w in zip((X, Y, dX, dT, loss, lse), want):
             assert torch.equal(t, w)
+
+
+# ------------------------------------- sizes that start the other large forms
+
+def large_reference(X, W, b, node, target, weight, scale, dt):
+    """R.vocab's results and bounds (dX, dW, db, lse) in float64 on the GPU."""
+    f = (lambda a: torch.from_numpy(np.ascontiguousarray(a, np.float64)).cuda())
+    x, Wd, t = f(X[node]), f(W), torch.from_numpy(target.astype(np.int64)).cuda()
+    H, V, rows = X.shape[1], W.shape[0], len(node)
+    Wt = Wd.t().contiguous()
+    z = torch.mm(x, Wt) + (0.0 if b is None else f(b))
+    dz = (H + 4) * R.U * (torch.mm(x.abs(), Wt.abs()).amax(1) + (0.0 if b is None else float(np.abs(b).max())))
+    lse = torch.logsumexp(z, 1)
+    lse_tol = dz + 2.0**-21 + V / 2 * R.U + 16 * R.U * (1 + lse.abs() + z.abs().amax(1))
+    has = t >= 0
+    g = torch.where(has, scale * (torch.ones(rows, device="cuda").double() if weight is None else f(weight)), 0.0)
+    P = torch.exp(z - lse[:, None])
+    del z
+    D = g[:, None] * P
+    at = (torch.arange(rows, device="cuda"), t.clamp(min=0))
+    eps = 2 * dz + lse_tol + 2.0**-20 + (2.0**-16 if dt == "bf16" else 0.0)
+    dX_tol = torch.mm(D.abs() * (eps[:, None] + (V + 8) * R.U), Wd.abs())
+    big = D.abs()
+    D[at] -= g
+    big[at] += g.abs()
+    dX_tol += 8 * R.U * torch.mm(big, Wd.abs())
+    big *= (eps + (rows + 8) * R.U)[:, None]
+    bigT, DT = big.t().contiguous(), D.t().contiguous()
+    c = (lambda a: a.cpu().numpy())
+    return dict(lse=c(lse), lse_tol=c(lse_tol), dX=c(torch.mm(D, Wd)), dX_tol=c(dX_tol), dW=c(torch.mm(DT, x)),
+                dW_tol=c(torch.mm(bigT, x.abs())), db=c(D.sum(0)), db_tol=c(big.sum(0)))
+
+
+@pytest.mark.parametrize("dt,H,rows,V,bias,weighted", [
+    ("bf16", 256, 33500, 333, True, False),    # whole 128-tiles of rows for every worker, then the rest
+    ("bf16", 256, 300, 33500, False, False),   # and of entries
+    ("f32", 128, 300, 33500, True, True),
+    ("bf16", 256, 33100, 4900, True, False),   # rows sorted by target
+    ("bf16", 64, 65600, 9800, False, True),
+    ("f32", 256, 33100, 4900, False, True),
+])
+def test_vocab_large_forms(dt, H, rows, V, bias, weighted):
+    say(f"vocab large dt={dt} H={H} rows={rows} V={V}")
+    rng = np.random.default_rng(V)
+    X, W, node, target, b = vocab_case(rng, dt, rows + 100, H, V, rows, bias)
+    target = np.where(rng.random(rows) < 0.3, 5, target).astype(np.int32)   # a frequent target
+    target[::9] = -1
+    weight = round_to("f32", rng.standard_normal(rows)) if weighted else None
+    want = large_reference(X, W, b, node, target, weight, 2.0 / rows, dt)
+    got = run_vocab(dt, X, W, b, node, target, weight, 2.0 / rows)
+    again = run_vocab(dt, X, W, b, node, target, weight, 2.0 / rows)
+    for k in got:
+        assert np.array_equal(got[k], again[k]), k
+    R.within(got["lse"], want["lse"], want["lse_tol"])
+    R.within(got["dX"][node], want["dX"], want["dX_tol"])
+    rest = np.ones(len(X), bool)
+    rest[node] = False
+    assert not got["dX"][rest].any()
+    for k in ("dW", "db"):   # added to ones
+        R.within(got[k], want[k], want[k + "_tol"] + 4 * R.U * (1 + np.abs(want[k])))
+    plain = run_vocab(dt, X, W, b, node, target, grad=False)
+    R.within(plain["lse"], want["lse"], want["lse_tol"])
