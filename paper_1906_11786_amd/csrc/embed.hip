@@ -691,26 +691,17 @@ hipError_t launch_embed_bwd(int n, int H, int V, const int32_t* tok_ptr, const i
 
 size_t target_rows_workspace(int H, int R) { return embed_layout(H, R).bytes; }
 
-namespace {
-template <typename S>
-hipError_t target_rows(int R, int H, int V, const int32_t* target, const void* x, float scale, const float* factor,
-                       float* dW, char* ws, hipStream_t st) {
+hipError_t launch_target_rows(int R, int H, int V, const int32_t* target, const void* x, float scale,
+                              const float* factor, float* dW, void* ws, hipStream_t st) {
   const Dropout none{};
+  char* w = static_cast<char*>(ws);
   switch (H) {
-    case 32: return embed_bwd_h<S, 32>(R, V, nullptr, target, R, scale, 0, factor, none, x, dW, ws, st);
-    case 64: return embed_bwd_h<S, 64>(R, V, nullptr, target, R, scale, 0, factor, none, x, dW, ws, st);
-    case 128: return embed_bwd_h<S, 128>(R, V, nullptr, target, R, scale, 0, factor, none, x, dW, ws, st);
-    case 256: return embed_bwd_h<S, 256>(R, V, nullptr, target, R, scale, 0, factor, none, x, dW, ws, st);
+    case 32: return embed_bwd_h<dev::bf16s, 32>(R, V, nullptr, target, R, scale, 0, factor, none, x, dW, w, st);
+    case 64: return embed_bwd_h<dev::bf16s, 64>(R, V, nullptr, target, R, scale, 0, factor, none, x, dW, w, st);
+    case 128: return embed_bwd_h<dev::bf16s, 128>(R, V, nullptr, target, R, scale, 0, factor, none, x, dW, w, st);
+    case 256: return embed_bwd_h<dev::bf16s, 256>(R, V, nullptr, target, R, scale, 0, factor, none, x, dW, w, st);
   }
   return hipErrorInvalidValue;
-}
-}  // namespace
-
-hipError_t launch_target_rows(int dt, int R, int H, int V, const int32_t* target, const void* x, float scale,
-                              const float* factor, float* dW, void* ws, hipStream_t st) {
-  char* w = static_cast<char*>(ws);
-  return dt == GGNN_BF16 ? target_rows<dev::bf16s>(R, H, V, target, x, scale, factor, dW, w, st)
-                         : target_rows<float>(R, H, V, target, x, scale, factor, dW, w, st);
 }
 #endif
 

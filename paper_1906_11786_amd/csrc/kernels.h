@@ -25,9 +25,9 @@ struct ReduceSeg {
   long stride;
 };
 // dW[target[r]] += factor_r x[r] over rows sorted by target (csrc/embed.hip; negative targets: none), factor_r =
-// scale, or -factor[r] where factor is given; x [R][H] dt, workspace of target_rows_workspace bytes.
+// scale, or -factor[r] where factor is given; x [R][H] bf16, workspace of target_rows_workspace bytes.
 size_t target_rows_workspace(int H, int R);
-hipError_t launch_target_rows(int dt, int R, int H, int V, const int32_t* target, const void* x, float scale,
+hipError_t launch_target_rows(int R, int H, int V, const int32_t* target, const void* x, float scale,
                               const float* factor, float* dW, void* ws, hipStream_t st);
 struct ReduceList {
   static constexpr int kMax = 8;

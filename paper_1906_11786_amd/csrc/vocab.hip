@@ -37,7 +37,13 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kMaskedBias = -1e30f;      // a bias at or below takes its entry out
 constexpr float kNoMax = -3e38f;           // running maximum before the first logit
 
-// Entries of an LDS tile: 64 in bf16, 32 in float32 (twice the bytes).
+// float32 states and rows enter the matrix cores as three bf16 each (x = x0 +
+// x1 + x2, exact), with the six products of order 2^-16 and up: 24 bits at 6
+// bf16 products, where the float32 matrix instructions take 16 times a bf16
+// product's time.  Probabilities, likewise, as three parts (two in bf16).
+template <typename S> constexpr int voc_planes() { return sizeof(S) == 2 ? 1 : 3; }
+template <typename S> constexpr int voc_parts() { return sizeof(S) == 2 ? 2 : 3; }
+// Entries of an LDS tile: 64 in bf16, 32 in float32 (three times the bytes).
 template <typename S> constexpr int voc_tile() { return sizeof(S) == 2 ? 64 : 32; }
 
 __device__ __forceinline__ void mma32(f32x16& acc, const bf16x8& a, const bf16x8& b) {
@@ -48,60 +54,33 @@ __device__ __forceinline__ void mma32(f32x16& acc, const f32x8& a, const f32x8& 
   for (int i = 0; i < 8; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], acc, 0, 0, 0);
 }
 
-// LDS tile of rows of H elements in 16-byte pieces; piece c of row r lies at
-// place c ^ swz(r) of its row.  Sixteen rows read at one piece (fragments along
+// LDS tile: planes of T rows of H bf16 in 16-byte pieces; piece c of row r lies
+// at place c ^ swz(r) of its row.  Sixteen rows read at one piece (fragments along
 // H) and four rows times four pieces (fragments across rows) then both fall on
 // different banks, without padding, so that the copies into LDS stay linear.
-template <typename S, int H>
+template <int H>
 __device__ __forceinline__ int swz(int r) {
-  constexpr int CPR = H * (int)sizeof(S) / 16;
+  constexpr int CPR = H / 8;
   if constexpr (CPR >= 16) return ((r & 3) << 2) | ((r >> 2) & 3);
   if constexpr (CPR == 8) return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
   return (r >> 2) & 3;
 }
 
-// Copies tile rows row0 .. row0 + T - 1 (the last one's where beyond) to LDS.
-template <typename S, int H>
-__device__ __forceinline__ void stage_tile(const S* __restrict__ src, long row0, long last, uint32_t lds, int wave,
-                                           int lane) {
-  constexpr int CPR = H * (int)sizeof(S) / 16;
-  constexpr int PIECES = voc_tile<S>() * CPR / 64;   // 1 KB copies
+// Copies rows row0 .. row0 + T - 1 (the last one's where beyond) of each plane
+// to LDS; a plane holds `plane` elements.
+template <int H, int NP, int T>
+__device__ __forceinline__ void stage_tile(const bf16s* __restrict__ src, size_t plane, long row0, long last,
+                                           uint32_t lds, int wave, int lane) {
+  constexpr int CPR = H / 8, EACH = T * CPR / 64, PIECES = NP * EACH;   // 1 KB copies of a plane, and in all
 #pragma unroll
-  for (int p = 0; p < PIECES / kVocWaves; ++p) {
-    const int piece = p * kVocWaves + wave, q = piece * 64 + lane;
-    const int r = q / CPR, c = (q % CPR) ^ swz<S, H>(r);
+  for (int p = 0; p < (PIECES + kVocWaves - 1) / kVocWaves; ++p) {
+    const int piece = p * kVocWaves + wave, q = piece % EACH * 64 + lane;
+    if (PIECES % kVocWaves != 0 && piece >= PIECES) break;
+    const int r = q / CPR, c = (q % CPR) ^ swz<H>(r);
     const long row = row0 + r < last ? row0 + r : last;
-    dma16(reinterpret_cast<const char*>(src + row * H) + 16 * c,
+    dma16(src + piece / EACH * plane + row * H + 8 * c,
           __builtin_amdgcn_readfirstlane(lds + (uint32_t)piece * 1024u));
   }
-}
-
-// Fragment along H: row r0 + lane % 32, elements 16 kk + 8 (lane / 32) .. + 7.
-template <typename S, int H>
-__device__ __forceinline__ frag_t<S> row_frag(const S* tile, int r0, int kk, int lane) {
-  constexpr int CPR = H * (int)sizeof(S) / 16;
-  const int r = r0 + lane % 32, g = lane / 32;
-  if constexpr (sizeof(S) == 2) {
-    return load8(tile + ((size_t)r * CPR + ((2 * kk + g) ^ swz<S, H>(r))) * 8);
-  } else {
-    const int c = 4 * kk + 2 * g, s = swz<S, H>(r);
-    return load4x2(tile + (r * CPR + (c ^ s)) * 4, tile + (r * CPR + ((c + 1) ^ s)) * 4);
-  }
-}
-
-// Fragment across rows: column 32 ht + lane % 32, rows r0 + {0, 8} + 4 (lane / 32) + 0 .. 3
-// (the order in which a lane holds the accumulators of a 32 x 32 tile).
-template <int H>
-__device__ __forceinline__ f32x8 col_frag(const float* tile, int r0, int ht, int lane) {
-  constexpr int CPR = H * 4 / 16;
-  const int q = lane % 32, g = lane / 32;
-  f32x8 v;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const int r = r0 + (e / 4) * 8 + 4 * g + e % 4;
-    v[e] = tile[(r * CPR + ((8 * ht + q / 4) ^ swz<float, H>(r))) * 4 + q % 4];
-  }
-  return v;
 }
 
 // ---- the two products of a 32 x 32 tile -----------------------------------
@@ -113,36 +92,31 @@ __device__ __forceinline__ f32x8 col_frag(const float* tile, int r0, int ht, int
 // compiler's scheduler kept from moving anything between these slots (its own
 // order read one fragment ahead and left the rest of the latency open).
 //
-// A step on tile rows r0 .. r0 + 31: logits of the next tile (NS products),
-// then the second product of this one (NO fragments, each times the hi and the
-// lo part of p).
+// A step on tile rows r0 .. r0 + 31: logits of the next tile (fragments along
+// H), then the second product of this one (fragments across rows, times the
+// parts of p).  Of NP planes, products a, b with a + b >= 3 are left out.
 
-// Keeps the compiler from moving what forms v past this point.
-__device__ __forceinline__ void keep_here(float& v) { asm volatile("" : "+v"(v)); }
-
-#if GGNN_DT_BF16
 typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
 
-template <int H>
+template <int H, int NP, int T>
 struct VocStep {
-  static constexpr int NS = H / 16, NO = H / 16;
-  static constexpr int kAhead = NS < 8 ? NS : 8;
-  static constexpr int CPR = H * 2 / 16;
-  static constexpr uint32_t ROW = H * 2;                       // bytes of a tile row
+  static constexpr int NS = H / 16, NF = NS * NP;              // k steps; fragments of either product
+  static constexpr int kAhead = NF < 8 ? NF : 8;
+  static constexpr uint32_t ROW = H * 2, PLANE = T * ROW;      // bytes of a tile row and of a plane
   static constexpr int VS = NS < 8 ? NS : 8, VO = H / 32 < 4 ? H / 32 : 4;
-  uint32_t as[VS], ao[2][VO];   // LDS addresses of the fragments; the other ones lie 256 bytes or whole rows on
-  bf16x8 f[NS + NO];            // at most kAhead are alive
+  uint32_t as[VS], ao[2][VO];   // LDS addresses of the fragments; the other ones lie 256 bytes, rows or planes on
+  bf16x8 f[2 * NF];             // at most kAhead are alive
 
   __device__ __forceinline__ void init(uint32_t lds, int lane) {
     const int r = lane % 32, g = lane / 32, p = lane % 16;
 #pragma unroll
-    for (int k = 0; k < VS; ++k) as[k] = lds + (uint32_t)r * ROW + 16u * ((2 * k + g) ^ swz<bf16s, H>(r));
+    for (int k = 0; k < VS; ++k) as[k] = lds + (uint32_t)r * ROW + 16u * ((2 * k + g) ^ swz<H>(r));
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int ht = 0; ht < VO; ++ht) {
         const int row = 8 * i + 4 * g + p / 4, c = 4 * ht + 2 * ((lane / 16) & 1) + (p % 4) / 2;
-        ao[i][ht] = lds + (uint32_t)row * ROW + 16u * (c ^ swz<bf16s, H>(row)) + 8u * (p % 2);
+        ao[i][ht] = lds + (uint32_t)row * ROW + 16u * (c ^ swz<H>(row)) + 8u * (p % 2);
       }
   }
   __device__ __forceinline__ void move_s(uint32_t by) {
@@ -155,15 +129,20 @@ struct VocStep {
 #pragma unroll
       for (int ht = 0; ht < VO; ++ht) ao[i][ht] += by;
   }
-  // Fragment n of a step: n < NS along H of the next tile (rows rs), else
-  // across the rows of this one (rows ro); see row_frag and col_frag.
+  // Fragment n of a step.  n < NF: along H of the next tile, row rs + lane % 32,
+  // elements 16 kk + 8 (lane / 32) .. + 7 of plane n % NP.  Else across the rows
+  // of this one: column 32 ht + lane % 32, rows ro + 16 ks + {0, 8} + 4 (lane /
+  // 32) + 0 .. 3, the order in which a lane holds the accumulators of a 32 x 32
+  // tile.
   __device__ __forceinline__ void read(int n, int rs, int ro) {
-    if (n < NS) {
-      f[n] = __builtin_bit_cast(bf16x8, *(lds_u32x4*)(as[n % VS] + 256u * (n / VS) + (uint32_t)rs * ROW));
+    if (n < NF) {
+      const int kk = n / NP;
+      f[n] = __builtin_bit_cast(bf16x8, *(lds_u32x4*)(as[kk % VS] + 256u * (kk / VS) + (uint32_t)rs * ROW +
+                                                      (uint32_t)(n % NP) * PLANE));
     } else {
-      const int ks = (n - NS) / (H / 32), ht = (n - NS) % (H / 32);
+      const int q = (n - NF) / NP, ks = q / (H / 32), ht = q % (H / 32);
       typedef short v8i16 __attribute__((ext_vector_type(8)));
-      const uint32_t off = 256u * (ht / VO) + (uint32_t)(ro + 16 * ks) * ROW;
+      const uint32_t off = 256u * (ht / VO) + (uint32_t)(ro + 16 * ks) * ROW + (uint32_t)((n - NF) % NP) * PLANE;
       const tr_v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr_v4i16*)(ao[0][ht % VO] + off));
       const tr_v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr_v4i16*)(ao[1][ht % VO] + off));
       f[n] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -178,13 +157,14 @@ struct VocStep {
   }
   // s += logits of the next tile; work(i), i < 16, is done alongside.
   template <int LAST, typename Work>
-  __device__ __forceinline__ void logits(f32x16& s, const bf16x8 (&x)[NS], int rs, int ro, Work work) {
+  __device__ __forceinline__ void logits(f32x16& s, const bf16x8 (&x)[NP][NS], int rs, int ro, Work work) {
 #pragma unroll
-    for (int n = 0; n < NS; ++n) {
+    for (int n = 0; n < NF; ++n) {
       if (n + kAhead <= LAST) read(n + kAhead, rs, ro);
-      mma32(s, f[n], x[n]);
 #pragma unroll
-      for (int i = n * 16 / NS; i < (n + 1) * 16 / NS; ++i) work(i);
+      for (int b = 0; b + n % NP < NP; ++b) mma32(s, f[n], x[b][n / NP]);
+#pragma unroll
+      for (int i = n * 16 / NF; i < (n + 1) * 16 / NF; ++i) work(i);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
@@ -194,25 +174,26 @@ struct VocStep {
   template <int PARTS, typename Work>
   __device__ __forceinline__ void product(f32x16 (&acc)[H / 32], const u32x4 (&part)[PARTS][2], int rs, int ro,
                                           Work work) {
+    constexpr int TOP = NP == 1 ? PARTS : NP;
 #pragma unroll
-    for (int n = 0; n < NO; ++n) {
-      const int ks = n / (H / 32), ht = n % (H / 32);
-      if (n + kAhead < NO) read(NS + n + kAhead, rs, ro);
-      mma32(acc[ht], f[NS + n], __builtin_bit_cast(bf16x8, part[0][ks]));
-      if (ks == 0) {
+    for (int n = 0; n < NF; ++n) {
+      const int a = n % NP, ks = n / NP / (H / 32), ht = n / NP % (H / 32);
+      if (n + kAhead < NF) read(NF + n + kAhead, rs, ro);
+      mma32(acc[ht], f[NF + n], __builtin_bit_cast(bf16x8, part[0][ks]));
+      if (ks == 0 && a == 0) {
 #pragma unroll
         for (int i = ht * 4 / (H / 32); i < (ht + 1) * 4 / (H / 32); ++i) work(i);
       }
 #pragma unroll
-      for (int q = 1; q < PARTS; ++q) mma32(acc[ht], f[NS + n], __builtin_bit_cast(bf16x8, part[q][ks]));
+      for (int b = 1; b < PARTS && a + b < TOP; ++b) mma32(acc[ht], f[NF + n], __builtin_bit_cast(bf16x8, part[b][ks]));
       __builtin_amdgcn_sched_barrier(0);
     }
   }
 };
 
-// Two values as the i-th words of a bf16 pair: hi rounds each to nearest, lo
-// the rest, which a two-element dot product with (-1, 0) or (0, -1) forms
-// exactly, without unpacking hi.  (From registers: the hardware does not read
+// Two values as the i-th words of PARTS bf16 each: the first rounds to nearest,
+// the next one the rest, which a two-element dot product with (-1, 0) or (0, -1)
+// forms exactly, without unpacking.  (From registers: the hardware does not read
 // the compiler's inline -1 as the low element.)
 struct Split {
   bf16x2_t neg_lo, neg_hi;
@@ -223,55 +204,23 @@ struct Split {
     neg_lo = __builtin_bit_cast(bf16x2_t, l);
     neg_hi = __builtin_bit_cast(bf16x2_t, h);
   }
-  __device__ __forceinline__ void operator()(float a, float b, u32x4 (&part)[2][2], int ks, int i) const {
-    const uint32_t h = pk2(a, b);
-    const bf16x2_t v = __builtin_bit_cast(bf16x2_t, h);
-    part[0][ks][i] = h;
-    part[1][ks][i] = pk2(__builtin_amdgcn_fdot2_f32_bf16(v, neg_lo, a, false),
-                         __builtin_amdgcn_fdot2_f32_bf16(v, neg_hi, b, false));
+  template <int PARTS>
+  __device__ __forceinline__ void operator()(float a, float b, u32x4 (&part)[PARTS][2], int ks, int i) const {
+#pragma unroll
+    for (int q = 0; q < PARTS; ++q) {
+      const uint32_t h = pk2(a, b);
+      part[q][ks][i] = h;
+      if (q + 1 < PARTS) {
+        const bf16x2_t v = __builtin_bit_cast(bf16x2_t, h);
+        a = __builtin_amdgcn_fdot2_f32_bf16(v, neg_lo, a, false);
+        b = __builtin_amdgcn_fdot2_f32_bf16(v, neg_hi, b, false);
+      }
+    }
   }
 };
-#else
-// float32: a fragment's product takes 16 times as long, so that two fragments
-// ahead are enough.
-template <int H>
-struct VocStep {
-  static constexpr int NS = H / 16, NO = H / 16, kAhead = 2;
-  const float *st, *ot;   // tiles of the logits and of the second product
-  int lane;
-  f32x8 f[NS + NO];       // at most kAhead are alive
 
-  __device__ __forceinline__ void read(int n, int rs, int ro) {
-    if (n < NS) f[n] = row_frag<float, H>(st, rs, n, lane);
-    else f[n] = col_frag<H>(ot, ro + 16 * ((n - NS) / (H / 32)), (n - NS) % (H / 32), lane);
-  }
-  template <int LAST>
-  __device__ __forceinline__ void begin(int rs, int ro) {
-#pragma unroll
-    for (int n = 0; n < kAhead; ++n)
-      if (n <= LAST) read(n, rs, ro);
-  }
-  template <int LAST, typename Work>
-  __device__ __forceinline__ void logits(f32x16& s, const f32x8 (&x)[NS], int rs, int ro, Work work) {
-#pragma unroll
-    for (int n = 0; n < NS; ++n) {
-      if (n + kAhead <= LAST) read(n + kAhead, rs, ro);
-      mma32(s, f[n], x[n]);
-#pragma unroll
-      for (int i = n * 16 / NS; i < (n + 1) * 16 / NS; ++i) work(i);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  }
-  __device__ __forceinline__ void product(f32x16 (&acc)[H / 32], const float (&p)[16], int ro) {
-#pragma unroll
-    for (int n = 0; n < NO; ++n) {
-      if (n + kAhead < NO) read(NS + n + kAhead, 0, ro);
-      mma32(acc[n % (H / 32)], f[NS + n], pack8<float>(p + 8 * (n / (H / 32))));
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  }
-};
-#endif
+// Keeps the compiler from moving what forms v past this point.
+__device__ __forceinline__ void keep_here(float& v) { asm volatile("" : "+v"(v)); }
 
 __device__ __forceinline__ float entry_bias(const float* bias, int v, int V) {
   if (v >= V) return -INFINITY;
@@ -303,13 +252,57 @@ __device__ __forceinline__ int row_node(const int32_t* __restrict__ node, int r,
   const int i = node != nullptr ? node[r] : r;
   return (unsigned)i < (unsigned)n_nodes ? i : -1;
 }
+// A row's fragments along H, as they lie in memory (row < 0: zero).
 template <typename S, int H>
-__device__ __forceinline__ void load_row_frags(frag_t<S> (&f)[H / 16], const S* __restrict__ X, long row, int lane) {
+__device__ __forceinline__ void load_row(frag_t<S> (&f)[H / 16], const S* __restrict__ X, long row, int lane) {
 #pragma unroll
   for (int kk = 0; kk < H / 16; ++kk) {
     if (row >= 0) f[kk] = load8(X + row * H + 16 * kk + 8 * (lane / 32));
     else f[kk] = frag_t<S>{};
   }
+}
+// The same as planes of bf16.
+template <typename S, int H>
+__device__ __forceinline__ void load_planes(bf16x8 (&f)[voc_planes<S>()][H / 16], const S* __restrict__ X, long row,
+                                            int lane) {
+  frag_t<S> v[H / 16];
+  load_row<S, H>(v, X, row, lane);
+#pragma unroll
+  for (int kk = 0; kk < H / 16; ++kk) {
+    if constexpr (sizeof(S) == 2) {
+      f[0][kk] = v[kk];
+    } else {
+#pragma unroll
+      for (int a = 0; a < 3; ++a) {
+        u32x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          w[i] = pk2(v[kk][2 * i], v[kk][2 * i + 1]);
+          v[kk][2 * i] -= lo_f(w[i]);
+          v[kk][2 * i + 1] -= hi_f(w[i]);
+        }
+        f[a][kk] = __builtin_bit_cast(bf16x8, w);
+      }
+    }
+  }
+}
+// Four elements as planes, `plane` elements apart.
+__device__ __forceinline__ void store_planes(bf16s* p, size_t plane, f32x4 v, float) {
+#pragma unroll
+  for (int a = 0; a < 3; ++a) {
+    const u32x2 w = u32x2{pk2(v[0], v[1]), pk2(v[2], v[3])};
+    *reinterpret_cast<u32x2*>(p + a * plane) = w;
+    v -= f32x4{lo_f(w[0]), hi_f(w[0]), lo_f(w[1]), hi_f(w[1])};
+  }
+}
+__device__ __forceinline__ void store_planes(bf16s* p, size_t, f32x4 v, bf16s) { store4(p, v[0], v[1], v[2], v[3]); }
+
+// The planes of a float32 matrix, `count` (a multiple of 4) elements.
+template <typename S>
+__global__ __launch_bounds__(kVocThreads) void vocab_planes_kernel(size_t count, const S* __restrict__ W,
+                                                                   bf16s* __restrict__ out) {
+  const size_t i = 4 * ((size_t)blockIdx.x * kVocThreads + threadIdx.x);
+  if (i < count) store_planes(out + i, count, load4f(W + i), S{});
 }
 
 // The tiles of a workgroup's share pass through three LDS buffers: while one
@@ -380,7 +373,7 @@ struct Dealt {
 // accumulators and fragments that a wave keeps, and at H = 256 by the buffers.
 template <typename S>
 constexpr int voc_waves(int H, bool sum) {
-  if (sizeof(S) == 4) return H <= 64 ? 2 : 1;
+  if (sizeof(S) == 4) return H >= 256 ? 1 : H == 128 ? (sum ? 1 : 2) : H == 64 ? 2 : 3;
   return H >= 256 ? 1 : H == 128 ? (sum ? 2 : 3) : H == 64 ? 3 : 4;
 }
 
@@ -399,14 +392,16 @@ __device__ __forceinline__ uint32_t buf_step(int b) {
 // elsewhere).
 template <typename S, int H, bool SUM, bool BEST, bool BIAS>
 __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_kernel(int n_nodes, int R, int V, Deal deal,
-                                                                 const S* __restrict__ X, const S* __restrict__ W,
+                                                                 const S* __restrict__ X,
+                                                                 const bf16s* __restrict__ W,
                                                                  const float* __restrict__ bias,
                                                                  const int32_t* __restrict__ node,
                                                                  float* __restrict__ pm, float* __restrict__ pl,
                                                                  float* __restrict__ po, RowBest* __restrict__ pb,
                                                                  float* __restrict__ dX, int clear) {
-  constexpr int T = voc_tile<S>();
-  __shared__ __attribute__((aligned(1024))) S tile[kVocBufs][T * H];
+  constexpr int T = voc_tile<S>(), NP = voc_planes<S>(), P = voc_parts<S>();
+  using Step = VocStep<H, NP, T>;
+  __shared__ __attribute__((aligned(1024))) bf16s tile[kVocBufs][NP * T * H];
   __shared__ __attribute__((aligned(16))) float tb[BIAS ? kVocBufs : 1][T];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = lane / 32;
   const uint32_t lds0 = (uint32_t)(uintptr_t)tile[0];
@@ -423,7 +418,7 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
   Dealt dealt(deal, blockIdx.x);
   for (int round = 0; dealt.next(deal, blockIdx.x, &run); ++round) {
     const int t0 = run.t0, t1 = run.t1;
-    frag_t<S> xf[H / 16];
+    bf16x8 xf[NP][H / 16];
     f32x16 o[H / 32];
     if constexpr (SUM) {
 #pragma unroll
@@ -432,7 +427,8 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
     float m = kNoMax, l = 0.f;
     RowBest best{-INFINITY, INT_MAX};
     auto fetch = [&](int t, int buf) {   // start the copies of tile t < t1
-      stage_tile<S, H>(W, (long)t * T, V - 1, lds0 + (uint32_t)(buf * T * H * sizeof(S)), wave, lane);
+      stage_tile<H, NP, T>(W, (size_t)V * H, (long)t * T, V - 1, lds0 + (uint32_t)buf * NP * Step::PLANE, wave,
+                           lane);
       // (the raw value: a use here would wait for the copies too)
       if (BIAS && threadIdx.x < T) nb = bias[min(t * T + (int)threadIdx.x, V - 1)];
     };
@@ -446,24 +442,17 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
       if constexpr (BIAS) start32(s, tb[buf] + r0, lane);
       else s = f32x16{};
     };
-    VocStep<H> step;
+    Step step;
+    step.init(lds0, lane);
     f32x16 s;
     int buf = 0;
-    if (round > 0) __syncthreads();   // every wave has left the buffers of the run before
-    {
-      fetch(t0, 0);
-      load_row_frags<S, H>(xf, X, row_node(node, run.i * kVocRows + wave * 32 + lane % 32, R, n_nodes), lane);
-      land(t0, 0);
-      if (t0 + 1 < t1) fetch(t0 + 1, 1);
-      start(s, 0, 0);
-#pragma unroll
-      for (int kk = 0; kk < H / 16; ++kk) mma32(s, row_frag<S, H>(tile[0], 0, kk, lane), xf[kk]);
-    }
-#if GGNN_DT_BF16
-    step.init(lds0, lane);
-#else
-    step.lane = lane;
-#endif
+    fetch(t0, 0);
+    load_planes<S, H>(xf, X, row_node(node, run.i * kVocRows + wave * 32 + lane % 32, R, n_nodes), lane);
+    land(t0, 0);
+    if (t0 + 1 < t1) fetch(t0 + 1, 1);
+    start(s, 0, 0);
+    step.template begin<Step::NF - 1>(0, 0);
+    step.template logits<Step::NF - 1>(s, xf, 0, 0, [](int) {});
     for (int t = t0; t < t1; ++t) {
       const int nbuf = next_buf(buf);
 #pragma unroll
@@ -474,13 +463,8 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
           land(t + 1, nbuf);
           if (t + 2 < t1) fetch(t + 2, next_buf(nbuf));
         }
-        constexpr int LAST = SUM ? 2 * (H / 16) - 1 : H / 16 - 1;
-#if GGNN_DT_BF16
-        if (last) step.move_s(buf_step<T * H * 2>(nbuf));
-#else
-        step.st = tile[last ? nbuf : buf];
-        step.ot = tile[buf];
-#endif
+        constexpr int LAST = (SUM ? 2 : 1) * Step::NF - 1;
+        if (last) step.move_s(buf_step<NP * Step::PLANE>(nbuf));
         step.template begin<LAST>(rs, r0);
         f32x16 sn;
         start(sn, last ? nbuf : buf, rs);
@@ -516,8 +500,7 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
           p[j] = __builtin_amdgcn_exp2f(fmaf(s[j], kLog2e, -m));
           l += p[j];
         };
-#if GGNN_DT_BF16
-        u32x4 part[2][2];
+        u32x4 part[P][2];
         const Split split2;
         __builtin_amdgcn_sched_barrier(0);
         step.template logits<LAST>(sn, xf, rs, r0, [&](int j) {
@@ -525,17 +508,10 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
           if (SUM && j >= 8 && j % 2 == 1) split2(p[j - 9], p[j - 8], part, 0, (j - 9) / 2);
         });
         if constexpr (SUM)
-          step.template product<2>(o, part, rs, r0, [&](int i) { split2(p[8 + 2 * i], p[9 + 2 * i], part, 1, i); });
-#else
-        __builtin_amdgcn_sched_barrier(0);
-        step.template logits<LAST>(sn, xf, rs, r0, prob);
-        if constexpr (SUM) step.product(o, p, r0);
-#endif
+          step.template product<P>(o, part, rs, r0, [&](int i) { split2(p[8 + 2 * i], p[9 + 2 * i], part, 1, i); });
         s = sn;
       }
-#if GGNN_DT_BF16
-      if constexpr (SUM) step.move_o(buf_step<T * H * 2>(nbuf));
-#endif
+      if constexpr (SUM) step.move_o(buf_step<NP * Step::PLANE>(nbuf));
       buf = nbuf;
     }
     l += __shfl_xor(l, 32);
@@ -573,12 +549,12 @@ __global__ __launch_bounds__(kVocThreads) void vocab_few_kernel(int n_nodes, int
   const int split = blockIdx.x * kVocWaves + threadIdx.x / kWave;
   const int tiles = (V + 31) / 32, t0 = split * per, t1 = min(tiles, t0 + per);
   frag_t<S> xf[H / 16];
-  load_row_frags<S, H>(xf, X, row_node(node, r, R, n_nodes), lane);
+  load_row<S, H>(xf, X, row_node(node, r, R, n_nodes), lane);
   float m = kNoMax, l = 0.f;
   RowBest best{-INFINITY, INT_MAX};
   for (int t = t0; t < t1; ++t) {
     frag_t<S> wf[H / 16];
-    load_row_frags<S, H>(wf, W, min(t * 32 + r, V - 1), lane);
+    load_row<S, H>(wf, W, min(t * 32 + r, V - 1), lane);
     f32x16 s;
 #pragma unroll
     for (int j = 0; j < 16; ++j) s[j] = entry_bias(bias, t * 32 + 8 * (j / 4) + 4 * g + j % 4, V);
@@ -710,7 +686,7 @@ __global__ __launch_bounds__(kVocThreads) void vocab_join_kernel(
     const float* __restrict__ bias, const int32_t* __restrict__ node, const int32_t* __restrict__ target,
     const float* __restrict__ weight, float scale, const float* __restrict__ pm, const float* __restrict__ pl,
     const float* __restrict__ po, const RowBest* __restrict__ pb, float* __restrict__ loss, float* __restrict__ lse,
-    int32_t* __restrict__ best, float* __restrict__ dX, S* __restrict__ xg, float* __restrict__ lse_w,
+    int32_t* __restrict__ best, float* __restrict__ dX, bf16s* __restrict__ xg, float* __restrict__ lse_w,
     int32_t* __restrict__ tgt_w, float* __restrict__ fac_w) {
   constexpr int L = H / 4;
   const int r = (int)(((long)blockIdx.x * kVocThreads + threadIdx.x) / L);
@@ -739,7 +715,7 @@ __global__ __launch_bounds__(kVocThreads) void vocab_join_kernel(
   if constexpr (GRAD) {
     const float f = (weight != nullptr && r < R ? weight[r] : 1.f) * scale;
     const bool live = t >= 0 && sum != 0.f;
-    store4(xg + (size_t)r * H + h, x[0], x[1], x[2], x[3]);
+    store_planes(xg + (size_t)r * H + h, (size_t)Rp * H, x, S{});
     if (q == 0) {
       lse_w[r] = live ? v : INFINITY;
       tgt_w[r] = live ? t : -1;
@@ -763,7 +739,7 @@ __global__ __launch_bounds__(kVocThreads) void vocab_join_kernel(
 // own; otherwise all have `scale`.  TARGETS: see below.
 template <typename S, int H, bool WEIGHT, bool TARGETS>
 __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols_kernel(int V, int Rp, Deal deal, float scale,
-                                                                 const S* __restrict__ xg,
+                                                                 const bf16s* __restrict__ xg,
                                                                  const S* __restrict__ W,
                                                                  const float* __restrict__ bias,
                                                                  const float* __restrict__ lse_w,
@@ -771,8 +747,9 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
                                                                  const float* __restrict__ fac_w,
                                                                  float* __restrict__ dW, float* __restrict__ dbias,
                                                                  float* __restrict__ pw, float* __restrict__ pdb) {
-  constexpr int T = voc_tile<S>();
-  __shared__ __attribute__((aligned(1024))) S tile[kVocBufs][T * H];
+  constexpr int T = voc_tile<S>(), NP = voc_planes<S>(), P = voc_parts<S>();
+  using Step = VocStep<H, NP, T>;
+  __shared__ __attribute__((aligned(1024))) bf16s tile[kVocBufs][NP * T * H];
   __shared__ __attribute__((aligned(16))) float tl[kVocBufs][T], tf[kVocBufs][T];
   __shared__ __attribute__((aligned(16))) int tt[kVocBufs][T];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = lane / 32;
@@ -784,13 +761,14 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
   Dealt dealt(deal, blockIdx.x);
   for (int round = 0; dealt.next(deal, blockIdx.x, &run); ++round) {
     const int t0 = run.t0, t1 = run.t1, vw = run.i * kVocRows + wave * 32, v = vw + lane % 32;
-    frag_t<S> wf[H / 16];
+    bf16x8 wf[NP][H / 16];
     f32x16 a[H / 32];
 #pragma unroll
     for (int ht = 0; ht < H / 32; ++ht) a[ht] = f32x16{};
     float db = 0.f;
     auto fetch = [&](int t, int buf) {   // start the copies of tile t < t1
-      stage_tile<S, H>(xg, (long)t * T, Rp - 1, lds0 + (uint32_t)(buf * T * H * sizeof(S)), wave, lane);
+      stage_tile<H, NP, T>(xg, (size_t)Rp * H, (long)t * T, Rp - 1, lds0 + (uint32_t)buf * NP * Step::PLANE, wave,
+                           lane);
       if (threadIdx.x < T) {
         nl = lse_w[t * T + threadIdx.x];
         nt = tgt_w[t * T + threadIdx.x];
@@ -806,26 +784,18 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
       wait_copies<0>();
       __syncthreads();
     };
-    VocStep<H> step;
+    Step step;
+    step.init(lds0, lane);
     f32x16 s;
     int buf = 0;
-    if (round > 0) __syncthreads();   // every wave has left the buffers of the run before
-    float b2;
-    {
-      fetch(t0, 0);
-      load_row_frags<S, H>(wf, W, min(v, V - 1), lane);
-      b2 = entry_bias(bias, v, V) * kLog2e;
-      land(0);
-      if (t0 + 1 < t1) fetch(t0 + 1, 1);
-      start32(s, tl[0], lane);
-#pragma unroll
-      for (int kk = 0; kk < H / 16; ++kk) mma32(s, row_frag<S, H>(tile[0], 0, kk, lane), wf[kk]);
-    }
-#if GGNN_DT_BF16
-    step.init(lds0, lane);
-#else
-    step.lane = lane;
-#endif
+    fetch(t0, 0);
+    load_planes<S, H>(wf, W, min(v, V - 1), lane);
+    const float b2 = entry_bias(bias, v, V) * kLog2e;
+    land(0);
+    if (t0 + 1 < t1) fetch(t0 + 1, 1);
+    start32(s, tl[0], lane);
+    step.template begin<Step::NF - 1>(0, 0);
+    step.template logits<Step::NF - 1>(s, wf, 0, 0, [](int) {});
     for (int t = t0; t < t1; ++t) {
       const int nbuf = next_buf(buf);
 #pragma unroll
@@ -836,13 +806,8 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
           land(nbuf);
           if (t + 2 < t1) fetch(t + 2, next_buf(nbuf));
         }
-        constexpr int LAST = 2 * (H / 16) - 1;
-#if GGNN_DT_BF16
-        if (last) step.move_s(buf_step<T * H * 2>(nbuf));
-#else
-        step.st = tile[last ? nbuf : buf];
-        step.ot = tile[buf];
-#endif
+        constexpr int LAST = 2 * Step::NF - 1;
+        if (last) step.move_s(buf_step<NP * Step::PLANE>(nbuf));
         step.template begin<LAST>(rs, r0);
         f32x16 sn;
         start32(sn, tl[last ? nbuf : buf] + rs, lane);
@@ -872,25 +837,18 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
 #pragma unroll
           for (int j = 0; j < 16; ++j) p[j] *= tf[buf][r0 + 8 * (j / 4) + 4 * g + j % 4];
         }
-#if GGNN_DT_BF16
-        u32x4 part[2][2];
+        u32x4 part[P][2];
         const Split split2;
 #pragma unroll
         for (int i = 0; i < 4; ++i) split2(p[2 * i], p[2 * i + 1], part, 0, i);
-        step.template product<2>(a, part, rs, r0, [&](int i) {
+        step.template product<P>(a, part, rs, r0, [&](int i) {
           split2(p[8 + 2 * i], p[9 + 2 * i], part, 1, i);
           db += (p[4 * i] + p[4 * i + 1]) + (p[4 * i + 2] + p[4 * i + 3]);
         });
-#else
-#pragma unroll
-        for (int j = 0; j < 16; ++j) db += p[j];
-        step.product(a, p, r0);
-#endif
-#if GGNN_DT_BF16
-        // The target's share of dW is a product of its own, since a bf16 pair of
+        // In bf16 the target's share of dW is a product of its own, since a pair of
         // p - 1 would lose low bits of p to the 1.  (Without TARGETS it comes from
         // launch_target_rows.)
-        if (TARGETS && hit) {
+        if (sizeof(S) == 2 && TARGETS && hit) {
           float q[16];
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
@@ -908,16 +866,13 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
               q[2 * i + 1] -= hi_f(h);
             }
 #pragma unroll
-            for (int k = 0; k < step.kAhead; ++k) step.read(H / 16 + k, 0, r0);
+            for (int k = 0; k < step.kAhead; ++k) step.read(Step::NF + k, 0, r0);
             step.template product<1>(a, e, rs, r0, [](int) {});
           }
         }
-#endif
         s = sn;
       }
-#if GGNN_DT_BF16
-      step.move_o(buf_step<T * H * 2>(nbuf));
-#endif
+      step.move_o(buf_step<NP * Step::PLANE>(nbuf));
       buf = nbuf;
     }
     const float f = WEIGHT ? 1.f : scale;
@@ -1015,7 +970,8 @@ dev::Deal make_deal(int tiles128, int tiles, int workers) {
 // the most frequent targets late (by a fifth of the pass at 60,001 rows over
 // 50,021 entries, H = 256: 4,875 us against 3,810), the second takes five
 // launches (about 45 us).
-bool targets_sorted(int H, int R, int V) { return (double)R * V * H > 4e10; }
+// In float32 all parts of p - 1 are kept, without a product more.
+bool targets_sorted(int es, int H, int R, int V) { return es == 2 && (double)R * V * H > 4e10; }
 
 // How a call is cut, and where its shares lie in the workspace.
 struct VocabPlan {
@@ -1023,7 +979,7 @@ struct VocabPlan {
   int splits, per;     // few rows
   int row_tiles, Rp, col_tiles;
   dev::Deal rows, cols;
-  size_t pm, pl, pb, po, xg, lse, tgt, fac, pw, pdb, sort, bytes;
+  size_t pm, pl, pb, po, wp, xg, lse, tgt, fac, pw, pdb, sort, bytes;
 };
 template <typename S>
 VocabPlan vocab_plan(int H, int R, int V, bool grad) {
@@ -1051,21 +1007,36 @@ VocabPlan vocab_plan(int H, int R, int V, bool grad) {
   p.pm = take(shares * 4);
   p.pl = take(shares * 4);
   if (!grad) p.pb = take(shares * sizeof(dev::RowBest));
+  if (sizeof(S) == 4 && !p.few) p.wp = take((size_t)V * H * 6);
   if (grad) {
     p.col_tiles = cdiv(V, dev::kVocRows);
     p.cols = make_deal(p.col_tiles, p.Rp / T, voc_workers<S>(H, true));
     const size_t cshares = (size_t)p.col_tiles * p.cols.slots * dev::kVocRows;
     p.po = take(shares * H * 4);
-    p.xg = take((size_t)p.Rp * H * sizeof(S));
+    p.xg = take((size_t)p.Rp * H * 2 * dev::voc_planes<S>());
     p.lse = take((size_t)p.Rp * 4);
     p.tgt = take((size_t)p.Rp * 4);
     p.fac = take((size_t)p.Rp * 4);
     p.pw = take(cshares * H * 4);
     p.pdb = take(cshares * 4);
-    if (targets_sorted(H, R, V)) p.sort = take(target_rows_workspace(H, p.Rp));
+    if (targets_sorted(sizeof(S), H, R, V)) p.sort = take(target_rows_workspace(H, p.Rp));
   }
   p.bytes = at;
   return p;
+}
+
+// The rows that the passes stage: W itself, or its planes.
+template <typename S>
+const dev::bf16s* staged_rows(const VocabArgs& c, int H, void* planes, hipStream_t st) {
+  if constexpr (sizeof(S) == 2) {
+    return static_cast<const dev::bf16s*>(c.W);
+  } else {
+    const size_t count = (size_t)c.V * H;
+    hipLaunchKernelGGL(dev::vocab_planes_kernel<S>, dim3((unsigned)((count / 4 + dev::kVocThreads - 1) / dev::kVocThreads)),
+                       dim3(dev::kVocThreads), 0, st, count, static_cast<const S*>(c.W),
+                       static_cast<dev::bf16s*>(planes));
+    return static_cast<const dev::bf16s*>(planes);
+  }
 }
 
 template <typename S, int H, bool BEST>
@@ -1083,12 +1054,13 @@ hipError_t vocab_loss_h(const VocabArgs& c, hipStream_t st) {
                        p.splits, X, W, c.bias, c.node, c.target, pm, pl, pb, c.loss, c.lse, c.best);
     return hipGetLastError();
   }
+  const bf16s* Ws = staged_rows<S>(c, H, ws + p.wp, st);
   if (c.bias != nullptr)
     hipLaunchKernelGGL((vocab_rows_kernel<S, H, false, BEST, true>), dim3(p.rows.workers), dim3(kVocThreads), 0, st,
-                       c.n_nodes, c.R, c.V, p.rows, X, W, c.bias, c.node, pm, pl, nullptr, pb, nullptr, 0);
+                       c.n_nodes, c.R, c.V, p.rows, X, Ws, c.bias, c.node, pm, pl, nullptr, pb, nullptr, 0);
   else
     hipLaunchKernelGGL((vocab_rows_kernel<S, H, false, BEST, false>), dim3(p.rows.workers), dim3(kVocThreads), 0, st,
-                       c.n_nodes, c.R, c.V, p.rows, X, W, nullptr, c.node, pm, pl, nullptr, pb, nullptr, 0);
+                       c.n_nodes, c.R, c.V, p.rows, X, Ws, nullptr, c.node, pm, pl, nullptr, pb, nullptr, 0);
   hipLaunchKernelGGL((vocab_join_kernel<S, H, false, BEST>), dim3(cdiv((long)c.R * (H / 4), kVocThreads)),
                      dim3(kVocThreads), 0, st, c.n_nodes, c.R, c.V, p.Rp, p.rows, X, W, c.bias, c.node, c.target,
                      nullptr, 1.f, pm, pl, nullptr, pb, c.loss, c.lse, c.best, nullptr, nullptr, nullptr, nullptr,
@@ -1106,7 +1078,8 @@ hipError_t vocab_grad_h(const VocabArgs& c, hipStream_t st) {
   float *fac_w = reinterpret_cast<float*>(ws + p.fac), *pw = reinterpret_cast<float*>(ws + p.pw);
   float* pdb = reinterpret_cast<float*>(ws + p.pdb);
   int32_t* tgt_w = reinterpret_cast<int32_t*>(ws + p.tgt);
-  S* xg = reinterpret_cast<S*>(ws + p.xg);
+  bf16s* xg = reinterpret_cast<bf16s*>(ws + p.xg);
+  const bf16s* Ws = staged_rows<S>(c, H, ws + p.wp, st);
   const S *X = static_cast<const S*>(c.X), *W = static_cast<const S*>(c.W);
   // A small dX is cleared by the rows pass, one launch less (5 us of the 70 at
   // 3,001 rows); a large one, which would hold its products up, by its own.
@@ -1118,14 +1091,14 @@ hipError_t vocab_grad_h(const VocabArgs& c, hipStream_t st) {
   }
   if (c.bias != nullptr)
     hipLaunchKernelGGL((vocab_rows_kernel<S, H, true, false, true>), dim3(p.rows.workers), dim3(kVocThreads), 0, st,
-                       c.n_nodes, c.R, c.V, p.rows, X, W, c.bias, c.node, pm, pl, po, nullptr, c.dX, clear);
+                       c.n_nodes, c.R, c.V, p.rows, X, Ws, c.bias, c.node, pm, pl, po, nullptr, c.dX, clear);
   else
     hipLaunchKernelGGL((vocab_rows_kernel<S, H, true, false, false>), dim3(p.rows.workers), dim3(kVocThreads), 0, st,
-                       c.n_nodes, c.R, c.V, p.rows, X, W, nullptr, c.node, pm, pl, po, nullptr, c.dX, clear);
+                       c.n_nodes, c.R, c.V, p.rows, X, Ws, nullptr, c.node, pm, pl, po, nullptr, c.dX, clear);
   hipLaunchKernelGGL((vocab_join_kernel<S, H, true, false>), dim3(cdiv((long)p.Rp * (H / 4), kVocThreads)),
                      dim3(kVocThreads), 0, st, c.n_nodes, c.R, c.V, p.Rp, p.rows, X, W, c.bias, c.node, c.target,
                      c.weight, c.scale, pm, pl, po, nullptr, c.loss, c.lse, nullptr, c.dX, xg, lse_w, tgt_w, fac_w);
-  const bool sorted = targets_sorted(H, c.R, c.V);
+  const bool sorted = targets_sorted(sizeof(S), H, c.R, c.V);
 #define COLS(WEIGHT, TARGETS)                                                                                       \
   hipLaunchKernelGGL((vocab_cols_kernel<S, H, WEIGHT, TARGETS>), dim3(p.cols.workers), dim3(kVocThreads), 0, st, c.V, \
                      p.Rp, p.cols, c.scale, xg, W, c.bias, lse_w, tgt_w, fac_w, c.dW, c.dbias, pw, pdb)
@@ -1141,7 +1114,7 @@ hipError_t vocab_grad_h(const VocabArgs& c, hipStream_t st) {
                        p.cols, pw, pdb, c.dW, c.dbias);
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess || !sorted) return err;
-  return launch_target_rows(sizeof(S) == 2 ? GGNN_BF16 : GGNN_F32, p.Rp, H, c.V, tgt_w, xg, -c.scale,
+  return launch_target_rows(p.Rp, H, c.V, tgt_w, xg, -c.scale,
                             c.weight != nullptr ? fac_w : nullptr, c.dW, ws + p.sort, st);
 }
 
