@@ -191,36 +191,23 @@ struct VocStep {
   }
 };
 
-// Two values as the i-th words of PARTS bf16 each: the first rounds to nearest,
-// the next one the rest, which a two-element dot product with (-1, 0) or (0, -1)
-// forms exactly, without unpacking.  (From registers: the hardware does not read
-// the compiler's inline -1 as the low element.)
-struct Split {
-  bf16x2_t neg_lo, neg_hi;
-  __device__ __forceinline__ Split() {
-    uint32_t l, h;
-    asm("s_mov_b32 %0, 0xbf80" : "=s"(l));
-    asm("s_mov_b32 %0, 0xbf800000" : "=s"(h));
-    neg_lo = __builtin_bit_cast(bf16x2_t, l);
-    neg_hi = __builtin_bit_cast(bf16x2_t, h);
-  }
-  template <int PARTS>
-  __device__ __forceinline__ void operator()(float a, float b, u32x4 (&part)[PARTS][2], int ks, int i) const {
+// Two values as the i-th words of PARTS bf16 each, the next part the rest of the
+// one before.  (Forming the rest with a bf16 dot product, which needs no
+// unpacking, took 2% longer: its results may be read late only.)
+template <int PARTS>
+__device__ __forceinline__ void split2(float a, float b, u32x4 (&part)[PARTS][2], int ks, int i) {
 #pragma unroll
-    for (int q = 0; q < PARTS; ++q) {
-      const uint32_t h = pk2(a, b);
-      part[q][ks][i] = h;
-      if (q + 1 < PARTS) {
-        const bf16x2_t v = __builtin_bit_cast(bf16x2_t, h);
-        a = __builtin_amdgcn_fdot2_f32_bf16(v, neg_lo, a, false);
-        b = __builtin_amdgcn_fdot2_f32_bf16(v, neg_hi, b, false);
-      }
-    }
+  for (int q = 0; q < PARTS; ++q) {
+    const uint32_t h = pk2(a, b);
+    part[q][ks][i] = h;
+    a -= lo_f(h);
+    b -= hi_f(h);
   }
-};
+}
 
 // Keeps the compiler from moving what forms v past this point.
-__device__ __forceinline__ void keep_here(float& v) { asm volatile("" : "+v"(v)); }
+template <typename V>
+__device__ __forceinline__ void keep_here(V& v) { asm volatile("" : "+v"(v)); }
 
 __device__ __forceinline__ float entry_bias(const float* bias, int v, int V) {
   if (v >= V) return -INFINITY;
@@ -501,7 +488,6 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
           l += p[j];
         };
         u32x4 part[P][2];
-        const Split split2;
         __builtin_amdgcn_sched_barrier(0);
         step.template logits<LAST>(sn, xf, rs, r0, [&](int j) {
           prob(j);
@@ -813,9 +799,20 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
         start32(sn, tl[last ? nbuf : buf] + rs, lane);
         const int tj = tt[buf][r0 + lane % 32];
         float p[16];
+        u32x4 part[P][2];
+        constexpr bool kFinal = sizeof(S) == 2 && !WEIGHT;   // what follows leaves p as it is
         auto prob = [&](int j) {
           p[j] = __builtin_amdgcn_exp2f(fmaf(s[j], kLog2e, b2));
           keep_here(p[j]);
+          if (kFinal && j >= 8 && j % 2 == 1) {
+            split2(p[j - 9], p[j - 8], part, 0, (j - 9) / 2);
+#pragma unroll
+            for (int q = 0; q < P; ++q) {
+              uint32_t w = part[q][0][(j - 9) / 2];
+              keep_here(w);
+              part[q][0][(j - 9) / 2] = w;
+            }
+          }
         };
         __builtin_amdgcn_sched_barrier(0);
         step.template logits<LAST>(sn, wf, rs, r0, prob);
@@ -837,10 +834,10 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
 #pragma unroll
           for (int j = 0; j < 16; ++j) p[j] *= tf[buf][r0 + 8 * (j / 4) + 4 * g + j % 4];
         }
-        u32x4 part[P][2];
-        const Split split2;
+        if constexpr (!kFinal) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) split2(p[2 * i], p[2 * i + 1], part, 0, i);
+          for (int i = 0; i < 4; ++i) split2(p[2 * i], p[2 * i + 1], part, 0, i);
+        }
         step.template product<P>(a, part, rs, r0, [&](int i) {
           split2(p[8 + 2 * i], p[9 + 2 * i], part, 1, i);
           db += (p[4 * i] + p[4 * i + 1]) + (p[4 * i + 2] + p[4 * i + 3]);
