@@ -191,6 +191,9 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(int n_tok, int
     __shared__ int wm[kSortWaves];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     int listed0 = 0, listed1 = n_tok;   // positions that lists hold
+    int id[kSortPer];                   // (on their way while the rows are found)
+#pragma unroll
+    for (int i = 0; i < kSortPer; ++i) id[i] = tok[min(k0 + i * kSortThreads + (int)threadIdx.x, n_tok - 1)];
     if (tok_ptr != nullptr) {
       listed0 = tok_ptr[0];
       listed1 = tok_ptr[n];
@@ -198,11 +201,20 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(int n_tok, int
 #pragma unroll
       for (int i = 0; i < kSortPer; ++i) rows[i * kSortThreads + threadIdx.x] = first;
       __syncthreads();
-      for (long i0 = first; i0 < n; i0 += kSortThreads) {
-        const long i = i0 + threadIdx.x;
-        const int b = i < n ? tok_ptr[i] : INT_MAX;
-        if (i < n && b >= k0 && b < k0 + kSortTile && b < tok_ptr[i + 1]) rows[b - k0] = (int)i;
-        if (__syncthreads_or(b >= k0 + kSortTile)) break;   // lists begin in order: the rest begin later
+      constexpr int U = 4;   // rows of a thread at once
+      for (long i0 = first; i0 < n; i0 += U * kSortThreads) {
+        int b[U], e[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const long i = i0 + u * kSortThreads + threadIdx.x;
+          b[u] = i < n ? tok_ptr[i] : INT_MAX;
+          e[u] = i < n ? tok_ptr[i + 1] : INT_MAX;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (b[u] >= k0 && b[u] < k0 + kSortTile && b[u] < e[u])
+            rows[b[u] - k0] = (int)(i0 + u * kSortThreads + threadIdx.x);
+        if (__syncthreads_or(b[U - 1] >= k0 + kSortTile)) break;   // lists begin in order: the rest begin later
       }
       __syncthreads();
       int m[kSortPer], top = 0;
@@ -230,9 +242,8 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(int n_tok, int
     for (int i = 0; i < kSortPer; ++i) {
       const int k = k0 + i * kSortThreads + threadIdx.x;
       if (k < n_tok) {
-        const int id = tok[k];
-        const bool ok = (unsigned)id < (unsigned)V && k >= listed0 && k < listed1;
-        const uint32_t key = ok ? (uint32_t)id : (uint32_t)V;
+        const bool ok = (unsigned)id[i] < (unsigned)V && k >= listed0 && k < listed1;
+        const uint32_t key = ok ? (uint32_t)id[i] : (uint32_t)V;
         items[k] = u32x2{key, (uint32_t)(tok_ptr != nullptr ? rows[k - k0] : k)};
         atomicAdd(&c[(key >> shift) & mask], 1u);   // integers: the order does not matter
       }
@@ -291,17 +302,25 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(int n_tok, con
   __shared__ uint32_t cnt[kSortWaves][kDigits];
   __shared__ uint32_t ws[kSortWaves];
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, dig = threadIdx.x;
+  const int k0 = blockIdx.x * kSortTile + wave * (kSortTile / kSortWaves);
+  u32x2 it[kSortPer];   // on their way while the counts are added up
+#pragma unroll
+  for (int i = 0; i < kSortPer; ++i) {
+    const int k = k0 + i * kWave + lane;
+    it[i] = k < n_tok ? in[k] : u32x2{~0u, 0u};
+  }
 #pragma unroll
   for (int w = 0; w < kSortWaves; ++w) cnt[w][dig] = 0;
   // exclusive scan of the digit totals
   uint32_t tot = 0, before = 0;   // the digit's items in all tiles, and in the tiles before this one
   if (few) {
-    for (int t0 = 0; t0 < tiles; t0 += 8) {
-      uint32_t c[8];
+    constexpr int U = 16;
+    for (int t0 = 0; t0 < tiles; t0 += U) {
+      uint32_t c[U];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) c[u] = t0 + u < tiles ? count[(size_t)(t0 + u) * kDigits + dig] : 0u;
+      for (int u = 0; u < U; ++u) c[u] = t0 + u < tiles ? count[(size_t)(t0 + u) * kDigits + dig] : 0u;
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
+      for (int u = 0; u < U; ++u) {
         tot += c[u];
         if (t0 + u < (int)blockIdx.x) before += c[u];
       }
@@ -321,14 +340,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(int n_tok, con
   uint32_t base = s - tot + before;
   for (int w = 0; w < wave; ++w) base += ws[w];
 
-  const int k0 = blockIdx.x * kSortTile + wave * (kSortTile / kSortWaves);
-  u32x2 it[kSortPer];
   uint32_t rank[kSortPer];
-#pragma unroll
-  for (int i = 0; i < kSortPer; ++i) {
-    const int k = k0 + i * kWave + lane;
-    it[i] = k < n_tok ? in[k] : u32x2{~0u, 0u};
-  }
 #pragma unroll
   for (int i = 0; i < kSortPer; ++i) {
     const bool live = k0 + i * kWave + lane < n_tok;
@@ -413,7 +425,8 @@ __global__ __launch_bounds__(kEmbThreads) void embed_runs_kernel(int n_tok, int 
   if (lo < n_tok) {
     const int k0 = (int)lo, k1 = (int)min((long)n_tok, lo + chunk);
     cur = items[k0].x;
-    before = k0 > 0 && items[k0 - 1].x == cur;
+    const uint32_t left = items[max(k0 - 1, 0)].x, right = items[min(k1, n_tok - 1)].x;
+    before = k0 > 0 && left == cur;
     float old[8] = {};   // the gradient's row of the current token
     if (!before && cur < none) load8f<float>(dtable + (size_t)cur * H + h, old);
     for (int k = k0; k < k1; k += U) {
@@ -463,7 +476,7 @@ __global__ __launch_bounds__(kEmbThreads) void embed_runs_kernel(int n_tok, int 
         }
       }
     }
-    after = k1 < n_tok && items[k1].x == cur;
+    after = k1 < n_tok && right == cur;
     if (cur < none) {
       if (!before && !after) {
 #pragma unroll
@@ -482,14 +495,22 @@ __global__ __launch_bounds__(kEmbThreads) void embed_runs_kernel(int n_tok, int 
   if (lo >= n_tok || cur >= none) {
     // (group 0's head share of a run that ended in its chunk is written below)
   } else if (after && (!before || grp == 0)) {   // a run that leaves this chunk and is this one's to add up
-    int j = grp + 1;
-    for (bool open = true; open && j < G; ++j) {
-      float v[8];
-      load8f<float>(&head[j][h], v);
+    constexpr int W = 4;   // shares in flight
+    for (int j = grp + 1; after && j < G; j += W) {
+      float v[W][8];
+      int full[W];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) acc[i] += v[i];
-      open = hfull[j] != 0;
-      after = open;
+      for (int u = 0; u < W; ++u) {
+        full[u] = hfull[min(j + u, G - 1)];
+        load8f<float>(&head[min(j + u, G - 1)][h], v[u]);   // nothing of this run past its end: unused
+      }
+#pragma unroll
+      for (int u = 0; u < W; ++u) {
+        if (!after || j + u >= G) break;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[i] += v[u][i];
+        after = full[u] != 0;
+      }
     }
     if (before || after) store8f(part + ((size_t)2 * blockIdx.x + (before ? 0 : 1)) * H + h, acc);
     else add_row(dtable + (size_t)cur * H + h, acc);
@@ -503,11 +524,11 @@ __global__ __launch_bounds__(kEmbThreads) void embed_runs_kernel(int n_tok, int 
   }
 }
 
-// Adds up the runs that cross blocks.  A workgroup looks at kJoinBlocks
-// blocks: a group adds up a run that begins in its block and ends within
-// kJoinShort more; a longer one is added by all groups, each a fixed share of
-// its blocks, joined in a fixed tree.
-constexpr int kJoinThreads = 1024, kJoinBlocks = 64, kJoinShort = 16;
+// Adds up the runs that cross blocks.  Two workgroups look at kJoinBlocks
+// blocks: in one (y = 0) a group adds up a run that begins in its block and ends
+// within kJoinShort more; a longer one is added by all groups of the other, each
+// a fixed share of its blocks, joined in a fixed tree.
+constexpr int kJoinThreads = 1024, kJoinBlocks = 16, kJoinShort = 16;
 
 template <int H>
 __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(int n_tok, int V, int block, int blocks,
@@ -528,24 +549,27 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(int n_tok, int
     const uint32_t key = first(b + 1), last = items[((long)b + 1) * block - 1].x, start = first(b),
                    prev = items[max((long)b * block - 1, 0l)].x, farkey = first(far);
     if (key >= (uint32_t)V || last != key || (start == key && b > 0 && prev == key)) continue;
-    if (b + kJoinShort + 1 < blocks && farkey == key) {
+    const bool far_too = b + kJoinShort + 1 < blocks && farkey == key;
+    if (far_too != (blockIdx.y == 1)) continue;
+    if (far_too) {
       if (h == 0) is_long[b - b0] = 1;
       continue;
     }
+    constexpr int U = 6;   // blocks' keys and shares in flight
     float acc[8];
     load8f<float>(part + ((size_t)2 * b + 1) * H + h, acc);
     bool open = true;
-    for (long j = b + 1; open; j += 4) {   // four blocks' keys and shares in flight
-      float w[4][8];
-      uint32_t k[4];
+    for (long j = b + 1; open; j += U) {
+      float w[U][8];
+      uint32_t k[U];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < U; ++u) {
         const long ju = min(j + u, (long)blocks - 1);
         k[u] = j + u < blocks ? first(ju) : ~0u;
         load8f<float>(part + (size_t)2 * ju * H + h, w[u]);   // not of this run where the key differs: unused
       }
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < U; ++u) {
         open = open && k[u] == key;
         if (open) {
 #pragma unroll
@@ -555,6 +579,7 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(int n_tok, int
     }
     add_row(dtable + (size_t)key * H + h, acc);
   }
+  if (blockIdx.y == 0) return;
   __syncthreads();
   for (int i = 0; i < kJoinBlocks; ++i) {   // at most one in kJoinShort blocks begins a long run
     if (is_long[i] == 0) continue;
@@ -668,7 +693,7 @@ hipError_t embed_bwd_h(int n, int V, const int32_t* tok_ptr, const int32_t* tok,
                        a, tok_ptr, scale, mean, factor, d, dX, dtable, part);
   }
   if (l.blocks > 1)
-    hipLaunchKernelGGL((embed_join_kernel<H>), dim3((l.blocks + kJoinBlocks - 1) / kJoinBlocks), dim3(kJoinThreads),
+    hipLaunchKernelGGL((embed_join_kernel<H>), dim3((l.blocks + kJoinBlocks - 1) / kJoinBlocks, 2), dim3(kJoinThreads),
                        0, st, n_tok, V, l.block, l.blocks, a, part, dtable);
   return hipGetLastError();
 }
