@@ -429,6 +429,7 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
       if constexpr (BIAS) start32(s, tb[buf] + r0, lane);
       else s = f32x16{};
     };
+    if (round > 0) __syncthreads();   // every wave has left the buffers of the run before
     Step step;
     step.init(lds0, lane);
     f32x16 s;
@@ -770,6 +771,7 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
       wait_copies<0>();
       __syncthreads();
     };
+    if (round > 0) __syncthreads();   // every wave has left the buffers of the run before
     Step step;
     step.init(lds0, lane);
     f32x16 s;
