@@ -707,17 +707,19 @@ size_t ggnn_vocab_workspace_bytes(ggnn_dtype dt, int32_t H, int32_t n_rows, int3
  *   z_v = X[i] . W[v] + bias[v];  lse[r] = log sum_v exp z_v;  loss[r] = lse[r] - z_target[r]
  *   n_nodes  rows of X;  n_rows <= 2^24 chosen nodes;  V entries, V * H < 2^31
  *   X [n_nodes][H] dt;  W [V][H] dt;  bias [V] float or NULL.  A bias of -1e30 or
- *            less (-inf and the lowest float among them) takes its entry out.
+ *            less (-inf and the lowest float among them) takes its entry out (its
+ *            row of W is still read and must be finite).
  *   node     [n_rows] int32, or NULL: row r is node r.  One outside [0, n_nodes)
  *            counts as a zero state without a target.
  *   target   [n_rows] int32, or NULL (no losses).  A negative one: the row has no
- *            loss (0) and no gradient; one at or above V: loss NaN, no gradient.
+ *            loss (0) and no gradient, whatever its state and weight hold; one at or above V: loss NaN, no gradient.
  *   loss     [n_rows] float (written; NULL allowed without targets)
  *   lse      [n_rows] float (written; -inf where every entry is taken out, the
  *            loss then +inf, without a gradient)
  *   best     [n_rows] int32 (written: the entry with the largest logit, the lowest
  *            one of equals, -1 where every entry is taken out), or NULL
- * A NaN or +inf logit makes its row's lse and loss NaN. */
+ * A NaN or +inf logit makes its row's lse and loss NaN, and so may, in float32,
+ * a state or entry that is not finite (they enter the products as three bf16). */
 ggnn_status ggnn_vocab_loss(ggnn_dtype dt, int32_t n_nodes, int32_t H, int32_t n_rows, int32_t V, const void* X,
                             const void* W, const float* bias, const int32_t* node, const int32_t* target,
                             float* loss, float* lse, int32_t* best, void* workspace, size_t workspace_bytes,
@@ -730,7 +732,9 @@ ggnn_status ggnn_vocab_loss(ggnn_dtype dt, int32_t n_nodes, int32_t H, int32_t n
  *        node may be chosen once (otherwise its row holds one of the contributions).
  *   dW   [V][H] float += sum_r dz_v X[node[r]];  dbias [V] float += sum_r dz_v, or NULL
  *   weight [n_rows] float, or NULL for 1
- * In bf16 a probability enters the two gradient products as a bf16 pair (hi + lo). */
+ * In bf16 a probability enters the two gradient products as a bf16 pair (hi + lo,
+ * 16 bits); in float32 states, entries and probabilities are three bf16 each (24
+ * bits) and a product is six. */
 ggnn_status ggnn_vocab_loss_grad(ggnn_dtype dt, int32_t n_nodes, int32_t H, int32_t n_rows, int32_t V, const void* X,
                                  const void* W, const float* bias, const int32_t* node, const int32_t* target,
                                  const float* weight, float scale, float* loss, float* lse, float* dX, float* dW,

@@ -664,9 +664,10 @@ __global__ __launch_bounds__(kVocThreads) void vocab_few_join_kernel(
 }
 
 // Joins the shares of a row: H / 4 lanes per row, four features each.  GRAD:
-// writes dX's row, and what the columns pass reads: the row's state (zero rows
-// up to the end of the last 128-tile), its lse (infinite for rows without a
-// gradient, whose probabilities then vanish), target (-1) and factor.
+// writes dX's row, and what the columns pass reads: the row's state, its lse,
+// target and factor.  A row without a gradient, and those that fill the last
+// 128-tile, has a zero state, an infinite lse (its probabilities vanish), target
+// -1 and factor 0.
 template <typename S, int H, bool GRAD, bool BEST>
 __global__ __launch_bounds__(kVocThreads) void vocab_join_kernel(
     int n_nodes, int R, int V, int Rp, Deal deal, const S* __restrict__ X, const S* __restrict__ W,
@@ -702,11 +703,11 @@ __global__ __launch_bounds__(kVocThreads) void vocab_join_kernel(
   if constexpr (GRAD) {
     const float f = (weight != nullptr && r < R ? weight[r] : 1.f) * scale;
     const bool live = t >= 0 && sum != 0.f;
-    store_planes(xg + (size_t)r * H + h, (size_t)Rp * H, x, S{});
+    store_planes(xg + (size_t)r * H + h, (size_t)Rp * H, live ? x : f32x4{}, S{});
     if (q == 0) {
       lse_w[r] = live ? v : INFINITY;
       tgt_w[r] = live ? t : -1;
-      fac_w[r] = f;
+      fac_w[r] = live ? f : 0.f;   // (whatever an ignored row holds: a product with its zero probability)
     }
     if (live) {
       f32x4 o = {};

@@ -329,6 +329,29 @@ def test_vocab_nan_stays_in_its_row(rows):
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("weighted", [False, True])
+def test_vocab_ignored_rows_may_hold_anything(dt, weighted):
+    """NaN and infinite states, and NaN weights, of rows without a target leave every gradient as if they were zero."""
+    rng = np.random.default_rng(10)
+    X, W, node, target, b = vocab_case(rng, dt, 400, 64, 500, 300, bias=True)
+    weight = round_to("f32", rng.standard_normal(300)) if weighted else None
+    target[::5] = -1
+    out = np.arange(0, 300, 5)
+    X[node[out]] = 0.0
+    want = R.vocab(X, W, b, node, target, weight, 0.5, dt)
+    X[node[out[::2]], 3], X[node[out[1::2]], 60] = np.nan, np.inf
+    if weighted:
+        weight[out] = np.nan
+    got = run_vocab(dt, X, W, b, node, target, weight, 0.5)
+    keep = np.delete(np.arange(300), out)
+    R.within(got["loss"], want["loss"], want["loss_tol"])
+    R.within(got["lse"][keep], want["lse"][keep], want["lse_tol"][keep])
+    R.within(got["dX"], want["dX"], want["dX_tol"])
+    for k in ("dW", "db"):   # added to ones
+        R.within(got[k], want[k], want[k + "_tol"] + 4 * R.U * (1 + np.abs(want[k])))
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("H", [32, 256])
 @pytest.mark.parametrize("rows,V", [(1, 40), (32, 3000), (33, 3000), (300, 1001)])
 def test_vocab_best_entry_ties_go_to_the_lowest(dt, H, rows, V):
