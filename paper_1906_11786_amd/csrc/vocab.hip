@@ -13,13 +13,29 @@
 // fragment order of the second product.  The shares (m, l, O) of the
 // vocabulary's splits are joined per row, which gives loss, lse and dX.
 // Columns pass: the same with the roles of X and W exchanged, p from the known
-// lse, which gives dW and db.  Logits are formed twice, 2 RVH operations each,
-// and the two other products cost 2 RVH each (4 in bf16, see below).
+// lse, which gives dW and db.
+//
+// Operations: the logits are formed twice, 2 RVH each (kept in memory they would
+// be 6 GB at 60,001 rows over 50,021 entries in bf16, written once and read
+// twice), and the two other products cost 4 RVH each in bf16: 12 RVH on the
+// matrix cores.  In float32 every product is six bf16 ones: 48 RVH.
 //
 // Precision: dX and dW are float32, so in bf16 a probability enters the
 // products as a bf16 pair (hi + lo, 16 bits); one bf16 would put the rounding
-// of every probability, 2^-9, into both gradients.  Logits, maxima, sums and
-// accumulators are float32.
+// of every probability, 2^-8, into both gradients.  In float32 states, entries
+// and probabilities are three bf16 each.  Logits, maxima, sums and accumulators
+// are float32.
+//
+// What bounds them: at H = 256 the matrix cores.  60,001 rows over 50,021 entries
+// in bf16: rows pass 3,690 us, columns pass 3,870 to 4,050, 1.25 and 1.17 PFLOP/s,
+// where a plain 8,192^3 product of the library runs at 1.32.  At H = 64 a step has a
+// quarter of the products for the same 16 exponentials a lane, whose vector
+// instructions take longer than the products: 3,001 rows over 10,007 entries
+// 22.5 and 23.6 us (0.51 PFLOP/s), then 8.4 and 6.9 us to add up the shares (25 and
+// 23 MB, at memory speed).  Loss alone at H = 128, 2,999 rows over 50,021 entries:
+// 54 us, 0.71 PFLOP/s, exponentials again.  float32 at H = 128, 1,229 rows over
+// 4,999 entries: 29.0 and 27.8 us (0.65 PFLOP/s of bf16 products: 250 workgroups
+// of 4 waves, one per SIMD, and a run of 6 to 7 tiles).
 #include <type_traits>
 
 #include "device_common.h"
@@ -49,6 +65,7 @@ template <typename S> constexpr int voc_tile() { return sizeof(S) == 2 ? 64 : 32
 __device__ __forceinline__ void mma32(f32x16& acc, const bf16x8& a, const bf16x8& b) {
   acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, acc, 0, 0, 0);
 }
+// (vocab_few_kernel's in float32, which waits for memory)
 __device__ __forceinline__ void mma32(f32x16& acc, const f32x8& a, const f32x8& b) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], acc, 0, 0, 0);
@@ -284,7 +301,9 @@ __device__ __forceinline__ void store_planes(bf16s* p, size_t plane, f32x4 v, fl
 }
 __device__ __forceinline__ void store_planes(bf16s* p, size_t, f32x4 v, bf16s) { store4(p, v[0], v[1], v[2], v[3]); }
 
-// The planes of a float32 matrix, `count` (a multiple of 4) elements.
+// The planes of a float32 matrix, `count` (a multiple of 4) elements: once a
+// call, so that no workgroup splits the rows that it stages.  3.1 us for 4,999 x
+// 128.
 template <typename S>
 __global__ __launch_bounds__(kVocThreads) void vocab_planes_kernel(size_t count, const S* __restrict__ W,
                                                                    bf16s* __restrict__ out) {
@@ -305,6 +324,8 @@ __global__ __launch_bounds__(kVocThreads) void vocab_planes_kernel(size_t count,
 // equal runs of units, so that all workgroups end together.  Few: each is cut
 // into `parts` runs, one a worker, so that no worker starts twice.  A 128-tile is
 // thus one share, or several workers' shares, joined afterwards in their order.
+// (60,001 rows over 50,021 entries, 469 and 391 128-tiles for 256 workgroups: a
+// round of whole tiles alone would leave the chip half idle in the last one.)
 struct Deal {
   int workers, tiles;   // workgroups; LDS tiles against one 128-tile
   int whole, rest;      // 128-tiles dealt whole (a multiple of workers), and cut up
@@ -524,7 +545,8 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
 
 // Rows pass for at most 32 rows (loss only): every wave holds the same rows
 // and takes `per` tiles of 32 entries, read straight from memory, since no
-// other wave needs them.
+// other wave needs them.  Bound by memory's latency and the launch: 4.8 us for
+// one row over 10,007 entries at H = 64 (1.3 MB).
 template <typename S, int H, bool BEST>
 __global__ __launch_bounds__(kVocThreads) void vocab_few_kernel(int n_nodes, int R, int V, int per,
                                                                 const S* __restrict__ X, const S* __restrict__ W,
@@ -619,7 +641,7 @@ __device__ __forceinline__ float row_loss(float lse, float zt, int t, bool bad) 
 }
 
 // The loss of at most 32 rows from the many shares of vocab_few_kernel: one
-// workgroup per row.
+// workgroup per row.  3.0 us, latency.
 template <typename S, int H, bool BEST>
 __global__ __launch_bounds__(kVocThreads) void vocab_few_join_kernel(
     int n_nodes, int R, int V, int splits, const S* __restrict__ X, const S* __restrict__ W,
@@ -667,7 +689,8 @@ __global__ __launch_bounds__(kVocThreads) void vocab_few_join_kernel(
 // writes dX's row, and what the columns pass reads: the row's state, its lse,
 // target and factor.  A row without a gradient, and those that fill the last
 // 128-tile, has a zero state, an infinite lse (its probabilities vanish), target
-// -1 and factor 0.
+// -1 and factor 0.  Bound by the shares' bytes: 8.4 us for 3,001 rows of 32 shares
+// at H = 64 (25 MB), 54 us for 60,001 rows at H = 256.
 template <typename S, int H, bool GRAD, bool BEST>
 __global__ __launch_bounds__(kVocThreads) void vocab_join_kernel(
     int n_nodes, int R, int V, int Rp, Deal deal, const S* __restrict__ X, const S* __restrict__ W,
@@ -721,10 +744,11 @@ __global__ __launch_bounds__(kVocThreads) void vocab_join_kernel(
   }
 }
 
-// Columns pass: 128 entries of a workgroup (32 per wave) against the gathered states.  Adds to dW [V][H] and db [V] (dbias NULL:
-// none) where the 128-tile is one share, else writes its share to pw
-// [slot][128][H] and pdb [slot][128].  WEIGHT: each row has a factor of its
-// own; otherwise all have `scale`.  TARGETS: see below.
+// Columns pass: 128 entries of a workgroup (32 per wave) against the gathered
+// states.  Adds to dW [V][H] and db [V] (dbias NULL: none) where the 128-tile is
+// one share, else writes its share to pw [slot][128][H] and pdb [slot][128].
+// WEIGHT: each row has a factor of its own; otherwise all have `scale`.  TARGETS:
+// see below.
 template <typename S, int H, bool WEIGHT, bool TARGETS>
 __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols_kernel(int V, int Rp, Deal deal, float scale,
                                                                  const bf16s* __restrict__ xg,
@@ -899,7 +923,8 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
 }
 
 // dW and db of the 128-tiles that several shares make up: += their sum, in
-// share order.  H / 4 lanes per entry, four features each.
+// share order.  H / 4 lanes per entry, four features each.  Bound by the shares'
+// bytes: 6.9 us for 79 tiles of 9 shares at H = 64 (23 MB).
 template <int H>
 __global__ __launch_bounds__(kVocThreads) void vocab_wsum_kernel(int V, Deal deal, const float* __restrict__ pw,
                                                                  const float* __restrict__ pdb,
@@ -967,11 +992,13 @@ dev::Deal make_deal(int tiles128, int tiles, int workers) {
 // Where the targets' share of dW, -g x of each row on its target's row, comes
 // from: a product beside the probabilities in the columns pass, or the sum over
 // rows sorted by target (csrc/embed.hip).  The first makes the workgroups with
-// the most frequent targets late (by a fifth of the pass at 60,001 rows over
-// 50,021 entries, H = 256: 4,875 us against 3,810), the second takes five
-// launches (about 45 us).
+// the most frequent targets late, the more the wider the rows; the second takes
+// six launches (42 us at 60,001 rows, H = 256).  The whole call, first against
+// second: H = 64, 12,001 x 20,011 259 / 272 us, 30,001 x 50,021 1,262 / 1,251; H =
+// 128, 8,001 x 30,011 376 / 392, 16,001 x 30,011 701 / 707; H = 256, 3,001 x 10,007
+// 143 / 159, 6,001 x 20,011 414 / 401, 16,001 x 50,021 2,267 / 2,102.
 // In float32 all parts of p - 1 are kept, without a product more.
-bool targets_sorted(int es, int H, int R, int V) { return es == 2 && (double)R * V * H > 4e10; }
+bool targets_sorted(int es, int H, int R, int V) { return es == 2 && (double)R * V * H * H > 6.5e12; }
 
 // How a call is cut, and where its shares lie in the workspace.
 struct VocabPlan {

@@ -494,6 +494,8 @@ def large_reference(X, W, b, node, target, weight, scale, dt):
     ("bf16", 256, 33100, 4900, True, False),   # rows sorted by target
     ("bf16", 64, 65600, 9800, False, True),
     ("f32", 256, 33100, 4900, False, True),
+    ("bf16", 64, 65600, 24500, True, True),
+    ("bf16", 128, 33100, 12300, False, False),
 ])
 def test_vocab_large_forms(dt, H, rows, V, bias, weighted):
     say(f"vocab large dt={dt} H={H} rows={rows} V={V}")
