@@ -187,19 +187,25 @@ struct VocStep {
   }
   // acc[ht] += (tile rows)^T p (lane's column, rows in accumulator order), p as
   // PARTS bf16 each; work(i), i < 4, is done alongside the first half, which
-  // needs part[.][0] only.
-  template <int PARTS, typename Work>
+  // needs part[.][0] only, and late(i), i < 4, alongside the second.  NEXT: the
+  // next step's first fragments, from rows rs, are read towards the end.
+  template <int PARTS, bool NEXT, typename Work, typename Late>
   __device__ __forceinline__ void product(f32x16 (&acc)[H / 32], const u32x4 (&part)[PARTS][2], int rs, int ro,
-                                          Work work) {
+                                          Work work, Late late) {
     constexpr int TOP = NP == 1 ? PARTS : NP;
 #pragma unroll
     for (int n = 0; n < NF; ++n) {
       const int a = n % NP, ks = n / NP / (H / 32), ht = n / NP % (H / 32);
       if (n + kAhead < NF) read(NF + n + kAhead, rs, ro);
+      else if (NEXT) read(n + kAhead - NF, rs, ro);
       mma32(acc[ht], f[NF + n], __builtin_bit_cast(bf16x8, part[0][ks]));
       if (ks == 0 && a == 0) {
 #pragma unroll
         for (int i = ht * 4 / (H / 32); i < (ht + 1) * 4 / (H / 32); ++i) work(i);
+      }
+      if (ks == 1 && a == 0) {
+#pragma unroll
+        for (int i = ht * 4 / (H / 32); i < (ht + 1) * 4 / (H / 32); ++i) late(i);
       }
 #pragma unroll
       for (int b = 1; b < PARTS && a + b < TOP; ++b) mma32(acc[ht], f[NF + n], __builtin_bit_cast(bf16x8, part[b][ks]));
@@ -462,29 +468,37 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
     start(s, 0, 0);
     step.template begin<Step::NF - 1>(0, 0);
     step.template logits<Step::NF - 1>(s, xf, 0, 0, [](int) {});
+    auto mask = [&](f32x16& z, int first) {   // the last tile: entries beyond V (with a bias, the bias is -inf there)
+      if (!BIAS && first + 32 > V) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          if (first + 8 * (j / 4) + 4 * g + j % 4 >= V) z[j] = -INFINITY;
+      }
+    };
+    mask(s, t0 * T);
+    float top = s[0];
+#pragma unroll
+    for (int j = 1; j < 16; ++j) top = fmaxf(top, s[j]);
+    constexpr bool kPipe = SUM && T == 64;   // the next tile is waited for within the first step, fragments read a step ahead
+    constexpr int LAST = (SUM ? 2 : 1) * Step::NF - 1;
+    if constexpr (kPipe) step.template begin<LAST>(32, 0);
     for (int t = t0; t < t1; ++t) {
       const int nbuf = next_buf(buf);
 #pragma unroll
       for (int r0 = 0; r0 < T; r0 += 32) {
         const bool last = r0 + 32 >= T;
         const int rs = last ? 0 : r0 + 32;   // of the next tile (after the last one: of what the buffer holds, not used)
-        if (last) {
+        auto turn = [&]() {
           land(t + 1, nbuf);
           if (t + 2 < t1) fetch(t + 2, next_buf(nbuf));
+          step.move_s(buf_step<NP * Step::PLANE>(nbuf));
+        };
+        if constexpr (!kPipe) {
+          if (last) turn();
+          step.template begin<LAST>(rs, r0);
         }
-        constexpr int LAST = (SUM ? 2 : 1) * Step::NF - 1;
-        if (last) step.move_s(buf_step<NP * Step::PLANE>(nbuf));
-        step.template begin<LAST>(rs, r0);
         f32x16 sn;
         start(sn, last ? nbuf : buf, rs);
-        if (!BIAS && (t + 1) * T > V) {   // the last tile: beyond V (with a bias, the bias is -inf there)
-#pragma unroll
-          for (int j = 0; j < 16; ++j)
-            if (t * T + r0 + 8 * (j / 4) + 4 * g + j % 4 >= V) s[j] = -INFINITY;
-        }
-        float top = s[0];
-#pragma unroll
-        for (int j = 1; j < 16; ++j) top = fmaxf(top, s[j]);
         top *= kLog2e;
         // The maximum follows only where it would grow by more than 2^8: until
         // then the terms stay below 2^8 and the sums lose nothing.
@@ -515,9 +529,22 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
           prob(j);
           if (SUM && j >= 8 && j % 2 == 1) split2(p[j - 9], p[j - 8], part, 0, (j - 9) / 2);
         });
-        if constexpr (SUM)
-          step.template product<P>(o, part, rs, r0, [&](int i) { split2(p[8 + 2 * i], p[9 + 2 * i], part, 1, i); });
+        if (kPipe && !last) turn();
+        mask(sn, (last ? (t + 1) * T : t * T) + rs);
+        float topn = sn[0];
+        auto grow = [&](int i) {
+#pragma unroll
+          for (int j = 4 * i; j < 4 * i + 4; ++j) topn = fmaxf(topn, sn[j]);
+        };
+        if constexpr (SUM) {
+          step.template product<P, kPipe>(o, part, last ? 32 : 0, r0,
+                                          [&](int i) { split2(p[8 + 2 * i], p[9 + 2 * i], part, 1, i); }, grow);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) grow(i);
+        }
         s = sn;
+        top = topn;
       }
       if constexpr (SUM) step.move_o(buf_step<NP * Step::PLANE>(nbuf));
       buf = nbuf;
@@ -809,19 +836,24 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
     start32(s, tl[0], lane);
     step.template begin<Step::NF - 1>(0, 0);
     step.template logits<Step::NF - 1>(s, wf, 0, 0, [](int) {});
+    constexpr bool kPipe = T == 64;   // as in the rows pass
+    constexpr int LAST = 2 * Step::NF - 1;
+    if constexpr (kPipe) step.template begin<LAST>(32, 0);
     for (int t = t0; t < t1; ++t) {
       const int nbuf = next_buf(buf);
 #pragma unroll
       for (int r0 = 0; r0 < T; r0 += 32) {
         const bool last = r0 + 32 >= T;
         const int rs = last ? 0 : r0 + 32;   // of the next tile (after the last one: of what the buffer holds, not used)
-        if (last) {
+        auto turn = [&]() {
           land(nbuf);
           if (t + 2 < t1) fetch(t + 2, next_buf(nbuf));
+          step.move_s(buf_step<NP * Step::PLANE>(nbuf));
+        };
+        if constexpr (!kPipe) {
+          if (last) turn();
+          step.template begin<LAST>(rs, r0);
         }
-        constexpr int LAST = 2 * Step::NF - 1;
-        if (last) step.move_s(buf_step<NP * Step::PLANE>(nbuf));
-        step.template begin<LAST>(rs, r0);
         f32x16 sn;
         start32(sn, tl[last ? nbuf : buf] + rs, lane);
         const int tj = tt[buf][r0 + lane % 32];
@@ -865,10 +897,15 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
 #pragma unroll
           for (int i = 0; i < 4; ++i) split2(p[2 * i], p[2 * i + 1], part, 0, i);
         }
-        step.template product<P>(a, part, rs, r0, [&](int i) {
-          split2(p[8 + 2 * i], p[9 + 2 * i], part, 1, i);
-          db += (p[4 * i] + p[4 * i + 1]) + (p[4 * i + 2] + p[4 * i + 3]);
-        });
+        if (kPipe && !last) turn();
+        const int rn = last ? 32 : 0;   // of the next step's logits
+        step.template product<P, kPipe>(
+            a, part, rn, r0,
+            [&](int i) {
+              split2(p[8 + 2 * i], p[9 + 2 * i], part, 1, i);
+              db += (p[4 * i] + p[4 * i + 1]) + (p[4 * i + 2] + p[4 * i + 3]);
+            },
+            [](int) {});
         // In bf16 the target's share of dW is a product of its own, since a pair of
         // p - 1 would lose low bits of p to the 1.  (Without TARGETS it comes from
         // launch_target_rows.)
@@ -891,8 +928,9 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
             }
 #pragma unroll
             for (int k = 0; k < step.kAhead; ++k) step.read(Step::NF + k, 0, r0);
-            step.template product<1>(a, e, rs, r0, [](int) {});
+            step.template product<1, false>(a, e, 0, r0, [](int) {}, [](int) {});
           }
+          if constexpr (kPipe) step.template begin<Step::NF - 1>(rn, r0);   // (rather than kept during these products)
         }
         s = sn;
       }
