@@ -27,14 +27,14 @@
 // are float32.
 //
 // What bounds them: at H = 256 the matrix cores.  60,001 rows over 50,021 entries
-// in bf16: rows pass 3,690 us, columns pass 3,870 to 4,050, 1.25 and 1.17 PFLOP/s,
-// where a plain 8,192^3 product of the library runs at 1.32.  At H = 64 a step has a
+// in bf16: rows pass 3,730 us, columns pass 4,000, 1.24 and 1.15 PFLOP/s, where a
+// plain 8,192^3 product of the library runs at 1.32.  At H = 64 a step has a
 // quarter of the products for the same 16 exponentials a lane, whose vector
 // instructions take longer than the products: 3,001 rows over 10,007 entries
-// 22.5 and 23.6 us (0.51 PFLOP/s), then 8.4 and 6.9 us to add up the shares (25 and
+// 22.4 and 23.1 us (0.51 PFLOP/s), then 8.2 and 6.9 us to add up the shares (25 and
 // 23 MB, at memory speed).  Loss alone at H = 128, 2,999 rows over 50,021 entries:
-// 54 us, 0.71 PFLOP/s, exponentials again.  float32 at H = 128, 1,229 rows over
-// 4,999 entries: 29.0 and 27.8 us (0.65 PFLOP/s of bf16 products: 250 workgroups
+// 53 us, 0.72 PFLOP/s, exponentials again.  float32 at H = 128, 1,229 rows over
+// 4,999 entries: 28.8 and 27.7 us (0.65 PFLOP/s of bf16 products: 250 workgroups
 // of 4 waves, one per SIMD, and a run of 6 to 7 tiles).
 #include <type_traits>
 
@@ -322,7 +322,11 @@ __global__ __launch_bounds__(kVocThreads) void vocab_planes_kernel(size_t count,
 // after it go to the buffer that every wave left before the last barrier.
 // Within a wave the logits of the next 32 entries are formed before the
 // current ones are turned into probabilities, so that the matrix cores have
-// work during the exponentials.
+// work during the exponentials.  With two steps to a tile (bf16) the next tile is
+// waited for between the two products of the first step, so that either step's
+// first fragments are read during the products before it (against reading them at
+// the step's start: rows pass 3,775 -> 3,713 us, columns pass 4,090 -> 3,980, 60,001
+// rows, in turn on one card).
 //
 // Work is dealt in units of one LDS tile against one tile of 128 rows (or, in
 // the columns pass, entries).  Many 128-tiles: `workers` workgroups first take
