@@ -11,6 +11,8 @@ node's final state with its row, plus a bias per token.
 """
 from __future__ import annotations
 
+import contextlib
+
 import numpy as np
 
 from . import capi
@@ -30,7 +32,11 @@ def token_lists(lists, n_pad: int):
 
 
 class NodeTokens:
-    """Token table [V][H], per-token bias [V] and token lists of one workload."""
+    """Token table [V][H], per-token bias [V] and token lists of one workload.
+
+    stream arguments: a torch stream or its handle, None for the current one; all
+    of a call's work, fills and uploads among it, goes to that stream.  Work on
+    other streams, the set-up's among it, is the caller's to order."""
 
     def __init__(self, model: BandedGGNN, table, tok_ptr, tok, bias=None, scale: float = 1.0, mean: bool = True,
                  p_in: float = 0.0, p_out: float = 0.0, seed: int = 0):
@@ -71,6 +77,15 @@ class NodeTokens:
 
     # ---------------------------------------------------------------- parts
 
+    def _on(self, stream):
+        """The context in which `stream` is the current one."""
+        t = self.torch
+        if stream is None:
+            return contextlib.nullcontext()
+        if isinstance(stream, int):
+            stream = t.cuda.ExternalStream(stream) if stream else t.cuda.default_stream(self.model.device)
+        return t.cuda.stream(stream)
+
     def embed(self, step: int = -1, stream=None):
         """X[0] from the tokens; step >= 0: with the dropout of that step."""
         m = self.model
@@ -94,7 +109,9 @@ class NodeTokens:
     def _space(self, name: str, nbytes: int):
         if not hasattr(self, name) or getattr(self, name).numel() < nbytes:
             setattr(self, name, self.torch.empty((max(nbytes, 16),), dtype=self.torch.uint8, device=self.model.device))
-        return getattr(self, name)
+        ws = getattr(self, name)
+        ws.record_stream(self.torch.cuda.current_stream())   # which need not be the one that it was allocated on
+        return ws
 
     # ------------------------------------------------------------- serving
 
@@ -102,18 +119,19 @@ class NodeTokens:
         """Forward pass without dropout and, for the chosen nodes, the best
         token and log sum of the logits' exponentials (and, with targets, the
         losses): dict of device tensors."""
-        node, target = self._rows(node, target)
-        m, t = self.model, self.torch
-        R = len(node)
-        out = {"best": t.empty((R,), dtype=t.int32, device=m.device), "lse": t.empty((R,), device=m.device)}
-        if target is not None:
-            out["loss"] = t.empty((R,), device=m.device)
-        self.embed(stream=stream)
-        m.forward(stream)
-        ws = self._space("eval_ws", capi.ggnn_vocab_workspace_bytes(m.dt, m.H, R, self.V, False))
-        capi.ggnn_vocab_loss(m.dt, m.comp.n_pad, m.H, R, self.V, m.X[m.T], self.table, self.bias, node, target,
-                             out.get("loss"), out["lse"], out["best"], ws, ws.numel(), stream)
-        return out
+        with self._on(stream):
+            node, target = self._rows(node, target)
+            m, t = self.model, self.torch
+            R = len(node)
+            out = {"best": t.empty((R,), dtype=t.int32, device=m.device), "lse": t.empty((R,), device=m.device)}
+            if target is not None:
+                out["loss"] = t.empty((R,), device=m.device)
+            self.embed()
+            m.forward()
+            ws = self._space("eval_ws", capi.ggnn_vocab_workspace_bytes(m.dt, m.H, R, self.V, False))
+            capi.ggnn_vocab_loss(m.dt, m.comp.n_pad, m.H, R, self.V, m.X[m.T], self.table, self.bias, node, target,
+                                 out.get("loss"), out["lse"], out["best"], ws, ws.numel())
+            return out
 
     # ------------------------------------------------------------ training
 
@@ -141,18 +159,19 @@ class NodeTokens:
         model's grad_buf.  self.loss holds the rows' losses."""
         m = self.model
         n, H = m.comp.n_pad, m.H
-        self.embed(step, stream)
-        m.forward(stream)
-        capi.ggnn_dropout(m.dt, n * H, m.X[m.T], self.p_out, self.seed, 2 * step + 1, self.XT, stream)
-        self.grad.zero_()
-        m.grad_buf.zero_()
-        capi.ggnn_vocab_loss_grad(m.dt, n, H, self.n_rows, self.V, self.XT, self.table, self.bias, self.node,
-                                  self.target, None, 1.0 / max(self.n_live, 1), self.loss, self.lse, m.dX,
-                                  self.dtable, self.dbias, self.loss_ws, self.loss_ws.numel(), stream)
-        capi.ggnn_dropout("f32", n * H, m.dX, self.p_out, self.seed, 2 * step + 1, m.dX, stream)
-        capi.ggnn_backward(m.model, m.act, m.grads, stream)
-        capi.ggnn_embed_bwd(n, H, self.V, self.tok_ptr, self.tok, self.n_tok, self.scale, self.mean, self.p_in,
-                            self.seed, 2 * step, m.dX, self.dtable, self.embed_ws, self.embed_ws.numel(), stream)
+        with self._on(stream):
+            self.embed(step)
+            m.forward()
+            capi.ggnn_dropout(m.dt, n * H, m.X[m.T], self.p_out, self.seed, 2 * step + 1, self.XT)
+            self.grad.zero_()
+            m.grad_buf.zero_()
+            capi.ggnn_vocab_loss_grad(m.dt, n, H, self.n_rows, self.V, self.XT, self.table, self.bias, self.node,
+                                      self.target, None, 1.0 / max(self.n_live, 1), self.loss, self.lse, m.dX,
+                                      self.dtable, self.dbias, self.loss_ws, self.loss_ws.numel())
+            capi.ggnn_dropout("f32", n * H, m.dX, self.p_out, self.seed, 2 * step + 1, m.dX)
+            capi.ggnn_backward(m.model, m.act, m.grads)
+            capi.ggnn_embed_bwd(n, H, self.V, self.tok_ptr, self.tok, self.n_tok, self.scale, self.mean, self.p_in,
+                                self.seed, 2 * step, m.dX, self.dtable, self.embed_ws, self.embed_ws.numel())
 
     def train_step(self, stream=None):
         """One training step: gradients(), then the Momentum update of the

@@ -97,6 +97,29 @@ def test_serving_answers_with_the_largest_logit(dt):
     assert np.max(np.abs(host(out["loss"]) - want)) <= 1e-4
 
 
+@pytest.mark.parametrize("as_handle", [False, True])
+def test_all_of_a_call_runs_on_the_given_stream(as_handle):
+    """Three calls behind a stream that is still busy: the fills between them wait for it as the kernels do."""
+    m, t, *_, node, target, _ = setup("bf16", 64)
+    t.setup_training(node, target)
+    t.gradients(2)
+    want = (t.grad.clone(), m.grad_buf.clone(), t.loss.clone())
+    best = t.evaluate(node)["best"]
+    a = torch.randn((4096, 4096), device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            a = torch.mm(a, a).mul_(1.0 / 4096)
+    given = side.cuda_stream if as_handle else side
+    t.gradients(1, stream=given)
+    t.gradients(2, stream=given)
+    got = t.evaluate(node, stream=given)["best"]
+    torch.cuda.synchronize()
+    assert torch.equal(t.grad, want[0]) and torch.equal(m.grad_buf, want[1]) and torch.equal(t.loss, want[2])
+    assert torch.equal(got, best)
+
+
 def test_refusals():
     m, t, comp, params, ptr, tok, table, bias, node, target, (_, _, V, _) = setup("f32", 64)
     with pytest.raises(ValueError, match="table"):
