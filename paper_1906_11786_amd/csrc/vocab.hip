@@ -347,7 +347,11 @@ struct Deal {
     const uint32_t k = more * (each + 1);
     return (int)(u < k ? u / (each + 1) : more + (u - k) / each);
   }
-  // Shares of 128-tile i; share s of it is written to slot i * slots + s.
+  // Where share 0 of 128-tile i is written: a whole one is one share, each of the
+  // rest has room for `slots`.
+  __host__ __device__ int slot(int i) const { return i < whole ? i : whole + (i - whole) * slots; }
+  __host__ __device__ int all_slots() const { return whole + rest * slots; }
+  // Shares of 128-tile i; share s of it is written to slot(i) + s.
   __host__ __device__ int shares(int i) const {
     if (i < whole) return 1;
     if (parts > 0) return parts;
@@ -367,13 +371,13 @@ struct Dealt {
   __device__ __forceinline__ bool next(const Deal& d, int w, Run* r) {
     if (step * d.workers < d.whole) {
       const int i = step * d.workers + w;
-      *r = Run{i, 0, d.tiles, i * d.slots};
+      *r = Run{i, 0, d.tiles, d.slot(i)};
       ++step;
       return true;
     }
     if (u >= end) return false;
     if (d.parts > 0) {
-      *r = Run{w / d.parts, (int)u, (int)end, w / d.parts * d.slots + w % d.parts};
+      *r = Run{w / d.parts, (int)u, (int)end, d.slot(w / d.parts) + w % d.parts};
       u = end;
       return true;
     }
@@ -381,7 +385,7 @@ struct Dealt {
     r->i = d.whole + (int)k;
     r->t0 = (int)(u - k * d.tiles);
     r->t1 = min(d.tiles, r->t0 + (int)(end - u));
-    r->slot = r->i * d.slots + (r->t0 == 0 ? 0 : w - d.owner(k * d.tiles));
+    r->slot = d.slot(r->i) + (r->t0 == 0 ? 0 : w - d.owner(k * d.tiles));
     u += r->t1 - r->t0;
     return true;
   }
@@ -737,7 +741,7 @@ __global__ __launch_bounds__(kVocThreads) void vocab_join_kernel(
   const int n = row_node(node, r, R, n_nodes);
   const f32x4 x = n >= 0 ? load4f(X + (size_t)n * H + h) : f32x4{};
   const int shares = r < R ? deal.shares(r / kVocRows) : 0;
-  const size_t at0 = (size_t)(r / kVocRows) * deal.slots * kVocRows + r % kVocRows;
+  const size_t at0 = (size_t)deal.slot(r / kVocRows) * kVocRows + r % kVocRows;
   int t = n >= 0 && target != nullptr ? target[r] : -1;
   const bool bad = t >= V;
   if (bad) t = -1;
@@ -777,7 +781,8 @@ __global__ __launch_bounds__(kVocThreads) void vocab_join_kernel(
 
 // Columns pass: 128 entries of a workgroup (32 per wave) against the gathered
 // states.  Adds to dW [V][H] and db [V] (dbias NULL: none) where the 128-tile is
-// one share, else writes its share to pw [slot][128][H] and pdb [slot][128].
+// one share, else writes its share to pw [slot][128][H] and pdb [slot][128], slots
+// from the first tile of the rest on.
 // WEIGHT: each row has a factor of its own; otherwise all have `scale`.  TARGETS:
 // see below.
 template <typename S, int H, bool WEIGHT, bool TARGETS>
@@ -945,7 +950,7 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
     db = (db + __shfl_xor(db, 32)) * f;
     if (v < V) {
       const bool only = deal.shares(run.i) == 1;   // no one else adds to these rows
-      const size_t at = (size_t)run.slot * kVocRows + wave * 32 + lane % 32;
+      const size_t at = only ? 0 : (size_t)(run.slot - deal.whole) * kVocRows + wave * 32 + lane % 32;
       if (dbias != nullptr && g == 0) {
         if (only) dbias[v] += db;
         else pdb[at] = db;
@@ -977,7 +982,7 @@ __global__ __launch_bounds__(kVocThreads) void vocab_wsum_kernel(int V, Deal dea
   if (v >= V) return;
   const int i = (int)(v / kVocRows), n = deal.shares(i);
   if (n == 1) return;
-  const size_t at = (size_t)i * deal.slots * kVocRows + v % kVocRows;
+  const size_t at = (size_t)(i - deal.whole) * deal.slots * kVocRows + v % kVocRows;
   f32x4 w = {};
 #pragma unroll 8
   for (int s = 0; s < n; ++s) w += *reinterpret_cast<const f32x4*>(pw + (at + (size_t)s * kVocRows) * H + 4 * q);
@@ -1065,7 +1070,7 @@ VocabPlan vocab_plan(int H, int R, int V, bool grad) {
     p.row_tiles = cdiv(R, dev::kVocRows);
     p.Rp = p.row_tiles * dev::kVocRows;
     p.rows = make_deal(p.row_tiles, cdiv(V, T), voc_workers<S>(H, grad));
-    shares = (size_t)p.row_tiles * p.rows.slots * dev::kVocRows;
+    shares = (size_t)p.rows.all_slots() * dev::kVocRows;
   }
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -1080,7 +1085,7 @@ VocabPlan vocab_plan(int H, int R, int V, bool grad) {
   if (grad) {
     p.col_tiles = cdiv(V, dev::kVocRows);
     p.cols = make_deal(p.col_tiles, p.Rp / T, voc_workers<S>(H, true));
-    const size_t cshares = (size_t)p.col_tiles * p.cols.slots * dev::kVocRows;
+    const size_t cshares = p.cols.slots > 1 ? (size_t)p.cols.rest * p.cols.slots * dev::kVocRows : 0;
     p.po = take(shares * H * 4);
     p.xg = take((size_t)p.Rp * H * 2 * dev::voc_planes<S>());
     p.lse = take((size_t)p.Rp * 4);

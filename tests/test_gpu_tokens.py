@@ -518,3 +518,41 @@ def test_vocab_large_forms(dt, H, rows, V, bias, weighted):
         R.within(got[k], want[k], want[k + "_tol"] + 4 * R.U * (1 + np.abs(want[k])))
     plain = run_vocab(dt, X, W, b, node, target, grad=False)
     R.within(plain["lse"], want["lse"], want["lse_tol"])
+
+
+def check_large(dt, H, rows, V, bias, weighted=False):
+    """As test_vocab_large_forms, the losses too."""
+    rng = np.random.default_rng(V)
+    X, W, node, target, b = vocab_case(rng, dt, rows + 100, H, V, rows, bias)
+    target[::9] = -1
+    weight = round_to("f32", rng.standard_normal(rows)) if weighted else None
+    want = large_reference(X, W, b, node, target, weight, 2.0 / rows, dt)
+    has = target >= 0
+    t = np.where(has, target, 0)
+    zt = (X[node] * W[t]).sum(1) + (0.0 if b is None else b[t])
+    zt_tol = (H + 4) * R.U * ((np.abs(X[node]) * np.abs(W[t])).sum(1) + (0.0 if b is None else np.abs(b[t])))
+    loss = np.where(has, want["lse"] - zt, 0.0)
+    loss_tol = want["lse_tol"] + zt_tol + 4 * R.U * np.abs(zt)
+    got = run_vocab(dt, X, W, b, node, target, weight, 2.0 / rows)
+    plain = run_vocab(dt, X, W, b, node, target, grad=False)
+    for o in (got, plain):
+        R.within(o["lse"], want["lse"], want["lse_tol"])
+        R.within(o["loss"], loss, loss_tol)
+    R.within(got["dX"][node], want["dX"], want["dX_tol"])
+    rest = np.ones(len(X), bool)
+    rest[node] = False
+    assert not got["dX"][rest].any()
+    for k in ("dW", "db"):   # added to ones
+        R.within(got[k], want[k], want[k + "_tol"] + 4 * R.U * (1 + np.abs(want[k])))
+
+
+@pytest.mark.parametrize("dt,H,rows,V", [
+    ("bf16", 256, 256 * 128 + 5, 2570),    # one 128-tile of rows more than there are workgroups, cut into many shares
+    ("bf16", 256, 300, 256 * 128 + 3),     # and of entries
+    ("f32", 256, 256 * 128 + 1, 333),
+    ("f32", 128, 1000, 256 * 128 + 130),
+    ("bf16", 64, 768 * 128 + 9, 1500),
+])
+def test_vocab_one_left_over_tile(dt, H, rows, V):
+    say(f"vocab left-over tile dt={dt} H={H} rows={rows} V={V}")
+    check_large(dt, H, rows, V, bias=True)

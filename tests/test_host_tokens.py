@@ -146,3 +146,28 @@ def test_token_lists_layout():
     assert ptr.tolist() == [0, 0, 0, 0, 0] and len(tok) == 1
     with pytest.raises(ValueError, match="3 token lists for 2 nodes"):
         tokens.token_lists([[], [], []], 2)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("H", [32, 64, 128, 256])
+def test_vocab_workspace_grows_with_its_rows_and_entries(dt, H):
+    """One row, or one entry, more than the workgroups take in whole tiles costs shares of that tile only: every tile
+    dealt whole has one share, and the others of a pass at most four per workgroup."""
+    workers = 256 * {32: 4, 64: 3, 128: 3, 256: 1}[H]          # that the compute units hold, at most
+    share = 128 * (4 * H + 16)                                  # O (or dW), maximum, sum, best entry
+    up = (lambda x: -(-x // 128) * 128)
+
+    def bound(rows, V, grad):
+        per_row = 16 + (4 * H + 6 * H + 64 + H * H // 1024 if grad else 0)   # shares; state, sort and its partial sums
+        return up(rows) * per_row + (6 * V * H if dt == "f32" else 0) + (2 if grad else 1) * 4 * workers * share + (1 << 20)
+
+    most = ((1 << 31) - 1) // H
+    sizes = [(128 * w * k + d, 50021) for w in (256, 512, 768, 1024) for k in (1, 3) for d in (-1, 0, 1, 129)]
+    sizes += [(r, 128 * w + d) for r in (33, 3001, 30000) for w in (256, 512, 768, 1024, 2048) for d in (0, 2, 200)]
+    sizes += [(1 << 24, 50021), ((1 << 24) - 32767, 50021), (3001, most), (3001, most - 127)]
+    for rows, V in sizes:
+        if V > most:
+            continue
+        for grad in (False, True):
+            need = capi.ggnn_vocab_workspace_bytes(dt, H, rows, V, grad)
+            assert 0 < need <= bound(rows, V, grad), (rows, V, grad, need, bound(rows, V, grad))
