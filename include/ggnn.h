@@ -558,7 +558,9 @@ ggnn_status ggnn_readout_loss_bwd_noalloc(ggnn_dtype dt, int32_t n_pad, int32_t 
  * parameters, element-wise:
  *   g = grad + weight_decay * param;  velocity = momentum * velocity + g;
  *   param -= lr * (nesterov ? g + momentum * velocity : velocity)
- * param, velocity [count] float (updated in place); grad [count] float.
+ * param, velocity [count] float (updated in place; a param of -inf, an entry
+ * that a bias takes out of a softmax, stays as it is, and so does its velocity);
+ * grad [count] float.
  * param_copy: NULL, or a [count] tensor of copy_dtype rewritten from the new
  * param (round to nearest even for bf16) -- the compute copy that the
  * propagation reads.  The four buffers must not overlap.  momentum and

@@ -194,6 +194,8 @@ namespace dev {
 // Momentum update of float32 master parameters, element-wise:
 //   g = grad + wd * theta;  v = mu * v + g;  theta -= lr * (nesterov ? g + mu * v : v)
 // and the compute copy (COPY: 0 none, 1 bf16, 2 float32) rewritten from theta.
+// A theta of -inf (an entry that a bias takes out of a softmax) stays, with its
+// velocity: wd * theta, even with wd = 0, would make a NaN of it.
 template <int COPY>
 __global__ __launch_bounds__(256) void sgd_momentum_kernel(long count, float* __restrict__ theta,
                                                            float* __restrict__ vel, const float* __restrict__ grad,
@@ -202,9 +204,10 @@ __global__ __launch_bounds__(256) void sgd_momentum_kernel(long count, float* __
   for (long i = (long)blockIdx.x * blockDim.x + threadIdx.x; i < count; i += (long)gridDim.x * blockDim.x) {
     const float th = theta[i];
     const float g = grad[i] + wd * th;
-    const float v = mu * vel[i] + g;
-    const float nt = th - lr * (nesterov ? g + mu * v : v);
-    vel[i] = v;
+    const bool out = th == -INFINITY;
+    const float old = vel[i], v = mu * old + g;
+    const float nt = out ? th : th - lr * (nesterov ? g + mu * v : v);
+    vel[i] = out ? old : v;
     theta[i] = nt;
     if constexpr (COPY == 1) static_cast<bf16s*>(copy)[i] = f2bf(nt);
     if constexpr (COPY == 2) static_cast<float*>(copy)[i] = nt;

@@ -42,8 +42,10 @@ class NodeTokens:
                  p_in: float = 0.0, p_out: float = 0.0, seed: int = 0):
         """model: its X[0] is written from the tokens.  table: float array [V, H]
         (exact in the model's dtype, as the model's parameters are).  tok_ptr,
-        tok: as ggnn_embed takes them (token_lists() makes them).  p_in, p_out:
-        dropout of the first and of the final states while training."""
+        tok: as ggnn_embed takes them (token_lists() makes them).  bias: -1e30 or
+        less takes a token out of the answers, in training for good (it is kept
+        as -inf, which the update leaves alone).  p_in, p_out: dropout of the
+        first and of the final states while training."""
         import torch
         self.torch, self.model = torch, model
         table = np.asarray(table, np.float64)
@@ -64,7 +66,8 @@ class NodeTokens:
         self.master[:self.V * H].copy_(torch.from_numpy(table.astype(np.float32).reshape(-1)))
         self.bias = self.master[self.V * H:self.V * H + self.V]
         if bias is not None:
-            self.bias.copy_(torch.from_numpy(np.asarray(bias, np.float32)))
+            bias = np.asarray(bias, np.float32)
+            self.bias.copy_(torch.from_numpy(np.where(bias <= -1e30, np.float32(-np.inf), bias)))
         self.compute_copy = self.master.to(torch_dtype(dt)) if dt == "bf16" else None
         self.table = (self.master if self.compute_copy is None else self.compute_copy)[:self.V * H].view(self.V, H)
         self.grad = torch.zeros_like(self.master)

@@ -142,3 +142,29 @@ def test_example_learns():
     losses = hidden_tokens.main(steps=40)
     assert losses[0] > 5.0                       # about log 500 at the start
     assert np.mean(losses[-5:]) < 0.5 * losses[0]
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("low", [-np.inf, R.LOWEST, -1e30])
+@pytest.mark.parametrize("weight_decay", [0.0, 0.125])
+def test_masked_tokens_stay_masked_in_training(dt, low, weight_decay):
+    """Tokens that the bias takes out: their bias stays, what is updated stays finite, and after three steps the log
+    sums are those over the other tokens."""
+    m, t, comp, params, ptr, tok, table, bias, node, target, (_, _, V, _) = setup(dt, 64)
+    out = np.arange(V) % 3 == 0
+    bias[out] = low
+    t = NodeTokens(m, table, ptr, tok, bias=bias, scale=8.0, p_in=0.25, p_out=0.25, seed=5)
+    target = np.where(out[np.maximum(target, 0)], -1, target)
+    t.setup_training(node, target, lr=0.125, momentum=0.5, weight_decay=weight_decay)
+    start = t.bias.clone()
+    for _ in range(3):
+        t.train_step()
+        assert bool(torch.isfinite(t.loss).all()) and bool(torch.isfinite(m.master).all())
+    assert bool((t.bias[torch.from_numpy(out).cuda()] <= -1e30).all())
+    keep = torch.from_numpy(~out).cuda()
+    assert bool(torch.isfinite(t.table).all()) and bool(torch.isfinite(t.bias[keep]).all())
+    assert not torch.equal(t.bias[keep], start[keep])
+    got = t.evaluate(node[:50], target[:50])
+    z = (host(m.X[m.T])[node[:50]] @ host(t.table).T + np.where(out, 0.0, host(t.bias)))[:, ~out]
+    assert np.max(np.abs(host(got["lse"]) - np.log(np.exp(z).sum(1)))) <= 1e-4
+    assert not np.any(out[got["best"].cpu().numpy()])

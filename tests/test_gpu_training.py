@@ -150,3 +150,21 @@ def test_train_step_matches_oracle(dt, n, B, E, H, T, band_format):
             say(f"  step {step} {k}: {err:.2e}")
             assert err <= TOL[dt], (step, k, err)
         p_or, prev = nxt, got
+
+
+@pytest.mark.parametrize("nesterov", [False, True])
+@pytest.mark.parametrize("weight_decay", [0.0, 0.5])
+def test_sgd_momentum_leaves_a_parameter_of_minus_infinity(nesterov, weight_decay):
+    """-inf stays, with its velocity, whatever its gradient; its neighbours are updated as ever."""
+    inf = float("inf")
+    p = torch.tensor([1.0, -inf, -2.0, -inf, 3.0], device="cuda")
+    v = torch.tensor([0.5, 0.0, 0.25, 0.75, -1.0], device="cuda")
+    g = torch.tensor([1.0, 0.0, -1.0, 2.0, 0.5], device="cuda")
+    copy = torch.zeros((5,), device="cuda", dtype=torch.bfloat16)
+    th, vel = host(p), host(v)
+    at = [0, 2, 4]
+    want, wv = O.momentum_update(th[at], vel[at], host(g)[at], 0.25, 0.5, weight_decay, nesterov)   # exact here
+    capi.ggnn_sgd_momentum(5, p, v, g, 0.25, 0.5, weight_decay, nesterov, "bf16", copy)
+    assert np.array_equal(host(p)[at], want) and np.array_equal(host(v)[at], wv)
+    assert p[1].item() == p[3].item() == -inf and v[1].item() == 0.0 and v[3].item() == 0.75
+    assert copy[1].item() == copy[3].item() == -inf
