@@ -720,8 +720,9 @@ size_t ggnn_vocab_workspace_bytes(ggnn_dtype dt, int32_t H, int32_t n_rows, int3
  *            loss then +inf, without a gradient)
  *   best     [n_rows] int32 (written: the entry with the largest logit, the lowest
  *            one of equals, -1 where every entry is taken out), or NULL
- * A NaN or +inf logit makes its row's lse and loss NaN, and so may, in float32,
- * a state or entry that is not finite (they enter the products as three bf16). */
+ * Logits may have any size up to 1e38.  A NaN or +inf one makes its row's lse and
+ * loss NaN, and so may, in float32, a state or entry that is not finite (they
+ * enter the products as three bf16). */
 ggnn_status ggnn_vocab_loss(ggnn_dtype dt, int32_t n_nodes, int32_t H, int32_t n_rows, int32_t V, const void* X,
                             const void* W, const float* bias, const int32_t* node, const int32_t* target,
                             float* loss, float* lse, int32_t* best, void* workspace, size_t workspace_bytes,
@@ -734,6 +735,9 @@ ggnn_status ggnn_vocab_loss(ggnn_dtype dt, int32_t n_nodes, int32_t H, int32_t n
  *        node may be chosen once (otherwise its row holds one of the contributions).
  *   dW   [V][H] float += sum_r dz_v X[node[r]];  dbias [V] float += sum_r dz_v, or NULL
  *   weight [n_rows] float, or NULL for 1
+ * dW and dbias take exp(z_v - lse[r]) from the rounded lse: the relative error of
+ * these probabilities grows as |lse| 2^-23, so rows with a gradient should keep
+ * |lse| below about 1e5 (dX, lse and loss have no such limit).
  * In bf16 a probability enters the two gradient products as a bf16 pair (hi + lo,
  * 16 bits); in float32 states, entries and probabilities are three bf16 each (24
  * bits) and a product is six. */

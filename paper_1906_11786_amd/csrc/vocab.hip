@@ -53,6 +53,20 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kMaskedBias = -1e30f;      // a bias at or below takes its entry out
 constexpr float kNoMax = -3e38f;           // running maximum before the first logit
 
+// Exponents of a row's terms are z * k - m with m = z_max * k, in one fused
+// multiply-add: k = log2 e, and the rounding of m is one factor of all terms, which
+// the log sum takes out again.  From 2^29 on that rounding would pass the range of
+// an exponential.  There k = 2, which makes m exact: logits of this size are equal
+// or at least 32 apart, so that any k gives the terms 1 and (to 2^-46) 0.  Maxima of
+// both sizes keep their order, and differences that vanish, when compared as m.
+constexpr float kFarLogit = 536870912.f;
+__device__ __forceinline__ float exponent_factor(float z) { return fabsf(z) >= kFarLogit ? 2.f : kLog2e; }
+// The log sum of a row from its m and the sum of its terms.
+__device__ __forceinline__ float log_of(float m, float sum) {
+  const float s = __log2f(sum);
+  return fabsf(m) >= 2.f * kFarLogit ? 0.5f * m + s * kLn2 : (m + s) * kLn2;
+}
+
 // float32 states and rows enter the matrix cores as three bf16 each (x = x0 +
 // x1 + x2, exact), with the six products of order 2^-16 and up: 24 bits at 6
 // bf16 products, where the float32 matrix instructions take 16 times a bf16
@@ -446,7 +460,7 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
 #pragma unroll
       for (int ht = 0; ht < H / 32; ++ht) o[ht] = f32x16{};
     }
-    float m = kNoMax, l = 0.f;
+    float m = kNoMax, k = kLog2e, l = 0.f;   // k: the row's exponent_factor
     RowBest best{-INFINITY, INT_MAX};
     auto fetch = [&](int t, int buf) {   // start the copies of tile t < t1
       stage_tile<H, NP, T>(W, (size_t)V * H, (long)t * T, V - 1, lds0 + (uint32_t)buf * NP * Step::PLANE, wave,
@@ -507,12 +521,13 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
         }
         f32x16 sn;
         start(sn, last ? nbuf : buf, rs);
-        top *= kLog2e;
         // The maximum follows only where it would grow by more than 2^8: until
         // then the terms stay below 2^8 and the sums lose nothing.
-        if (__ballot(top > m + 8.f)) {
+        if (__ballot(top * k > m + 8.f)) {
           const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-          const float mn = fmaxf(m, fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])));
+          const float z = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])), kn = exponent_factor(z);
+          const float mn = fmaxf(m, z * kn);
+          if (mn > m) k = kn;
           const float f = __builtin_amdgcn_exp2f(m - mn);
           m = mn;
           l *= f;
@@ -528,7 +543,7 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
           if constexpr (BEST) {
             if (s[j] > best.z) best = RowBest{s[j], t * T + r0 + 8 * (j / 4) + 4 * g + j % 4};
           }
-          p[j] = __builtin_amdgcn_exp2f(fmaf(s[j], kLog2e, -m));
+          p[j] = __builtin_amdgcn_exp2f(fmaf(s[j], k, -m));
           l += p[j];
         };
         u32x4 part[P][2];
@@ -594,7 +609,7 @@ __global__ __launch_bounds__(kVocThreads) void vocab_few_kernel(int n_nodes, int
   const int tiles = (V + 31) / 32, t0 = split * per, t1 = min(tiles, t0 + per);
   frag_t<S> xf[H / 16];
   load_row<S, H>(xf, X, row_node(node, r, R, n_nodes), lane);
-  float m = kNoMax, l = 0.f;
+  float m = kNoMax, k = kLog2e, l = 0.f;
   RowBest best{-INFINITY, INT_MAX};
   for (int t = t0; t < t1; ++t) {
     frag_t<S> wf[H / 16];
@@ -607,7 +622,8 @@ __global__ __launch_bounds__(kVocThreads) void vocab_few_kernel(int n_nodes, int
     float top = s[0];
 #pragma unroll
     for (int j = 1; j < 16; ++j) top = fmaxf(top, s[j]);
-    const float mn = fmaxf(m, top * kLog2e);
+    const float kn = exponent_factor(top), mn = fmaxf(m, top * kn);
+    if (mn > m) k = kn;
     l *= __builtin_amdgcn_exp2f(m - mn);
     m = mn;
 #pragma unroll
@@ -615,7 +631,7 @@ __global__ __launch_bounds__(kVocThreads) void vocab_few_kernel(int n_nodes, int
       if constexpr (BEST) {
         if (s[j] > best.z) best = RowBest{s[j], t * 32 + 8 * (j / 4) + 4 * g + j % 4};
       }
-      l += __builtin_amdgcn_exp2f(fmaf(s[j], kLog2e, -m));
+      l += __builtin_amdgcn_exp2f(fmaf(s[j], k, -m));
     }
   }
   const float m2 = __shfl_xor(m, 32), l2 = __shfl_xor(l, 32), mn = fmaxf(m, m2);
@@ -669,7 +685,7 @@ __device__ __forceinline__ void join_shares(int n, size_t at0, size_t stride, in
 }
 // lse of a row: -inf where every entry is masked.
 __device__ __forceinline__ float row_lse(float M, float sum) {
-  return sum == 0.f ? -INFINITY : (M + __log2f(sum)) * kLn2;
+  return sum == 0.f ? -INFINITY : log_of(M, sum);
 }
 __device__ __forceinline__ float row_loss(float lse, float zt, int t, bool bad) {
   return bad ? NAN : t < 0 ? 0.f : lse == -INFINITY ? INFINITY : lse - zt;

@@ -556,3 +556,56 @@ def check_large(dt, H, rows, V, bias, weighted=False):
 def test_vocab_one_left_over_tile(dt, H, rows, V):
     say(f"vocab left-over tile dt={dt} H={H} rows={rows} V={V}")
     check_large(dt, H, rows, V, bias=True)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [3, 130])
+@pytest.mark.parametrize("low", [-3e9, -1e10, -7.7e10, -1e15, -1e20, -9.9e29])
+def test_vocab_very_low_logits_have_no_weight(dt, rows, low):
+    """Biases far below the others, short of those that take an entry out, on the first entries and scattered: the
+    results are those without these entries, whose exponentials vanish."""
+    rng = np.random.default_rng(12)
+    for H in (64, 256):
+        X, W, node, target, b = vocab_case(rng, dt, 140, H, 300, rows, bias=True)
+        far = rng.random(300) < 0.3
+        far[:70] = True
+        target[far[target]] = 299
+        far[299] = False
+        b[far] = np.float32(low) * (1 + rng.random(int(far.sum()))).astype(np.float32)
+        b[3] = low
+        b = np.maximum(round_to("f32", b), -9.9e29)
+        want = R.vocab(X, W, np.where(far, -np.inf, b), node, target, None, 1.0, dt)
+        got = run_vocab(dt, X, W, b, node, target)
+        plain = run_vocab(dt, X, W, b, node, target, grad=False, best=True)
+        for o in (got, plain):
+            R.within(o["lse"], want["lse"], want["lse_tol"])
+            R.within(o["loss"], want["loss"], want["loss_tol"])
+        assert np.array_equal(plain["best"], want["best"])
+        R.within(got["dX"], want["dX"], want["dX_tol"])
+        for k in ("dW", "db"):   # added to ones
+            R.within(got[k], want[k], want[k + "_tol"] + 4 * R.U * (1 + np.abs(want[k])))
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [3, 130])
+@pytest.mark.parametrize("size", [-1e8, 1e8, -7.7e10, 7.7e10, -1e20, 1e20, -9e29])
+def test_vocab_logits_of_any_size(dt, rows, size):
+    """Every logit of one size, up to a few float32 steps: their log sum is theirs, to the same steps, and dX is the
+    mean row of W over equal entries less the target's."""
+    rng = np.random.default_rng(13)
+    X, W, node, target, b = vocab_case(rng, dt, 140, 64, 300, rows, bias=True)
+    b[:] = size
+    b[200:] = size if size in (-1e8, 1e8) else size - 40 * abs(size) * 2.0**-23
+    b = round_to("f32", b)
+    X *= 2.0**-10 if abs(size) == 1e8 else 1.0
+    top = 300 if abs(size) == 1e8 else 200
+    want = R.vocab(X, W, b, node, target, None, 1.0, dt)
+    got = run_vocab(dt, X, W, b, node, target)
+    plain = run_vocab(dt, X, W, b, node, target, grad=False, best=True)
+    for o in (got, plain):
+        R.within(o["lse"], want["lse"], want["lse_tol"])
+        R.within(o["loss"], want["loss"], want["loss_tol"])
+    assert np.all((plain["best"] >= 0) & (plain["best"] < top))
+    dX = np.zeros_like(X)
+    dX[node] = W[:top].mean(0) - W[target]
+    R.within(got["dX"], dX, 1e-4 * np.abs(W).max())
