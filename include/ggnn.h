@@ -679,7 +679,8 @@ ggnn_status ggnn_dropout(ggnn_dtype dt, int64_t count, const void* X, float p, u
  * ggnn_dropout's mask; p = 0: none).  Sums are float32, rounded to dt once.
  *   tok_ptr  [n + 1] int32, non-decreasing: node i lists tok[tok_ptr[i]] ..
  *            tok[tok_ptr[i+1] - 1] (none: a zero row).  NULL: one token per node,
- *            node i's is tok[i]; nodes n_tok .. n - 1 have none.
+ *            node i's is tok[i]; nodes n_tok .. n - 1 have none.  Parts of a list
+ *            before position 0 or from n_tok on are left out, of its length too.
  *   tok      [n_tok] int32 token ids (n_tok <= 2^30); an id outside [0, V) adds nothing
  *   scale, mean   c_i = scale, or scale / (length of the list) where mean is not 0
  *   table    [V][H] dt;  X [n][H] dt (written whole; must not overlap the table) */

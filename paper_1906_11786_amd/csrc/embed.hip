@@ -407,8 +407,9 @@ __device__ __forceinline__ void add_row(float* __restrict__ o, const float (&acc
   store8f(o, v);
 }
 
-// S: type of the summed rows.  Row r's factor is scale (over its list's length
-// for the mean), or -factor[r] where factor is given.
+// S: type of the summed rows.  Row r's factor is scale (over the length of its list
+// for the mean, cut at the list's ends as the lookup cuts it), or -factor[r] where
+// factor is given.
 template <typename S, int H, bool DROP>
 __global__ __launch_bounds__(kEmbThreads) void embed_runs_kernel(int n_tok, int n, int V, int chunk,
                                                                  const u32x2* __restrict__ items,
@@ -453,7 +454,10 @@ __global__ __launch_bounds__(kEmbThreads) void embed_runs_kernel(int n_tok, int 
         if (ok) {
           load8f<S>(dX + (size_t)row * H + h, v[u]);
           if (factor != nullptr) f[u] = -factor[row];
-          if (tok_ptr != nullptr && mean) f[u] = scale / (float)max(tok_ptr[row + 1] - tok_ptr[row], 1);
+          if (tok_ptr != nullptr && mean) {
+            const int b = clampi(tok_ptr[row], 0, n_tok), e = clampi(tok_ptr[row + 1], b, n_tok);
+            f[u] = scale / (float)max(e - b, 1);
+          }
           if (it[u].x != (u > 0 ? it[u - 1].x : cur)) load8f<float>(dtable + (size_t)it[u].x * H + h, w[u]);
         }
       }

@@ -609,3 +609,28 @@ def test_vocab_logits_of_any_size(dt, rows, size):
     dX = np.zeros_like(X)
     dX[node] = W[:top].mean(0) - W[target]
     R.within(got["dX"], dX, 1e-4 * np.abs(W).max())
+
+
+@pytest.mark.parametrize("H", [32, 256])
+@pytest.mark.parametrize("n_tok", [1, 7, 300, 2049])
+@pytest.mark.parametrize("p", [0.0, 0.25])
+def test_lists_are_cut_at_n_tok_both_ways(H, n_tok, p):
+    """Offsets that pass n_tok, and some before 0: the lookup takes the mean over the tokens that remain, and the
+    gradient divides by as many."""
+    rng = np.random.default_rng(n_tok)
+    n, V = 700, 50
+    ptr = np.concatenate([[0], np.cumsum(rng.integers(0, 9, n))]).astype(np.int32) - 3
+    ptr[0] = -3
+    assert ptr[-1] > n_tok
+    tok = rng.integers(0, V, n_tok).astype(np.int32)
+    cut = np.clip(ptr, 0, n_tok)
+    table = round_to("f32", rng.standard_normal((V, H)))
+    X = torch.empty((n, H), device="cuda")
+    capi.ggnn_embed("f32", n, H, V, dev(table), ints(ptr), ints(tok), n_tok, 1.5, True, p, 3, 4, X)
+    want, mag, lens = R.embed(table, n, cut, tok, n_tok, 1.5, True, p, 3, 4)
+    R.within(host(X), want, (lens[:, None] + 4) * R.U * mag)
+    dX = round_to("f32", rng.standard_normal((n, H)))
+    got = torch.zeros((V, H), device="cuda")
+    embed_bwd(n, H, V, ptr, tok, n_tok, 1.5, True, p, 3, 4, dev(dX), got)
+    want, mag, cnt = R.embed_grad(dX, V, cut, tok, n_tok, 1.5, True, p, 3, 4)
+    R.within(host(got), want, (cnt[:, None] + 6) * R.U * mag)
