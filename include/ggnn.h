@@ -688,7 +688,7 @@ ggnn_status ggnn_embed(ggnn_dtype dt, int32_t n, int32_t H, int32_t V, const voi
                        const int32_t* tok, int32_t n_tok, float scale, int32_t mean, float p, uint64_t seed,
                        uint64_t offset, void* X, void* stream);
 
-/* Workspace bytes of ggnn_embed_bwd (0 for unsupported sizes or no tokens). */
+/* Workspace bytes of ggnn_embed_bwd (0 for unsupported sizes, no nodes or no tokens). */
 size_t ggnn_embed_bwd_workspace_bytes(int32_t n, int32_t H, int32_t V, int32_t n_tok);
 
 /* Reverse of ggnn_embed for the gradient dX of X (ggnn_backward's dL/dX_0):

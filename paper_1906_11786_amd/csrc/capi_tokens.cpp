@@ -129,7 +129,7 @@ ggnn_status ggnn_embed(ggnn_dtype dt, int32_t n, int32_t H, int32_t V, const voi
 }
 
 size_t ggnn_embed_bwd_workspace_bytes(int32_t n, int32_t H, int32_t V, int32_t n_tok) {
-  if (n < 0 || !supported_H(H) || V < 1 || n_tok < 0 || n_tok > kMaxTokens) return 0;
+  if (n <= 0 || !supported_H(H) || V < 1 || n_tok <= 0 || n_tok > kMaxTokens) return 0;
   return embed_bwd_workspace(H, n_tok);
 }
 

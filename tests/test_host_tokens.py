@@ -171,3 +171,10 @@ def test_vocab_workspace_grows_with_its_rows_and_entries(dt, H):
         for grad in (False, True):
             need = capi.ggnn_vocab_workspace_bytes(dt, H, rows, V, grad)
             assert 0 < need <= bound(rows, V, grad), (rows, V, grad, need, bound(rows, V, grad))
+
+
+def test_table_gradient_of_nothing_needs_no_workspace():
+    assert capi.ggnn_embed_bwd_workspace_bytes(10, 64, 20, 0) == 0
+    assert capi.ggnn_embed_bwd_workspace_bytes(0, 64, 20, 30) == 0
+    capi.ggnn_embed_bwd(10, 64, 20, Q, None, 0, 1.0, True, 0.0, 0, 0, P, S, None, 0, stream=0)
+    capi.ggnn_embed_bwd(0, 64, 20, Q, Q, 30, 1.0, True, 0.0, 0, 0, P, S, None, 0, stream=0)
