@@ -634,3 +634,51 @@ def test_lists_are_cut_at_n_tok_both_ways(H, n_tok, p):
     embed_bwd(n, H, V, ptr, tok, n_tok, 1.5, True, p, 3, 4, dev(dX), got)
     want, mag, cnt = R.embed_grad(dX, V, cut, tok, n_tok, 1.5, True, p, 3, 4)
     R.within(host(got), want, (cnt[:, None] + 6) * R.U * mag)
+
+
+def sparse_lists(kind, n, n_tok, V, rng):
+    """n_tok tokens on a few of n nodes: the first ones, the first and the last ones, or ones spread over all."""
+    lens = np.zeros(n, np.int64)
+    if kind == "spread":
+        lens[np.sort(rng.permutation(n)[:n_tok])] = 1
+    else:
+        half = n_tok if kind == "first" else n_tok // 2
+        lens[:half] = 1
+        lens[n - (n_tok - half):] += 1 if half < n_tok else 0
+    ptr = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    return ptr, rng.integers(0, V, n_tok).astype(np.int32)
+
+
+@pytest.mark.parametrize("kind", ["first", "ends", "spread"])
+@pytest.mark.parametrize("n,n_tok", [(300000, 3000), (300000, 5), (40000, 9000), (20000, 2048)])
+def test_table_gradient_of_few_lists_among_many_nodes(kind, n, n_tok):
+    say(f"embed_bwd {kind} n={n} n_tok={n_tok}")
+    ptr, tok = sparse_lists(kind, n, n_tok, 77, np.random.default_rng(n_tok))
+    check_embed_bwd(n, 32, 77, ptr, tok, n_tok, True, 0.1)
+
+
+@pytest.mark.parametrize("kind", ["first", "ends", "spread"])
+def test_table_gradient_takes_no_longer_for_nodes_without_tokens(kind):
+    """3,000 tokens among 1M nodes against the same tokens on 3,008 nodes: no workgroup passes over all rows by itself
+    (that took a barrier per 1,024 of them, hundreds of microseconds).  Medians of calls in turn."""
+    H, V, n_tok = 32, 997, 3000
+    rng = np.random.default_rng(3)
+    cases = []
+    for n, k in ((3008, "first"), (1 << 20, kind)):
+        ptr, tok = sparse_lists(k, n, n_tok, V, rng)
+        need = capi.ggnn_embed_bwd_workspace_bytes(n, H, V, n_tok)
+        cases.append((n, ints(ptr), ints(tok), torch.zeros((n, H), device="cuda"), torch.zeros((V, H), device="cuda"),
+                      scratch(need), need))
+    us = [[], []]
+    for i in range(40):
+        for c, (n, ptr, tok, dX, dT, ws, need) in enumerate(cases):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            for _ in range(4):
+                capi.ggnn_embed_bwd(n, H, V, ptr, tok, n_tok, 1.0, True, 0.0, 0, 0, dX, dT, ws, need)
+            b.record()
+            torch.cuda.synchronize()
+            us[c].append(a.elapsed_time(b) * 250)
+    few, many = np.median(us[0][10:]), np.median(us[1][10:])
+    say(f"  3,008 nodes {few:.1f} us, 1M nodes {many:.1f} us")
+    assert many <= 2 * few + 20
