@@ -19,16 +19,28 @@ from . import capi
 from .driver import BandedGGNN, torch_dtype
 
 
+MAX_TOKENS = 1 << 30   # listed tokens that the library takes
+
+
+def _ids32(ids) -> np.ndarray:
+    """Token ids as int32; those past 32 bits become -1, which names no token either."""
+    ids = np.asarray(ids, np.int64)
+    return np.where((ids < 0) | (ids >= 2**31), -1, ids).astype(np.int32)
+
+
 def token_lists(lists, n_pad: int):
     """(tok_ptr [n_pad + 1], tok) of one list of token ids per node, in the
     final labels; nodes beyond the lists have none."""
     if len(lists) > n_pad:
         raise ValueError(f"{len(lists)} token lists for {n_pad} nodes")
+    ends = np.cumsum([len(x) for x in lists], dtype=np.int64)
+    total = int(ends[-1]) if len(lists) else 0
+    if total > MAX_TOKENS:
+        raise ValueError(f"{total} listed tokens, at most 2^30 are taken")
     ptr = np.zeros(n_pad + 1, np.int32)
-    ptr[1:len(lists) + 1] = np.cumsum([len(x) for x in lists], dtype=np.int64)
-    ptr[len(lists) + 1:] = ptr[len(lists)]
-    tok = np.concatenate([np.asarray(x, np.int32) for x in lists]) if ptr[-1] else np.zeros(1, np.int32)
-    return ptr, tok.astype(np.int32)
+    ptr[1:len(lists) + 1] = ends
+    ptr[len(lists) + 1:] = total
+    return ptr, np.concatenate([_ids32(x) for x in lists]) if total else np.zeros(1, np.int32)
 
 
 class NodeTokens:
@@ -56,9 +68,11 @@ class NodeTokens:
         if len(tok_ptr) != n + 1 or tok_ptr[0] != 0 or np.any(np.diff(tok_ptr) < 0) or tok_ptr[-1] > len(tok):
             raise ValueError(f"tok_ptr must hold n_pad + 1 = {n + 1} offsets that start at 0, do not decrease and end "
                              "within the token list")
+        if tok_ptr[-1] > MAX_TOKENS:
+            raise ValueError(f"{tok_ptr[-1]} listed tokens, at most 2^30 are taken")
         self.n_tok = int(tok_ptr[-1])
         self.tok_ptr = torch.from_numpy(tok_ptr.astype(np.int32)).to(dev)
-        self.tok = torch.from_numpy(tok.astype(np.int32) if len(tok) else np.zeros(1, np.int32)).to(dev)
+        self.tok = torch.from_numpy(_ids32(tok) if len(tok) else np.zeros(1, np.int32)).to(dev)
         self.scale, self.mean, self.p_in, self.p_out, self.seed = scale, mean, p_in, p_out, seed
         # table and bias in one buffer, so that one fill clears their gradients and one launch updates both
         nb = -(-self.V // 64) * 64
@@ -107,6 +121,7 @@ class NodeTokens:
                 raise ValueError("one target per chosen node is needed")
             if len(target) and target.max() >= self.V:
                 raise ValueError(f"targets must lie below V={self.V} (negative: no loss)")
+            target = np.maximum(target, -1)
         return up(node), None if target is None else up(target)
 
     def _space(self, name: str, nbytes: int):

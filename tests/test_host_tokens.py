@@ -178,3 +178,41 @@ def test_table_gradient_of_nothing_needs_no_workspace():
     assert capi.ggnn_embed_bwd_workspace_bytes(0, 64, 20, 30) == 0
     capi.ggnn_embed_bwd(10, 64, 20, Q, None, 0, 1.0, True, 0.0, 0, 0, P, S, None, 0, stream=0)
     capi.ggnn_embed_bwd(0, 64, 20, Q, Q, 30, 1.0, True, 0.0, 0, 0, P, S, None, 0, stream=0)
+
+
+def node_tokens(n=4, H=32, V=20, **kw):
+    """NodeTokens on host buffers (nothing is launched)."""
+    import types
+    torch = pytest.importorskip("torch")
+    tokens = pytest.importorskip("paper_1906_11786_amd.tokens")
+    model = types.SimpleNamespace(comp=types.SimpleNamespace(n_pad=n), H=H, T=1, dt="f32", device="cpu",
+                                  X=torch.zeros((2, n, H)), master=torch.zeros((64,)))
+    a = dict(table=np.zeros((V, H)), tok_ptr=[0, 2, 5, 5, 6], tok=[1, 2, 3, 4, 5, 6])
+    a.update(kw)
+    return tokens.NodeTokens(model, **a)
+
+
+@pytest.mark.parametrize("wide", [2**32 + 5, 2**31 + 7, 2**40, -2**32 + 3, -2**63])
+def test_node_tokens_of_ids_past_32_bits_are_no_tokens(wide):
+    """An id outside the table adds nothing; its low 32 bits would name another token."""
+    t = node_tokens(tok=np.array([1, wide, 3, 4, 5, 6], np.int64))
+    got = t.tok.tolist()
+    assert got[0] == 1 and got[2:] == [3, 4, 5, 6] and not 0 <= got[1] < 20
+    tokens = pytest.importorskip("paper_1906_11786_amd.tokens")
+    _, tok = tokens.token_lists([np.array([3, wide], np.int64), [wide], [2]], 4)
+    assert tok.dtype == np.int32 and tok[[0, 3]].tolist() == [3, 2] and tok[1] == tok[2] and not 0 <= tok[1] < 2**31 - 1
+
+
+@pytest.mark.parametrize("target", [-2**32, -2**33 + 4, -2**63])
+def test_node_tokens_targets_below_32_bits_stay_negative(target):
+    t = node_tokens()
+    t.setup_training([0, 2], np.array([3, target], np.int64))
+    assert t.target[0].item() == 3 and t.target[1].item() < 0 and t.n_live == 1
+
+
+def test_node_tokens_counts_past_32_bits_are_refused():
+    tokens = pytest.importorskip("paper_1906_11786_amd.tokens")
+    with pytest.raises(ValueError, match="2\\^30"):
+        tokens.token_lists([range(1 << 30), range(5)], 4)
+    with pytest.raises(ValueError, match="2\\^30"):
+        tokens.token_lists([range(1 << 31), range(1 << 31), [1]], 4)
