@@ -81,6 +81,8 @@ class NodeTokens:
         self.bias = self.master[self.V * H:self.V * H + self.V]
         if bias is not None:
             bias = np.asarray(bias, np.float32)
+            if bias.shape != (self.V,):
+                raise ValueError(f"bias of shape {bias.shape}, ({self.V},) is needed")
             self.bias.copy_(torch.from_numpy(np.where(bias <= -1e30, np.float32(-np.inf), bias)))
         self.compute_copy = self.master.to(torch_dtype(dt)) if dt == "bf16" else None
         self.table = (self.master if self.compute_copy is None else self.compute_copy)[:self.V * H].view(self.V, H)

@@ -216,3 +216,10 @@ def test_node_tokens_counts_past_32_bits_are_refused():
         tokens.token_lists([range(1 << 30), range(5)], 4)
     with pytest.raises(ValueError, match="2\\^30"):
         tokens.token_lists([range(1 << 31), range(1 << 31), [1]], 4)
+
+
+@pytest.mark.parametrize("bias", [0.5, [0.5], np.zeros(19), np.zeros(21), np.zeros((20, 1)), np.zeros((2, 20))])
+def test_node_tokens_bias_of_another_shape_is_refused(bias):
+    with pytest.raises(ValueError, match="bias"):
+        node_tokens(bias=bias)
+    assert node_tokens(bias=np.arange(20.0)).bias.tolist() == list(range(20))
