@@ -682,3 +682,53 @@ def test_table_gradient_takes_no_longer_for_nodes_without_tokens(kind):
     few, many = np.median(us[0][10:]), np.median(us[1][10:])
     say(f"  3,008 nodes {few:.1f} us, 1M nodes {many:.1f} us")
     assert many <= 2 * few + 20
+
+
+@pytest.mark.parametrize("V,p", [(70001, 0.1), (501, 0.0)])
+def test_table_gradient_of_many_lists(V, p):
+    """Above 524,288 listings (the scan of the tiles' counts takes more than one turn) in lists with long stretches of
+    empty ones; three digits of token numbers, and two."""
+    say(f"embed_bwd many lists V={V}")
+    rng = np.random.default_rng(V)
+    n = 400000
+    lens = rng.integers(0, 6, n)
+    lens[rng.random(n) < 0.2] = 0
+    for at, size in ((0, 3000), (100000, 40000), (200000, 900), (n - 5000, 5000)):
+        lens[at:at + size] = 0
+    ptr = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    assert ptr[-1] > 524288
+    tok = np.minimum((V ** rng.random(int(ptr[-1]))).astype(np.int64) - 1, V - 1).astype(np.int32)
+    tok[rng.random(len(tok)) < 0.01] = V
+    check_embed_bwd(n, 32, V, ptr, tok, int(ptr[-1]), True, p)
+
+
+@pytest.mark.parametrize("dt,H,rows,V", [("bf16", 64, 300, 901), ("f32", 64, 300, 901), ("bf16", 256, 33100, 300),
+                                         ("bf16", 256, 300, 33100), ("f32", 128, 300, 33100), ("bf16", 256, 33100, 4900)])
+def test_vocab_gradients_without_the_biases_gradient(dt, H, rows, V):
+    """dbias NULL, in every deal of the columns pass: what else is written has the same bits as with it."""
+    rng = np.random.default_rng(rows)
+    X, W, node, target, b = vocab_case(rng, dt, rows + 20, H, V, rows, bias=True)
+    want = run_vocab(dt, X, W, b, node, target, scale=0.25)
+    n = rows + 20
+    dX, dW = torch.full((n, H), 5.0, device="cuda"), torch.ones((V, H), device="cuda")
+    loss, lse = torch.empty((rows,), device="cuda"), torch.empty((rows,), device="cuda")
+    need = capi.ggnn_vocab_workspace_bytes(dt, H, rows, V, True)
+    capi.ggnn_vocab_loss_grad(dt, n, H, rows, V, dev(X, dt), dev(W, dt), dev(b), ints(node), ints(target), None, 0.25,
+                              loss, lse, dX, dW, None, scratch(need), need)
+    for got, k in ((loss, "loss"), (lse, "lse"), (dX, "dX"), (dW, "dW")):
+        assert np.array_equal(host(got) - (1.0 if k == "dW" else 0.0), want[k]), k
+
+
+@pytest.mark.parametrize("dt,H", [("bf16", 256), ("f32", 256), ("bf16", 128)])
+def test_vocab_best_entry_where_a_workgroup_has_several_runs(dt, H):
+    """More 128-tiles of rows than workgroups; small whole numbers, so that every logit is exact and many are equal."""
+    rng = np.random.default_rng(14)
+    rows, V = (256 if H == 256 else 768) * 128 + 300, 301
+    X = rng.integers(-1, 2, (rows, H)).astype(np.float64)
+    W = rng.integers(-1, 2, (V, H)).astype(np.float64)
+    W[V // 2:] = W[:V - V // 2]
+    b = rng.integers(-3, 4, V).astype(np.float64)
+    b[V // 2:] = b[:V - V // 2]
+    b[rng.random(V) < 0.3] = -np.inf
+    o = run_vocab(dt, X, W, b, None, np.zeros(rows, np.int32), grad=False, best=True)
+    assert np.array_equal(o["best"], np.argmax(X.astype(np.float32) @ W.T.astype(np.float32) + b, 1))
