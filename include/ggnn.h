@@ -733,7 +733,8 @@ ggnn_status ggnn_vocab_loss(ggnn_dtype dt, int32_t n_nodes, int32_t H, int32_t n
  *   dz_v = scale * weight[r] * (exp(z_v - lse[r]) - [v = target[r]])
  *   dX   [n_nodes][H] float (written whole: sum_v dz_v W[v] on the row of each
  *        chosen node, zero elsewhere) -- the dL/dX_T that ggnn_backward takes.  A
- *        node may be chosen once (otherwise its row holds one of the contributions).
+ *        node may be chosen once (otherwise each value of its row is one of the
+ *        contributions, not necessarily all of the same one).
  *   dW   [V][H] float += sum_r dz_v X[node[r]];  dbias [V] float += sum_r dz_v, or NULL
  *   weight [n_rows] float, or NULL for 1
  * dW and dbias take exp(z_v - lse[r]) from the rounded lse: the relative error of

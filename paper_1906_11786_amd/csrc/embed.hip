@@ -67,6 +67,9 @@ __global__ __launch_bounds__(kEmbThreads) void embed_rows_kernel(int n, int V, c
 
 // Lists: four tokens of a list in flight, added in list order.  4.8 us for 20,000
 // lists of 0 to 6 at H = 64 in bf16: the launch and three dependent loads.
+// 1,047,000 of them over 50,021 tokens: 74 us at H = 64 (0.40 GB of table rows
+// gathered, 0.13 written), 273 us at H = 256 (1.6 and 0.54): the gathers, 7.9 TB/s
+// with the states written.
 template <typename S, int H, bool DROP>
 __global__ __launch_bounds__(kEmbThreads) void embed_lists_kernel(int n, int V, const S* __restrict__ table,
                                                                   const int32_t* __restrict__ tok_ptr,
@@ -154,8 +157,8 @@ namespace dev {
 // Least significant digit first.  A pass is a count of each tile's digits, a
 // scan of the counts over the tiles of each digit, and a placement that ranks
 // a tile's items in order.  Items of tokens outside [0, V) sort to the end.
-// 2.1 M tokens (8 bytes an item) of 50,021, two passes: count 15.5 and 9.8 us, scan
-// 5.1, placement 17; 59,900 of 10,007: count 5.7 and 4.6, placement 6.7, which is
+// 2.1 M tokens (8 bytes an item) of 50,021, two passes: count 15.6 and 10.1 us, scan
+// 5.2, placement 16.5; 59,900 of 10,007: count 5.9 and 4.3, placement 6.8, which is
 // the latency of a launch and a few dependent loads.
 
 constexpr int kSortThreads = 256, kSortWaves = kSortThreads / kWave;
@@ -420,7 +423,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(int n_tok, con
 // in block order.
 //
 // Bound by the gathered rows: 2.1 M of 1 KB (1.05 M rows, each read for every
-// listing of it) in 435 us, 4.9 TB/s.  59,900 rows of 256 bytes: 9 us.
+// listing of it) in 437 us, 4.9 TB/s.  59,900 rows of 256 bytes: 9 us.
 
 // One row of the gradient += acc.
 __device__ __forceinline__ void add_row(float* __restrict__ o, const float (&acc)[8]) {

@@ -27,15 +27,16 @@
 // are float32.
 //
 // What bounds them: at H = 256 the matrix cores.  60,001 rows over 50,021 entries
-// in bf16: rows pass 3,730 us, columns pass 4,000, 1.24 and 1.15 PFLOP/s, where a
+// in bf16: rows pass 3,740 us, columns pass 3,900, 1.23 and 1.18 PFLOP/s, where a
 // plain 8,192^3 product of the library runs at 1.32.  At H = 64 a step has a
-// quarter of the products for the same 16 exponentials a lane, whose vector
-// instructions take longer than the products: 3,001 rows over 10,007 entries
-// 22.4 and 23.1 us (0.51 PFLOP/s), then 8.2 and 6.9 us to add up the shares (25 and
-// 23 MB, at memory speed).  Loss alone at H = 128, 2,999 rows over 50,021 entries:
-// 53 us, 0.72 PFLOP/s, exponentials again.  float32 at H = 128, 1,229 rows over
-// 4,999 entries: 28.8 and 27.7 us (0.65 PFLOP/s of bf16 products: 250 workgroups
-// of 4 waves, one per SIMD, and a run of 6 to 7 tiles).
+// quarter of the products for the same 16 exponentials a lane, and no unit is full
+// (vector issue 53% and 46%, matrix cores 32% and 30%, waiting 37% and 34%): 3,001 rows over
+// 10,007 entries 22.8 and 23.2 us (0.51 PFLOP/s), then 8.5 and 6.9 us to add up the
+// shares (25 and 23 MB, at memory speed).  Loss alone at H = 128, 2,999 rows over
+// 50,021 entries: 53 us, 0.72 PFLOP/s (vector issue 57%, matrix cores 40%, waiting
+// 44%); with the best entry 70.  float32 at H = 128, 1,229 rows over 4,999 entries:
+// 28.7 and 27.9 us (0.65 PFLOP/s of bf16 products, matrix cores 40% busy: 250
+// workgroups of 4 waves, one per SIMD, a wait for the copies every 32 entries).
 #include <type_traits>
 
 #include "device_common.h"
@@ -1060,6 +1061,8 @@ dev::Deal make_deal(int tiles128, int tiles, int workers) {
 // second: H = 64, 12,001 x 20,011 259 / 272 us, 30,001 x 50,021 1,262 / 1,251; H =
 // 128, 8,001 x 30,011 376 / 392, 16,001 x 30,011 701 / 707; H = 256, 3,001 x 10,007
 // 143 / 159, 6,001 x 20,011 414 / 401, 16,001 x 50,021 2,267 / 2,102.
+// The rule puts all of these on their faster side but 30,001 x 50,021 at H = 64 and
+// 16,001 x 30,011 at H = 128, where both forms are within 1%.
 // In float32 all parts of p - 1 are kept, without a product more.
 bool targets_sorted(int es, int H, int R, int V) { return es == 2 && (double)R * V * H * H > 6.5e12; }
 
