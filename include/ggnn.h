@@ -47,7 +47,7 @@
 extern "C" {
 #endif
 
-#define GGNN_ABI_VERSION 13
+#define GGNN_ABI_VERSION 14
 
 typedef enum {
   GGNN_OK = 0,
@@ -747,6 +747,54 @@ ggnn_status ggnn_vocab_loss_grad(ggnn_dtype dt, int32_t n_nodes, int32_t H, int3
                                  const void* W, const float* bias, const int32_t* node, const int32_t* target,
                                  const float* weight, float scale, float* loss, float* lse, float* dX, float* dW,
                                  float* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Workspace bytes of ggnn_vocab_distill (grad = 0) or ggnn_vocab_distill_grad
+ * (grad != 0); 0 for unsupported sizes or no rows. */
+size_t ggnn_vocab_distill_workspace_bytes(ggnn_dtype dt, int32_t H, int32_t n_rows, int32_t V, int32_t K, int32_t grad);
+
+/* Distillation of chosen nodes from a teacher's top logits (device): row r has a
+ * list of up to K entries v with the teacher's logits, and with z as in
+ * ggnn_vocab_loss and t = temperature
+ *   q_k = exp(teacher_logit[r][k] / t - T);  lse[r] = log sum_v exp(z_v / t)
+ *   loss[r] = sum_k q_k (log q_k - z_{teacher_id[r][k]} / t + lse[r])
+ * T is the log sum of the row's own list (the q_k of a row then add up to 1), or
+ * teacher_lse[r], the teacher's log sum over its whole vocabulary at this
+ * temperature (they add up to the list's share of it).
+ *   K        entries of a list, 1 .. 64;  n_rows * K <= 2^30
+ *   teacher_id     [n_rows][K] int32; a negative one: no entry (any of a row's may
+ *            be).  One listed twice counts twice.  At or above V: loss NaN, no gradient.
+ *   teacher_logit  [n_rows][K] float, not read where there is no entry; -inf: q_k = 0;
+ *            a NaN or +inf one: loss NaN, no gradient
+ *   teacher_lse    [n_rows] float, or NULL.  One that is not finite: loss NaN, no
+ *            gradient (not read into a row without entries).
+ *   temperature    in [0.001, 1000]
+ *   loss, lse      [n_rows] float (written).  A row without entries, or whose
+ *            entries all have -inf, has no loss (0) and no gradient, whatever its
+ *            state and weight hold.  An entry of the vocabulary that its bias takes
+ *            out and that the list has with q_k > 0 makes the loss +inf.
+ * The other arguments, and nodes outside the graph, as in ggnn_vocab_loss. */
+ggnn_status ggnn_vocab_distill(ggnn_dtype dt, int32_t n_nodes, int32_t H, int32_t n_rows, int32_t V, const void* X,
+                               const void* W, const float* bias, const int32_t* node, int32_t K,
+                               const int32_t* teacher_id, const float* teacher_logit, const float* teacher_lse,
+                               float temperature, float* loss, float* lse, void* workspace, size_t workspace_bytes,
+                               void* stream);
+
+/* The same losses with the gradients of scale * sum_r weight[r] * loss[r] (a loss
+ * that is to weigh as much at every temperature takes t^2 into scale):
+ *   dz_v = scale * weight[r] / t * (s exp(z_v / t - lse[r]) - sum of the q_k with teacher_id[r][k] = v),
+ *   s = sum_k q_k
+ *   add      0: dX is written whole, as by ggnn_vocab_loss_grad; otherwise the
+ *            gradient is added to the rows of the chosen nodes and the others stay
+ *            as they are (after ggnn_vocab_loss_grad on the same nodes: both losses)
+ *   dX, dW, dbias, weight   as in ggnn_vocab_loss_grad
+ * The lists' share of dW and dbias is added in list order over the entries sorted
+ * by v: same inputs, same bits. */
+ggnn_status ggnn_vocab_distill_grad(ggnn_dtype dt, int32_t n_nodes, int32_t H, int32_t n_rows, int32_t V,
+                                    const void* X, const void* W, const float* bias, const int32_t* node, int32_t K,
+                                    const int32_t* teacher_id, const float* teacher_logit, const float* teacher_lse,
+                                    float temperature, const float* weight, float scale, int32_t add, float* loss,
+                                    float* lse, float* dX, float* dW, float* dbias, void* workspace,
+                                    size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

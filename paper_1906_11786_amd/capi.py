@@ -44,6 +44,7 @@ EXPORTS = [
     "ggnn_readout_loss_bwd_noalloc",
     "ggnn_dropout", "ggnn_embed", "ggnn_embed_bwd_workspace_bytes", "ggnn_embed_bwd",
     "ggnn_vocab_workspace_bytes", "ggnn_vocab_loss", "ggnn_vocab_loss_grad",
+    "ggnn_vocab_distill_workspace_bytes", "ggnn_vocab_distill", "ggnn_vocab_distill_grad",
 ]
 
 
@@ -140,6 +141,11 @@ _SIGS = {
     "ggnn_vocab_loss": (C.c_int, [C.c_int, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
     "ggnn_vocab_loss_grad": (C.c_int, [C.c_int, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, f32, vp, vp, vp, vp, vp,
                                        vp, sz, vp]),
+    "ggnn_vocab_distill_workspace_bytes": (sz, [C.c_int, i32, i32, i32, i32, i32]),
+    "ggnn_vocab_distill": (C.c_int, [C.c_int, i32, i32, i32, i32, vp, vp, vp, vp, i32, vp, vp, vp, f32, vp, vp, vp, sz,
+                                     vp]),
+    "ggnn_vocab_distill_grad": (C.c_int, [C.c_int, i32, i32, i32, i32, vp, vp, vp, vp, i32, vp, vp, vp, f32, vp, f32,
+                                          i32, vp, vp, vp, vp, vp, vp, sz, vp]),
 }
 
 
@@ -194,7 +200,7 @@ def _i32(a) -> np.ndarray:
 
 # Interface version this binding is written against (GGNN_ABI_VERSION of
 # include/ggnn.h); the library must report the same number.
-ABI_VERSION = 13
+ABI_VERSION = 14
 
 
 def ggnn_abi_version() -> int:
@@ -478,6 +484,27 @@ def ggnn_vocab_loss_grad(dt, n_nodes, H, n_rows, V, X, W, bias, node, target, we
     _check("ggnn_vocab_loss_grad", lib().ggnn_vocab_loss_grad(
         _dt(dt), n_nodes, H, n_rows, V, _ptr(X), _ptr(W), _ptr(bias), _ptr(node), _ptr(target), _ptr(weight), scale,
         _ptr(loss), _ptr(lse), _ptr(dX), _ptr(dW), _ptr(dbias), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def ggnn_vocab_distill_workspace_bytes(dt, H, n_rows, V, K, grad) -> int:
+    return int(lib().ggnn_vocab_distill_workspace_bytes(_dt(dt), H, n_rows, V, K, 1 if grad else 0))
+
+
+def ggnn_vocab_distill(dt, n_nodes, H, n_rows, V, X, W, bias, node, K, teacher_id, teacher_logit, teacher_lse,
+                       temperature, loss, lse, workspace, workspace_bytes, stream=None):
+    _check("ggnn_vocab_distill", lib().ggnn_vocab_distill(
+        _dt(dt), n_nodes, H, n_rows, V, _ptr(X), _ptr(W), _ptr(bias), _ptr(node), K, _ptr(teacher_id),
+        _ptr(teacher_logit), _ptr(teacher_lse), temperature, _ptr(loss), _ptr(lse), _ptr(workspace), workspace_bytes,
+        _stream(stream)))
+
+
+def ggnn_vocab_distill_grad(dt, n_nodes, H, n_rows, V, X, W, bias, node, K, teacher_id, teacher_logit, teacher_lse,
+                            temperature, weight, scale, add, loss, lse, dX, dW, dbias, workspace, workspace_bytes,
+                            stream=None):
+    _check("ggnn_vocab_distill_grad", lib().ggnn_vocab_distill_grad(
+        _dt(dt), n_nodes, H, n_rows, V, _ptr(X), _ptr(W), _ptr(bias), _ptr(node), K, _ptr(teacher_id),
+        _ptr(teacher_logit), _ptr(teacher_lse), temperature, _ptr(weight), scale, 1 if add else 0, _ptr(loss),
+        _ptr(lse), _ptr(dX), _ptr(dW), _ptr(dbias), _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
 # ------------------------------------------------ evaluation on every edge

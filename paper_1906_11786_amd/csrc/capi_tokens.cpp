@@ -1,6 +1,7 @@
 // C-ABI entry points of the token operators: dropout, node states from a token
-// table and its gradient, the cross entropy over a vocabulary.  Arguments are
-// checked on the host, then the kernels are launched on the caller's stream.
+// table and its gradient, the cross entropy over a vocabulary, distillation from
+// a teacher's lists.  Arguments are checked on the host, then the kernels are
+// launched on the caller's stream.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -85,6 +86,61 @@ ggnn_status check_vocab(int32_t dt, int32_t n_nodes, int32_t H, int32_t n_rows, 
   CHECK_OPT_PTR(node, "node");
   CHECK_OPT_PTR(target, "target");
   if (n_rows > 0) CHECK_PTR(lse, "lse");
+  return GGNN_OK;
+}
+
+// What the losses over a vocabulary share of their arguments.
+VocabArgs vocab_args(int32_t n_nodes, int32_t n_rows, int32_t V, const void* X, const void* W, const float* bias,
+                     const int32_t* node, float* loss, float* lse, void* workspace) {
+  VocabArgs c{};
+  c.n_nodes = n_nodes; c.R = n_rows; c.V = V;
+  c.X = X; c.W = W; c.bias = bias; c.node = node;
+  c.scale = 1.f;
+  c.loss = loss; c.lse = lse;
+  c.ws = workspace;
+  return c;
+}
+
+ggnn_status check_gradients(int32_t dt, int32_t n_nodes, int32_t H, int32_t V, const void* X, const void* W,
+                            const float* weight, float scale, const float* dX, const float* dW, const float* dbias) {
+  GGNN_CHECK_ARG(std::isfinite(scale), "scale must be finite");
+  CHECK_PTR(dX, "dX");
+  CHECK_PTR(dW, "dW");
+  CHECK_OPT_PTR(dbias, "dbias");
+  CHECK_OPT_PTR(weight, "weight");
+  const size_t es = dtype_bytes(dt), nx = (size_t)n_nodes * H, nw = (size_t)V * H;
+  GGNN_CHECK_ARG(disjoint(dX, nx * 4, X, nx * es) && disjoint(dX, nx * 4, W, nw * es), "dX overlaps X or W");
+  GGNN_CHECK_ARG(disjoint(dW, nw * 4, W, nw * es) && disjoint(dW, nw * 4, X, nx * es) &&
+                     disjoint(dW, nw * 4, dX, nx * 4),
+                 "dW overlaps W, X or dX");
+  return GGNN_OK;
+}
+
+constexpr int32_t kMaxList = 64;                              // entries of a row's list
+constexpr float kMinTemperature = 1e-3f, kMaxTemperature = 1e3f;
+
+ggnn_status check_temperature(float t) {
+  GGNN_CHECK_ARG(t >= kMinTemperature && t <= kMaxTemperature, "temperature=%g must be in [0.001, 1000]", (double)t);
+  return GGNN_OK;
+}
+
+bool distill_sizes(int32_t dt, int32_t H, int32_t n_rows, int32_t V, int32_t K) {
+  return supported_dtype(dt) && supported_H(H) && n_rows > 0 && n_rows <= kMaxRows && V >= 1 &&
+         (int64_t)V * H < ((int64_t)1 << 31) && K >= 1 && K <= kMaxList && (int64_t)n_rows * K <= kMaxTokens;
+}
+
+ggnn_status check_distill(int32_t n_rows, int32_t K, const int32_t* t_id, const float* t_logit, const float* t_lse,
+                          float temperature, const float* loss) {
+  GGNN_CHECK_ARG(K >= 1 && K <= kMaxList, "K=%d must be in [1, %d]", K, kMaxList);
+  GGNN_CHECK_ARG((int64_t)n_rows * K <= kMaxTokens, "n_rows*K exceeds 2^30 listings");
+  const ggnn_status st = check_temperature(temperature);
+  if (st != GGNN_OK) return st;
+  if (n_rows > 0) {
+    CHECK_PTR(t_id, "teacher_id");
+    CHECK_PTR(t_logit, "teacher_logit");
+    CHECK_PTR(loss, "loss");
+  }
+  CHECK_OPT_PTR(t_lse, "teacher_lse");
   return GGNN_OK;
 }
 
@@ -221,6 +277,58 @@ ggnn_status ggnn_vocab_loss_grad(ggnn_dtype dt, int32_t n_nodes, int32_t H, int3
   c.dX = dX; c.dW = dW; c.dbias = dbias;
   c.ws = workspace;
   return device_status(launch_vocab(dt, H, c, true, as_stream(stream)), "vocab_loss_grad");
+}
+
+size_t ggnn_vocab_distill_workspace_bytes(ggnn_dtype dt, int32_t H, int32_t n_rows, int32_t V, int32_t K,
+                                          int32_t grad) {
+  if (!distill_sizes(dt, H, n_rows, V, K)) return 0;
+  return vocab_workspace(dt, H, n_rows, V, grad != 0, K);
+}
+
+ggnn_status ggnn_vocab_distill(ggnn_dtype dt, int32_t n_nodes, int32_t H, int32_t n_rows, int32_t V, const void* X,
+                               const void* W, const float* bias, const int32_t* node, int32_t K,
+                               const int32_t* teacher_id, const float* teacher_logit, const float* teacher_lse,
+                               float temperature, float* loss, float* lse, void* workspace, size_t workspace_bytes,
+                               void* stream) {
+  clear_error();
+  ggnn_status st = check_vocab(dt, n_nodes, H, n_rows, V, X, W, bias, node, nullptr, lse);
+  if (st == GGNN_OK) st = check_distill(n_rows, K, teacher_id, teacher_logit, teacher_lse, temperature, loss);
+  if (st != GGNN_OK) return st;
+  if (n_rows == 0) return GGNN_OK;
+  const size_t need = vocab_workspace(dt, H, n_rows, V, false, K);
+  if (workspace == nullptr || workspace_bytes < need || !aligned16(workspace))
+    return fail(GGNN_ERR_WORKSPACE, "vocab_distill needs a 16-byte aligned workspace of %zu bytes (got %zu)", need,
+                workspace ? workspace_bytes : (size_t)0);
+  VocabArgs c = vocab_args(n_nodes, n_rows, V, X, W, bias, node, loss, lse, workspace);
+  c.temper = make_temper(temperature);
+  c.K = K; c.t_id = teacher_id; c.t_logit = teacher_logit; c.t_lse = teacher_lse;
+  return device_status(launch_vocab(dt, H, c, false, as_stream(stream)), "vocab_distill");
+}
+
+ggnn_status ggnn_vocab_distill_grad(ggnn_dtype dt, int32_t n_nodes, int32_t H, int32_t n_rows, int32_t V,
+                                    const void* X, const void* W, const float* bias, const int32_t* node, int32_t K,
+                                    const int32_t* teacher_id, const float* teacher_logit, const float* teacher_lse,
+                                    float temperature, const float* weight, float scale, int32_t add, float* loss,
+                                    float* lse, float* dX, float* dW, float* dbias, void* workspace,
+                                    size_t workspace_bytes, void* stream) {
+  clear_error();
+  ggnn_status st = check_vocab(dt, n_nodes, H, n_rows, V, X, W, bias, node, nullptr, lse);
+  if (st == GGNN_OK) st = check_distill(n_rows, K, teacher_id, teacher_logit, teacher_lse, temperature, loss);
+  if (st == GGNN_OK) st = check_gradients(dt, n_nodes, H, V, X, W, weight, scale, dX, dW, dbias);
+  if (st != GGNN_OK) return st;
+  if (n_rows == 0)
+    return add != 0 ? GGNN_OK
+                    : device_status(launch_fill_zero(dX, (size_t)n_nodes * H, as_stream(stream)), "vocab_distill_grad");
+  const size_t need = vocab_workspace(dt, H, n_rows, V, true, K);
+  if (workspace == nullptr || workspace_bytes < need || !aligned16(workspace))
+    return fail(GGNN_ERR_WORKSPACE, "vocab_distill_grad needs a 16-byte aligned workspace of %zu bytes (got %zu)", need,
+                workspace ? workspace_bytes : (size_t)0);
+  VocabArgs c = vocab_args(n_nodes, n_rows, V, X, W, bias, node, loss, lse, workspace);
+  c.temper = make_temper(temperature);
+  c.K = K; c.t_id = teacher_id; c.t_logit = teacher_logit; c.t_lse = teacher_lse;
+  c.weight = weight; c.scale = scale; c.add = add != 0;
+  c.dX = dX; c.dW = dW; c.dbias = dbias;
+  return device_status(launch_vocab(dt, H, c, true, as_stream(stream)), "vocab_distill_grad");
 }
 
 }  // extern "C"

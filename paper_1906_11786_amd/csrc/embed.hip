@@ -434,21 +434,37 @@ __device__ __forceinline__ void add_row(float* __restrict__ o, const float (&acc
   store8f(o, v);
 }
 
+// Lists of K ids a row (LIST): listing l is summed from row node[l / K] (l / K where
+// node is NULL) with factor[l], and dbias (NULL: none), one value a token, takes the
+// sum of the factors.
+struct ListRows {
+  int K;
+  const int32_t* node;
+  float* dbias;
+  float* part;   // shares of dbias, two a block as those of the rows
+};
+
 // S: type of the summed rows.  Row r's factor is scale (over the length of its list
 // for the mean, cut at the list's ends as the lookup cuts it), or -factor[r] where
 // factor is given.
-template <typename S, int H, bool DROP>
+template <typename S, int H, bool DROP, bool LIST = false>
 __global__ __launch_bounds__(kEmbThreads) void embed_runs_kernel(int n_tok, int n, int V, int chunk,
                                                                  const u32x2* __restrict__ items,
                                                                  const int32_t* __restrict__ tok_ptr, float scale,
                                                                  int mean, const float* __restrict__ factor, Dropout d,
                                                                  const S* __restrict__ dX,
                                                                  float* __restrict__ dtable,
-                                                                 float* __restrict__ part) {
+                                                                 float* __restrict__ part, ListRows list) {
   constexpr int L = H / 8, G = kEmbThreads / L, U = 4;
   __shared__ __attribute__((aligned(16))) float head[G][H];   // share of a run that began before the chunk
   __shared__ uint32_t hkey[G];    // its token; V: none
   __shared__ int hfull[G];        // whether it also leaves the chunk
+  __shared__ float hbias[LIST ? G : 1];
+  float accb = 0.f;
+  const bool bias = LIST && list.dbias != nullptr;
+  auto add_bias = [&](uint32_t token) {   // by one lane of a token's group
+    if (bias && threadIdx.x % L == 0) list.dbias[token] += accb;
+  };
   const int grp = threadIdx.x / L, h = 8 * (threadIdx.x % L);
   const long lo = ((long)blockIdx.x * G + grp) * chunk;
   const uint32_t none = (uint32_t)V;
@@ -475,12 +491,17 @@ __global__ __launch_bounds__(kEmbThreads) void embed_runs_kernel(int n_tok, int 
       float v[U][8], w[U][8], f[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int row = min((int)it[u].y, n - 1);
         const bool ok = it[u].x < none && k + u < k1;
+        int row = min((int)it[u].y, n - 1);
+        if constexpr (LIST) {
+          row = (int)it[u].y / list.K;
+          if (ok && list.node != nullptr) row = list.node[row];
+        }
         f[u] = scale;
         if (ok) {
           load8f<S>(dX + (size_t)row * H + h, v[u]);
-          if (factor != nullptr) f[u] = -factor[row];
+          if constexpr (LIST) f[u] = factor[it[u].y];
+          else if (factor != nullptr) f[u] = -factor[row];
           if (tok_ptr != nullptr && mean) {
             const int b = clampi(tok_ptr[row], 0, n_tok), e = clampi(tok_ptr[row + 1], b, n_tok);
             f[u] = scale / (float)max(e - b, 1);
@@ -496,14 +517,17 @@ __global__ __launch_bounds__(kEmbThreads) void embed_runs_kernel(int n_tok, int 
             if (before) {
               store8f(&head[grp][h], acc);
               if (lead) hkey[grp] = cur;
+              if (LIST && lead) hbias[grp] = accb;
             } else {
 #pragma unroll
               for (int i = 0; i < 8; ++i) old[i] += acc[i];
               store8f(dtable + (size_t)cur * H + h, old);
+              add_bias(cur);
             }
           }
           cur = it[u].x;
           before = false;
+          accb = 0.f;
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             acc[i] = 0.f;
@@ -514,6 +538,7 @@ __global__ __launch_bounds__(kEmbThreads) void embed_runs_kernel(int n_tok, int 
           if constexpr (DROP) drop8(v[u], ((uint64_t)it[u].y * H + h) / 8, d);
 #pragma unroll
           for (int i = 0; i < 8; ++i) acc[i] += f[u] * v[u][i];
+          if constexpr (LIST) accb += f[u];
         }
       }
     }
@@ -523,11 +548,13 @@ __global__ __launch_bounds__(kEmbThreads) void embed_runs_kernel(int n_tok, int 
 #pragma unroll
         for (int i = 0; i < 8; ++i) old[i] += acc[i];
         store8f(dtable + (size_t)cur * H + h, old);
+        add_bias(cur);
       } else if (before && grp > 0) {
         store8f(&head[grp][h], acc);
         if (lead) {
           hkey[grp] = cur;
           hfull[grp] = after;
+          if (LIST) hbias[grp] = accb;
         }
       }
     }
@@ -550,18 +577,26 @@ __global__ __launch_bounds__(kEmbThreads) void embed_runs_kernel(int n_tok, int 
         if (!after || j + u >= G) break;
 #pragma unroll
         for (int i = 0; i < 8; ++i) acc[i] += v[u][i];
+        if constexpr (LIST) accb += hbias[j + u];
         after = full[u] != 0;
       }
     }
-    if (before || after) store8f(part + ((size_t)2 * blockIdx.x + (before ? 0 : 1)) * H + h, acc);
-    else add_row(dtable + (size_t)cur * H + h, acc);
+    if (before || after) {
+      store8f(part + ((size_t)2 * blockIdx.x + (before ? 0 : 1)) * H + h, acc);
+      if (LIST && lead) list.part[(size_t)2 * blockIdx.x + (before ? 0 : 1)] = accb;
+    } else {
+      add_row(dtable + (size_t)cur * H + h, acc);
+      add_bias(cur);
+    }
   } else if (before && !after && grp == 0) {   // the chunk is all one run that ends with it
     store8f(part + (size_t)2 * blockIdx.x * H + h, acc);
+    if (LIST && lead) list.part[(size_t)2 * blockIdx.x] = accb;
   }
   if (grp == 0 && hkey[0] < none) {
     float v[8];
     load8f<float>(&head[0][h], v);
     store8f(part + (size_t)2 * blockIdx.x * H + h, v);
+    if (LIST && lead) list.part[(size_t)2 * blockIdx.x] = hbias[0];
   }
 }
 
@@ -573,13 +608,14 @@ __global__ __launch_bounds__(kEmbThreads) void embed_runs_kernel(int n_tok, int 
 // 256.
 constexpr int kJoinThreads = 1024, kJoinBlocks = 16, kJoinShort = 16;
 
-template <int H>
+template <int H, bool LIST = false>
 __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(int n_tok, int V, int block, int blocks,
                                                                   const u32x2* __restrict__ items,
                                                                   const float* __restrict__ part,
-                                                                  float* __restrict__ dtable) {
+                                                                  float* __restrict__ dtable, ListRows list) {
   constexpr int L = H / 8, G = kJoinThreads / L;
   __shared__ __attribute__((aligned(16))) float share[G][H];
+  __shared__ float bshare[LIST ? G : 1];
   __shared__ int is_long[kJoinBlocks];
   const int grp = threadIdx.x / L, h = 8 * (threadIdx.x % L);
   const int b0 = blockIdx.x * kJoinBlocks;
@@ -601,14 +637,16 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(int n_tok, int
     constexpr int U = 6;   // blocks' keys and shares in flight
     float acc[8];
     load8f<float>(part + ((size_t)2 * b + 1) * H + h, acc);
+    float accb = LIST ? list.part[(size_t)2 * b + 1] : 0.f;
     bool open = true;
     for (long j = b + 1; open; j += U) {
-      float w[U][8];
+      float w[U][8], wb[U];
       uint32_t k[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const long ju = min(j + u, (long)blocks - 1);
         k[u] = j + u < blocks ? first(ju) : ~0u;
+        wb[u] = LIST ? list.part[(size_t)2 * ju] : 0.f;
         load8f<float>(part + (size_t)2 * ju * H + h, w[u]);   // not of this run where the key differs: unused
       }
 #pragma unroll
@@ -617,10 +655,12 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(int n_tok, int
         if (open) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) acc[i] += w[u][i];
+          if constexpr (LIST) accb += wb[u];
         }
       }
     }
     add_row(dtable + (size_t)key * H + h, acc);
+    if (LIST && list.dbias != nullptr && h == 0) list.dbias[key] += accb;
   }
   if (blockIdx.y == 0) return;
   __syncthreads();
@@ -637,14 +677,18 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(int n_tok, int
       len = min(step, blocks - lo);
     }
     float acc[8] = {}, v[8];
+    float accb = 0.f;
     if (grp == 0) load8f<float>(part + ((size_t)2 * b + 1) * H + h, acc);
+    if (LIST && grp == 0) accb = list.part[(size_t)2 * b + 1];
 #pragma unroll 4
     for (long j = b + 1 + grp; j <= lo; j += G) {
       load8f<float>(part + (size_t)2 * j * H + h, v);
 #pragma unroll
       for (int i = 0; i < 8; ++i) acc[i] += v[i];
+      if constexpr (LIST) accb += list.part[(size_t)2 * j];
     }
     store8f(&share[grp][h], acc);
+    if (LIST && h == 0) bshare[grp] = accb;
     __syncthreads();
     for (int half = G / 2; half >= 1; half /= 2) {
       if (grp < half) {
@@ -653,12 +697,14 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(int n_tok, int
 #pragma unroll
         for (int i = 0; i < 8; ++i) acc[i] += v[i];
         store8f(&share[grp][h], acc);
+        if (LIST && h == 0) bshare[grp] += bshare[grp + half];
       }
       __syncthreads();
     }
     if (grp == 0) {
       load8f<float>(&share[0][h], acc);
       add_row(dtable + (size_t)key * H + h, acc);
+      if (LIST && list.dbias != nullptr && h == 0) list.dbias[key] += bshare[0];
     }
     __syncthreads();
   }
@@ -694,10 +740,10 @@ EmbedLayout embed_layout(int H, int n_tok) {
   return l;
 }
 
-template <typename S, int H>
+template <typename S, int H, bool LIST = false>
 hipError_t embed_bwd_h(int n, int V, const int32_t* tok_ptr, const int32_t* tok, int n_tok, float scale, int mean,
                        const float* factor, const Dropout& d, const void* grad, float* dtable, char* ws,
-                       hipStream_t st) {
+                       hipStream_t st, dev::ListRows list = {}) {
   const S* dX = static_cast<const S*>(grad);
   using namespace dev;
   const EmbedLayout l = embed_layout(H, n_tok);
@@ -728,16 +774,17 @@ hipError_t embed_bwd_h(int n, int V, const int32_t* tok_ptr, const int32_t* tok,
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
   }
-  if (d.cut != 0) {
+  if (d.cut != 0 && !LIST) {
     hipLaunchKernelGGL((embed_runs_kernel<S, H, true>), dim3(l.blocks), dim3(kEmbThreads), 0, st, n_tok, n, V, l.chunk,
-                       a, tok_ptr, scale, mean, factor, d, dX, dtable, part);
+                       a, tok_ptr, scale, mean, factor, d, dX, dtable, part, list);
   } else {
-    hipLaunchKernelGGL((embed_runs_kernel<S, H, false>), dim3(l.blocks), dim3(kEmbThreads), 0, st, n_tok, n, V, l.chunk,
-                       a, tok_ptr, scale, mean, factor, d, dX, dtable, part);
+    list.part = part + (size_t)2 * l.blocks * H;
+    hipLaunchKernelGGL((embed_runs_kernel<S, H, false, LIST>), dim3(l.blocks), dim3(kEmbThreads), 0, st, n_tok, n, V,
+                       l.chunk, a, tok_ptr, scale, mean, factor, d, dX, dtable, part, list);
   }
   if (l.blocks > 1)
-    hipLaunchKernelGGL((embed_join_kernel<H>), dim3((l.blocks + kJoinBlocks - 1) / kJoinBlocks, 2), dim3(kJoinThreads),
-                       0, st, n_tok, V, l.block, l.blocks, a, part, dtable);
+    hipLaunchKernelGGL((embed_join_kernel<H, LIST>), dim3((l.blocks + kJoinBlocks - 1) / kJoinBlocks, 2), dim3(kJoinThreads),
+                       0, st, n_tok, V, l.block, l.blocks, a, part, dtable, list);
   return hipGetLastError();
 }
 }  // namespace
@@ -754,6 +801,32 @@ hipError_t launch_embed_bwd(int n, int H, int V, const int32_t* tok_ptr, const i
     case 128: return embed_bwd_h<float, 128>(n, V, tok_ptr, tok, n_tok, scale, mean, nullptr, d, dX, dtable, w, st);
     case 256: return embed_bwd_h<float, 256>(n, V, tok_ptr, tok, n_tok, scale, mean, nullptr, d, dX, dtable, w, st);
   }
+  return hipErrorInvalidValue;
+}
+
+size_t list_rows_workspace(int H, int n) {
+  const EmbedLayout l = embed_layout(H, n);
+  return l.bytes + (size_t)2 * l.blocks * 4;   // the shares of dbias behind those of the rows
+}
+
+hipError_t launch_list_rows(int dt, int R, int K, int H, int V, int n_nodes, const int32_t* node, const int32_t* id,
+                            const float* coef, const void* x, float* dW, float* dbias, void* ws, hipStream_t st) {
+  const Dropout none{};
+  const dev::ListRows list{K, node, dbias, nullptr};
+  char* w = static_cast<char*>(ws);
+  const int n = R * K;
+#define LIST_ROWS(H)                                                                                              \
+  case H:                                                                                                         \
+    return dt == GGNN_BF16                                                                                        \
+               ? embed_bwd_h<dev::bf16s, H, true>(n_nodes, V, nullptr, id, n, 1.f, 0, coef, none, x, dW, w, st, list) \
+               : embed_bwd_h<float, H, true>(n_nodes, V, nullptr, id, n, 1.f, 0, coef, none, x, dW, w, st, list);
+  switch (H) {
+    LIST_ROWS(32)
+    LIST_ROWS(64)
+    LIST_ROWS(128)
+    LIST_ROWS(256)
+  }
+#undef LIST_ROWS
   return hipErrorInvalidValue;
 }
 

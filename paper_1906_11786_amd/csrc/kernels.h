@@ -10,6 +10,7 @@
 #pragma once
 
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <stddef.h>
 
 #include "../../include/ggnn.h"
@@ -29,6 +30,11 @@ struct ReduceSeg {
 size_t target_rows_workspace(int H, int R);
 hipError_t launch_target_rows(int R, int H, int V, const int32_t* target, const void* x, float scale,
                               const float* factor, float* dW, void* ws, hipStream_t st);
+// dW[id[l]] += coef[l] x[node[l / K]], dbias[id[l]] += coef[l] (NULL: none) over the R K listings l sorted by id
+// (negative: none); node NULL: row r is node r.  Workspace of list_rows_workspace bytes, n = R K listings.
+size_t list_rows_workspace(int H, int n);
+hipError_t launch_list_rows(int dt, int R, int K, int H, int V, int n_nodes, const int32_t* node, const int32_t* id,
+                            const float* coef, const void* x, float* dW, float* dbias, void* ws, hipStream_t st);
 struct ReduceList {
   static constexpr int kMax = 8;
   ReduceSeg seg[kMax];
@@ -57,7 +63,23 @@ struct Dropout {
   float scale;
 };
 
-// Arguments of the vocabulary loss (csrc/vocab.hip), as in include/ggnn.h.
+// Exponents of logits over a temperature (csrc/vocab_tile.h): factors of ordinary and of very large logits, the size at
+// which the second begins, 1 / (temperature far), 1 / temperature, and the temperature.
+struct Temper {
+  float near, far, limit, back, inv, tau;
+};
+inline Temper make_temper(float temperature) {
+  Temper te;
+  te.inv = 1.f / temperature;
+  te.near = 1.4426950408889634f * te.inv;
+  te.far = exp2f(floorf(log2f(te.near)) + 1.f);
+  te.limit = 536870912.f * temperature;
+  te.back = te.inv / te.far;
+  te.tau = temperature;
+  return te;
+}
+
+// Arguments of the vocabulary losses (csrc/vocab.hip), as in include/ggnn.h.
 struct VocabArgs {
   int n_nodes, R, V;
   const void *X, *W;
@@ -69,6 +91,12 @@ struct VocabArgs {
   int32_t* best;
   float *dX, *dW, *dbias;
   void* ws;
+  Temper temper = make_temper(1.f);
+  // A teacher's list of K entries a row (K = 0: `target` instead), its log sum or NULL; whether dX is added to.
+  int K = 0;
+  const int32_t* t_id;
+  const float *t_logit, *t_lse;
+  bool add;
 };
 
 // Supernode share of a fused bit-band step (the first 32 nodes are
@@ -124,7 +152,7 @@ struct SnStep {
   hipError_t launch_dropout(long count, const void* X, void* Y, const Dropout& d, hipStream_t st);                \
   hipError_t launch_embed(int n, int H, int V, const void* table, const int32_t* tok_ptr, const int32_t* tok,     \
                           int n_tok, float scale, int mean, const Dropout& d, void* X, hipStream_t st);           \
-  size_t vocab_workspace(int H, int R, int V, bool grad);                                                         \
+  size_t vocab_workspace(int H, int R, int V, bool grad, int K);                                                  \
   hipError_t launch_vocab(int H, const VocabArgs& c, bool grad, hipStream_t st);                                  \
   bool step_wide_applies(int B, int H);                                                                           \
   hipError_t launch_step_wide(bool rev, int n_pad, int B, int H, int E, const void* bits, const void* V,          \
@@ -448,8 +476,8 @@ inline hipError_t launch_embed(int dt, int n, int H, int V, const void* table, c
                                hipStream_t st) {
   return GGNN_DT_PICK(launch_embed, n, H, V, table, tok_ptr, tok, n_tok, scale, mean, d, X, st);
 }
-inline size_t vocab_workspace(int dt, int H, int R, int V, bool grad) {
-  return GGNN_DT_PICK(vocab_workspace, H, R, V, grad);
+inline size_t vocab_workspace(int dt, int H, int R, int V, bool grad, int K = 0) {
+  return GGNN_DT_PICK(vocab_workspace, H, R, V, grad, K);
 }
 inline hipError_t launch_vocab(int dt, int H, const VocabArgs& c, bool grad, hipStream_t st) {
   return GGNN_DT_PICK(launch_vocab, H, c, grad, st);

@@ -39,81 +39,10 @@
 // workgroups of 4 waves, one per SIMD, a wait for the copies every 32 entries).
 #include <type_traits>
 
-#include "device_common.h"
-#include "kernels.h"
-#include "lds_dma.h"
+#include "vocab_tile.h"
 
 namespace ggnn {
 namespace dev {
-
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-
-constexpr int kVocThreads = 256, kVocWaves = 4;
-constexpr int kVocRows = 128;              // rows (or vocabulary entries) of a workgroup, 32 per wave
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kMaskedBias = -1e30f;      // a bias at or below takes its entry out
-constexpr float kNoMax = -3e38f;           // running maximum before the first logit
-
-// Exponents of a row's terms are z * k - m with m = z_max * k, in one fused
-// multiply-add: k = log2 e, and the rounding of m is one factor of all terms, which
-// the log sum takes out again.  From 2^29 on that rounding would pass the range of
-// an exponential.  There k = 2, which makes m exact: logits of this size are equal
-// or at least 32 apart, so that any k gives the terms 1 and (to 2^-46) 0.  Maxima of
-// both sizes keep their order, and differences that vanish, when compared as m.
-constexpr float kFarLogit = 536870912.f;
-__device__ __forceinline__ float exponent_factor(float z) { return fabsf(z) >= kFarLogit ? 2.f : kLog2e; }
-// The log sum of a row from its m and the sum of its terms.
-__device__ __forceinline__ float log_of(float m, float sum) {
-  const float s = __log2f(sum);
-  return fabsf(m) >= 2.f * kFarLogit ? 0.5f * m + s * kLn2 : (m + s) * kLn2;
-}
-
-// float32 states and rows enter the matrix cores as three bf16 each (x = x0 +
-// x1 + x2, exact), with the six products of order 2^-16 and up: 24 bits at 6
-// bf16 products, where the float32 matrix instructions take 16 times a bf16
-// product's time.  Probabilities, likewise, as three parts (two in bf16).
-template <typename S> constexpr int voc_planes() { return sizeof(S) == 2 ? 1 : 3; }
-template <typename S> constexpr int voc_parts() { return sizeof(S) == 2 ? 2 : 3; }
-// Entries of an LDS tile: 64 in bf16, 32 in float32 (three times the bytes).
-template <typename S> constexpr int voc_tile() { return sizeof(S) == 2 ? 64 : 32; }
-
-__device__ __forceinline__ void mma32(f32x16& acc, const bf16x8& a, const bf16x8& b) {
-  acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, acc, 0, 0, 0);
-}
-// (vocab_few_kernel's in float32, which waits for memory)
-__device__ __forceinline__ void mma32(f32x16& acc, const f32x8& a, const f32x8& b) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], acc, 0, 0, 0);
-}
-
-// LDS tile: planes of T rows of H bf16 in 16-byte pieces; piece c of row r lies
-// at place c ^ swz(r) of its row.  Sixteen rows read at one piece (fragments along
-// H) and four rows times four pieces (fragments across rows) then both fall on
-// different banks, without padding, so that the copies into LDS stay linear.
-template <int H>
-__device__ __forceinline__ int swz(int r) {
-  constexpr int CPR = H / 8;
-  if constexpr (CPR >= 16) return ((r & 3) << 2) | ((r >> 2) & 3);
-  if constexpr (CPR == 8) return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
-  return (r >> 2) & 3;
-}
-
-// Copies rows row0 .. row0 + T - 1 (the last one's where beyond) of each plane
-// to LDS; a plane holds `plane` elements.
-template <int H, int NP, int T>
-__device__ __forceinline__ void stage_tile(const bf16s* __restrict__ src, size_t plane, long row0, long last,
-                                           uint32_t lds, int wave, int lane) {
-  constexpr int CPR = H / 8, EACH = T * CPR / 64, PIECES = NP * EACH;   // 1 KB copies of a plane, and in all
-#pragma unroll
-  for (int p = 0; p < (PIECES + kVocWaves - 1) / kVocWaves; ++p) {
-    const int piece = p * kVocWaves + wave, q = piece % EACH * 64 + lane;
-    if (PIECES % kVocWaves != 0 && piece >= PIECES) break;
-    const int r = q / CPR, c = (q % CPR) ^ swz<H>(r);
-    const long row = row0 + r < last ? row0 + r : last;
-    dma16(src + piece / EACH * plane + row * H + 8 * c,
-          __builtin_amdgcn_readfirstlane(lds + (uint32_t)piece * 1024u));
-  }
-}
 
 // ---- the two products of a 32 x 32 tile -----------------------------------
 //
@@ -243,85 +172,6 @@ __device__ __forceinline__ void split2(float a, float b, u32x4 (&part)[PARTS][2]
   }
 }
 
-// Keeps the compiler from moving what forms v past this point.
-template <typename V>
-__device__ __forceinline__ void keep_here(V& v) { asm volatile("" : "+v"(v)); }
-
-__device__ __forceinline__ float entry_bias(const float* bias, int v, int V) {
-  if (v >= V) return -INFINITY;
-  const float b = bias != nullptr ? bias[v] : 0.f;
-  return b <= kMaskedBias ? -INFINITY : b;
-}
-
-// Accumulator start values: a[8 (j / 4) + 4 (lane / 32) + j % 4] of 32 floats in LDS.
-__device__ __forceinline__ void start32(f32x16& acc, const float* a, int lane) {
-#pragma unroll
-  for (int j4 = 0; j4 < 4; ++j4) {
-    const f32x4 v = *reinterpret_cast<const f32x4*>(a + 8 * j4 + 4 * (lane / 32));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) acc[4 * j4 + i] = v[i];
-  }
-}
-
-struct RowBest {   // largest logit so far and the lowest entry that has it
-  float z;
-  int v;
-};
-__device__ __forceinline__ void take_best(RowBest& b, float z, int v) {
-  if (z > b.z || (z == b.z && v < b.v)) b = RowBest{z, v};
-}
-
-// The row a lane stands for: its node, or -1 (beyond R, or outside the graph).
-__device__ __forceinline__ int row_node(const int32_t* __restrict__ node, int r, int R, int n_nodes) {
-  if (r >= R) return -1;
-  const int i = node != nullptr ? node[r] : r;
-  return (unsigned)i < (unsigned)n_nodes ? i : -1;
-}
-// A row's fragments along H, as they lie in memory (row < 0: zero).
-template <typename S, int H>
-__device__ __forceinline__ void load_row(frag_t<S> (&f)[H / 16], const S* __restrict__ X, long row, int lane) {
-#pragma unroll
-  for (int kk = 0; kk < H / 16; ++kk) {
-    if (row >= 0) f[kk] = load8(X + row * H + 16 * kk + 8 * (lane / 32));
-    else f[kk] = frag_t<S>{};
-  }
-}
-// The same as planes of bf16.
-template <typename S, int H>
-__device__ __forceinline__ void load_planes(bf16x8 (&f)[voc_planes<S>()][H / 16], const S* __restrict__ X, long row,
-                                            int lane) {
-  frag_t<S> v[H / 16];
-  load_row<S, H>(v, X, row, lane);
-#pragma unroll
-  for (int kk = 0; kk < H / 16; ++kk) {
-    if constexpr (sizeof(S) == 2) {
-      f[0][kk] = v[kk];
-    } else {
-#pragma unroll
-      for (int a = 0; a < 3; ++a) {
-        u32x4 w;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          w[i] = pk2(v[kk][2 * i], v[kk][2 * i + 1]);
-          v[kk][2 * i] -= lo_f(w[i]);
-          v[kk][2 * i + 1] -= hi_f(w[i]);
-        }
-        f[a][kk] = __builtin_bit_cast(bf16x8, w);
-      }
-    }
-  }
-}
-// Four elements as planes, `plane` elements apart.
-__device__ __forceinline__ void store_planes(bf16s* p, size_t plane, f32x4 v, float) {
-#pragma unroll
-  for (int a = 0; a < 3; ++a) {
-    const u32x2 w = u32x2{pk2(v[0], v[1]), pk2(v[2], v[3])};
-    *reinterpret_cast<u32x2*>(p + a * plane) = w;
-    v -= f32x4{lo_f(w[0]), hi_f(w[0]), lo_f(w[1]), hi_f(w[1])};
-  }
-}
-__device__ __forceinline__ void store_planes(bf16s* p, size_t, f32x4 v, bf16s) { store4(p, v[0], v[1], v[2], v[3]); }
-
 // The planes of a float32 matrix, `count` (a multiple of 4) elements: once a
 // call, so that no workgroup splits the rows that it stages.  3.1 us for 4,999 x
 // 128.
@@ -343,69 +193,6 @@ __global__ __launch_bounds__(kVocThreads) void vocab_planes_kernel(size_t count,
 // the step's start: rows pass 3,775 -> 3,713 us, columns pass 4,090 -> 3,980, 60,001
 // rows, in turn on one card).
 //
-// Work is dealt in units of one LDS tile against one tile of 128 rows (or, in
-// the columns pass, entries).  Many 128-tiles: `workers` workgroups first take
-// whole ones, one each a round; those left over are laid end to end and cut into
-// equal runs of units, so that all workgroups end together.  Few: each is cut
-// into `parts` runs, one a worker, so that no worker starts twice.  A 128-tile is
-// thus one share, or several workers' shares, joined afterwards in their order.
-// (60,001 rows over 50,021 entries, 469 and 391 128-tiles for 256 workgroups: a
-// round of whole tiles alone would leave the chip half idle in the last one.)
-struct Deal {
-  int workers, tiles;   // workgroups; LDS tiles against one 128-tile
-  int whole, rest;      // 128-tiles dealt whole (a multiple of workers), and cut up
-  int slots;            // shares of a 128-tile, at most
-  int parts;            // of each 128-tile of the rest, or 0: cut end to end
-  uint32_t each, more;  // units of a worker (or a part); the first `more` have one more
-  __host__ __device__ uint32_t begin(uint32_t w) const { return w * each + (w < more ? w : more); }
-  __host__ __device__ int owner(uint32_t u) const {   // worker that has unit u of the rest (parts = 0)
-    const uint32_t k = more * (each + 1);
-    return (int)(u < k ? u / (each + 1) : more + (u - k) / each);
-  }
-  // Where share 0 of 128-tile i is written: a whole one is one share, each of the
-  // rest has room for `slots`.
-  __host__ __device__ int slot(int i) const { return i < whole ? i : whole + (i - whole) * slots; }
-  __host__ __device__ int all_slots() const { return whole + rest * slots; }
-  // Shares of 128-tile i; share s of it is written to slot(i) + s.
-  __host__ __device__ int shares(int i) const {
-    if (i < whole) return 1;
-    if (parts > 0) return parts;
-    const uint32_t u = (uint32_t)(i - whole) * tiles;
-    return owner(u + tiles - 1) - owner(u) + 1;
-  }
-};
-// The next run of worker w: 128-tile, LDS tiles t0 .. t1 - 1, its slot.
-struct Run {
-  int i, t0, t1, slot;
-};
-struct Dealt {
-  int step = 0;         // 128-tiles dealt whole so far
-  uint32_t u, end;      // units of the rest (parts: the worker's run, once)
-  __device__ __forceinline__ Dealt(const Deal& d, int w)
-      : u(d.begin(d.parts > 0 ? w % d.parts : w)), end(d.begin((d.parts > 0 ? w % d.parts : w) + 1)) {}
-  __device__ __forceinline__ bool next(const Deal& d, int w, Run* r) {
-    if (step * d.workers < d.whole) {
-      const int i = step * d.workers + w;
-      *r = Run{i, 0, d.tiles, d.slot(i)};
-      ++step;
-      return true;
-    }
-    if (u >= end) return false;
-    if (d.parts > 0) {
-      *r = Run{w / d.parts, (int)u, (int)end, d.slot(w / d.parts) + w % d.parts};
-      u = end;
-      return true;
-    }
-    const uint32_t k = u / (uint32_t)d.tiles;
-    r->i = d.whole + (int)k;
-    r->t0 = (int)(u - k * d.tiles);
-    r->t1 = min(d.tiles, r->t0 + (int)(end - u));
-    r->slot = d.slot(r->i) + (r->t0 == 0 ? 0 : w - d.owner(k * d.tiles));
-    u += r->t1 - r->t0;
-    return true;
-  }
-};
-
 // Workgroups of a pass that a compute unit holds (waves per SIMD): by the
 // accumulators and fragments that a wave keeps, and at H = 256 by the buffers.
 template <typename S>
@@ -414,21 +201,13 @@ constexpr int voc_waves(int H, bool sum) {
   return H >= 256 ? 1 : H == 128 ? (sum ? 2 : 3) : H == 64 ? 3 : 4;
 }
 
-constexpr int kVocBufs = 3;
-__device__ __forceinline__ int next_buf(int b) { return b == kVocBufs - 1 ? 0 : b + 1; }
-// Bytes from the buffer before `b` to buffer b.
-template <uint32_t BYTES>
-__device__ __forceinline__ uint32_t buf_step(int b) {
-  return b == 0 ? 0u - (kVocBufs - 1) * BYTES : BYTES;
-}
-
 // Rows pass.  Writes each row's (m in units of log 2, l) of a share to pm, pl
 // [slot][128]; SUM: O too; BEST: the largest logit's entry too; BIAS: there is
 // one (without, the logits' products start from zero, 16 registers less to set
 // a step).  A small dX is cleared here, `clear` 16-byte pieces per thread (0:
 // elsewhere).
 template <typename S, int H, bool SUM, bool BEST, bool BIAS>
-__global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_kernel(int n_nodes, int R, int V, Deal deal,
+__global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_kernel(int n_nodes, int R, int V, Deal deal, Temper te,
                                                                  const S* __restrict__ X,
                                                                  const bf16s* __restrict__ W,
                                                                  const float* __restrict__ bias,
@@ -461,7 +240,7 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
 #pragma unroll
       for (int ht = 0; ht < H / 32; ++ht) o[ht] = f32x16{};
     }
-    float m = kNoMax, k = kLog2e, l = 0.f;   // k: the row's exponent_factor
+    float m = kNoMax, k = te.near, l = 0.f;   // k: the row's exponent_factor
     RowBest best{-INFINITY, INT_MAX};
     auto fetch = [&](int t, int buf) {   // start the copies of tile t < t1
       stage_tile<H, NP, T>(W, (size_t)V * H, (long)t * T, V - 1, lds0 + (uint32_t)buf * NP * Step::PLANE, wave,
@@ -526,7 +305,7 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
         // then the terms stay below 2^8 and the sums lose nothing.
         if (__ballot(top * k > m + 8.f)) {
           const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-          const float z = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])), kn = exponent_factor(z);
+          const float z = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])), kn = exponent_factor(z, te);
           const float mn = fmaxf(m, z * kn);
           if (mn > m) k = kn;
           const float f = __builtin_amdgcn_exp2f(m - mn);
@@ -599,7 +378,7 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, SUM)) void vocab_rows_
 // other wave needs them.  Bound by memory's latency and the launch: 4.8 us for
 // one row over 10,007 entries at H = 64 (1.3 MB).
 template <typename S, int H, bool BEST>
-__global__ __launch_bounds__(kVocThreads) void vocab_few_kernel(int n_nodes, int R, int V, int per,
+__global__ __launch_bounds__(kVocThreads) void vocab_few_kernel(int n_nodes, int R, int V, int per, Temper te,
                                                                 const S* __restrict__ X, const S* __restrict__ W,
                                                                 const float* __restrict__ bias,
                                                                 const int32_t* __restrict__ node,
@@ -610,7 +389,7 @@ __global__ __launch_bounds__(kVocThreads) void vocab_few_kernel(int n_nodes, int
   const int tiles = (V + 31) / 32, t0 = split * per, t1 = min(tiles, t0 + per);
   frag_t<S> xf[H / 16];
   load_row<S, H>(xf, X, row_node(node, r, R, n_nodes), lane);
-  float m = kNoMax, k = kLog2e, l = 0.f;
+  float m = kNoMax, k = te.near, l = 0.f;
   RowBest best{-INFINITY, INT_MAX};
   for (int t = t0; t < t1; ++t) {
     frag_t<S> wf[H / 16];
@@ -623,7 +402,7 @@ __global__ __launch_bounds__(kVocThreads) void vocab_few_kernel(int n_nodes, int
     float top = s[0];
 #pragma unroll
     for (int j = 1; j < 16; ++j) top = fmaxf(top, s[j]);
-    const float kn = exponent_factor(top), mn = fmaxf(m, top * kn);
+    const float kn = exponent_factor(top, te), mn = fmaxf(m, top * kn);
     if (mn > m) k = kn;
     l *= __builtin_amdgcn_exp2f(m - mn);
     m = mn;
@@ -648,55 +427,11 @@ __global__ __launch_bounds__(kVocThreads) void vocab_few_kernel(int n_nodes, int
   }
 }
 
-// One row's (m, l, best) from its shares, held by L neighbouring lanes (q: the
-// lane's place); share s lies at at0 + s * stride.
-template <int L, bool BEST>
-__device__ __forceinline__ void join_shares(int n, size_t at0, size_t stride, int q, const float* __restrict__ pm,
-                                            const float* __restrict__ pl, const RowBest* __restrict__ pb, float& M,
-                                            float& sum, RowBest& best) {
-  M = kNoMax;
-  sum = 0.f;
-  best = RowBest{-INFINITY, INT_MAX};
-  constexpr int U = 4;   // shares in flight per lane
-  for (int s0 = q; s0 < n; s0 += L * U) {
-    float m[U], l[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int s = s0 + u * L;
-      const size_t at = at0 + (size_t)(s < n ? s : s0) * stride;
-      m[u] = s < n ? pm[at] : kNoMax;
-      l[u] = s < n ? pl[at] : 0.f;
-      if (BEST && s < n) take_best(best, pb[at].z, pb[at].v);
-    }
-    float top = M;
-#pragma unroll
-    for (int u = 0; u < U; ++u) top = fmaxf(top, m[u]);
-    sum *= __builtin_amdgcn_exp2f(M - top);
-#pragma unroll
-    for (int u = 0; u < U; ++u) sum += l[u] * __builtin_amdgcn_exp2f(m[u] - top);
-    M = top;
-  }
-#pragma unroll
-  for (int o = L / 2; o >= 1; o /= 2) {
-    const float m2 = __shfl_xor(M, o), s2 = __shfl_xor(sum, o), top = fmaxf(M, m2);
-    sum = sum * __builtin_amdgcn_exp2f(M - top) + s2 * __builtin_amdgcn_exp2f(m2 - top);
-    M = top;
-    if (BEST) take_best(best, __shfl_xor(best.z, o), __shfl_xor(best.v, o));
-  }
-}
-// lse of a row: -inf where every entry is masked.
-__device__ __forceinline__ float row_lse(float M, float sum) {
-  return sum == 0.f ? -INFINITY : log_of(M, sum);
-}
-__device__ __forceinline__ float row_loss(float lse, float zt, int t, bool bad) {
-  return bad ? NAN : t < 0 ? 0.f : lse == -INFINITY ? INFINITY : lse - zt;
-}
-
 // The loss of at most 32 rows from the many shares of vocab_few_kernel: one
 // workgroup per row.  3.0 us, latency.
 template <typename S, int H, bool BEST>
 __global__ __launch_bounds__(kVocThreads) void vocab_few_join_kernel(
-    int n_nodes, int R, int V, int splits, const S* __restrict__ X, const S* __restrict__ W,
+    int n_nodes, int R, int V, int splits, Temper te, const S* __restrict__ X, const S* __restrict__ W,
     const float* __restrict__ bias, const int32_t* __restrict__ node, const int32_t* __restrict__ target,
     const float* __restrict__ pm, const float* __restrict__ pl, const RowBest* __restrict__ pb,
     float* __restrict__ loss, float* __restrict__ lse, int32_t* __restrict__ best) {
@@ -731,7 +466,7 @@ __global__ __launch_bounds__(kVocThreads) void vocab_few_join_kernel(
     z += wz[w];
     if (BEST) take_best(b, wb[w].z, wb[w].v);
   }
-  const float v = row_lse(M, sum);
+  const float v = row_lse(M, sum, te);
   lse[r] = v;
   if (loss != nullptr) loss[r] = row_loss(v, t >= 0 ? z + entry_bias(bias, t, V) : 0.f, t, bad);
   if (BEST) best[r] = b.v == INT_MAX ? -1 : b.v;
@@ -745,7 +480,7 @@ __global__ __launch_bounds__(kVocThreads) void vocab_few_join_kernel(
 // at H = 64 (25 MB), 54 us for 60,001 rows at H = 256.
 template <typename S, int H, bool GRAD, bool BEST>
 __global__ __launch_bounds__(kVocThreads) void vocab_join_kernel(
-    int n_nodes, int R, int V, int Rp, Deal deal, const S* __restrict__ X, const S* __restrict__ W,
+    int n_nodes, int R, int V, int Rp, Deal deal, Temper te, const S* __restrict__ X, const S* __restrict__ W,
     const float* __restrict__ bias, const int32_t* __restrict__ node, const int32_t* __restrict__ target,
     const float* __restrict__ weight, float scale, const float* __restrict__ pm, const float* __restrict__ pl,
     const float* __restrict__ po, const RowBest* __restrict__ pb, float* __restrict__ loss, float* __restrict__ lse,
@@ -769,7 +504,7 @@ __global__ __launch_bounds__(kVocThreads) void vocab_join_kernel(
   float zt = x[0] * w[0] + x[1] * w[1] + x[2] * w[2] + x[3] * w[3];
 #pragma unroll
   for (int o = L / 2; o >= 1; o /= 2) zt += __shfl_xor(zt, o);
-  const float v = row_lse(M, sum);
+  const float v = row_lse(M, sum, te);
   if (r < R && q == 0) {
     lse[r] = v;
     if (loss != nullptr) loss[r] = row_loss(v, t >= 0 ? zt + entry_bias(bias, t, V) : 0.f, t, bad);
@@ -796,6 +531,145 @@ __global__ __launch_bounds__(kVocThreads) void vocab_join_kernel(
   }
 }
 
+// Distillation: joins the shares of a row, one wave per row, and forms what its
+// teacher's list adds.  With t_k the K listed logits over the temperature,
+//   q_k = exp(t_k - T), T = log sum_k exp t_k or the teacher's own log sum
+//   loss = sum_k q_k (t_k - T - z_k + lse);  dX = f (s O / l - sum_k q_k w_k)
+// with z_k the student's logit over the temperature, s = sum_k q_k (1 where T is the
+// list's own) and f = scale * weight / temperature.  A list's rows of W are read
+// once, for z_k and for the sum: H / 4 lanes hold one, 256 / H are formed side by
+// side, four of each in flight.  GRAD: also what the columns pass reads, as
+// vocab_join_kernel leaves it, and the factor -f q_k of each listing for
+// launch_list_rows (id -1: none).  splits: shares of a row from vocab_few_kernel (0:
+// dealt).
+template <typename S, int H, bool GRAD>
+__global__ __launch_bounds__(kVocThreads) void vocab_distill_join_kernel(
+    int n_nodes, int R, int V, int Rp, Deal deal, int splits, Temper te, int K, const S* __restrict__ X,
+    const S* __restrict__ W, const float* __restrict__ bias, const int32_t* __restrict__ node,
+    const int32_t* __restrict__ t_id, const float* __restrict__ t_logit, const float* __restrict__ t_lse,
+    const float* __restrict__ weight, float scale, const float* __restrict__ pm, const float* __restrict__ pl,
+    const float* __restrict__ po, float* __restrict__ loss, float* __restrict__ lse, float* __restrict__ dX, int add,
+    bf16s* __restrict__ xg, float* __restrict__ lse_w, int32_t* __restrict__ tgt_w, float* __restrict__ fac_w,
+    int32_t* __restrict__ id_w, float* __restrict__ coef_w) {
+  constexpr int L = H / 4, G = kWave / L, U = 4;
+  const int r = blockIdx.x * kVocWaves + threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  if (r >= (GRAD ? Rp : R)) return;   // whole waves leave together
+  const int grp = lane / L, h = 4 * (lane % L);
+  const int n = row_node(node, r, R, n_nodes);
+  const f32x4 x = n >= 0 ? load4f(X + (size_t)n * H + h) : f32x4{};
+  const size_t at = (size_t)r * K + lane;
+  int id = lane < K && n >= 0 ? t_id[at] : -1;
+  float t = id >= 0 ? t_logit[at] * te.inv : -INFINITY;
+  const int shares = r >= R ? 0 : splits > 0 ? splits : deal.shares(r / kVocRows);
+  const size_t stride = splits > 0 ? 32 : kVocRows;
+  const size_t at0 = splits > 0 ? r : (size_t)deal.slot(r / kVocRows) * kVocRows + r % kVocRows;
+  float M, sum;
+  RowBest none;
+  join_shares<kWave, false>(shares, at0, stride, lane, pm, pl, nullptr, M, sum, none);
+  const float v = row_lse(M, sum, te);
+
+  bool bad = __ballot(id >= V || !(t < INFINITY)) != 0;
+  const bool any = __ballot(t > -INFINITY) != 0;
+  float T, s = 1.f, q;
+  if (t_lse != nullptr) {
+    T = any ? t_lse[r] : 0.f;
+    bad |= any && !(fabsf(T) < INFINITY);
+    q = __builtin_amdgcn_exp2f((t - T) * kLog2e);
+    s = q;
+#pragma unroll
+    for (int o = kWave / 2; o >= 1; o /= 2) s += __shfl_xor(s, o);
+  } else {
+    float top = t;
+#pragma unroll
+    for (int o = kWave / 2; o >= 1; o /= 2) top = fmaxf(top, __shfl_xor(top, o));
+    q = any ? __builtin_amdgcn_exp2f((t - top) * kLog2e) : 0.f;
+    float all = q;
+#pragma unroll
+    for (int o = kWave / 2; o >= 1; o /= 2) all += __shfl_xor(all, o);
+    T = top + __log2f(all) * kLn2;
+    q = any ? q / all : 0.f;
+  }
+  if (bad || !(q > 0.f)) id = -1;   // listings that add nothing
+  const bool live = !bad && any && sum != 0.f;
+
+  float part = 0.f;
+  f32x4 qw = {};
+  if (!bad && any) {
+    for (int k0 = 0; k0 < K; k0 += G * U) {
+      f32x4 w[U];
+      float b[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int k = k0 + u * G + grp, i = __shfl(id, k % kWave);
+        w[u] = f32x4{};
+        b[u] = 0.f;
+        if (k < K && i >= 0) {
+          w[u] = load4f(W + (size_t)i * H + h);
+          b[u] = entry_bias(bias, i, V);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int k = k0 + u * G + grp;
+        // (exchanges by all lanes: one that a branch has turned off delivers nothing)
+        const int i = __shfl(id, k % kWave);
+        const float qi = __shfl(q, k % kWave), tk = __shfl(t, k % kWave);
+        const bool here = k < K && i >= 0;
+        const float qk = here ? qi : 0.f;
+        float z = x[0] * w[u][0] + x[1] * w[u][1] + x[2] * w[u][2] + x[3] * w[u][3];
+#pragma unroll
+        for (int o = L / 2; o >= 1; o /= 2) z += __shfl_xor(z, o);
+        // (differences of like logits first: they are what the loss is made of)
+        if (here) part += qk * (fmaf(-(z + b[u]), te.inv, tk) + (v - T));
+        if constexpr (GRAD) qw += w[u] * qk;
+      }
+    }
+#pragma unroll
+    for (int o = L; o < kWave; o *= 2) {
+      part += __shfl_xor(part, o);
+      if constexpr (GRAD) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) qw[i] += __shfl_xor(qw[i], o);
+      }
+    }
+  }
+  if (r < R && lane == 0) {
+    lse[r] = v;
+    loss[r] = bad ? NAN : !any ? 0.f : sum == 0.f ? INFINITY : part;
+  }
+  if constexpr (GRAD) {
+    const float f = live ? (weight != nullptr ? weight[r] : 1.f) * scale * te.inv : 0.f;
+    if (grp == 0) store_planes(xg + (size_t)r * H + h, (size_t)Rp * H, live ? x : f32x4{}, S{});
+    if (lane == 0) {
+      lse_w[r] = live ? v * te.tau : INFINITY;
+      tgt_w[r] = -1;
+      fac_w[r] = live ? f * s : 0.f;   // (s of a broken list may be anything)
+    }
+    if (lane < K && r < R) {
+      id_w[at] = live ? id : -1;
+      coef_w[at] = -f * q;
+    }
+    if (live) {
+      f32x4 o = {};
+#pragma unroll 4
+      for (int i = grp; i < shares; i += G) {
+        const size_t a = at0 + (size_t)i * stride;
+        o += *reinterpret_cast<const f32x4*>(po + a * H + h) * __builtin_amdgcn_exp2f(pm[a] - M);
+      }
+#pragma unroll
+      for (int d = L; d < kWave; d *= 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], d);
+      }
+      if (grp == 0) {
+        f32x4* out = reinterpret_cast<f32x4*>(dX + (size_t)n * H + h);
+        const f32x4 d = (o * (s / sum) - qw) * f;
+        *out = add ? *out + d : d;
+      }
+    }
+  }
+}
+
 // Columns pass: 128 entries of a workgroup (32 per wave) against the gathered
 // states.  Adds to dW [V][H] and db [V] (dbias NULL: none) where the 128-tile is
 // one share, else writes its share to pw [slot][128][H] and pdb [slot][128], slots
@@ -803,7 +677,7 @@ __global__ __launch_bounds__(kVocThreads) void vocab_join_kernel(
 // WEIGHT: each row has a factor of its own; otherwise all have `scale`.  TARGETS:
 // see below.
 template <typename S, int H, bool WEIGHT, bool TARGETS>
-__global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols_kernel(int V, int Rp, Deal deal, float scale,
+__global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols_kernel(int V, int Rp, Deal deal, Temper te, float scale,
                                                                  const bf16s* __restrict__ xg,
                                                                  const S* __restrict__ W,
                                                                  const float* __restrict__ bias,
@@ -856,7 +730,7 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
     int buf = 0;
     fetch(t0, 0);
     load_planes<S, H>(wf, W, min(v, V - 1), lane);
-    const float b2 = entry_bias(bias, v, V) * kLog2e;
+    const float b2 = entry_bias(bias, v, V) * te.near;
     land(0);
     if (t0 + 1 < t1) fetch(t0 + 1, 1);
     start32(s, tl[0], lane);
@@ -887,7 +761,7 @@ __global__ __launch_bounds__(kVocThreads, voc_waves<S>(H, true)) void vocab_cols
         u32x4 part[P][2];
         constexpr bool kFinal = sizeof(S) == 2 && !WEIGHT;   // what follows leaves p as it is
         auto prob = [&](int j) {
-          p[j] = __builtin_amdgcn_exp2f(fmaf(s[j], kLog2e, b2));
+          p[j] = __builtin_amdgcn_exp2f(fmaf(s[j], te.near, b2));
           keep_here(p[j]);
           if (kFinal && j >= 8 && j % 2 == 1) {
             split2(p[j - 9], p[j - 8], part, 0, (j - 9) / 2);
@@ -1015,42 +889,10 @@ __global__ __launch_bounds__(kVocThreads) void vocab_wsum_kernel(int V, Deal dea
 }  // namespace dev
 
 namespace {
-inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
-inline int cdiv(long a, long b) { return (int)((a + b - 1) / b); }
-
 // Workgroups that the chip's 256 compute units hold at once.
 template <typename S>
 int voc_workers(int H, bool sum) {
   return 256 * dev::voc_waves<S>(H, sum);
-}
-
-dev::Deal make_deal(int tiles128, int tiles, int workers) {
-  dev::Deal d{};
-  d.tiles = tiles;
-  // Four tiles a worker pay for its start and its share; fewer where that
-  // would leave compute units empty.
-  const long all = (long)tiles128 * tiles, few = all < 256 ? all : 256, want = all / 4 > few ? all / 4 : few;
-  d.workers = want < workers ? (int)want : workers;
-  d.parts = d.workers / tiles128 >= 4 ? d.workers / tiles128 : 0;
-  if (d.parts > 0) {
-    d.workers = d.parts * tiles128;
-    d.rest = tiles128;
-    d.each = (uint32_t)tiles / d.parts;
-    d.more = (uint32_t)tiles % d.parts;
-    d.slots = d.parts;
-    return d;
-  }
-  d.whole = tiles128 / d.workers * d.workers;
-  d.rest = tiles128 - d.whole;
-  const uint32_t units = (uint32_t)d.rest * (uint32_t)tiles;   // fewer than workers * tiles
-  d.each = units / d.workers;
-  d.more = units % d.workers;
-  d.slots = 1;
-  for (int i = d.whole; i < tiles128; ++i) {
-    const int n = d.shares(i);
-    if (n > d.slots) d.slots = n;
-  }
-  return d;
 }
 
 // Where the targets' share of dW, -g x of each row on its target's row, comes
@@ -1072,10 +914,10 @@ struct VocabPlan {
   int splits, per;     // few rows
   int row_tiles, Rp, col_tiles;
   dev::Deal rows, cols;
-  size_t pm, pl, pb, po, wp, xg, lse, tgt, fac, pw, pdb, sort, bytes;
+  size_t pm, pl, pb, po, wp, xg, lse, tgt, fac, pw, pdb, sort, id, coef, bytes;
 };
 template <typename S>
-VocabPlan vocab_plan(int H, int R, int V, bool grad) {
+VocabPlan vocab_plan(int H, int R, int V, bool grad, int K = 0) {
   constexpr int T = dev::voc_tile<S>();
   VocabPlan p{};
   p.few = !grad && R <= 32;
@@ -1112,7 +954,13 @@ VocabPlan vocab_plan(int H, int R, int V, bool grad) {
     p.fac = take((size_t)p.Rp * 4);
     p.pw = take(cshares * H * 4);
     p.pdb = take(cshares * 4);
-    if (targets_sorted(sizeof(S), H, R, V)) p.sort = take(target_rows_workspace(H, p.Rp));
+    if (K > 0) {
+      p.id = take((size_t)R * K * 4);
+      p.coef = take((size_t)R * K * 4);
+      p.sort = take(list_rows_workspace(H, R * K));
+    } else if (targets_sorted(sizeof(S), H, R, V)) {
+      p.sort = take(target_rows_workspace(H, p.Rp));
+    }
   }
   p.bytes = at;
   return p;
@@ -1135,27 +983,42 @@ const dev::bf16s* staged_rows(const VocabArgs& c, int H, void* planes, hipStream
 template <typename S, int H, bool BEST>
 hipError_t vocab_loss_h(const VocabArgs& c, hipStream_t st) {
   using namespace dev;
-  const VocabPlan p = vocab_plan<S>(H, c.R, c.V, false);
+  const VocabPlan p = vocab_plan<S>(H, c.R, c.V, false, c.K);
   char* ws = static_cast<char*>(c.ws);
   float *pm = reinterpret_cast<float*>(ws + p.pm), *pl = reinterpret_cast<float*>(ws + p.pl);
   RowBest* pb = reinterpret_cast<RowBest*>(ws + p.pb);
   const S *X = static_cast<const S*>(c.X), *W = static_cast<const S*>(c.W);
+  const int row_waves = cdiv(c.R, kVocWaves);   // workgroups where a wave joins a row
+#define DISTILL_JOIN()                                                                                               \
+  hipLaunchKernelGGL((vocab_distill_join_kernel<S, H, false>), dim3(row_waves), dim3(kVocThreads), 0, st, c.n_nodes, \
+                     c.R, c.V, p.Rp, p.rows, p.splits, c.temper, c.K, X, W, c.bias, c.node, c.t_id, c.t_logit,       \
+                     c.t_lse, nullptr, 1.f, pm, pl, nullptr, c.loss, c.lse, nullptr, 0, nullptr, nullptr, nullptr,    \
+                     nullptr, nullptr, nullptr)
   if (p.few) {
     hipLaunchKernelGGL((vocab_few_kernel<S, H, BEST>), dim3(p.splits / kVocWaves), dim3(kVocThreads), 0, st,
-                       c.n_nodes, c.R, c.V, p.per, X, W, c.bias, c.node, pm, pl, pb);
+                       c.n_nodes, c.R, c.V, p.per, c.temper, X, W, c.bias, c.node, pm, pl, pb);
+    if (c.K > 0) {
+      DISTILL_JOIN();
+      return hipGetLastError();
+    }
     hipLaunchKernelGGL((vocab_few_join_kernel<S, H, BEST>), dim3(c.R), dim3(kVocThreads), 0, st, c.n_nodes, c.R, c.V,
-                       p.splits, X, W, c.bias, c.node, c.target, pm, pl, pb, c.loss, c.lse, c.best);
+                       p.splits, c.temper, X, W, c.bias, c.node, c.target, pm, pl, pb, c.loss, c.lse, c.best);
     return hipGetLastError();
   }
   const bf16s* Ws = staged_rows<S>(c, H, ws + p.wp, st);
   if (c.bias != nullptr)
     hipLaunchKernelGGL((vocab_rows_kernel<S, H, false, BEST, true>), dim3(p.rows.workers), dim3(kVocThreads), 0, st,
-                       c.n_nodes, c.R, c.V, p.rows, X, Ws, c.bias, c.node, pm, pl, nullptr, pb, nullptr, 0);
+                       c.n_nodes, c.R, c.V, p.rows, c.temper, X, Ws, c.bias, c.node, pm, pl, nullptr, pb, nullptr, 0);
   else
     hipLaunchKernelGGL((vocab_rows_kernel<S, H, false, BEST, false>), dim3(p.rows.workers), dim3(kVocThreads), 0, st,
-                       c.n_nodes, c.R, c.V, p.rows, X, Ws, nullptr, c.node, pm, pl, nullptr, pb, nullptr, 0);
+                       c.n_nodes, c.R, c.V, p.rows, c.temper, X, Ws, nullptr, c.node, pm, pl, nullptr, pb, nullptr, 0);
+  if (c.K > 0) {
+    DISTILL_JOIN();
+    return hipGetLastError();
+  }
+#undef DISTILL_JOIN
   hipLaunchKernelGGL((vocab_join_kernel<S, H, false, BEST>), dim3(cdiv((long)c.R * (H / 4), kVocThreads)),
-                     dim3(kVocThreads), 0, st, c.n_nodes, c.R, c.V, p.Rp, p.rows, X, W, c.bias, c.node, c.target,
+                     dim3(kVocThreads), 0, st, c.n_nodes, c.R, c.V, p.Rp, p.rows, c.temper, X, W, c.bias, c.node, c.target,
                      nullptr, 1.f, pm, pl, nullptr, pb, c.loss, c.lse, c.best, nullptr, nullptr, nullptr, nullptr,
                      nullptr);
   return hipGetLastError();
@@ -1164,7 +1027,7 @@ hipError_t vocab_loss_h(const VocabArgs& c, hipStream_t st) {
 template <typename S, int H>
 hipError_t vocab_grad_h(const VocabArgs& c, hipStream_t st) {
   using namespace dev;
-  const VocabPlan p = vocab_plan<S>(H, c.R, c.V, true);
+  const VocabPlan p = vocab_plan<S>(H, c.R, c.V, true, c.K);
   char* ws = static_cast<char*>(c.ws);
   float *pm = reinterpret_cast<float*>(ws + p.pm), *pl = reinterpret_cast<float*>(ws + p.pl);
   float *po = reinterpret_cast<float*>(ws + p.po), *lse_w = reinterpret_cast<float*>(ws + p.lse);
@@ -1177,25 +1040,33 @@ hipError_t vocab_grad_h(const VocabArgs& c, hipStream_t st) {
   // A small dX is cleared by the rows pass, one launch less (5 us of the 70 at
   // 3,001 rows); a large one, which would hold its products up, by its own.
   const long pieces = (long)c.n_nodes * (H / 4), each = (long)p.rows.workers * kVocThreads;
-  const int clear = pieces <= 8 * each ? (int)((pieces + each - 1) / each) : 0;
-  if (clear == 0) {
+  const int clear = pieces <= 8 * each && !c.add ? (int)((pieces + each - 1) / each) : 0;
+  if (clear == 0 && !c.add) {
     const hipError_t err = launch_fill_zero(c.dX, (size_t)c.n_nodes * H, st);
     if (err != hipSuccess) return err;
   }
   if (c.bias != nullptr)
     hipLaunchKernelGGL((vocab_rows_kernel<S, H, true, false, true>), dim3(p.rows.workers), dim3(kVocThreads), 0, st,
-                       c.n_nodes, c.R, c.V, p.rows, X, Ws, c.bias, c.node, pm, pl, po, nullptr, c.dX, clear);
+                       c.n_nodes, c.R, c.V, p.rows, c.temper, X, Ws, c.bias, c.node, pm, pl, po, nullptr, c.dX, clear);
   else
     hipLaunchKernelGGL((vocab_rows_kernel<S, H, true, false, false>), dim3(p.rows.workers), dim3(kVocThreads), 0, st,
-                       c.n_nodes, c.R, c.V, p.rows, X, Ws, nullptr, c.node, pm, pl, po, nullptr, c.dX, clear);
-  hipLaunchKernelGGL((vocab_join_kernel<S, H, true, false>), dim3(cdiv((long)p.Rp * (H / 4), kVocThreads)),
-                     dim3(kVocThreads), 0, st, c.n_nodes, c.R, c.V, p.Rp, p.rows, X, W, c.bias, c.node, c.target,
-                     c.weight, c.scale, pm, pl, po, nullptr, c.loss, c.lse, nullptr, c.dX, xg, lse_w, tgt_w, fac_w);
-  const bool sorted = targets_sorted(sizeof(S), H, c.R, c.V);
+                       c.n_nodes, c.R, c.V, p.rows, c.temper, X, Ws, nullptr, c.node, pm, pl, po, nullptr, c.dX, clear);
+  if (c.K > 0)
+    hipLaunchKernelGGL((vocab_distill_join_kernel<S, H, true>), dim3(cdiv(p.Rp, kVocWaves)), dim3(kVocThreads), 0, st,
+                       c.n_nodes, c.R, c.V, p.Rp, p.rows, 0, c.temper, c.K, X, W, c.bias, c.node, c.t_id, c.t_logit,
+                       c.t_lse, c.weight, c.scale, pm, pl, po, c.loss, c.lse, c.dX, c.add ? 1 : 0, xg, lse_w, tgt_w,
+                       fac_w, reinterpret_cast<int32_t*>(ws + p.id), reinterpret_cast<float*>(ws + p.coef));
+  else
+    hipLaunchKernelGGL((vocab_join_kernel<S, H, true, false>), dim3(cdiv((long)p.Rp * (H / 4), kVocThreads)),
+                       dim3(kVocThreads), 0, st, c.n_nodes, c.R, c.V, p.Rp, p.rows, c.temper, X, W, c.bias, c.node,
+                       c.target, c.weight, c.scale, pm, pl, po, nullptr, c.loss, c.lse, nullptr, c.dX, xg, lse_w, tgt_w,
+                       fac_w);
+  const bool sorted = c.K > 0 || targets_sorted(sizeof(S), H, c.R, c.V);   // what the lists or targets add is
+  const float scale = c.scale * c.temper.inv;
 #define COLS(WEIGHT, TARGETS)                                                                                       \
   hipLaunchKernelGGL((vocab_cols_kernel<S, H, WEIGHT, TARGETS>), dim3(p.cols.workers), dim3(kVocThreads), 0, st, c.V, \
-                     p.Rp, p.cols, c.scale, xg, W, c.bias, lse_w, tgt_w, fac_w, c.dW, c.dbias, pw, pdb)
-  if (c.weight != nullptr) {
+                     p.Rp, p.cols, c.temper, scale, xg, W, c.bias, lse_w, tgt_w, fac_w, c.dW, c.dbias, pw, pdb)
+  if (c.weight != nullptr || (c.K > 0 && c.t_lse != nullptr)) {
     if (sorted) COLS(true, false); else COLS(true, true);
   } else {
     if (sorted) COLS(false, false); else COLS(false, true);
@@ -1207,6 +1078,10 @@ hipError_t vocab_grad_h(const VocabArgs& c, hipStream_t st) {
                        p.cols, pw, pdb, c.dW, c.dbias);
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess || !sorted) return err;
+  if (c.K > 0)
+    return launch_list_rows(sizeof(S) == 2 ? GGNN_BF16 : GGNN_F32, c.R, c.K, H, c.V, c.n_nodes, c.node,
+                            reinterpret_cast<int32_t*>(ws + p.id), reinterpret_cast<float*>(ws + p.coef), X, c.dW,
+                            c.dbias, ws + p.sort, st);
   return launch_target_rows(p.Rp, H, c.V, tgt_w, xg, -c.scale,
                             c.weight != nullptr ? fac_w : nullptr, c.dW, ws + p.sort, st);
 }
@@ -1219,7 +1094,9 @@ hipError_t vocab_h(const VocabArgs& c, bool grad, hipStream_t st) {
 }  // namespace
 
 namespace GGNN_IMPL_NS {
-size_t vocab_workspace(int H, int R, int V, bool grad) { return vocab_plan<dev::dt_t>(H, R, V, grad).bytes; }
+size_t vocab_workspace(int H, int R, int V, bool grad, int K) {
+  return vocab_plan<dev::dt_t>(H, R, V, grad, K).bytes;
+}
 
 hipError_t launch_vocab(int H, const VocabArgs& c, bool grad, hipStream_t st) {
   using S = dev::dt_t;
