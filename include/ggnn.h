@@ -748,6 +748,64 @@ ggnn_status ggnn_vocab_loss_grad(ggnn_dtype dt, int32_t n_nodes, int32_t H, int3
                                  const float* weight, float scale, float* loss, float* lse, float* dX, float* dW,
                                  float* dbias, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Rules for the answers of chosen nodes, row by row (ggnn_vocab_top).  They act on a
+ * row's logits z in this order, each step rounded to float:
+ *   1. an entry that the row has seen c > 0 times: z = z / repetition where z > 0, else z * repetition;
+ *      then z = z - (presence + frequency * c)
+ *   2. an entry that has biases of its own in this row: z = z + (their sum, in list order)
+ *   3. an entry whose bit in the row's mask is 0: taken out
+ * All pointers are to the device.  Entries outside [0, V) in the lists are passed over.
+ *   mask       [n_masks][mask_words] uint32: bit v % 32 of word v / 32 is 1 where entry v
+ *              may be answered; mask_words >= V / 32, rounded up.  n_masks = 0: none
+ *   mask_of    [n_rows] int32: which mask a row has; one outside [0, n_masks): all
+ *              entries may be answered.  NULL: row r has mask r
+ *   seen_ptr, seen   [n_rows + 1] and [n_seen] int32: row r has seen seen[seen_ptr[r]] ..
+ *              seen[seen_ptr[r+1] - 1], in any order, as often as listed (e.g. the
+ *              tokens of nodes nearby, or those answered before).  n_seen = 0: none
+ *   repetition, presence, frequency   finite; repetition > 0 (1, 0, 0: no change)
+ *   add_ptr, add, value   [n_rows + 1], [n_add] int32 and [n_add] float: biases by row;
+ *              -inf takes an entry out.  n_add = 0: none
+ * Offsets are non-decreasing; parts of a list before position 0 or from its end on
+ * are left out.  n_seen + n_add <= 2^30. */
+typedef struct {
+  const uint32_t* mask;
+  int32_t n_masks, mask_words;
+  const int32_t* mask_of;
+  const int32_t* seen_ptr;
+  const int32_t* seen;
+  int32_t n_seen;
+  float repetition, presence, frequency;
+  const int32_t* add_ptr;
+  const int32_t* add;
+  const float* value;
+  int32_t n_add;
+} ggnn_token_rules;
+
+/* Workspace bytes of ggnn_vocab_top; 0 for unsupported sizes or no rows.
+ * n_listed: n_seen + n_add of the rules (0 without). */
+size_t ggnn_vocab_top_workspace_bytes(ggnn_dtype dt, int32_t H, int32_t n_rows, int32_t V, int32_t K, int64_t n_listed);
+
+/* The best entries of chosen nodes over a vocabulary (device), without the
+ * [n_rows][V] logits in memory: with z as in ggnn_vocab_loss, changed by the rules
+ *   rules    host struct, or NULL (not kept)
+ *   K        1 .. 64
+ *   top, logit   [n_rows][K] int32 and float (written): the entries with the largest
+ *            z, in descending order, the lower one first where they are equal, and
+ *            their z; -1 and -inf from where no entry is left.  -0 counts as 0; an
+ *            entry whose z is NaN or -inf is not answered.
+ *   lse      [n_rows] float (written: log sum_v exp(z_v / temperature) over the entries
+ *            that are left, -inf for none), or NULL
+ *   temperature  in [0.001, 1000], of lse alone
+ * Logits are float32 sums, formed a second time for the entries returned: entries
+ * whose exact logits differ by less than the rounding of such a sum may be returned
+ * in either order, or one in place of the other.  The other arguments, and nodes
+ * outside the graph (a zero state), as in ggnn_vocab_loss.  ggnn_vocab_distill takes
+ * top, logit and, at its temperature, lse as a teacher's lists. */
+ggnn_status ggnn_vocab_top(ggnn_dtype dt, int32_t n_nodes, int32_t H, int32_t n_rows, int32_t V, const void* X,
+                           const void* W, const float* bias, const int32_t* node, const ggnn_token_rules* rules,
+                           float temperature, int32_t K, int32_t* top, float* logit, float* lse, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
 /* Workspace bytes of ggnn_vocab_distill (grad = 0) or ggnn_vocab_distill_grad
  * (grad != 0); 0 for unsupported sizes or no rows. */
 size_t ggnn_vocab_distill_workspace_bytes(ggnn_dtype dt, int32_t H, int32_t n_rows, int32_t V, int32_t K, int32_t grad);

@@ -44,6 +44,7 @@ EXPORTS = [
     "ggnn_readout_loss_bwd_noalloc",
     "ggnn_dropout", "ggnn_embed", "ggnn_embed_bwd_workspace_bytes", "ggnn_embed_bwd",
     "ggnn_vocab_workspace_bytes", "ggnn_vocab_loss", "ggnn_vocab_loss_grad",
+    "ggnn_vocab_top_workspace_bytes", "ggnn_vocab_top",
     "ggnn_vocab_distill_workspace_bytes", "ggnn_vocab_distill", "ggnn_vocab_distill_grad",
 ]
 
@@ -73,6 +74,13 @@ class ggnn_grads(C.Structure):
     _fields_ = [("dX", C.c_void_p), ("dW", C.c_void_p), ("dbias", C.c_void_p), ("dWi", C.c_void_p),
                 ("dU", C.c_void_p), ("db", C.c_void_p), ("da", C.c_void_p), ("dM", C.c_void_p),
                 ("dh", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class ggnn_token_rules(C.Structure):
+    _fields_ = [("mask", C.c_void_p), ("n_masks", C.c_int32), ("mask_words", C.c_int32), ("mask_of", C.c_void_p),
+                ("seen_ptr", C.c_void_p), ("seen", C.c_void_p), ("n_seen", C.c_int32), ("repetition", C.c_float),
+                ("presence", C.c_float), ("frequency", C.c_float), ("add_ptr", C.c_void_p), ("add", C.c_void_p),
+                ("value", C.c_void_p), ("n_add", C.c_int32)]
 
 
 _lib = None
@@ -141,6 +149,9 @@ _SIGS = {
     "ggnn_vocab_loss": (C.c_int, [C.c_int, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
     "ggnn_vocab_loss_grad": (C.c_int, [C.c_int, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, f32, vp, vp, vp, vp, vp,
                                        vp, sz, vp]),
+    "ggnn_vocab_top_workspace_bytes": (sz, [C.c_int, i32, i32, i32, i32, i64]),
+    "ggnn_vocab_top": (C.c_int, [C.c_int, i32, i32, i32, i32, vp, vp, vp, vp, C.POINTER(ggnn_token_rules), f32, i32, vp,
+                                 vp, vp, vp, sz, vp]),
     "ggnn_vocab_distill_workspace_bytes": (sz, [C.c_int, i32, i32, i32, i32, i32]),
     "ggnn_vocab_distill": (C.c_int, [C.c_int, i32, i32, i32, i32, vp, vp, vp, vp, i32, vp, vp, vp, f32, vp, vp, vp, sz,
                                      vp]),
@@ -484,6 +495,25 @@ def ggnn_vocab_loss_grad(dt, n_nodes, H, n_rows, V, X, W, bias, node, target, we
     _check("ggnn_vocab_loss_grad", lib().ggnn_vocab_loss_grad(
         _dt(dt), n_nodes, H, n_rows, V, _ptr(X), _ptr(W), _ptr(bias), _ptr(node), _ptr(target), _ptr(weight), scale,
         _ptr(loss), _ptr(lse), _ptr(dX), _ptr(dW), _ptr(dbias), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def token_rules(mask=None, n_masks=0, mask_words=0, mask_of=None, seen_ptr=None, seen=None, n_seen=0, repetition=1.0,
+                presence=0.0, frequency=0.0, add_ptr=None, add=None, value=None, n_add=0) -> ggnn_token_rules:
+    """The struct of ggnn_vocab_top's rules; the arrays stay the caller's to keep until the call is made."""
+    return ggnn_token_rules(_ptr(mask), n_masks, mask_words, _ptr(mask_of), _ptr(seen_ptr), _ptr(seen), n_seen, repetition,
+                            presence, frequency, _ptr(add_ptr), _ptr(add), _ptr(value), n_add)
+
+
+def ggnn_vocab_top_workspace_bytes(dt, H, n_rows, V, K, n_listed=0) -> int:
+    return int(lib().ggnn_vocab_top_workspace_bytes(_dt(dt), H, n_rows, V, K, n_listed))
+
+
+def ggnn_vocab_top(dt, n_nodes, H, n_rows, V, X, W, bias, node, rules, temperature, K, top, logit, lse, workspace,
+                   workspace_bytes, stream=None):
+    _check("ggnn_vocab_top", lib().ggnn_vocab_top(
+        _dt(dt), n_nodes, H, n_rows, V, _ptr(X), _ptr(W), _ptr(bias), _ptr(node),
+        None if rules is None else C.byref(rules), temperature, K, _ptr(top), _ptr(logit), _ptr(lse), _ptr(workspace),
+        workspace_bytes, _stream(stream)))
 
 
 def ggnn_vocab_distill_workspace_bytes(dt, H, n_rows, V, K, grad) -> int:

@@ -69,9 +69,8 @@ ggnn_status check_embed(int32_t n, int32_t H, int32_t V, const int32_t* tok_ptr,
   return GGNN_OK;
 }
 
-ggnn_status check_vocab(int32_t dt, int32_t n_nodes, int32_t H, int32_t n_rows, int32_t V, const void* X,
-                        const void* W, const float* bias, const int32_t* node, const int32_t* target,
-                        const float* lse) {
+ggnn_status check_rows(int32_t dt, int32_t n_nodes, int32_t H, int32_t n_rows, int32_t V, const void* X,
+                       const void* W, const float* bias, const int32_t* node) {
   GGNN_CHECK_ARG(supported_dtype(dt), "unknown dtype %d", dt);
   GGNN_CHECK_ARG(n_nodes >= 1, "n_nodes=%d must be at least 1", n_nodes);
   GGNN_CHECK_ARG(supported_H(H), "H=%d must be one of 32, 64, 128, 256", H);
@@ -84,6 +83,14 @@ ggnn_status check_vocab(int32_t dt, int32_t n_nodes, int32_t H, int32_t n_rows, 
   CHECK_PTR(W, "W");
   CHECK_OPT_PTR(bias, "bias");
   CHECK_OPT_PTR(node, "node");
+  return GGNN_OK;
+}
+
+ggnn_status check_vocab(int32_t dt, int32_t n_nodes, int32_t H, int32_t n_rows, int32_t V, const void* X,
+                        const void* W, const float* bias, const int32_t* node, const int32_t* target,
+                        const float* lse) {
+  const ggnn_status st = check_rows(dt, n_nodes, H, n_rows, V, X, W, bias, node);
+  if (st != GGNN_OK) return st;
   CHECK_OPT_PTR(target, "target");
   if (n_rows > 0) CHECK_PTR(lse, "lse");
   return GGNN_OK;
@@ -141,6 +148,37 @@ ggnn_status check_distill(int32_t n_rows, int32_t K, const int32_t* t_id, const 
     CHECK_PTR(loss, "loss");
   }
   CHECK_OPT_PTR(t_lse, "teacher_lse");
+  return GGNN_OK;
+}
+
+bool top_sizes(int32_t dt, int32_t H, int32_t n_rows, int32_t V, int32_t K, int64_t n_listed) {
+  return supported_dtype(dt) && supported_H(H) && n_rows > 0 && n_rows <= kMaxRows && V >= 1 &&
+         (int64_t)V * H < ((int64_t)1 << 31) && K >= 1 && K <= kMaxList && n_listed >= 0 && n_listed <= kMaxTokens;
+}
+
+ggnn_status check_rules(int32_t V, const ggnn_token_rules* u) {
+  if (u == nullptr) return GGNN_OK;
+  GGNN_CHECK_ARG(u->n_masks >= 0, "n_masks=%d must not be negative", u->n_masks);
+  if (u->n_masks > 0) {
+    CHECK_PTR(u->mask, "mask");
+    GGNN_CHECK_ARG(u->mask_words >= (V + 31) / 32, "mask_words=%d must be at least %d for V=%d", u->mask_words,
+                   (V + 31) / 32, V);
+    CHECK_OPT_PTR(u->mask_of, "mask_of");
+  }
+  GGNN_CHECK_ARG(u->n_seen >= 0 && u->n_add >= 0 && (int64_t)u->n_seen + u->n_add <= kMaxTokens,
+                 "n_seen=%d and n_add=%d must not be negative, nor exceed 2^30 together", u->n_seen, u->n_add);
+  if (u->n_seen > 0) {
+    CHECK_PTR(u->seen_ptr, "seen_ptr");
+    CHECK_PTR(u->seen, "seen");
+    GGNN_CHECK_ARG(std::isfinite(u->repetition) && u->repetition > 0.f, "repetition=%g must be finite and positive",
+                   (double)u->repetition);
+    GGNN_CHECK_ARG(std::isfinite(u->presence) && std::isfinite(u->frequency), "presence and frequency must be finite");
+  }
+  if (u->n_add > 0) {
+    CHECK_PTR(u->add_ptr, "add_ptr");
+    CHECK_PTR(u->add, "add");
+    CHECK_PTR(u->value, "value");
+  }
   return GGNN_OK;
 }
 
@@ -329,6 +367,54 @@ ggnn_status ggnn_vocab_distill_grad(ggnn_dtype dt, int32_t n_nodes, int32_t H, i
   c.weight = weight; c.scale = scale; c.add = add != 0;
   c.dX = dX; c.dW = dW; c.dbias = dbias;
   return device_status(launch_vocab(dt, H, c, true, as_stream(stream)), "vocab_distill_grad");
+}
+
+size_t ggnn_vocab_top_workspace_bytes(ggnn_dtype dt, int32_t H, int32_t n_rows, int32_t V, int32_t K,
+                                      int64_t n_listed) {
+  if (!top_sizes(dt, H, n_rows, V, K, n_listed)) return 0;
+  return top_workspace(dt, H, n_rows, V, (int)n_listed);
+}
+
+ggnn_status ggnn_vocab_top(ggnn_dtype dt, int32_t n_nodes, int32_t H, int32_t n_rows, int32_t V, const void* X,
+                           const void* W, const float* bias, const int32_t* node, const ggnn_token_rules* rules,
+                           float temperature, int32_t K, int32_t* top, float* logit, float* lse, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+  clear_error();
+  ggnn_status st = check_rows(dt, n_nodes, H, n_rows, V, X, W, bias, node);
+  if (st != GGNN_OK) return st;
+  GGNN_CHECK_ARG(K >= 1 && K <= kMaxList, "K=%d must be in [1, %d]", K, kMaxList);
+  st = check_temperature(temperature);
+  if (st == GGNN_OK) st = check_rules(V, rules);
+  if (st != GGNN_OK) return st;
+  if (n_rows == 0) return GGNN_OK;
+  CHECK_PTR(top, "top");
+  CHECK_PTR(logit, "logit");
+  CHECK_OPT_PTR(lse, "lse");
+  TopArgs a{};
+  a.n_nodes = n_nodes; a.R = n_rows; a.V = V; a.K = K;
+  a.X = X; a.W = W; a.bias = bias; a.node = node;
+  a.temper = make_temper(temperature);
+  a.top = top; a.logit = logit; a.lse = lse;
+  a.repetition = 1.f;
+  if (rules != nullptr) {
+    if (rules->n_masks > 0) {
+      a.mask = rules->mask; a.mask_of = rules->mask_of;
+      a.n_masks = rules->n_masks; a.mask_words = rules->mask_words;
+    }
+    if (rules->n_seen > 0) {
+      a.seen_ptr = rules->seen_ptr; a.seen = rules->seen; a.n_seen = rules->n_seen;
+      a.repetition = rules->repetition; a.presence = rules->presence; a.frequency = rules->frequency;
+    }
+    if (rules->n_add > 0) {
+      a.add_ptr = rules->add_ptr; a.add = rules->add; a.value = rules->value; a.n_add = rules->n_add;
+    }
+  }
+  const size_t need = top_workspace(dt, H, n_rows, V, a.n_seen + a.n_add);
+  if (workspace == nullptr || workspace_bytes < need || !aligned16(workspace))
+    return fail(GGNN_ERR_WORKSPACE, "vocab_top needs a 16-byte aligned workspace of %zu bytes (got %zu)", need,
+                workspace ? workspace_bytes : (size_t)0);
+  a.ws = workspace;
+  return device_status(launch_top(dt, H, a, as_stream(stream)), "vocab_top");
 }
 
 }  // extern "C"

@@ -99,6 +99,26 @@ struct VocabArgs {
   bool add;
 };
 
+// Arguments of the best entries (csrc/vocab_top.hip), as in include/ggnn.h; without rules mask, seen_ptr and add_ptr are
+// NULL and the counts 0.
+struct TopArgs {
+  int n_nodes, R, V, K;
+  const void *X, *W;
+  const float* bias;
+  const int32_t* node;
+  Temper temper;
+  const uint32_t* mask;
+  const int32_t* mask_of;
+  int n_masks, mask_words;
+  const int32_t *seen_ptr, *seen, *add_ptr, *add;
+  const float* value;
+  int n_seen, n_add;
+  float repetition, presence, frequency;
+  int32_t* top;
+  float *logit, *lse;
+  void* ws;
+};
+
 // Supernode share of a fused bit-band step (the first 32 nodes are
 // supernodes): the slice bits of the step's direction, [E][n_pad][s/8] (the
 // column slice forward, the transposed row slice reverse), and the record
@@ -154,6 +174,9 @@ struct SnStep {
                           int n_tok, float scale, int mean, const Dropout& d, void* X, hipStream_t st);           \
   size_t vocab_workspace(int H, int R, int V, bool grad, int K);                                                  \
   hipError_t launch_vocab(int H, const VocabArgs& c, bool grad, hipStream_t st);                                  \
+  hipError_t launch_vocab_planes(size_t count, const void* W, void* planes, hipStream_t st);                      \
+  size_t top_workspace(int H, int R, int V, int n_listed);                                                        \
+  hipError_t launch_top(int H, const TopArgs& a, hipStream_t st);                                                 \
   bool step_wide_applies(int B, int H);                                                                           \
   hipError_t launch_step_wide(bool rev, int n_pad, int B, int H, int E, const void* bits, const void* V,          \
                               const void* Wsrc, const float* bias, float* out, const float* dX_in, void* dM,      \
@@ -481,6 +504,13 @@ inline size_t vocab_workspace(int dt, int H, int R, int V, bool grad, int K = 0)
 }
 inline hipError_t launch_vocab(int dt, int H, const VocabArgs& c, bool grad, hipStream_t st) {
   return GGNN_DT_PICK(launch_vocab, H, c, grad, st);
+}
+// The K best entries of chosen rows, under rules (n_listed: seen and added ones of all rows).
+inline size_t top_workspace(int dt, int H, int R, int V, int n_listed) {
+  return GGNN_DT_PICK(top_workspace, H, R, V, n_listed);
+}
+inline hipError_t launch_top(int dt, int H, const TopArgs& a, hipStream_t st) {
+  return GGNN_DT_PICK(launch_top, H, a, st);
 }
 // The table's gradient (float32 whatever the table's type), dtable +=; workspace
 // of embed_bwd_workspace bytes.

@@ -966,16 +966,18 @@ VocabPlan vocab_plan(int H, int R, int V, bool grad, int K = 0) {
   return p;
 }
 
+template <typename S>
+void make_planes(size_t count, const void* W, void* planes, hipStream_t st) {
+  hipLaunchKernelGGL(dev::vocab_planes_kernel<S>, dim3((unsigned)((count / 4 + dev::kVocThreads - 1) / dev::kVocThreads)),
+                     dim3(dev::kVocThreads), 0, st, count, static_cast<const S*>(W), static_cast<dev::bf16s*>(planes));
+}
 // The rows that the passes stage: W itself, or its planes.
 template <typename S>
 const dev::bf16s* staged_rows(const VocabArgs& c, int H, void* planes, hipStream_t st) {
   if constexpr (sizeof(S) == 2) {
     return static_cast<const dev::bf16s*>(c.W);
   } else {
-    const size_t count = (size_t)c.V * H;
-    hipLaunchKernelGGL(dev::vocab_planes_kernel<S>, dim3((unsigned)((count / 4 + dev::kVocThreads - 1) / dev::kVocThreads)),
-                       dim3(dev::kVocThreads), 0, st, count, static_cast<const S*>(c.W),
-                       static_cast<dev::bf16s*>(planes));
+    make_planes<S>((size_t)c.V * H, c.W, planes, st);
     return static_cast<const dev::bf16s*>(planes);
   }
 }
@@ -1096,6 +1098,11 @@ hipError_t vocab_h(const VocabArgs& c, bool grad, hipStream_t st) {
 namespace GGNN_IMPL_NS {
 size_t vocab_workspace(int H, int R, int V, bool grad, int K) {
   return vocab_plan<dev::dt_t>(H, R, V, grad, K).bytes;
+}
+
+hipError_t launch_vocab_planes(size_t count, const void* W, void* planes, hipStream_t st) {
+  make_planes<dev::dt_t>(count, W, planes, st);
+  return hipGetLastError();
 }
 
 hipError_t launch_vocab(int H, const VocabArgs& c, bool grad, hipStream_t st) {

@@ -73,6 +73,60 @@ def test_distillation_without_rows_succeeds_without_a_device():
                                  stream=0)   # add: nothing is cleared either
 
 
+TOP = dict(dt="bf16", n_nodes=100, H=64, n_rows=50, V=1000, X=P, W=Q, bias=None, node=S, rules=None, temperature=1.0, K=8,
+           top=S, logit=S, lse=None, workspace=S, workspace_bytes=1 << 40)
+
+
+def rules(**kw):
+    a = dict(mask=P, n_masks=3, mask_words=32, mask_of=Q, seen_ptr=P, seen=Q, n_seen=5, repetition=1.2, presence=0.1,
+             frequency=0.1, add_ptr=P, add=Q, value=P, n_add=4)
+    a.update(kw)
+    return dict(rules=capi.token_rules(**a))
+
+
+@pytest.mark.parametrize("kw,text", [
+    (dict(dt=5), "dtype"), (dict(n_nodes=0), "n_nodes"), (dict(H=16), "H="), (dict(n_rows=-1), "n_rows"),
+    (dict(n_rows=(1 << 24) + 1), "n_rows"), (dict(node=None, n_rows=101), "n_rows=101 exceeds"), (dict(V=0), "V="),
+    (dict(V=1 << 25), "V="), (dict(X=None), "X is NULL"), (dict(W=None), "W is NULL"), (dict(bias=P + 2), "bias is not"),
+    (dict(node=P + 4), "node is not"), (dict(K=0), "K=0"), (dict(K=65), "K=65"), (dict(temperature=0.0), "temperature"),
+    (dict(temperature=NAN), "temperature"), (dict(top=None), "top is NULL"), (dict(top=S + 4), "top is not"),
+    (dict(logit=None), "logit is NULL"), (dict(lse=S + 8), "lse is not"), (rules(n_masks=-1), "n_masks"),
+    (rules(mask=None), "mask is NULL"), (rules(mask_words=31), "mask_words=31"), (rules(mask_of=P + 4), "mask_of is not"),
+    (rules(n_seen=-1), "n_seen"), (rules(n_add=-2), "n_add"), (rules(n_seen=1 << 30), "2^30"),
+    (rules(seen_ptr=None), "seen_ptr is NULL"), (rules(seen=None), "seen is NULL"), (rules(repetition=0.0), "repetition"),
+    (rules(repetition=float("inf")), "repetition"), (rules(presence=NAN), "presence"),
+    (rules(frequency=float("inf")), "frequency"), (rules(add_ptr=None), "add_ptr is NULL"), (rules(add=None), "add is NULL"),
+    (rules(value=None), "value is NULL"), (rules(value=P + 8), "value is not")])
+def test_top_refuses(kw, text):
+    refused("GGNN_ERR_INVALID_ARG", text, capi.ggnn_vocab_top, *dict(TOP, **kw).values())
+
+
+def test_top_wants_its_workspace():
+    for ru, listed in ((None, 0), (rules()["rules"], 9), (rules(n_seen=0)["rules"], 4), (rules(n_add=0)["rules"], 5)):
+        need = capi.ggnn_vocab_top_workspace_bytes("bf16", 64, 50, 1000, 8, listed)
+        assert need > 0
+        for ws, size in ((None, need), (S, need - 1), (S + 8, need)):
+            refused("GGNN_ERR_WORKSPACE", f"{need} bytes", capi.ggnn_vocab_top,
+                    *dict(TOP, rules=ru, workspace=ws, workspace_bytes=size).values())
+    for bad in ((64, 0, 1000, 8, 0), (48, 50, 1000, 8, 0), (64, 50, 1 << 25, 8, 0), (64, 50, 1000, 65, 0),
+                (64, 50, 1000, 8, -1), (64, 50, 1000, 8, (1 << 30) + 1)):
+        assert capi.ggnn_vocab_top_workspace_bytes("bf16", *bad) == 0
+
+
+def test_top_without_rows_succeeds_without_a_device():
+    capi.ggnn_vocab_top(*dict(TOP, n_rows=0, top=None, logit=None, workspace=None, workspace_bytes=0).values(), stream=0)
+
+
+def test_rules_reference():
+    z = np.array([[2.0, -2.0, 1.0, 0.5]])
+    out = L.apply_rules(z, dict(seen=[[0, 1, 1, 9]], repetition=2.0, presence=0.5, frequency=0.25, add=[[(2, 1.0), (2, -3.0)]],
+                                mask=[[1, 1, 1, 0]]))
+    np.testing.assert_array_equal(out, [[1.0 - 0.75, -4.0 - 1.0, -1.0, -np.inf]])
+    ids, zk = L.best(out, 5)
+    np.testing.assert_array_equal(ids, [[0, 2, 1, -1, -1]])
+    np.testing.assert_array_equal(zk, [[0.25, -1.0, -5.0, -np.inf, -np.inf]])
+
+
 def test_distillation_reference_against_differences():
     rng = np.random.default_rng(0)
     n, H, V, rows, K = 9, 5, 13, 6, 4
