@@ -372,7 +372,7 @@ ggnn_status ggnn_vocab_distill_grad(ggnn_dtype dt, int32_t n_nodes, int32_t H, i
 size_t ggnn_vocab_top_workspace_bytes(ggnn_dtype dt, int32_t H, int32_t n_rows, int32_t V, int32_t K,
                                       int64_t n_listed) {
   if (!top_sizes(dt, H, n_rows, V, K, n_listed)) return 0;
-  return top_workspace(dt, H, n_rows, V, (int)n_listed);
+  return top_workspace(dt, H, n_rows, V, K, (int)n_listed);
 }
 
 ggnn_status ggnn_vocab_top(ggnn_dtype dt, int32_t n_nodes, int32_t H, int32_t n_rows, int32_t V, const void* X,
@@ -409,7 +409,7 @@ ggnn_status ggnn_vocab_top(ggnn_dtype dt, int32_t n_nodes, int32_t H, int32_t n_
       a.add_ptr = rules->add_ptr; a.add = rules->add; a.value = rules->value; a.n_add = rules->n_add;
     }
   }
-  const size_t need = top_workspace(dt, H, n_rows, V, a.n_seen + a.n_add);
+  const size_t need = top_workspace(dt, H, n_rows, V, K, a.n_seen + a.n_add);
   if (workspace == nullptr || workspace_bytes < need || !aligned16(workspace))
     return fail(GGNN_ERR_WORKSPACE, "vocab_top needs a 16-byte aligned workspace of %zu bytes (got %zu)", need,
                 workspace ? workspace_bytes : (size_t)0);

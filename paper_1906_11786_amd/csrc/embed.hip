@@ -740,16 +740,12 @@ EmbedLayout embed_layout(int H, int n_tok) {
   return l;
 }
 
-template <typename S, int H, bool LIST = false>
-hipError_t embed_bwd_h(int n, int V, const int32_t* tok_ptr, const int32_t* tok, int n_tok, float scale, int mean,
-                       const float* factor, const Dropout& d, const void* grad, float* dtable, char* ws,
-                       hipStream_t st, dev::ListRows list = {}) {
-  const S* dX = static_cast<const S*>(grad);
+// Sorts the listings by token, those outside [0, V) last, into *sorted (token, row or position).
+hipError_t sort_listings(const EmbedLayout& l, int n_tok, int n, int V, const int32_t* tok_ptr, const int32_t* tok,
+                         char* ws, dev::u32x2** sorted, hipStream_t st) {
   using namespace dev;
-  const EmbedLayout l = embed_layout(H, n_tok);
   u32x2 *a = reinterpret_cast<u32x2*>(ws + l.a), *b = reinterpret_cast<u32x2*>(ws + l.b);
   uint32_t *count = reinterpret_cast<uint32_t*>(ws + l.count), *total = reinterpret_cast<uint32_t*>(ws + l.total);
-  float* part = reinterpret_cast<float*>(ws + l.part);
   int bits = 1;
   while (bits < 31 && (V >> bits) != 0) ++bits;   // keys 0 .. V
   const int passes = (bits + 7) / 8, per = (bits + passes - 1) / passes;
@@ -774,6 +770,21 @@ hipError_t embed_bwd_h(int n, int V, const int32_t* tok_ptr, const int32_t* tok,
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
   }
+  *sorted = a;
+  return hipSuccess;
+}
+
+template <typename S, int H, bool LIST = false>
+hipError_t embed_bwd_h(int n, int V, const int32_t* tok_ptr, const int32_t* tok, int n_tok, float scale, int mean,
+                       const float* factor, const Dropout& d, const void* grad, float* dtable, char* ws,
+                       hipStream_t st, dev::ListRows list = {}) {
+  const S* dX = static_cast<const S*>(grad);
+  using namespace dev;
+  const EmbedLayout l = embed_layout(H, n_tok);
+  float* part = reinterpret_cast<float*>(ws + l.part);
+  u32x2* a = nullptr;
+  const hipError_t err = sort_listings(l, n_tok, n, V, tok_ptr, tok, ws, &a, st);
+  if (err != hipSuccess) return err;
   if (d.cut != 0 && !LIST) {
     hipLaunchKernelGGL((embed_runs_kernel<S, H, true>), dim3(l.blocks), dim3(kEmbThreads), 0, st, n_tok, n, V, l.chunk,
                        a, tok_ptr, scale, mean, factor, d, dX, dtable, part, list);
@@ -802,6 +813,15 @@ hipError_t launch_embed_bwd(int n, int H, int V, const int32_t* tok_ptr, const i
     case 256: return embed_bwd_h<float, 256>(n, V, tok_ptr, tok, n_tok, scale, mean, nullptr, d, dX, dtable, w, st);
   }
   return hipErrorInvalidValue;
+}
+
+size_t sort_workspace(int n) { return embed_layout(32, n).part; }
+
+hipError_t launch_sort(int n, int V, const int32_t* id, void* ws, const void** sorted, hipStream_t st) {
+  dev::u32x2* a = nullptr;
+  const hipError_t err = sort_listings(embed_layout(32, n), n, n, V, nullptr, id, static_cast<char*>(ws), &a, st);
+  *sorted = a;
+  return err;
 }
 
 size_t list_rows_workspace(int H, int n) {

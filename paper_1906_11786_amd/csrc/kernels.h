@@ -30,6 +30,10 @@ struct ReduceSeg {
 size_t target_rows_workspace(int H, int R);
 hipError_t launch_target_rows(int R, int H, int V, const int32_t* target, const void* x, float scale,
                               const float* factor, float* dW, void* ws, hipStream_t st);
+// (id[i], i) of n ids sorted by id (stable; those outside [0, V) last, as V), 8 bytes each, at *sorted within the
+// workspace of sort_workspace bytes (csrc/embed.hip).
+size_t sort_workspace(int n);
+hipError_t launch_sort(int n, int V, const int32_t* id, void* ws, const void** sorted, hipStream_t st);
 // dW[id[l]] += coef[l] x[node[l / K]], dbias[id[l]] += coef[l] (NULL: none) over the R K listings l sorted by id
 // (negative: none); node NULL: row r is node r.  Workspace of list_rows_workspace bytes, n = R K listings.
 size_t list_rows_workspace(int H, int n);
@@ -175,7 +179,7 @@ struct SnStep {
   size_t vocab_workspace(int H, int R, int V, bool grad, int K);                                                  \
   hipError_t launch_vocab(int H, const VocabArgs& c, bool grad, hipStream_t st);                                  \
   hipError_t launch_vocab_planes(size_t count, const void* W, void* planes, hipStream_t st);                      \
-  size_t top_workspace(int H, int R, int V, int n_listed);                                                        \
+  size_t top_workspace(int H, int R, int V, int K, int n_listed);                                                 \
   hipError_t launch_top(int H, const TopArgs& a, hipStream_t st);                                                 \
   bool step_wide_applies(int B, int H);                                                                           \
   hipError_t launch_step_wide(bool rev, int n_pad, int B, int H, int E, const void* bits, const void* V,          \
@@ -506,8 +510,8 @@ inline hipError_t launch_vocab(int dt, int H, const VocabArgs& c, bool grad, hip
   return GGNN_DT_PICK(launch_vocab, H, c, grad, st);
 }
 // The K best entries of chosen rows, under rules (n_listed: seen and added ones of all rows).
-inline size_t top_workspace(int dt, int H, int R, int V, int n_listed) {
-  return GGNN_DT_PICK(top_workspace, H, R, V, n_listed);
+inline size_t top_workspace(int dt, int H, int R, int V, int K, int n_listed) {
+  return GGNN_DT_PICK(top_workspace, H, R, V, K, n_listed);
 }
 inline hipError_t launch_top(int dt, int H, const TopArgs& a, hipStream_t st) {
   return GGNN_DT_PICK(launch_top, H, a, st);

@@ -23,17 +23,30 @@ namespace dev {
 constexpr int kTopMost = 64;   // K at most: a lane holds one of a wave's best
 constexpr int kTopBlock = 16;
 
-// 32-row tiles of a wave: an LDS fragment serves both of two.  (float32 at H = 256
-// has no registers for a second one's planes.)
+// The first pass walks the entries in units of 128, in LDS chunks of top_chunk.
+constexpr int kTopUnit = 128;
+template <typename S>
+constexpr int top_chunk(int H) {
+  return sizeof(S) == 2 || H <= 64 ? 128 : H == 128 ? 64 : 32;
+}
+// 32-row tiles of a wave: an LDS fragment serves both of two.
 template <typename S>
 constexpr int top_tiles(int H) {
-  return sizeof(S) == 4 && H >= 256 ? 1 : 2;
+  return sizeof(S) == 4 ? (H >= 128 ? 1 : 2) : H >= 256 ? 2 : 1;
 }
-// Waves of a SIMD, by the registers of a wave's rows and at H >= 128 the buffers.
+// Waves of a workgroup, which share its LDS chunks, and its rows.
+template <typename S>
+constexpr int top_group(int H) {
+  return sizeof(S) == 4 && H >= 256 ? 4 : 8;
+}
+template <typename S>
+constexpr int top_rows(int H) {
+  return 32 * top_tiles<S>(H) * top_group<S>(H);
+}
+// Waves of a SIMD, by the registers of a wave's rows and the buffers.
 template <typename S>
 constexpr int top_waves(int H) {
-  if (sizeof(S) == 4) return H >= 128 ? 1 : H == 64 ? 2 : 3;
-  return H >= 256 ? 1 : H == 128 ? 2 : H == 64 ? 3 : 4;
+  return sizeof(S) == 4 ? (H >= 256 ? 1 : 2) : H >= 256 ? 2 : 4;
 }
 
 // A 32 x 32 tile of logits has entries as its rows.  Entry r of a tile is put on row
@@ -41,23 +54,6 @@ constexpr int top_waves(int H) {
 // block, in order.
 __device__ __forceinline__ int top_row(int r) { return 8 * ((r >> 2) & 3) + 4 * (r >> 4) + (r & 3); }
 __device__ __forceinline__ int top_entry(int i) { return 16 * ((i >> 2) & 1) + 4 * (i >> 3) + (i & 3); }
-
-// As stage_tile, with the places of a row's pieces by its row in the tile of logits
-// (the rows that sixteen lanes read at once).
-template <int H, int NP, int T>
-__device__ __forceinline__ void stage_entries(const bf16s* __restrict__ src, size_t plane, long row0, long last,
-                                              uint32_t lds, int wave, int lane) {
-  constexpr int CPR = H / 8, EACH = T * CPR / 64, PIECES = NP * EACH;
-#pragma unroll
-  for (int p = 0; p < (PIECES + kVocWaves - 1) / kVocWaves; ++p) {
-    const int piece = p * kVocWaves + wave, q = piece % EACH * 64 + lane;
-    if (PIECES % kVocWaves != 0 && piece >= PIECES) break;
-    const int r = q / CPR, c = (q % CPR) ^ swz<H>(top_row(r % 32));
-    const long row = row0 + r < last ? row0 + r : last;
-    dma16(src + piece / EACH * plane + row * H + 8 * c,
-          __builtin_amdgcn_readfirstlane(lds + (uint32_t)piece * 1024u));
-  }
-}
 
 // Bit masks over the entries, one a row: index of[r] (r where of is NULL); one
 // outside [0, n) excludes nothing.
@@ -91,49 +87,71 @@ struct RowSum {
   float m, k, l;
 };
 
-// First pass.  A workgroup holds 128 NT rows, NT tiles of 32 a wave, and walks a share of
-// the vocabulary in tiles staged in LDS, dealt and buffered as in the losses' rows
-// pass (csrc/vocab.hip).  Writes block maxima to bmax [R][nbs] and, where LSE, (m, l)
-// of a share to pm, pl [slot][128 NT].
+// First pass.  A workgroup holds its waves' rows (NT tiles of 32 a wave) and
+// walks a share of the vocabulary, dealt in units of 128 entries as the losses' passes
+// deal theirs (csrc/vocab.hip).  Writes block maxima to bmax [R][nbs] and, where LSE,
+// (m, l) of a share to pm, pl [slot][rows of a workgroup].
+//
+// There is no second product here, so a step is its products and then its
+// exponentials, and the waves that share a SIMD fill each other's.  LDS holds the
+// entries in the order in which lanes read them as fragments, 1 KB a fragment, so
+// that a read's place is a constant; the copies, 32 bytes a row each, pay for that
+// order, and their addresses are constants too but in the last chunk.
 template <typename S, int H, bool LSE, bool MASK>
-__global__ __launch_bounds__(kVocThreads, top_waves<S>(H)) void vocab_max_kernel(
+__global__ __launch_bounds__(kWave* top_group<S>(H), top_waves<S>(H)) void vocab_max_kernel(
     int n_nodes, int R, int V, Deal deal, Temper te, const S* __restrict__ X, const bf16s* __restrict__ W,
     const float* __restrict__ bias, const int32_t* __restrict__ node, RowMask rm, float* __restrict__ bmax, int nbs,
     float* __restrict__ pm, float* __restrict__ pl) {
-  constexpr int T = voc_tile<S>(), NP = voc_planes<S>(), NT = top_tiles<S>(H), SUB = T / 32, NS = H / 16, NF = NS * NP;
-  constexpr int kAhead = NF < 8 ? NF : 8, VS = NS < 8 ? NS : 8;
-  constexpr uint32_t ROW = H * 2, PLANE = T * ROW, TILE = NP * PLANE;
-  __shared__ __attribute__((aligned(1024))) bf16s tile[kVocBufs][NP * T * H];
-  __shared__ __attribute__((aligned(16))) float tb[kVocBufs][T];
+  constexpr int T = top_chunk<S>(H), NP = voc_planes<S>(), NT = top_tiles<S>(H), NS = H / 16, NF = NS * NP;
+  constexpr int SUB = T / 32, CH = kTopUnit / T, ROWS = top_rows<S>(H), WAVES = top_group<S>(H);
+  constexpr int kAhead = NF < 4 ? NF : 4, STEPS = kTopUnit / 32;
+  constexpr uint32_t ROW = H * 2, CHUNK = SUB * NF * 1024;   // bytes of a row and of a buffer
+  __shared__ __attribute__((aligned(1024))) char buffer[2][CHUNK];
+  __shared__ __attribute__((aligned(16))) float tb[2][T];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), g = lane / 32;
-  const uint32_t lds0 = (uint32_t)(uintptr_t)tile[0];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)buffer[0];
   typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
 
+  const uint32_t from = (uint32_t)top_entry(lane % 32) * ROW + 16u * g;   // of a lane's copies, from a step's first row
   float nb = 0.f;
   Run run;
   Dealt dealt(deal, blockIdx.x);
-  for (int round = 0; dealt.next(deal, blockIdx.x, &run); ++round) {
-    const int t0 = run.t0, t1 = run.t1;
-    const int row0 = run.i * (kVocRows * NT) + wave * 32 * NT + lane % 32;   // of the lane's first tile
+  while (dealt.next(deal, blockIdx.x, &run)) {
+    const int q0 = run.t0 * CH, q1 = run.t1 * CH;                  // chunks
+    const int row0 = run.i * ROWS + wave * 32 * NT + lane % 32;   // of the lane's first tile
     bf16x8 x[NT][NP][NS];
     RowSum sum[NT];
     const uint32_t* mrow[NT];
-    uint32_t word[NT][SUB], next_word[NT][SUB];   // mask bits of the tile in use and of the one on its way
-    auto fetch = [&](int t, int buf) {   // start the copies of tile t < t1
-      stage_entries<H, NP, T>(W, (size_t)V * H, (long)t * T, V - 1, lds0 + (uint32_t)buf * TILE, wave, lane);
+    uint32_t word[NT][SUB], next_word[NT][SUB];   // mask bits of the chunk in use and of the one on its way
+    auto fetch = [&](int q) {   // start the copies of chunk q
+      const char* src = reinterpret_cast<const char*>(W) + (size_t)q * T * ROW;
+      const uint32_t to = lds0 + (uint32_t)(q & 1) * CHUNK;
+      const bool whole = (q + 1) * T <= V;
+#pragma unroll
+      for (int p = 0; p < (SUB * NF + WAVES - 1) / WAVES; ++p) {
+        const int i = p * WAVES + wave, s = i / NF, n = i % NF;
+        if (SUB * NF % WAVES != 0 && i >= SUB * NF) break;
+        const size_t at = (size_t)(n % NP) * V * ROW + (uint32_t)(32 * s) * ROW + 32u * (n / NP);
+        if (whole) {
+          dma16(src + at, from, to + (uint32_t)i * 1024u);
+        } else {   // the last entry's row in place of those beyond
+          const int row = min(q * T + 32 * s + top_entry(lane % 32), V - 1);
+          dma16(W + (size_t)(n % NP) * V * H + (size_t)row * H + 16 * (n / NP) + 8 * g, to + (uint32_t)i * 1024u);
+        }
+      }
       // (raw values: a use here would wait for the copies too)
-      if (bias != nullptr && threadIdx.x < T) nb = bias[min(t * T + (int)threadIdx.x, V - 1)];
+      if (bias != nullptr && threadIdx.x < T) nb = bias[min(q * T + (int)threadIdx.x, V - 1)];
       if constexpr (MASK) {
 #pragma unroll
         for (int a = 0; a < NT; ++a)
 #pragma unroll
           for (int i = 0; i < SUB; ++i)
-            next_word[a][i] = mrow[a] != nullptr ? mrow[a][min(t * SUB + i, rm.words - 1)] : ~0u;
+            next_word[a][i] = mrow[a] != nullptr ? mrow[a][min(q * SUB + i, rm.words - 1)] : ~0u;
       }
     };
-    auto land = [&](int t, int buf) {   // and wait for those started last, of tile t
+    auto land = [&](int q) {   // and wait for those of chunk q; every wave has left the other buffer
       if (threadIdx.x < T)
-        tb[buf][threadIdx.x] = t * T + (int)threadIdx.x >= V || nb <= kMaskedBias ? -INFINITY : nb;
+        tb[q & 1][threadIdx.x] = q * T + (int)threadIdx.x >= V || nb <= kMaskedBias ? -INFINITY : nb;
       if constexpr (MASK) {
 #pragma unroll
         for (int a = 0; a < NT; ++a)
@@ -143,129 +161,69 @@ __global__ __launch_bounds__(kVocThreads, top_waves<S>(H)) void vocab_max_kernel
       wait_copies<0>();
       __syncthreads();
     };
-    if (round > 0) __syncthreads();   // every wave has left the buffers of the run before
+    const uint32_t place = (uint32_t)(lane % 32) * (uint32_t)nbs + 4u * g;   // in bmax, from the wave's first row on
+    float* wave_max = bmax + (size_t)(run.i * ROWS + wave * 32 * NT) * nbs;
+
+    __syncthreads();   // every wave has left the buffers of the run before
 #pragma unroll
     for (int a = 0; a < NT; ++a) mrow[a] = MASK ? rm.row(row0 + 32 * a, R) : nullptr;
-    uint32_t as[VS];   // LDS addresses of the fragments; the other ones lie 256 bytes, rows or planes on
-#pragma unroll
-    for (int k = 0; k < VS; ++k)
-      as[k] = lds0 + (uint32_t)top_entry(lane % 32) * ROW + 16u * ((2 * k + g) ^ swz<H>(lane % 32));
-    bf16x8 f[NF];   // at most kAhead are alive
-    auto read = [&](int n, int rs) {   // fragment n of the tile rows from rs on: k step n / NP, plane n % NP
-      const int kk = n / NP;
-      f[n] = __builtin_bit_cast(bf16x8, *(lds_u32x4*)(as[kk % VS] + 256u * (kk / VS) + (uint32_t)rs * ROW +
-                                                      (uint32_t)(n % NP) * PLANE));
-    };
-    f32x16 s[NT];
-    float top[NT];
-    auto start = [&](f32x16 (&acc)[NT], int buf, int rs) {   // biases of a tile's entries
-      f32x16 b;
-#pragma unroll
-      for (int j4 = 0; j4 < 4; ++j4) {
-        const f32x4 v = *reinterpret_cast<const f32x4*>(tb[buf] + rs + 16 * g + 4 * j4);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) b[4 * j4 + i] = v[i];
-      }
-#pragma unroll
-      for (int a = 0; a < NT; ++a) acc[a] = b;
-    };
-    // acc += logits of the tile rows from rs on; work(i), i < 16 NT, is done alongside
-    auto logits = [&](f32x16 (&acc)[NT], int rs, auto work) {
-#pragma unroll
-      for (int n = 0; n < kAhead; ++n) read(n, rs);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int n = 0; n < NF; ++n) {
-        if (n + kAhead < NF) read(n + kAhead, rs);
-#pragma unroll
-        for (int b = 0; b + n % NP < NP; ++b)
-#pragma unroll
-          for (int a = 0; a < NT; ++a) mma32(acc[a], f[n], x[a][b][n / NP]);
-#pragma unroll
-        for (int i = n * 16 * NT / NF; i < (n + 1) * 16 * NT / NF; ++i) work(i);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    };
-    auto finish = [&](f32x16 (&acc)[NT], float (&t)[NT], int sub) {
-#pragma unroll
-      for (int a = 0; a < NT; ++a) {
-        if constexpr (MASK) take_out(acc[a], word[a][sub]);
-        t[a] = max16(acc[a]);
-      }
-    };
-    // Block maxima: four tiles' are kept, then a row's eight blocks are stored as 32 bytes
-    // by its two lanes; at a run's ends, one by one.
-    float kept[NT][4];
-    int n_kept = 0;
-    auto store_kept = [&](int last, bool whole) {   // `last`: tile of kept[.][3]
-#pragma unroll
-      for (int a = 0; a < NT; ++a) {
-        const int r = row0 + 32 * a;
-        if (whole) {
-          const auto u = __builtin_amdgcn_permlane32_swap(__float_as_uint(kept[a][0]), __float_as_uint(kept[a][2]),
-                                                          false, false);
-          const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(kept[a][1]), __float_as_uint(kept[a][3]),
-                                                          false, false);
-          if (r < R)
-            *reinterpret_cast<u32x4*>(bmax + (size_t)r * nbs + 2 * (last - 3) + 4 * g) = u32x4{u[0], u[1], w[0], w[1]};
-        } else if (r < R) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (e < n_kept) bmax[(size_t)r * nbs + 2 * (last - e) + g] = kept[a][3 - e];
-        }
-      }
-      n_kept = 0;
-    };
-    auto keep = [&](int t) {   // maxima of tile t
-#pragma unroll
-      for (int a = 0; a < NT; ++a) {
-#pragma unroll
-        for (int e = 0; e < 3; ++e) kept[a][e] = kept[a][e + 1];
-        kept[a][3] = top[a];
-      }
-      ++n_kept;
-      if (t % 4 == 3) store_kept(t, n_kept == 4);
-    };
-
-    int buf = 0;
-    fetch(t0, 0);
+    fetch(q0);
 #pragma unroll
     for (int a = 0; a < NT; ++a) {
       load_planes<S, H>(x[a], X, row_node(node, row0 + 32 * a, R, n_nodes), lane);
       sum[a] = RowSum{kNoMax, te.near, 0.f};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) kept[a][e] = -INFINITY;
     }
-    land(t0, 0);
-    if (t0 + 1 < t1) fetch(t0 + 1, 1);
-    start(s, 0, 0);
-    logits(s, 0, [](int) {});
-    finish(s, top, 0);
-    for (int t = t0; t < t1; ++t) {
-      const int nbuf = next_buf(buf);
+#pragma unroll 1
+    for (int q = q0; q < q1; q += CH) {
+      float kept[NT][STEPS];   // block maxima of the unit
 #pragma unroll
-      for (int r0 = 0; r0 < T; r0 += 32) {
-        const bool last = r0 + 32 >= T;
-        const int rs = last ? 0 : r0 + 32;   // of the next tile (after the last one: of what the buffer holds, not used)
-        if (last) {
-          land(t + 1, nbuf);
-          if (t + 2 < t1) fetch(t + 2, next_buf(nbuf));
-#pragma unroll
-          for (int k = 0; k < VS; ++k) as[k] += buf_step<TILE>(nbuf);
+      for (int step = 0; step < STEPS; ++step) {
+        const int c = q + step / SUB, sub = step % SUB;
+        if (sub == 0) {
+          land(c);
+          if (c + 1 < q1) fetch(c + 1);
         }
-        f32x16 sn[NT];
-        start(sn, last ? nbuf : buf, rs);
-        keep(t * SUB + r0 / 32);
+        const uint32_t at = lds0 + (uint32_t)(c & 1) * CHUNK + 16u * lane;
+        bf16x8 f[NF];   // at most kAhead are alive
+        auto read = [&](int n) {   // fragment n: k step n / NP, plane n % NP
+          f[n] = __builtin_bit_cast(bf16x8, *(lds_u32x4*)(at + (uint32_t)(sub * NF + n) * 1024u));
+        };
+#pragma unroll
+        for (int n = 0; n < kAhead; ++n) read(n);
+        f32x16 s[NT], b;
+#pragma unroll
+        for (int j4 = 0; j4 < 4; ++j4) {
+          const f32x4 v = *reinterpret_cast<const f32x4*>(tb[c & 1] + 32 * sub + 16 * g + 4 * j4);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) b[4 * j4 + i] = v[i];
+        }
+#pragma unroll
+        for (int a = 0; a < NT; ++a) s[a] = b;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int n = 0; n < NF; ++n) {
+          if (n + kAhead < NF) read(n + kAhead);
+#pragma unroll
+          for (int p = 0; p + n % NP < NP; ++p)
+#pragma unroll
+            for (int a = 0; a < NT; ++a) mma32(s[a], f[n], x[a][p][n / NP]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int a = 0; a < NT; ++a) {
+          if constexpr (MASK) take_out(s[a], word[a][sub]);
+          kept[a][step] = max16(s[a]);
+        }
         if constexpr (LSE) {
           // (the maximum follows where it would grow by more than 2^8, as in the losses' rows pass)
           bool grows = false;
 #pragma unroll
-          for (int a = 0; a < NT; ++a) grows |= top[a] * sum[a].k > sum[a].m + 8.f;
+          for (int a = 0; a < NT; ++a) grows |= kept[a][step] * sum[a].k > sum[a].m + 8.f;
           if (__ballot(grows)) {
 #pragma unroll
             for (int a = 0; a < NT; ++a) {
-              const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top[a]), __float_as_uint(top[a]), false,
-                                                               false);
+              const uint32_t own = __float_as_uint(kept[a][step]);
+              const auto sw = __builtin_amdgcn_permlane32_swap(own, own, false, false);
               const float z = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])), kn = exponent_factor(z, te);
               const float mn = fmaxf(sum[a].m, z * kn);
               if (mn > sum[a].m) sum[a].k = kn;
@@ -273,26 +231,38 @@ __global__ __launch_bounds__(kVocThreads, top_waves<S>(H)) void vocab_max_kernel
               sum[a].m = mn;
             }
           }
-          __builtin_amdgcn_sched_barrier(0);
-          logits(sn, rs, [&](int i) {
-            const int a = i / 16, j = i % 16;
-            sum[a].l += __builtin_amdgcn_exp2f(fmaf(s[a][j], sum[a].k, -sum[a].m));
-          });
-        } else {
-          logits(sn, rs, [](int) {});
-        }
-        finish(sn, top, last ? 0 : r0 / 32 + 1);
 #pragma unroll
-        for (int a = 0; a < NT; ++a) s[a] = sn[a];
+          for (int a = 0; a < NT; ++a)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              sum[a].l += __builtin_amdgcn_exp2f(fmaf(s[a][j], sum[a].k, -sum[a].m));
+              if (j % 8 == 7) {   // (or all arguments are held at once, and the next step's products come first)
+                keep_here(sum[a].l);
+                __builtin_amdgcn_sched_barrier(0);
+              }
+            }
+        } else {
+#pragma unroll
+          for (int a = 0; a < NT; ++a) keep_here(kept[a][step]);
+        }
       }
-      buf = nbuf;
+      // A row's eight maxima are stored as 32 bytes by its two lanes.
+#pragma unroll
+      for (int a = 0; a < NT; ++a) {
+        const auto u = __builtin_amdgcn_permlane32_swap(__float_as_uint(kept[a][0]), __float_as_uint(kept[a][2]), false,
+                                                        false);
+        const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(kept[a][1]), __float_as_uint(kept[a][3]), false,
+                                                        false);
+        if (row0 + 32 * a < R)
+          *reinterpret_cast<u32x4*>(wave_max + (size_t)(32 * a) * nbs + (q / CH) * (kTopUnit / kTopBlock) + place) =
+              u32x4{u[0], u[1], w[0], w[1]};
+      }
     }
-    if (n_kept > 0) store_kept(t1 * SUB - 1, false);
     if constexpr (LSE) {
 #pragma unroll
       for (int a = 0; a < NT; ++a) {
         const float l = sum[a].l + __shfl_xor(sum[a].l, 32);
-        const size_t at = (size_t)run.slot * (kVocRows * NT) + wave * 32 * NT + 32 * a + lane % 32;
+        const size_t at = (size_t)run.slot * ROWS + wave * 32 * NT + 32 * a + lane % 32;
         if (g == 0) {
           pm[at] = sum[a].m;
           pl[at] = l;
@@ -470,29 +440,42 @@ __global__ __launch_bounds__(kVocThreads) void vocab_rules_kernel(int R, int V, 
 
 // ---- second pass -----------------------------------------------------------
 
-// A candidate as one number that orders by value, then by the lower index; 0: none
-// (-inf and NaN too).
-typedef unsigned long long pick_t;
-__device__ __forceinline__ pick_t key_of(float z, uint32_t index) {
-  z += 0.f;   // -0 counts as 0
+// A float as a whole number that orders alike, 0 for -inf and NaN; -0 counts as 0.
+__device__ __forceinline__ uint32_t order_of(float z) {
+  z += 0.f;
   const uint32_t u = __float_as_uint(z);
-  return z > -INFINITY ? (pick_t)(u ^ (u >> 31 ? ~0u : 0x80000000u)) << 32 | (uint32_t)~index : 0;
+  return z > -INFINITY ? u ^ (u >> 31 ? ~0u : 0x80000000u) : 0u;
 }
-__device__ __forceinline__ uint32_t key_index(pick_t k) { return ~(uint32_t)k; }
-__device__ __forceinline__ float key_value(pick_t k) {
+// A candidate as one number that orders by value, then by the lower index; 0: none.
+typedef unsigned long long pick_t;
+__device__ __forceinline__ pick_t pick_of(uint32_t order, uint32_t index) {
+  return order != 0 ? (pick_t)order << 32 | (uint32_t)~index : 0;
+}
+__device__ __forceinline__ uint32_t pick_index(pick_t k) { return ~(uint32_t)k; }
+__device__ __forceinline__ float pick_value(pick_t k) {
   const uint32_t u = (uint32_t)(k >> 32);
   return k == 0 ? -INFINITY : __uint_as_float(u ^ (u >> 31 ? 0x80000000u : ~0u));
 }
-__device__ __forceinline__ pick_t key_at(pick_t k, int lane) {   // lane: the same in the whole wave
+__device__ __forceinline__ pick_t pick_at(pick_t k, int lane) {   // lane: the same in the whole wave
   return (pick_t)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32 |
          (uint32_t)__builtin_amdgcn_readlane((int)k, lane);
 }
+// The K-th largest of the wave's numbers a and b (0 where fewer are not 0), bit by bit.
+__device__ __forceinline__ uint32_t kth_of(uint32_t a, uint32_t b, int K) {
+  uint32_t t = 0;
+#pragma unroll
+  for (int bit = 31; bit >= 0; --bit) {
+    const uint32_t c = t | 1u << bit;
+    if (__popcll(__ballot(a >= c)) + __popcll(__ballot(b >= c)) >= K) t = c;
+  }
+  return t;
+}
 
-// The 64 largest keys seen, in descending order over the lanes.
+// The 64 largest picks seen, in descending order over the lanes.
 struct Best {
   pick_t k = 0;
-  // Bitonic steps over lanes at distances d, d / 2, ... 1 within groups of `group` lanes,
-  // descending where the group's number is even.
+  // Bitonic steps over lanes at distances d, d / 2, ... 1, descending where the number of
+  // a group of `group` lanes is even.
   static __device__ __forceinline__ void steps(pick_t& v, int group, int d, int lane) {
     for (; d >= 1; d /= 2) {
       const pick_t o = __shfl_xor(v, d);
@@ -501,6 +484,7 @@ struct Best {
     }
   }
   static __device__ __forceinline__ void sort(pick_t& v, int lane) {
+#pragma unroll
     for (int group = 2; group <= kWave; group *= 2) steps(v, group, group / 2, lane);
   }
   // Joins another descending list.
@@ -508,17 +492,16 @@ struct Best {
     k = max(k, __shfl(other, kWave - 1 - lane));
     steps(k, kWave, kWave / 2, lane);
   }
-  // Adds one key a lane; K: how many of the largest matter.
+  // Adds one pick a lane; K: how many of the largest matter.
   __device__ __forceinline__ void add(pick_t c, int K, int lane) {
-    pick_t least = key_at(k, K - 1);
-    uint64_t in = __ballot(c > least);
+    uint64_t in = __ballot(c > pick_at(k, K - 1));
     if (__popcll(in) > 6) {   // about where sorting all costs less than one at a time
       sort(c, lane);
       join(c, lane);
       return;
     }
     while (in != 0) {
-      const pick_t one = key_at(c, (int)__builtin_ctzll(in));
+      const pick_t one = pick_at(c, (int)__builtin_ctzll(in));
       in &= in - 1;
       const int place = __popcll(__ballot(k > one));
       const pick_t up = __shfl_up(k, 1);
@@ -526,6 +509,31 @@ struct Best {
     }
   }
 };
+
+// Writes a row's answers from its n <= 64 picks in LDS, in no order: each lane counts
+// how many come before its own.
+__device__ __forceinline__ void answer(const pick_t* picks, int n, int r, int K, int lane, int32_t* __restrict__ top,
+                                       float* __restrict__ logit) {
+  const pick_t own = lane < n ? picks[lane] : 0;
+  int rank = 0;
+#pragma unroll 8
+  for (int i = 0; i < n; ++i) rank += picks[i] > own;
+  if (lane < n && rank < K) {
+    top[(size_t)r * K + rank] = (int32_t)pick_index(own);
+    logit[(size_t)r * K + rank] = pick_value(own);
+  }
+  if (lane >= n && lane < K) {
+    top[(size_t)r * K + lane] = -1;
+    logit[(size_t)r * K + lane] = -INFINITY;
+  }
+}
+// The same from a list in order, one pick a lane.
+__device__ __forceinline__ void answer_list(pick_t k, int r, int K, int lane, int32_t* __restrict__ top,
+                                            float* __restrict__ logit) {
+  if (lane >= K) return;
+  top[(size_t)r * K + lane] = k != 0 ? (int32_t)pick_index(k) : -1;
+  logit[(size_t)r * K + lane] = pick_value(k);
+}
 
 struct TopRows {   // arguments of the second pass
   int n_nodes, R, V, K, nbs, splits, share_rows;
@@ -537,75 +545,36 @@ struct TopRows {   // arguments of the second pass
   const float *bmax, *pm, *pl;
   Listing list;
   const int32_t* ent_id;
-  const uint32_t* ent_count;
+  uint32_t* ent_count;   // taken over for order_of the ruled logits
   const float* ent_add;
   float repetition, presence, frequency;
   int32_t* top;
   float *logit, *lse;
 };
 
-// Second pass: WPR waves per row (1: four rows a workgroup).  Blocks are picked from
-// their maxima, 64 entries at a time are formed as four 16 x 16 tiles (the state in all
-// columns, so that each lane finds one entry's logit among its accumulators).
-template <typename S, int H, int WPR>
-__global__ __launch_bounds__(WPR == 1 ? kVocThreads : kWave* WPR) void vocab_pick_kernel(TopRows c,
-                                                                                        const S* __restrict__ X,
-                                                                                        const S* __restrict__ W) {
-  __shared__ pick_t lists[WPR == 1 ? 1 : WPR][kWave];
-  __shared__ float sums[WPR][4];
-  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int r = WPR == 1 ? blockIdx.x * kVocWaves + wave : blockIdx.x, w0 = WPR == 1 ? 0 : wave;
-  if (r >= c.R) return;   // whole waves, and where a workgroup shares a row all of it, leave together
-  const int n = row_node(c.node, r, c.R, c.n_nodes), q = lane % 16, kg = lane / 16;
+// A row's state as fragments of 16 x 16 tiles, the same in all columns, so that each
+// lane finds one entry's logit among the accumulators of four tiles: that of entry
+// form_place(lane) of the 64.
+template <typename S, int H>
+struct RowState {
   frag_t<S> x[H / 32];
+  int lane;
+  __device__ __forceinline__ RowState(const S* __restrict__ X, int n, int lane) : lane(lane) {
 #pragma unroll
-  for (int kk = 0; kk < H / 32; ++kk) {
-    if (n >= 0) x[kk] = load8(X + (size_t)n * H + 32 * kk + 8 * kg);
-    else x[kk] = frag_t<S>{};
-  }
-  const uint32_t* mrow = c.rm.row(r, c.R);
-  // Joins the waves' lists; every wave has the result.
-  auto share = [&](Best& b) {
-    if constexpr (WPR > 1) {
-      lists[wave][lane] = b.k;
-      __syncthreads();
-      for (int half = WPR / 2; half >= 1; half /= 2) {
-        if (wave < half) {
-          b.join(lists[wave + half][lane], lane);
-          lists[wave][lane] = b.k;
-        }
-        __syncthreads();
-      }
-      b.k = lists[0][lane];
-      __syncthreads();
+    for (int kk = 0; kk < H / 32; ++kk) {
+      if (n >= 0) x[kk] = load8(X + (size_t)n * H + 32 * kk + 8 * (lane / 16));
+      else x[kk] = frag_t<S>{};
     }
-  };
-
-  Best blocks;
-  const int nb = (c.V + kTopBlock - 1) / kTopBlock;
-  constexpr int U = 4;
-  for (int b0 = w0 * kWave; b0 < nb; b0 += WPR * kWave * U) {
-    float m[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int b = b0 + u * WPR * kWave + lane;
-      m[u] = b < nb ? c.bmax[(size_t)r * c.nbs + b] : -INFINITY;
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) blocks.add(key_of(m[u], (uint32_t)(b0 + u * WPR * kWave + lane)), c.K, lane);
   }
-  share(blocks);
-
-  // 64 entries, entry e of tile u given by lanes e of id[u] (negative: none); each lane
-  // gets the logit of entry 4 kg + q % 4 of tile q / 4
-  auto form = [&](const int (&id)[4]) {
+  // id[u], lanes 0 .. 15: the 16 entries of tile u (negative: none)
+  __device__ __forceinline__ float form(const S* __restrict__ W, const int (&id)[4]) const {
     f32x4 acc[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       acc[u] = f32x4{};
       frag_t<S> w[H / 32];
 #pragma unroll
-      for (int kk = 0; kk < H / 32; ++kk) w[kk] = load8(W + (size_t)max(id[u], 0) * H + 32 * kk + 8 * kg);
+      for (int kk = 0; kk < H / 32; ++kk) w[kk] = load8(W + (size_t)max(id[u], 0) * H + 32 * kk + 8 * (lane / 16));
 #pragma unroll
       for (int kk = 0; kk < H / 32; ++kk) mma(acc[u], w[kk], x[kk]);
     }
@@ -614,97 +583,454 @@ __global__ __launch_bounds__(WPR == 1 ? kVocThreads : kWave* WPR) void vocab_pic
     for (int u = 0; u < 4; ++u)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        if (q == 4 * u + j) z = acc[u][j];
+        if (lane % 16 == 4 * u + j) z = acc[u][j];
     return z;
-  };
-  Best best;
-  for (int b0 = 4 * w0; b0 < c.K; b0 += 4 * WPR) {
-    int id[4], mine = -1;
+  }
+};
+__device__ __forceinline__ int form_place(int lane) { return 16 * (lane % 16 / 4) + 4 * (lane / 16) + lane % 4; }
+
+// Logit and exponential of what a row's lists name, from the raw logit z of place e.
+__device__ __forceinline__ float ruled(const TopRows& c, float z, size_t e) {
+  const uint32_t times = c.ent_count[e];
+  if (times > 0) {   // each step rounded, none fused
+    z = z > 0.f ? __fdiv_rn(z, c.repetition) : __fmul_rn(z, c.repetition);
+    z = __fsub_rn(z, __fadd_rn(c.presence, __fmul_rn(c.frequency, (float)times)));
+  }
+  return __fadd_rn(z, c.ent_add[e]);
+}
+__device__ __forceinline__ void add_exponential(RowSum& s, float z, const Temper& te) {
+  const float kz = exponent_factor(z, te), mz = z * kz;
+  if (mz > s.m) {
+    s.l = s.l * __builtin_amdgcn_exp2f(s.m - mz) + 1.f;
+    s.m = mz;
+    s.k = kz;
+  } else if (z != -INFINITY) {   // (NaN makes the sum NaN)
+    s.l += __builtin_amdgcn_exp2f(fmaf(z, s.k, -s.m));
+  }
+}
+
+// The ruled logits of what row r's lists name: wave w of `waves` takes every waves-th 64.
+// Adds their exponentials to `own`, leaves order_of them in ent_count and calls
+// visit(order, entry) with a lane's (0: none) in step.
+template <typename S, int H, typename Visit>
+__device__ __forceinline__ void rule_lists(const TopRows& c, const RowState<S, H>& row, const S* __restrict__ W, int r,
+                                           int w, int waves, RowSum& own, Visit visit) {
+  const int lane = row.lane;
+  int slo, shi, alo, ahi;
+  list_range(c.list.seen_ptr, c.list.n_seen, r, slo, shi);
+  list_range(c.list.add_ptr, c.list.n_add, r, alo, ahi);
+  const int count = shi - slo + ahi - alo;
+  const size_t at = (size_t)slo + alo;
+  for (int e0 = w * kWave; e0 < count; e0 += waves * kWave) {
+    int ids[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const pick_t k = key_at(blocks.k, min(b0 + u, kWave - 1));
-      const int at = b0 + u < c.K && k != 0 ? (int)key_index(k) * kTopBlock : -1;
-      id[u] = at >= 0 && at + q < c.V ? at + q : -1;
-      if (q / 4 == u && at >= 0 && at + 4 * kg + q % 4 < c.V) mine = at + 4 * kg + q % 4;
+      const int e = e0 + 16 * u + lane % 16;
+      ids[u] = e < count ? c.ent_id[at + e] : -1;
     }
-    float z = form(id);
+    const int e = e0 + form_place(lane), mine = e < count ? c.ent_id[at + e] : -1;
+    float v = row.form(W, ids);
+    uint32_t o = 0;
     if (mine >= 0) {
-      z += entry_bias(c.bias, mine, c.V);
-      if (mrow != nullptr && !(mrow[mine / 32] >> (mine % 32) & 1)) z = -INFINITY;
+      v = ruled(c, v + entry_bias(c.bias, mine, c.V), at + e);
+      add_exponential(own, v, c.te);
+      o = order_of(v);
+      c.ent_count[at + e] = o;
     }
-    best.add(mine >= 0 ? key_of(z, (uint32_t)mine) : 0, c.K, lane);
+    visit(o, (uint32_t)mine);
   }
-
-  // what the lists name
-  float m = kNoMax, k = c.te.near, l = 0.f;
-  if (c.ent_id != nullptr) {
-    int slo, shi, alo, ahi;
-    list_range(c.list.seen_ptr, c.list.n_seen, r, slo, shi);
-    list_range(c.list.add_ptr, c.list.n_add, r, alo, ahi);
-    const int count = shi - slo + ahi - alo;
-    const size_t at = (size_t)slo + alo;
-    for (int e0 = w0 * kWave; e0 < count; e0 += WPR * kWave) {
-      int id[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) id[u] = e0 + 16 * u + q < count ? c.ent_id[at + e0 + 16 * u + q] : -1;
-      const int e = e0 + 16 * (q / 4) + 4 * kg + q % 4;
-      const int mine = e < count ? c.ent_id[at + e] : -1;
-      float z = form(id);
-      if (mine >= 0) {
-        z += entry_bias(c.bias, mine, c.V);
-        const uint32_t times = c.ent_count[at + e];
-        if (times > 0) {   // each step rounded, none fused
-          z = z > 0.f ? __fdiv_rn(z, c.repetition) : __fmul_rn(z, c.repetition);
-          z = __fsub_rn(z, __fadd_rn(c.presence, __fmul_rn(c.frequency, (float)times)));
-        }
-        z = __fadd_rn(z, c.ent_add[at + e]);
-        const float kz = exponent_factor(z, c.te), mz = z * kz;
-        if (mz > m) {
-          l = l * __builtin_amdgcn_exp2f(m - mz) + 1.f;
-          m = mz;
-          k = kz;
-        } else if (z != -INFINITY) {   // (NaN makes the sum NaN)
-          l += __builtin_amdgcn_exp2f(fmaf(z, k, -m));
-        }
-      }
-      best.add(mine >= 0 ? key_of(z, (uint32_t)mine) : 0, c.K, lane);
-    }
+}
+// The same places again, from what rule_lists left (by the same waves).
+template <typename Visit>
+__device__ __forceinline__ void ruled_lists(const TopRows& c, int r, int lane, int w, int waves, Visit visit) {
+  int slo, shi, alo, ahi;
+  list_range(c.list.seen_ptr, c.list.n_seen, r, slo, shi);
+  list_range(c.list.add_ptr, c.list.n_add, r, alo, ahi);
+  const int count = shi - slo + ahi - alo;
+  const size_t at = (size_t)slo + alo;
+  for (int e0 = w * kWave; e0 < count; e0 += waves * kWave) {
+    const int e = e0 + form_place(lane), mine = e < count ? c.ent_id[at + e] : -1;
+    visit(mine >= 0 ? c.ent_count[at + e] : 0u, (uint32_t)mine);
   }
-  share(best);
-  if ((WPR == 1 || wave == 0) && lane < c.K) {
-    c.top[(size_t)r * c.K + lane] = best.k != 0 ? (int32_t)key_index(best.k) : -1;
-    c.logit[(size_t)r * c.K + lane] = key_value(best.k);
-  }
-  if (c.lse == nullptr) return;
-  // the log sum: the first pass's shares, each wave every WPR-th, and the lists'
-  const int shares = c.splits > 0 ? c.splits : c.deal.shares(r / c.share_rows);
-  const size_t at0 = (c.splits > 0 ? 0 : (size_t)c.deal.slot(r / c.share_rows) * c.share_rows) + r % c.share_rows;
-  float M, sum;
-  RowBest none;
-  join_shares<kWave, false>((shares - w0 + WPR - 1) / WPR, at0 + (size_t)w0 * c.share_rows, (size_t)c.share_rows * WPR,
-                            lane, c.pm, c.pl, nullptr, M, sum, none);
+}
+// Joins the lanes' sums, and with them the row's share (M, sum).
+__device__ __forceinline__ void join_own(RowSum own, float& M, float& sum) {
 #pragma unroll
   for (int o = kWave / 2; o >= 1; o /= 2) {
-    const float m2 = __shfl_xor(m, o), l2 = __shfl_xor(l, o), mn = fmaxf(m, m2);
-    l = l * __builtin_amdgcn_exp2f(m - mn) + l2 * __builtin_amdgcn_exp2f(m2 - mn);
-    m = mn;
+    const float m2 = __shfl_xor(own.m, o), l2 = __shfl_xor(own.l, o), t = fmaxf(own.m, m2);
+    own.l = own.l * __builtin_amdgcn_exp2f(own.m - t) + l2 * __builtin_amdgcn_exp2f(m2 - t);
+    own.m = t;
   }
-  const float mn = fmaxf(M, m);
-  sum = sum * __builtin_amdgcn_exp2f(M - mn) + l * __builtin_amdgcn_exp2f(m - mn);
-  M = mn;
-  if constexpr (WPR > 1) {
+  const float t = fmaxf(M, own.m);
+  sum = sum * __builtin_amdgcn_exp2f(M - t) + own.l * __builtin_amdgcn_exp2f(own.m - t);
+  M = t;
+}
+
+// Second pass, all in one: a workgroup of WPR waves per row.
+//
+// Both choices, of blocks and of entries, begin with a bound below the K-th largest:
+// the K-th largest of numbers that are maxima of disjoint parts.  What reaches it is
+// seldom much more than K, and goes to LDS as one list; where it does not fit 64
+// places (many equal ones), the waves' own lists are joined instead.
+template <typename S, int H, int WPR>
+__global__ __launch_bounds__(kWave* WPR) void vocab_pick_kernel(TopRows c, const S* __restrict__ X,
+                                                                const S* __restrict__ W) {
+  constexpr int U = 4;
+  __shared__ pick_t lists[WPR][kWave];
+  __shared__ uint32_t tops[kWave];
+  __shared__ float sums[WPR][2];
+  __shared__ int n_blocks, n_best;
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), r = blockIdx.x;
+  const RowState<S, H> row(X, row_node(c.node, r, c.R, c.n_nodes), lane);
+  const uint32_t* mrow = c.rm.row(r, c.R);
+  // the first pass's shares of the sum: each wave takes every WPR-th
+  float M = kNoMax, sum = 0.f;
+  if (c.lse != nullptr) {
+    const int shares = c.splits > 0 ? c.splits : c.deal.shares(r / c.share_rows);
+    const size_t at0 = (c.splits > 0 ? 0 : (size_t)c.deal.slot(r / c.share_rows) * c.share_rows) + r % c.share_rows;
+    RowBest none;
+    join_shares<kWave, false>((shares - wave + WPR - 1) / WPR, at0 + (size_t)wave * c.share_rows,
+                              (size_t)c.share_rows * WPR, lane, c.pm, c.pl, nullptr, M, sum, none);
+  }
+  // Joins the waves' lists; every wave has the result.
+  auto share = [&](Best& b) {
+    lists[wave][lane] = b.k;
+    __syncthreads();
+    for (int half = WPR / 2; half >= 1; half /= 2) {
+      if (wave < half) {
+        b.join(lists[wave + half][lane], lane);
+        lists[wave][lane] = b.k;
+      }
+      __syncthreads();
+    }
+    b.k = lists[0][lane];
+    __syncthreads();
+  };
+
+  // Blocks.  Wave w looks at every WPR-th 64 of them.
+  const float* bm = c.bmax + (size_t)r * c.nbs;
+  const int nb = (c.V + kTopBlock - 1) / kTopBlock, first = wave * kWave + lane;
+  auto load = [&](uint32_t (&o)[U], int b0) {
+    float m[U];   // (all on their way before the first is looked at)
+#pragma unroll
+    for (int u = 0; u < U; ++u) m[u] = bm[min(b0 + u * WPR * kWave, nb - 1)];
+#pragma unroll
+    for (int u = 0; u < U; ++u) o[u] = b0 + u * WPR * kWave < nb ? order_of(m[u]) : 0u;
+  };
+  uint32_t head[U], most = 0;   // the first of them stay in registers
+  load(head, first);
+#pragma unroll
+  for (int u = 0; u < U; ++u) most = max(most, head[u]);
+  for (int b0 = first + U * WPR * kWave; b0 < nb + lane; b0 += U * WPR * kWave) {
+    uint32_t o[U];
+    load(o, b0);
+#pragma unroll
+    for (int u = 0; u < U; ++u) most = max(most, o[u]);
+  }
+  uint32_t* maxima = reinterpret_cast<uint32_t*>(lists);
+  maxima[threadIdx.x] = most;
+  if (threadIdx.x == 0) n_blocks = n_best = 0;
+  __syncthreads();
+  uint32_t even = 0, odd = 0;
+#pragma unroll
+  for (int w = 0; w < WPR; w += 2) {
+    even = max(even, maxima[w * kWave + lane]);
+    odd = max(odd, maxima[(w + 1) * kWave + lane]);
+  }
+  uint32_t bound = max(kth_of(even, odd, c.K), 1u);
+  __syncthreads();
+  pick_t* chosen = lists[0];
+  auto gather = [&](int* counter, uint32_t o, uint32_t index) {   // what reaches the bound
+    if (o < bound) return;
+    const int at = atomicAdd(counter, 1);
+    if (at < kWave) chosen[at] = pick_of(o, index);
+  };
+#pragma unroll
+  for (int u = 0; u < U; ++u) gather(&n_blocks, head[u], (uint32_t)(first + u * WPR * kWave));
+  for (int b0 = first + U * WPR * kWave; b0 < nb + lane; b0 += U * WPR * kWave) {
+    uint32_t o[U];
+    load(o, b0);
+#pragma unroll
+    for (int u = 0; u < U; ++u) gather(&n_blocks, o[u], (uint32_t)(b0 + u * WPR * kWave));
+  }
+  __syncthreads();
+  int n = n_blocks;
+  pick_t block = 0;   // one a lane
+  if (n <= kWave) {
+    block = lane < n ? chosen[lane] : 0;
+    __syncthreads();
+  } else {
+    __syncthreads();
+    Best b;
+    for (int b0 = first; b0 < nb + lane; b0 += WPR * kWave)
+      b.add(b0 < nb ? pick_of(order_of(bm[b0]), (uint32_t)b0) : 0, c.K, lane);
+    share(b);
+    n = c.K;
+    block = lane < n ? b.k : 0;
+  }
+
+  // Their entries, four blocks at a time.
+  constexpr int G = (kWave / 4 + WPR - 1) / WPR;   // fours of a wave
+  uint32_t z[G], id[G];
+#pragma unroll
+  for (int i = 0; i < G; ++i) {
+    const int b0 = 4 * (wave + i * WPR);
+    z[i] = 0;
+    id[i] = 0;
+    if (b0 < n) {
+      int ids[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const pick_t k = pick_at(block, b0 + u);
+        const int e = (int)pick_index(k) * kTopBlock + lane % 16;
+        ids[u] = k != 0 && e < c.V ? e : -1;
+      }
+      const pick_t k = __shfl(block, b0 + lane % 16 / 4);
+      const int e = (int)pick_index(k) * kTopBlock + form_place(lane) % 16;
+      const float raw = row.form(W, ids);
+      if (k != 0 && e < c.V && (mrow == nullptr || (mrow[e / 32] >> (e % 32) & 1))) {
+        z[i] = order_of(raw + entry_bias(c.bias, e, c.V));
+        id[i] = (uint32_t)e;
+      }
+      uint32_t m = z[i];   // of the block: lanes that differ in bits 0, 1, 4, 5
+      m = max(m, __shfl_xor(m, 1));
+      m = max(m, __shfl_xor(m, 2));
+      m = max(m, __shfl_xor(m, 16));
+      m = max(m, __shfl_xor(m, 32));
+      if (lane < 16 && lane % 4 == 0) tops[b0 + lane / 4] = m;
+    }
+  }
+  __syncthreads();
+  bound = max(kth_of(lane < n ? tops[lane] : 0u, 0u, c.K), 1u);
+#pragma unroll
+  for (int i = 0; i < G; ++i) gather(&n_best, z[i], id[i]);
+  RowSum own{kNoMax, c.te.near, 0.f};
+  if (c.ent_id != nullptr)
+    rule_lists(c, row, W, r, wave, WPR, own, [&](uint32_t o, uint32_t e) { gather(&n_best, o, e); });
+  if (c.lse != nullptr) {
+    join_own(own, M, sum);
     if (lane == 0) {
       sums[wave][0] = M;
       sums[wave][1] = sum;
     }
+  }
+  __syncthreads();
+  const int picked = n_best;
+  if (picked > kWave) {
     __syncthreads();
-    for (int w = 1; w < WPR && wave == 0; ++w) {
-      const float t = fmaxf(M, sums[w][0]);
-      sum = sum * __builtin_amdgcn_exp2f(M - t) + sums[w][1] * __builtin_amdgcn_exp2f(sums[w][0] - t);
-      M = t;
+    Best best;
+#pragma unroll
+    for (int i = 0; i < G; ++i) best.add(pick_of(z[i], id[i]), c.K, lane);
+    if (c.ent_id != nullptr)
+      ruled_lists(c, r, lane, wave, WPR, [&](uint32_t o, uint32_t e) { best.add(pick_of(o, e), c.K, lane); });
+    share(best);
+    if (wave == 0) answer_list(best.k, r, c.K, lane, c.top, c.logit);
+  } else if (wave == 0) {
+    answer(chosen, picked, r, c.K, lane, c.top, c.logit);
+  }
+  if (wave != WPR - 1 || c.lse == nullptr) return;
+  M = sums[0][0];
+  sum = sums[0][1];
+  for (int w = 1; w < WPR; ++w) {
+    const float t = fmaxf(M, sums[w][0]);
+    sum = sum * __builtin_amdgcn_exp2f(M - t) + sums[w][1] * __builtin_amdgcn_exp2f(sums[w][0] - t);
+    M = t;
+  }
+  if (lane == 0) c.lse[r] = row_lse(M, sum, c.te);
+}
+
+// ---- second pass over many rows ---------------------------------------------
+//
+// A block's 16 rows of W are 16 times a state, so where many rows pick blocks it is
+// the states that move: the picked (row, block) pairs are sorted by block, and a wave
+// forms the logits of 16 pairs, mostly of one block, as one 16 x 16 tile.
+
+// The K best blocks of each row, one wave a row: block [R][K], -1 from where none is
+// left.
+constexpr int kReach = 2 * kWave;   // blocks that reach the bound, at most
+template <typename S>   // (the same for both types)
+__global__ __launch_bounds__(kVocThreads) void vocab_blocks_kernel(int R, int nb, int nbs, int K,
+                                                                   const float* __restrict__ bmax,
+                                                                   int32_t* __restrict__ block) {
+  constexpr int U = 8;
+  __shared__ u32x2 reach[kVocWaves][kReach];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int r = blockIdx.x * kVocWaves + wave;
+  if (r >= R) return;   // whole waves leave together
+  const float* bm = bmax + (size_t)r * nbs;
+  int32_t* out = block + (size_t)r * K;
+  auto load = [&](uint32_t (&o)[U], int b0) {
+    float m[U];   // (all on their way before the first is looked at)
+#pragma unroll
+    for (int u = 0; u < U; ++u) m[u] = bm[min(b0 + u * kWave + lane, nb - 1)];
+#pragma unroll
+    for (int u = 0; u < U; ++u) o[u] = b0 + u * kWave + lane < nb ? order_of(m[u]) : 0u;
+  };
+  uint32_t most[2] = {};
+  for (int b0 = 0; b0 < nb; b0 += U * kWave) {
+    uint32_t o[U];
+    load(o, b0);
+#pragma unroll
+    for (int u = 0; u < U; ++u) most[u % 2] = max(most[u % 2], o[u]);
+  }
+  const uint32_t bound = max(kth_of(most[0], most[1], K), 1u);
+  const uint64_t below = (1ull << lane) - 1;
+  int n = 0;
+  for (int b0 = 0; b0 < nb; b0 += U * kWave) {
+    uint32_t o[U];
+    load(o, b0);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint64_t in = __ballot(o[u] >= bound);
+      const int at = n + __popcll(in & below);
+      if (o[u] >= bound && at < kReach) reach[wave][at] = u32x2{o[u], (uint32_t)(b0 + u * kWave + lane)};
+      n += __popcll(in);
     }
   }
-  if ((WPR == 1 || wave == 0) && lane == 0) c.lse[r] = row_lse(M, sum, c.te);
+  if (n > kReach) {   // many equal ones
+    Best best;
+    for (int b0 = 0; b0 < nb; b0 += kWave) {
+      const int b = b0 + lane;
+      best.add(b < nb ? pick_of(order_of(bm[b]), (uint32_t)b) : 0, K, lane);
+    }
+    if (lane < K) out[lane] = best.k != 0 ? (int32_t)pick_index(best.k) : -1;
+    return;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  // in the order of their blocks: those above the K-th largest, then the first of its equals
+  const u32x2 a = lane < n ? reach[wave][lane] : u32x2{}, b = lane + kWave < n ? reach[wave][lane + kWave] : u32x2{};
+  const uint32_t kth = kth_of(a[0], b[0], K);
+  const bool above_a = a[0] > kth, above_b = b[0] > kth, same_a = a[0] == kth && kth != 0, same_b = b[0] == kth && kth != 0;
+  const uint64_t ma = __ballot(above_a), mb = __ballot(above_b), sa = __ballot(same_a), sb = __ballot(same_b);
+  const int na = __popcll(ma), above = na + __popcll(mb), equal_a = __popcll(sa);
+  const int pa = above_a ? __popcll(ma & below) : above + __popcll(sa & below);
+  const int pb = above_b ? na + __popcll(mb & below) : above + equal_a + __popcll(sb & below);
+  if ((above_a || same_a) && pa < K) out[pa] = (int32_t)a[1];
+  if ((above_b || same_b) && pb < K) out[pb] = (int32_t)b[1];
+  const int all = above + equal_a + __popcll(sb);
+  if (lane >= all && lane < K) out[lane] = -1;
+}
+
+// The logits of the picked blocks' entries, z [R][K][16], from the sorted pairs (block,
+// row and place).
+template <typename S, int H>
+__global__ __launch_bounds__(kVocThreads) void vocab_pairs_kernel(TopRows c, const u32x2* __restrict__ pairs, int n_pairs,
+                                                                  const S* __restrict__ X, const S* __restrict__ W,
+                                                                  float* __restrict__ z) {
+  const int lane = threadIdx.x % kWave, q = lane % 16, kg = lane / 16;
+  const int i = (blockIdx.x * kVocWaves + threadIdx.x / kWave) * 16 + q, nb = (c.V + kTopBlock - 1) / kTopBlock;
+  const u32x2 pair = i < n_pairs ? pairs[i] : u32x2{(uint32_t)nb, 0u};
+  const int b = (int)pair[0];
+  uint64_t left = __ballot(b < nb) & 0xFFFFu;
+  if (left == 0) return;   // whole waves leave together
+  const int r = (int)pair[1] / c.K, n = b < nb ? row_node(c.node, r, c.R, c.n_nodes) : -1;
+  frag_t<S> x[H / 32];
+#pragma unroll
+  for (int kk = 0; kk < H / 32; ++kk) {
+    if (n >= 0) x[kk] = load8(X + (size_t)n * H + 32 * kk + 8 * kg);
+    else x[kk] = frag_t<S>{};
+  }
+  const uint32_t* mrow = b < nb ? c.rm.row(r, c.R) : nullptr;
+  const uint32_t may = mrow != nullptr ? mrow[b / 2] >> (16 * (b & 1) + 4 * kg) : ~0u;
+  while (left != 0) {
+    const int one = __builtin_amdgcn_readlane(b, (int)__builtin_ctzll(left));
+    left &= ~__ballot(b == one);
+    const int e0 = one * kTopBlock;
+    frag_t<S> w[H / 32];
+#pragma unroll
+    for (int kk = 0; kk < H / 32; ++kk) w[kk] = load8(W + (size_t)min(e0 + q, c.V - 1) * H + 32 * kk + 8 * kg);
+    f32x4 acc = {};
+#pragma unroll
+    for (int kk = 0; kk < H / 32; ++kk) mma(acc, w[kk], x[kk]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      acc[j] += entry_bias(c.bias, e0 + 4 * kg + j, c.V);
+      if (!(may >> j & 1)) acc[j] = -INFINITY;
+    }
+    if (b == one) *reinterpret_cast<f32x4*>(z + (size_t)pair[1] * kTopBlock + 4 * kg) = acc;
+  }
+}
+
+// The answers from those logits, one wave a row.
+template <typename S, int H>
+__global__ __launch_bounds__(kVocThreads) void vocab_answer_kernel(TopRows c, const int32_t* __restrict__ block,
+                                                                   const float* __restrict__ z,
+                                                                   const S* __restrict__ X, const S* __restrict__ W) {
+  __shared__ pick_t picks[kVocWaves][kWave];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int r = blockIdx.x * kVocWaves + wave;
+  if (r >= c.R) return;   // whole waves leave together
+  const int32_t* bl = block + (size_t)r * c.K;
+  const float* zr = z + (size_t)r * c.K * kTopBlock;
+  constexpr int G = kTopMost * kTopBlock / kWave;   // 64 entries, of four blocks, at a time
+  // all blocks hold an entry that reaches the least of their maxima, and there are K
+  uint32_t o[G], bound = ~0u;
+  float zs[G];
+  int of[G];   // (all on their way before the first is looked at)
+#pragma unroll
+  for (int i = 0; i < G; ++i) {
+    if (4 * i < c.K) {
+      of[i] = bl[min(4 * i + lane / 16, c.K - 1)];
+      zs[i] = zr[min(64 * i + lane, c.K * kTopBlock - 1)];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < G; ++i) {
+    const int at = 4 * i + lane / 16;
+    o[i] = 0;
+    if (4 * i < c.K) {
+      o[i] = at < c.K && of[i] >= 0 ? order_of(zs[i]) : 0u;
+      uint32_t m = o[i];
+#pragma unroll
+      for (int d = 1; d < 16; d *= 2) m = max(m, __shfl_xor(m, d));
+      if (at < c.K) bound = min(bound, m);
+    }
+  }
+#pragma unroll
+  for (int d = 16; d < kWave; d *= 2) bound = min(bound, __shfl_xor(bound, d));
+  bound = max(bound, 1u);
+  Best best;
+  bool spilled = false;
+  int n = 0;
+  const uint64_t below = (1ull << lane) - 1;
+  auto take = [&](uint32_t v, uint32_t e) {   // what reaches the bound, to the list, which goes to `best` when full
+    const uint64_t in = __ballot(v >= bound);
+    if (in == 0) return;
+    const int m = __popcll(in);
+    if (n + m > kWave) {
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      best.add(lane < n ? picks[wave][lane] : 0, c.K, lane);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      n = 0;
+      spilled = true;
+    }
+    if (v >= bound) picks[wave][n + __popcll(in & below)] = pick_of(v, e);
+    n += m;
+  };
+#pragma unroll
+  for (int i = 0; i < G; ++i) {
+    if (4 * i < c.K) take(o[i], (uint32_t)(of[i] * kTopBlock + lane % 16));
+  }
+  RowSum own{kNoMax, c.te.near, 0.f};
+  if (c.ent_id != nullptr) {
+    const RowState<S, H> row(X, row_node(c.node, r, c.R, c.n_nodes), lane);
+    rule_lists(c, row, W, r, 0, 1, own, take);
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  if (spilled) {
+    best.add(lane < n ? picks[wave][lane] : 0, c.K, lane);
+    answer_list(best.k, r, c.K, lane, c.top, c.logit);
+  } else {
+    answer(picks[wave], n, r, c.K, lane, c.top, c.logit);
+  }
+  if (c.lse == nullptr) return;
+  const int shares = c.deal.shares(r / c.share_rows);
+  const size_t at0 = (size_t)c.deal.slot(r / c.share_rows) * c.share_rows + r % c.share_rows;
+  float M, sum;
+  RowBest none;
+  join_shares<kWave, false>(shares, at0, c.share_rows, lane, c.pm, c.pl, nullptr, M, sum, none);
+  join_own(own, M, sum);
+  if (lane == 0) c.lse[r] = row_lse(M, sum, c.te);
 }
 
 }  // namespace dev
@@ -712,14 +1038,17 @@ __global__ __launch_bounds__(WPR == 1 ? kVocThreads : kWave* WPR) void vocab_pic
 namespace {
 // How a call is cut, and where its parts lie in the workspace.
 struct TopPlan {
-  bool few;
+  bool few, sorted;
   int nt, splits, per, nbs, words;
   dev::Deal deal;
-  size_t id, count, add, mask, bmax, pm, pl, wp, bytes;
+  size_t id, count, add, mask, bmax, pm, pl, wp, block, z, sort, bytes;
 };
+// Whether the picked blocks are sorted.
+bool pairs_sorted(int es, int H, int R, int K) {
+  return R > 64 && (double)R * K * dev::kTopBlock * H * es > 2e8 && (long)R * K <= 1L << 30;
+}
 template <typename S>
-TopPlan top_plan(int H, int R, int V, int n_listed) {
-  constexpr int T = dev::voc_tile<S>();
+TopPlan top_plan(int H, int R, int V, int K, int n_listed) {
   TopPlan p{};
   size_t shares;
   p.few = R <= 64;
@@ -731,10 +1060,11 @@ TopPlan top_plan(int H, int R, int V, int n_listed) {
     shares = (size_t)p.splits * 32 * p.nt;
   } else {
     p.nt = dev::top_tiles<S>(H);
-    p.deal = make_deal(cdiv(R, dev::kVocRows * p.nt), cdiv(V, T), 256 * dev::top_waves<S>(H));
-    shares = (size_t)p.deal.all_slots() * dev::kVocRows * p.nt;
+    p.deal = make_deal(cdiv(R, dev::top_rows<S>(H)), cdiv(V, dev::kTopUnit),
+                       256 * dev::top_waves<S>(H) * 4 / dev::top_group<S>(H));
+    shares = (size_t)p.deal.all_slots() * dev::top_rows<S>(H);
   }
-  p.nbs = cdiv(cdiv(V, T) * (T / dev::kTopBlock), 8) * 8;
+  p.nbs = cdiv(V, dev::kTopUnit) * (dev::kTopUnit / dev::kTopBlock);
   p.words = cdiv(cdiv(V, 32), 4) * 4;
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -750,6 +1080,12 @@ TopPlan top_plan(int H, int R, int V, int n_listed) {
   p.pm = take(shares * 4);
   p.pl = take(shares * 4);
   if (sizeof(S) == 4 && !p.few) p.wp = take((size_t)V * H * 6);
+  p.sorted = pairs_sorted(sizeof(S), H, R, K);
+  if (p.sorted) {
+    p.block = take((size_t)R * K * 4);
+    p.z = take((size_t)R * K * dev::kTopBlock * 4);
+    p.sort = take(sort_workspace(R * K));
+  }
   p.bytes = at;
   return p;
 }
@@ -757,11 +1093,11 @@ TopPlan top_plan(int H, int R, int V, int n_listed) {
 template <typename S, int H>
 hipError_t top_h(const TopArgs& a, hipStream_t st) {
   using namespace dev;
-  const TopPlan p = top_plan<S>(H, a.R, a.V, a.n_seen + a.n_add);
+  const TopPlan p = top_plan<S>(H, a.R, a.V, a.K, a.n_seen + a.n_add);
   char* ws = static_cast<char*>(a.ws);
   TopRows c{};
   c.n_nodes = a.n_nodes; c.R = a.R; c.V = a.V; c.K = a.K; c.nbs = p.nbs;
-  c.splits = p.splits; c.share_rows = p.few ? 32 * p.nt : kVocRows * p.nt; c.deal = p.deal;
+  c.splits = p.splits; c.share_rows = p.few ? 32 * p.nt : top_rows<S>(H); c.deal = p.deal;
   c.te = a.temper; c.bias = a.bias; c.node = a.node;
   c.rm = RowMask{a.mask, a.mask_of, a.n_masks, a.mask_words};
   c.list = Listing{a.seen_ptr, a.seen, a.add_ptr, a.add, a.value, a.n_seen, a.n_add};
@@ -799,7 +1135,7 @@ hipError_t top_h(const TopArgs& a, hipStream_t st) {
       hipLaunchKernelGGL((vocab_max_few_kernel<S, H, 2, LSE, MASK>), dim3(p.splits / kVocWaves), dim3(kVocThreads), 0, st, \
                          a.n_nodes, a.R, a.V, p.per, a.temper, X, W, a.bias, a.node, c.rm, bmax, p.nbs, pm, pl);       \
     else                                                                                                              \
-      hipLaunchKernelGGL((vocab_max_kernel<S, H, LSE, MASK>), dim3(p.deal.workers), dim3(kVocThreads), 0, st,         \
+      hipLaunchKernelGGL((vocab_max_kernel<S, H, LSE, MASK>), dim3(p.deal.workers), dim3(kWave* top_group<S>(H)), 0, st, \
                          a.n_nodes, a.R, a.V, p.deal, a.temper, X, Ws, a.bias, a.node, c.rm, bmax, p.nbs, pm, pl);     \
   } while (0)
   if (a.lse != nullptr) {
@@ -808,18 +1144,32 @@ hipError_t top_h(const TopArgs& a, hipStream_t st) {
     if (c.rm.bits != nullptr) MAXIMA(false, true); else MAXIMA(false, false);
   }
 #undef MAXIMA
+  if (p.sorted) {
+    int32_t* block = reinterpret_cast<int32_t*>(ws + p.block);
+    float* z = reinterpret_cast<float*>(ws + p.z);
+    const int nb = cdiv(a.V, kTopBlock), pairs = a.R * a.K;
+    hipLaunchKernelGGL(vocab_blocks_kernel<S>, dim3(cdiv(a.R, kVocWaves)), dim3(kVocThreads), 0, st, a.R, nb, p.nbs, a.K,
+                       bmax, block);
+    const void* sorted;
+    const hipError_t err = launch_sort(pairs, nb, block, ws + p.sort, &sorted, st);
+    if (err != hipSuccess) return err;
+    hipLaunchKernelGGL((vocab_pairs_kernel<S, H>), dim3(cdiv(pairs, 16 * kVocWaves)), dim3(kVocThreads), 0, st, c,
+                       static_cast<const u32x2*>(sorted), pairs, X, W, z);
+    hipLaunchKernelGGL((vocab_answer_kernel<S, H>), dim3(cdiv(a.R, kVocWaves)), dim3(kVocThreads), 0, st, c, block, z, X, W);
+    return hipGetLastError();
+  }
   if (a.R <= 64)
     hipLaunchKernelGGL((vocab_pick_kernel<S, H, 16>), dim3(a.R), dim3(16 * kWave), 0, st, c, X, W);
-  else if (a.R <= 2048)
-    hipLaunchKernelGGL((vocab_pick_kernel<S, H, 4>), dim3(a.R), dim3(4 * kWave), 0, st, c, X, W);
   else
-    hipLaunchKernelGGL((vocab_pick_kernel<S, H, 1>), dim3(cdiv(a.R, kVocWaves)), dim3(kVocThreads), 0, st, c, X, W);
+    hipLaunchKernelGGL((vocab_pick_kernel<S, H, 4>), dim3(a.R), dim3(4 * kWave), 0, st, c, X, W);
   return hipGetLastError();
 }
 }  // namespace
 
 namespace GGNN_IMPL_NS {
-size_t top_workspace(int H, int R, int V, int n_listed) { return top_plan<dev::dt_t>(H, R, V, n_listed).bytes; }
+size_t top_workspace(int H, int R, int V, int K, int n_listed) {
+  return top_plan<dev::dt_t>(H, R, V, K, n_listed).bytes;
+}
 
 hipError_t launch_top(int H, const TopArgs& a, hipStream_t st) {
   using S = dev::dt_t;
