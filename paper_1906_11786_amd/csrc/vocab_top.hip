@@ -340,7 +340,7 @@ __global__ __launch_bounds__(kVocThreads) void vocab_max_few_kernel(
 // below, which count and take minima) and takes them out of the row's mask.  Entries
 // are held in a table in LDS: a hash table while the lists are short; else the
 // vocabulary is passed over in parts whose entries have a place each.
-constexpr int kTable = 2048, kHashed = kTable / 2;   // places; longest lists that are hashed
+constexpr int kTable = 4096, kHashed = kTable / 2;   // places; longest lists that are hashed
 
 struct Listing {
   const int32_t *seen_ptr, *seen, *add_ptr, *add;
@@ -353,15 +353,19 @@ __device__ __forceinline__ void list_range(const int32_t* ptr, int n, int r, int
   hi = ptr != nullptr ? min(max(ptr[r + 1], lo), n) : 0;
 }
 
-template <typename S>   // (the same for both types)
-__global__ __launch_bounds__(kVocThreads) void vocab_rules_kernel(int R, int V, Listing list, RowMask rm, int words,
-                                                                  uint32_t* __restrict__ out,
-                                                                  int32_t* __restrict__ ent_id,
-                                                                  uint32_t* __restrict__ ent_count,
-                                                                  float* __restrict__ ent_add) {
-  __shared__ int key[kTable];
-  __shared__ uint32_t first[kTable], seen[kTable], adds[kTable];
-  __shared__ float value[kTable];
+// THREADS a row.
+template <typename S, int THREADS>   // (the same for both types S)
+__global__ __launch_bounds__(THREADS) void vocab_rules_kernel(int R, int V, Listing list, RowMask rm, int words,
+                                                              int table, uint32_t* __restrict__ out,
+                                                              int32_t* __restrict__ ent_id,
+                                                              uint32_t* __restrict__ ent_count,
+                                                              float* __restrict__ ent_add) {
+  // Entry, place of its first listing, times seen (low half: hashed lists have at most
+  // 2048 listings) and biases (high half), a bias; a table without hashing holds the
+  // biases' count in place of the entry.
+  extern __shared__ uint32_t lds[];
+  uint32_t *key = lds, *first = lds + table, *seen = lds + 2 * table;
+  float* value = reinterpret_cast<float*>(lds + 3 * table);
   const int r = blockIdx.x;
   int slo, shi, alo, ahi;
   list_range(list.seen_ptr, list.n_seen, r, slo, shi);
@@ -370,37 +374,45 @@ __global__ __launch_bounds__(kVocThreads) void vocab_rules_kernel(int R, int V, 
   const size_t at = (size_t)slo + alo;   // the row's places
   const uint32_t* mask = rm.row(r, R);
   uint32_t* mine = out + (size_t)r * words;
-  const bool hashed = n <= kHashed;
+  const bool hashed = n <= table / 2;
   int bits = 6;
   while (hashed && (1 << bits) < 2 * n) ++bits;
-  const int size = hashed ? 1 << bits : kTable;
-  const long parts = hashed ? 1 : ((long)V + kTable - 1) / kTable;
-  auto token = [&](int i) { return i < n_seen ? list.seen[slo + i] : list.add[alo + i - n_seen]; };
+  const int size = hashed ? 1 << bits : table;
+  const long parts = hashed ? 1 : ((long)V + table - 1) / table;
+  constexpr int kKeep = 2;   // listings that a thread keeps from the first look to the second
+  int id[kKeep];
+#pragma unroll
+  for (int u = 0; u < kKeep; ++u) {
+    const int i = u * THREADS + threadIdx.x;
+    const int s = list.n_seen > 0 ? list.seen[min(slo + min(i, max(n_seen - 1, 0)), list.n_seen - 1)] : -1;
+    const int a = list.n_add > 0 ? list.add[min(alo + max(i - n_seen, 0), list.n_add - 1)] : -1;
+    id[u] = i >= n ? -1 : i < n_seen ? s : a;
+  }
+  auto token = [&](int u, int i) {
+    if (u == 0) return id[0];
+    if (u == 1) return id[1];
+    return i < n_seen ? list.seen[slo + i] : list.add[alo + i - n_seen];
+  };
+  auto hash = [&](int e) { return (uint32_t)e * 0x9E3779B1u >> (32 - bits); };
   for (long p = blockIdx.y; p < parts; p += gridDim.y) {
-    const int lo = hashed ? 0 : (int)(p * kTable), hi = hashed ? V : (int)min((long)V, (long)lo + kTable);
-    for (int i = threadIdx.x; i < size; i += kVocThreads) {
-      key[i] = -1;
+    const int lo = hashed ? 0 : (int)(p * table), hi = hashed ? V : (int)min((long)V, (long)lo + table);
+    for (int i = threadIdx.x; i < size; i += THREADS) {
+      key[i] = hashed ? ~0u : 0u;
       first[i] = ~0u;
-      seen[i] = adds[i] = 0;
+      seen[i] = 0;
     }
-    for (int w = lo / 32 + threadIdx.x; w < (hi + 31) / 32; w += kVocThreads) mine[w] = mask != nullptr ? mask[w] : ~0u;
+    for (int w = lo / 32 + threadIdx.x; w < (hi + 31) / 32; w += THREADS) mine[w] = mask != nullptr ? mask[w] : ~0u;
     __threadfence_block();
     __syncthreads();
-    auto place = [&](int id) {   // of an entry that the table has
-      if (!hashed) return id - lo;
-      uint32_t h = (uint32_t)id * 0x9E3779B1u >> (32 - bits);
-      while (key[h] != id) h = (h + 1) & (size - 1);
-      return (int)h;
-    };
-    for (int i = threadIdx.x; i < n; i += kVocThreads) {
-      const int id = token(i);
-      if (id < lo || id >= hi) continue;
-      int h = id - lo;
+    for (int i = threadIdx.x, u = 0; i < n; i += THREADS, ++u) {
+      const int e = token(u, i);
+      if (e < lo || e >= hi) continue;
+      uint32_t h = (uint32_t)(e - lo);
       if (hashed) {   // at most half of the places are taken, so a free one is found
-        h = (int)((uint32_t)id * 0x9E3779B1u >> (32 - bits));
+        h = hash(e);
         for (;;) {
-          const int old = atomicCAS(&key[h], -1, id);
-          if (old == -1 || old == id) break;
+          const uint32_t old = atomicCAS(&key[h], ~0u, (uint32_t)e);
+          if (old == ~0u || old == (uint32_t)e) break;
           h = (h + 1) & (size - 1);
         }
       }
@@ -408,31 +420,37 @@ __global__ __launch_bounds__(kVocThreads) void vocab_rules_kernel(int R, int V, 
       if (i < n_seen) {
         atomicAdd(&seen[h], 1u);
       } else {
-        atomicAdd(&adds[h], 1u);
+        if (hashed) atomicAdd(&seen[h], 1u << 16);
+        else atomicAdd(&key[h], 1u);
         value[h] = list.value[alo + i - n_seen];   // (used where it is the only one)
       }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += kVocThreads) {
-      const int id = token(i);
-      const bool known = id >= 0 && id < V;
-      if (known ? id < lo || id >= hi : p != 0) continue;   // another part's
-      int e = -1;
+    for (int i = threadIdx.x, u = 0; i < n; i += THREADS, ++u) {
+      const int e = token(u, i);
+      const bool known = e >= 0 && e < V;
+      if (known ? e < lo || e >= hi : p != 0) continue;   // another part's
+      int found = -1;
       if (known) {
-        const int h = place(id);
-        if (first[h] == (uint32_t)i && (mask == nullptr || (mask[id / 32] >> (id % 32) & 1))) {
-          e = id;
-          float a = adds[h] == 1 ? value[h] : 0.f;
-          if (adds[h] > 1) {   // in list order
+        uint32_t h = (uint32_t)(e - lo);
+        if (hashed) {
+          h = hash(e);
+          while (key[h] != (uint32_t)e) h = (h + 1) & (size - 1);
+        }
+        if (first[h] == (uint32_t)i && (mask == nullptr || (mask[e / 32] >> (e % 32) & 1))) {
+          found = e;
+          const uint32_t adds = hashed ? seen[h] >> 16 : key[h];
+          float a = adds == 1 ? value[h] : 0.f;
+          if (adds > 1) {   // in list order
             for (int k = alo; k < ahi; ++k)
-              if (list.add[k] == id) a += list.value[k];
+              if (list.add[k] == e) a += list.value[k];
           }
-          ent_count[at + i] = seen[h];
+          ent_count[at + i] = hashed ? seen[h] & 0xFFFFu : seen[h];
           ent_add[at + i] = a;
-          atomicAnd(&mine[id / 32], ~(1u << (id % 32)));
+          atomicAnd(&mine[e / 32], ~(1u << (e % 32)));
         }
       }
-      ent_id[at + i] = e;
+      ent_id[at + i] = found;
     }
     __syncthreads();
   }
@@ -460,13 +478,16 @@ __device__ __forceinline__ pick_t pick_at(pick_t k, int lane) {   // lane: the s
   return (pick_t)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32 |
          (uint32_t)__builtin_amdgcn_readlane((int)k, lane);
 }
-// The K-th largest of the wave's numbers a and b (0 where fewer are not 0), bit by bit.
+// A bound that K or more of the wave's numbers a and b reach, bit by bit: the K-th
+// largest, or any between it and the next; 0 where fewer are not 0.
 __device__ __forceinline__ uint32_t kth_of(uint32_t a, uint32_t b, int K) {
   uint32_t t = 0;
-#pragma unroll
-  for (int bit = 31; bit >= 0; --bit) {
-    const uint32_t c = t | 1u << bit;
-    if (__popcll(__ballot(a >= c)) + __popcll(__ballot(b >= c)) >= K) t = c;
+#pragma unroll 1
+  for (uint32_t bit = 1u << 31; bit != 0; bit >>= 1) {
+    const uint32_t c = t | bit;
+    const int n = __popcll(__ballot(a >= c)) + __popcll(__ballot(b >= c));
+    if (n >= K) t = c;
+    if (n == K) break;
   }
   return t;
 }
@@ -552,11 +573,14 @@ struct TopRows {   // arguments of the second pass
   float *logit, *lse;
 };
 
-// A row's state as fragments of 16 x 16 tiles, the same in all columns, so that each
-// lane finds one entry's logit among the accumulators of four tiles: that of entry
-// form_place(lane) of the 64.
+// A row's state, and the logits of 64 entries at a time, one a lane, as four tiles of
+// 16 x 16 whose entries lie along the rows: lane l holds row l % 16, k group l / 16.  In
+// bf16 the state stands in all columns of the other operand, so that each lane
+// finds one entry's logit among the accumulators.  In float32, where that would take
+// 32 cycles for 64 useful products, each lane adds up its own and four lanes join.
 template <typename S, int H>
 struct RowState {
+  static constexpr bool kMatrix = sizeof(S) == 2;
   frag_t<S> x[H / 32];
   int lane;
   __device__ __forceinline__ RowState(const S* __restrict__ X, int n, int lane) : lane(lane) {
@@ -566,37 +590,63 @@ struct RowState {
       else x[kk] = frag_t<S>{};
     }
   }
-  // id[u], lanes 0 .. 15: the 16 entries of tile u (negative: none)
-  __device__ __forceinline__ float form(const S* __restrict__ W, const int (&id)[4]) const {
-    f32x4 acc[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      acc[u] = f32x4{};
-      frag_t<S> w[H / 32];
-#pragma unroll
-      for (int kk = 0; kk < H / 32; ++kk) w[kk] = load8(W + (size_t)max(id[u], 0) * H + 32 * kk + 8 * (lane / 16));
-#pragma unroll
-      for (int kk = 0; kk < H / 32; ++kk) mma(acc[u], w[kk], x[kk]);
-    }
+  // Tile of the lane's entry, and its row there.
+  __device__ __forceinline__ int tile() const { return kMatrix ? lane % 16 / 4 : lane / 16; }
+  __device__ __forceinline__ int entry() const { return kMatrix ? 4 * (lane / 16) + lane % 4 : lane % 16; }
+  // Largest of the tile's sixteen values; whether the lane is the tile's first.
+  __device__ __forceinline__ uint32_t tile_max(uint32_t m) const {
+    m = max(m, __shfl_xor(m, 1));
+    m = max(m, __shfl_xor(m, 2));
+    m = max(m, __shfl_xor(m, kMatrix ? 16 : 4));
+    return max(m, __shfl_xor(m, kMatrix ? 32 : 8));
+  }
+  __device__ __forceinline__ bool leads() const { return kMatrix ? lane < 16 && lane % 4 == 0 : lane % 16 == 0; }
+  // id[u], lanes l % 16: the entries of tile u < tiles (negative: none).  Two tiles' rows
+  // of W are on their way at a time.
+  __device__ __forceinline__ float form(const S* __restrict__ W, const int (&id)[4], int tiles) const {
     float z = 0.f;
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
+    for (int u0 = 0; u0 < 4; u0 += 2) {
+      if (u0 >= tiles) break;
+      frag_t<S> w[2][H / 32];
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (lane % 16 == 4 * u + j) z = acc[u][j];
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int kk = 0; kk < H / 32; ++kk)
+          w[u][kk] = load8(W + (size_t)max(id[u0 + u], 0) * H + 32 * kk + 8 * (lane / 16));
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        if constexpr (kMatrix) {
+          f32x4 acc = {};
+#pragma unroll
+          for (int kk = 0; kk < H / 32; ++kk) mma(acc, w[u][kk], x[kk]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (lane % 16 == 4 * (u0 + u) + j) z = acc[j];
+        } else {
+          float part[2] = {};
+#pragma unroll
+          for (int kk = 0; kk < H / 32; ++kk)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) part[i % 2] = fmaf(w[u][kk][i], x[kk][i], part[i % 2]);
+          float a = part[0] + part[1];
+          a += __shfl_xor(a, 16);
+          a += __shfl_xor(a, 32);
+          if (lane / 16 == u0 + u) z = a;
+        }
+      }
+    }
     return z;
   }
 };
-__device__ __forceinline__ int form_place(int lane) { return 16 * (lane % 16 / 4) + 4 * (lane / 16) + lane % 4; }
 
-// Logit and exponential of what a row's lists name, from the raw logit z of place e.
-__device__ __forceinline__ float ruled(const TopRows& c, float z, size_t e) {
-  const uint32_t times = c.ent_count[e];
+// The logit of an entry that a row's lists name, from the raw one z.
+__device__ __forceinline__ float ruled(const TopRows& c, float z, uint32_t times, float add) {
   if (times > 0) {   // each step rounded, none fused
     z = z > 0.f ? __fdiv_rn(z, c.repetition) : __fmul_rn(z, c.repetition);
     z = __fsub_rn(z, __fadd_rn(c.presence, __fmul_rn(c.frequency, (float)times)));
   }
-  return __fadd_rn(z, c.ent_add[e]);
+  return __fadd_rn(z, add);
 }
 __device__ __forceinline__ void add_exponential(RowSum& s, float z, const Temper& te) {
   const float kz = exponent_factor(z, te), mz = z * kz;
@@ -609,30 +659,35 @@ __device__ __forceinline__ void add_exponential(RowSum& s, float z, const Temper
   }
 }
 
-// The ruled logits of what row r's lists name: wave w of `waves` takes every waves-th 64.
-// Adds their exponentials to `own`, leaves order_of them in ent_count and calls
-// visit(order, entry) with a lane's (0: none) in step.
+// The ruled logits of what row r's lists name: wave w of `waves` takes every waves-th 16
+// places, four at a time.  Adds their exponentials to `own`, leaves order_of them in
+// ent_count and calls visit(order, entry) with a lane's (0: none) in step.
 template <typename S, int H, typename Visit>
 __device__ __forceinline__ void rule_lists(const TopRows& c, const RowState<S, H>& row, const S* __restrict__ W, int r,
                                            int w, int waves, RowSum& own, Visit visit) {
-  const int lane = row.lane;
   int slo, shi, alo, ahi;
   list_range(c.list.seen_ptr, c.list.n_seen, r, slo, shi);
   list_range(c.list.add_ptr, c.list.n_add, r, alo, ahi);
-  const int count = shi - slo + ahi - alo;
+  const int count = shi - slo + ahi - alo, lane = row.lane;
   const size_t at = (size_t)slo + alo;
-  for (int e0 = w * kWave; e0 < count; e0 += waves * kWave) {
+  for (int e0 = 16 * w; e0 < count; e0 += 64 * waves) {
+    // one load of the 64 names, passed on between the lanes; what changes them is on its way with it
+    const int e = e0 + 16 * waves * row.tile() + row.entry();
+    const int all = c.ent_id[at + min(e0 + 16 * waves * (lane / 16) + lane % 16, count - 1)];
+    const uint32_t times = c.ent_count[at + min(e, count - 1)];
+    const float add = c.ent_add[at + min(e, count - 1)];
     int ids[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const int e = e0 + 16 * u + lane % 16;
-      ids[u] = e < count ? c.ent_id[at + e] : -1;
+      const int id = __shfl(all, 16 * u + lane % 16);
+      ids[u] = e0 + 16 * waves * u + lane % 16 < count ? id : -1;
     }
-    const int e = e0 + form_place(lane), mine = e < count ? c.ent_id[at + e] : -1;
-    float v = row.form(W, ids);
+    const int own_id = __shfl(all, 16 * row.tile() + row.entry()), mine = e < count ? own_id : -1;
+    const float b = entry_bias(c.bias, max(mine, 0), c.V);
+    float v = row.form(W, ids, (count - e0 + 16 * waves - 1) / (16 * waves)) + b;
     uint32_t o = 0;
     if (mine >= 0) {
-      v = ruled(c, v + entry_bias(c.bias, mine, c.V), at + e);
+      v = ruled(c, v, times, add);
       add_exponential(own, v, c.te);
       o = order_of(v);
       c.ent_count[at + e] = o;
@@ -641,15 +696,16 @@ __device__ __forceinline__ void rule_lists(const TopRows& c, const RowState<S, H
   }
 }
 // The same places again, from what rule_lists left (by the same waves).
-template <typename Visit>
-__device__ __forceinline__ void ruled_lists(const TopRows& c, int r, int lane, int w, int waves, Visit visit) {
+template <typename S, int H, typename Visit>
+__device__ __forceinline__ void ruled_lists(const TopRows& c, const RowState<S, H>& row, int r, int w, int waves,
+                                            Visit visit) {
   int slo, shi, alo, ahi;
   list_range(c.list.seen_ptr, c.list.n_seen, r, slo, shi);
   list_range(c.list.add_ptr, c.list.n_add, r, alo, ahi);
   const int count = shi - slo + ahi - alo;
   const size_t at = (size_t)slo + alo;
-  for (int e0 = w * kWave; e0 < count; e0 += waves * kWave) {
-    const int e = e0 + form_place(lane), mine = e < count ? c.ent_id[at + e] : -1;
+  for (int e0 = 16 * w; e0 < count; e0 += 64 * waves) {
+    const int e = e0 + 16 * waves * row.tile() + row.entry(), mine = e < count ? c.ent_id[at + e] : -1;
     visit(mine >= 0 ? c.ent_count[at + e] : 0u, (uint32_t)mine);
   }
 }
@@ -683,15 +739,6 @@ __global__ __launch_bounds__(kWave* WPR) void vocab_pick_kernel(TopRows c, const
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), r = blockIdx.x;
   const RowState<S, H> row(X, row_node(c.node, r, c.R, c.n_nodes), lane);
   const uint32_t* mrow = c.rm.row(r, c.R);
-  // the first pass's shares of the sum: each wave takes every WPR-th
-  float M = kNoMax, sum = 0.f;
-  if (c.lse != nullptr) {
-    const int shares = c.splits > 0 ? c.splits : c.deal.shares(r / c.share_rows);
-    const size_t at0 = (c.splits > 0 ? 0 : (size_t)c.deal.slot(r / c.share_rows) * c.share_rows) + r % c.share_rows;
-    RowBest none;
-    join_shares<kWave, false>((shares - wave + WPR - 1) / WPR, at0 + (size_t)wave * c.share_rows,
-                              (size_t)c.share_rows * WPR, lane, c.pm, c.pl, nullptr, M, sum, none);
-  }
   // Joins the waves' lists; every wave has the result.
   auto share = [&](Best& b) {
     lists[wave][lane] = b.k;
@@ -719,6 +766,15 @@ __global__ __launch_bounds__(kWave* WPR) void vocab_pick_kernel(TopRows c, const
   };
   uint32_t head[U], most = 0;   // the first of them stay in registers
   load(head, first);
+  // the first pass's shares of the sum: each wave takes every WPR-th
+  float M = kNoMax, sum = 0.f;
+  if (c.lse != nullptr) {
+    const int shares = c.splits > 0 ? c.splits : c.deal.shares(r / c.share_rows);
+    const size_t at0 = (c.splits > 0 ? 0 : (size_t)c.deal.slot(r / c.share_rows) * c.share_rows) + r % c.share_rows;
+    RowBest none;
+    join_shares<kWave, false>((shares - wave + WPR - 1) / WPR, at0 + (size_t)wave * c.share_rows,
+                              (size_t)c.share_rows * WPR, lane, c.pm, c.pl, nullptr, M, sum, none);
+  }
 #pragma unroll
   for (int u = 0; u < U; ++u) most = max(most, head[u]);
   for (int b0 = first + U * WPR * kWave; b0 < nb + lane; b0 += U * WPR * kWave) {
@@ -769,35 +825,35 @@ __global__ __launch_bounds__(kWave* WPR) void vocab_pick_kernel(TopRows c, const
     block = lane < n ? b.k : 0;
   }
 
-  // Their entries, four blocks at a time.
-  constexpr int G = (kWave / 4 + WPR - 1) / WPR;   // fours of a wave
+  // Their entries: each wave takes every WPR-th block, four at a time.
+  constexpr int G = kWave / 4 / WPR;
   uint32_t z[G], id[G];
 #pragma unroll
   for (int i = 0; i < G; ++i) {
-    const int b0 = 4 * (wave + i * WPR);
+    const int b0 = wave + 4 * WPR * i, tiles = (n - b0 + WPR - 1) / WPR;
     z[i] = 0;
     id[i] = 0;
-    if (b0 < n) {
+    if (tiles > 0) {
       int ids[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        const pick_t k = pick_at(block, b0 + u);
+        const pick_t k = pick_at(block, min(b0 + WPR * u, kWave - 1));
         const int e = (int)pick_index(k) * kTopBlock + lane % 16;
-        ids[u] = k != 0 && e < c.V ? e : -1;
+        ids[u] = u < tiles && k != 0 && e < c.V ? e : -1;
       }
-      const pick_t k = __shfl(block, b0 + lane % 16 / 4);
-      const int e = (int)pick_index(k) * kTopBlock + form_place(lane) % 16;
-      const float raw = row.form(W, ids);
-      if (k != 0 && e < c.V && (mrow == nullptr || (mrow[e / 32] >> (e % 32) & 1))) {
-        z[i] = order_of(raw + entry_bias(c.bias, e, c.V));
+      const int at = b0 + WPR * row.tile();
+      const pick_t k = __shfl(block, min(at, kWave - 1));
+      const int e = (int)pick_index(k) * kTopBlock + row.entry();
+      const bool is = at < n && k != 0 && e < c.V;
+      const float b = entry_bias(c.bias, is ? e : 0, c.V);   // (on their way before the rows of W)
+      const uint32_t may = mrow != nullptr ? mrow[is ? e / 32 : 0] : ~0u;
+      const float raw = row.form(W, ids, tiles);
+      if (is && (may >> (e % 32) & 1)) {
+        z[i] = order_of(raw + b);
         id[i] = (uint32_t)e;
       }
-      uint32_t m = z[i];   // of the block: lanes that differ in bits 0, 1, 4, 5
-      m = max(m, __shfl_xor(m, 1));
-      m = max(m, __shfl_xor(m, 2));
-      m = max(m, __shfl_xor(m, 16));
-      m = max(m, __shfl_xor(m, 32));
-      if (lane < 16 && lane % 4 == 0) tops[b0 + lane / 4] = m;
+      const uint32_t m = row.tile_max(z[i]);
+      if (row.leads() && at < n) tops[at] = m;
     }
   }
   __syncthreads();
@@ -822,7 +878,7 @@ __global__ __launch_bounds__(kWave* WPR) void vocab_pick_kernel(TopRows c, const
 #pragma unroll
     for (int i = 0; i < G; ++i) best.add(pick_of(z[i], id[i]), c.K, lane);
     if (c.ent_id != nullptr)
-      ruled_lists(c, r, lane, wave, WPR, [&](uint32_t o, uint32_t e) { best.add(pick_of(o, e), c.K, lane); });
+      ruled_lists(c, row, r, wave, WPR, [&](uint32_t o, uint32_t e) { best.add(pick_of(o, e), c.K, lane); });
     share(best);
     if (wave == 0) answer_list(best.k, r, c.K, lane, c.top, c.logit);
   } else if (wave == 0) {
@@ -1043,9 +1099,16 @@ struct TopPlan {
   dev::Deal deal;
   size_t id, count, add, mask, bmax, pm, pl, wp, block, z, sort, bytes;
 };
-// Whether the picked blocks are sorted.
+// Whether the picked blocks are sorted, which takes seven launches in place of one: by the
+// bytes of W that they would gather, and some of its work a pair.  One launch against
+// seven, the whole call in us: bf16, V = 10,007, H = 64, K = 16, 1,000 rows 24 / 44, 3,001
+// 44 / 55; V = 50,021, H = 128, K = 32, 1,500 rows 69 / 82, 2,999 118 / 110; H = 256, K =
+// 16, 1,000 rows 68 / 89, 2,000 108 / 111 (taken to be the other way), K = 8, 4,000 rows
+// 159 / 156; V = 4,999, H = 32, K = 16, 8,000 rows 75 / 69; V = 50,021, K = 4, 129 / 141;
+// float32, V = 4,999, H = 128, K = 16, 1,229 rows 56 / 59, 2,000 77 / 69.
 bool pairs_sorted(int es, int H, int R, int K) {
-  return R > 64 && (double)R * K * dev::kTopBlock * H * es > 2e8 && (long)R * K <= 1L << 30;
+  const double pairs = (double)R * K;
+  return R > 64 && pairs * (dev::kTopBlock * H * es + 1000) > 2.55e8 && pairs <= 1 << 30;
 }
 template <typename S>
 TopPlan top_plan(int H, int R, int V, int K, int n_listed) {
@@ -1110,11 +1173,20 @@ hipError_t top_h(const TopArgs& a, hipStream_t st) {
     int32_t* id = reinterpret_cast<int32_t*>(ws + p.id);
     uint32_t *count = reinterpret_cast<uint32_t*>(ws + p.count), *out = reinterpret_cast<uint32_t*>(ws + p.mask);
     float* add = reinterpret_cast<float*>(ws + p.add);
-    // Workgroups of a row: one, but where few rows may have lists that are passed over in parts.
-    const int parts = cdiv(a.V, kTable), most = a.R < 1024 ? 1024 / a.R : 1;
-    const int each = a.n_seen + a.n_add > kHashed ? (parts < most ? parts : most) : 1;
-    hipLaunchKernelGGL(vocab_rules_kernel<S>, dim3(a.R, each), dim3(kVocThreads), 0, st, a.R, a.V, c.list, c.rm, p.words,
-                       out, id, count, add);
+    // A row's threads and its table's places by how long the lists are on average; its
+    // workgroups: one, but where few rows may have lists that are passed over in parts.
+    const int listed = a.n_seen + a.n_add;
+    const bool longer = listed / a.R > 256;
+    const int table = longer ? kTable : kTable / 4;
+    const int parts = cdiv(a.V, table), most = a.R < 1024 ? 1024 / a.R : 1;
+    const dim3 grid(a.R, listed > table / 2 ? (parts < most ? parts : most) : 1);
+    const size_t lds = (size_t)table * 16;
+    if (longer)
+      hipLaunchKernelGGL((vocab_rules_kernel<S, 1024>), grid, dim3(1024), lds, st, a.R, a.V, c.list, c.rm, p.words, table,
+                         out, id, count, add);
+    else
+      hipLaunchKernelGGL((vocab_rules_kernel<S, 256>), grid, dim3(256), lds, st, a.R, a.V, c.list, c.rm, p.words, table, out,
+                         id, count, add);
     c.rm = RowMask{out, nullptr, a.R, p.words};
     c.ent_id = id; c.ent_count = count; c.ent_add = add;
   }
