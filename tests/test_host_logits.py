@@ -149,3 +149,36 @@ def test_distillation_reference_against_differences():
             lo[a][i] -= h
             hi[a][i] += h
             assert abs((total(*hi) - total(*lo)) / (2 * h) - r[name][i]) < 1e-8
+
+
+def test_rules_of_rows_as_they_are_uploaded():
+    from paper_1906_11786_amd.tokens import TokenRules
+    V = 70
+    allowed = np.zeros((2, V), bool)
+    allowed[0, [0, 31, 32, 69]] = True
+    allowed[1] = True
+    r = TokenRules(V, 3, allowed=allowed, allowed_of=[1, -1, 0], seen=[[5, 5, 2**40], [], [7]], repetition=1.5,
+                   bias=[{3: 1.0}, [(4, -np.inf), (4, 2.0)], []], device="cpu")
+    mask, of, sp, seen, ap, add, value = [x.numpy() for x in r.tensors]
+    np.testing.assert_array_equal(mask.view(np.uint32), [[0x80000001, 1, 0x20], [0xFFFFFFFF, 0xFFFFFFFF, 0x3F]])
+    np.testing.assert_array_equal(of, [1, -1, 0])
+    np.testing.assert_array_equal(sp, [0, 3, 3, 4])
+    np.testing.assert_array_equal(seen, [5, 5, -1, 7])
+    np.testing.assert_array_equal(ap, [0, 1, 3, 3])
+    np.testing.assert_array_equal(add, [3, 4, 4])
+    np.testing.assert_array_equal(value, np.float32([1.0, -np.inf, 2.0]))
+    assert r.n_listed == 7 and r.struct.n_masks == 2 and r.struct.mask_words == 3 and r.struct.repetition == 1.5
+    empty = TokenRules(V, 2, seen=[[], []], bias=[{}, []], device="cpu")
+    assert empty.n_listed == 0 and empty.struct.n_seen == 0 and empty.struct.seen_ptr is None
+
+
+@pytest.mark.parametrize("kw,text", [
+    (dict(allowed=np.zeros((2, 5), bool)), "allowed"), (dict(allowed=np.zeros((2, 6))), "allowed"),
+    (dict(allowed=np.zeros((2, 6), bool), allowed_of=[0]), "allowed_of"), (dict(allowed_of=[0, 0, 0]), "without allowed"),
+    (dict(seen=[[1]]), "1 seen lists for 3 rows"), (dict(bias=[{}] * 4), "4 bias lists for 3 rows"),
+    (dict(repetition=0.0), "penalties"), (dict(presence=float("nan")), "penalties"),
+    (dict(frequency=float("inf")), "penalties")])
+def test_rules_of_rows_refuse(kw, text):
+    from paper_1906_11786_amd.tokens import TokenRules
+    with pytest.raises(ValueError, match=text):
+        TokenRules(6, 3, device="cpu", **kw)
