@@ -426,27 +426,59 @@ __global__ __launch_bounds__(THREADS) void vocab_rules_kernel(int R, int V, List
       }
     }
     __syncthreads();
+    auto place = [&](int e) {   // of an entry that the table has
+      if (!hashed) return (uint32_t)(e - lo);
+      uint32_t h = hash(e);
+      while (key[h] != (uint32_t)e) h = (h + 1) & (size - 1);
+      return h;
+    };
+    auto adds = [&](uint32_t h) { return hashed ? seen[h] >> 16 : key[h]; };
+    // Entries with several biases: zero, then added up in list order, a wave at a time.
+    int again = 0;
+    for (int i = alo + threadIdx.x; i < ahi; i += THREADS) {
+      const int e = list.add[i];
+      if (e < lo || e >= hi) continue;
+      const uint32_t h = place(e);
+      if (adds(h) > 1) {
+        value[h] = 0.f;
+        again = 1;
+      }
+    }
+    if (__syncthreads_or(again)) {
+      for (int i0 = alo; i0 < ahi; i0 += kWave) {
+        if (i0 / kWave % (THREADS / kWave) == threadIdx.x / kWave) {
+          const int i = i0 + threadIdx.x % kWave, e = i < ahi ? list.add[i] : -1;
+          const float v = i < ahi ? list.value[i] : 0.f;
+          int h = -1;
+          if (e >= lo && e < hi) {
+            h = (int)place(e);
+            if (adds((uint32_t)h) < 2) h = -1;
+          }
+          uint64_t left = __ballot(h >= 0);
+          while (left != 0) {
+            const int one = __builtin_amdgcn_readlane(h, (int)__builtin_ctzll(left));
+            uint64_t same = __ballot(h == one);
+            left &= ~same;
+            float sum = value[one];
+            for (; same != 0; same &= same - 1)
+              sum += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), (int)__builtin_ctzll(same)));
+            value[one] = sum;   // (the same from every lane)
+          }
+        }
+        __syncthreads();
+      }
+    }
     for (int i = threadIdx.x, u = 0; i < n; i += THREADS, ++u) {
       const int e = token(u, i);
       const bool known = e >= 0 && e < V;
       if (known ? e < lo || e >= hi : p != 0) continue;   // another part's
       int found = -1;
       if (known) {
-        uint32_t h = (uint32_t)(e - lo);
-        if (hashed) {
-          h = hash(e);
-          while (key[h] != (uint32_t)e) h = (h + 1) & (size - 1);
-        }
+        const uint32_t h = place(e);
         if (first[h] == (uint32_t)i && (mask == nullptr || (mask[e / 32] >> (e % 32) & 1))) {
           found = e;
-          const uint32_t adds = hashed ? seen[h] >> 16 : key[h];
-          float a = adds == 1 ? value[h] : 0.f;
-          if (adds > 1) {   // in list order
-            for (int k = alo; k < ahi; ++k)
-              if (list.add[k] == e) a += list.value[k];
-          }
           ent_count[at + i] = hashed ? seen[h] & 0xFFFFu : seen[h];
-          ent_add[at + i] = a;
+          ent_add[at + i] = adds(h) > 0 ? value[h] : 0.f;
           atomicAnd(&mine[e / 32], ~(1u << (e % 32)));
         }
       }

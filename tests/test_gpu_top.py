@@ -237,6 +237,43 @@ def test_rules_with_long_lists(rows, V, seen):
     check_exact("bf16", X, W, b, node, 16, 1.0, rules)
 
 
+@pytest.mark.parametrize("rows,adds", [(2, 300), (90, 40), (1, 9000)])
+def test_biases_of_one_entry_are_added_in_list_order(rows, adds):
+    """Values whose float sum depends on the order: the list's own, term by term."""
+    rng = np.random.default_rng(adds)
+    H, V = 32, 1500
+    W, X = np.zeros((V, H)), np.zeros((rows, H))
+    tok = rng.integers(0, 20, (rows, adds)) * 70
+    val = (rng.standard_normal((rows, adds)) * 10.0 ** rng.integers(-4, 4, (rows, adds))).astype(np.float32)
+    top, logit, _ = run("f32", X, W, None, np.arange(rows), 64, 1.0, dict(add=[list(zip(a, b)) for a, b in zip(tok, val)]))
+    for r in range(rows):
+        want = {}
+        for t, v in zip(tok[r].tolist(), val[r]):
+            want[t] = np.float32(want.get(t, np.float32(0)) + v)
+        got = dict(zip(top[r].tolist(), logit[r].tolist()))
+        for t, v in want.items():
+            if v > 0:
+                assert got[t] == float(v)
+
+
+def test_logits_of_any_size():
+    """From 2^-100 to 2^100: the same entries, and log sums by the largest."""
+    for dt in ("f32", "bf16"):
+        for rows in (3, 150):
+            X, W, b, node = exact_case(32, rows, 700, seed=12)
+            for power in (-100, 20, 31, 60, 100):
+                s = 2.0 ** power
+                z, _, _, _ = L.logits(X * s, W, b * s, node)
+                for tau in (1.0, 0.3, 7.0):
+                    top, logit, lse = run(dt, X * s, W, b * s, node, 9, tau)
+                    ids, zk = L.best(z, 9)
+                    np.testing.assert_array_equal(top, ids)
+                    np.testing.assert_array_equal(logit, zk)
+                    want = L.log_sum(z / tau, np.zeros_like(z))[0]
+                    # the rounding of 1 / tau and of two products; a sum of equals and its logarithm
+                    R.within(lse, want, 8 * R.U * np.abs(want) + 2.0 ** -20 + 700 * R.U)
+
+
 def test_a_mask_of_its_own_for_each_row_and_wider_words():
     rng = np.random.default_rng(1)
     X, W, b, node = exact_case(64, 80, 700, seed=4)
