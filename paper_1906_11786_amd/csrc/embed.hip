@@ -710,6 +710,99 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(int n_tok, int
   }
 }
 
+// The same sums over at most kFewListings listings, without a sort: a workgroup per
+// listing looks through all of them and, where its own is the first of its id, adds
+// up the id's, each group of H / 8 lanes every G-th in list order, joined in a fixed
+// tree.  One launch in place of six.  Taken while no id can have more rows than the
+// groups add up in time (rows * H): the whole distillation call in us, this against
+// the sort, 101 rows of 4 at H = 32 27 / 42, 256 of 8 at H = 128 61 / 80, 128 of 16 at
+// H = 256 63 / 82; 2,000 rows of one and the same id at H = 256 253 / 179.
+constexpr int kFewListings = 2048, kFewRows = 1 << 17;
+
+template <typename S, int H>
+__global__ __launch_bounds__(kEmbThreads) void list_rows_few_kernel(int n, int V, ListRows list,
+                                                                    const int32_t* __restrict__ id,
+                                                                    const float* __restrict__ coef,
+                                                                    const S* __restrict__ x, float* __restrict__ dW) {
+  constexpr int L = H / 8, G = kEmbThreads / L, PER = kFewListings / kEmbThreads, U = 2;
+  __shared__ uint16_t match[kFewListings];
+  __shared__ int upto[kFewListings / kWave];   // matches of each 64 listings
+  __shared__ __attribute__((aligned(16))) float share[G][H + 1];
+  const int own = blockIdx.x, key = id[own], lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  if ((unsigned)key >= (unsigned)V) return;
+  int at[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) at[i] = id[min(i * kEmbThreads + (int)threadIdx.x, n - 1)];
+  uint64_t same[PER];
+  int before = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int k = i * kEmbThreads + threadIdx.x;
+    const bool hit = k < n && at[i] == key;
+    if (hit && k < own) before = 1;
+    same[i] = __ballot(hit);
+    if (lane == 0) upto[i * (kEmbThreads / kWave) + wave] = __popcll(same[i]);
+  }
+  if (__syncthreads_or(before)) return;   // an earlier listing's workgroup adds them up
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    int first = 0;
+    const int chunk = i * (kEmbThreads / kWave) + wave;
+    if (same[i] != 0) {
+      for (int c = 0; c < chunk; ++c) first += upto[c];
+      if (same[i] >> lane & 1) match[first + __popcll(same[i] & ((1ull << lane) - 1))] = (uint16_t)(i * kEmbThreads + threadIdx.x);
+    }
+  }
+  int total = 0;
+#pragma unroll
+  for (int c = 0; c < kFewListings / kWave; ++c) total += upto[c];
+  __syncthreads();
+  const int grp = threadIdx.x / L, h = 8 * (threadIdx.x % L);
+  float acc[8] = {}, accb = 0.f;
+  for (int j = grp; j < total; j += G * U) {
+    int row[U];
+    float f[U], v[U][8];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = match[min(j + u * G, total - 1)];
+      row[u] = k / list.K;
+      if (list.node != nullptr) row[u] = list.node[row[u]];
+      f[u] = j + u * G < total ? coef[k] : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) load8f<S>(x + (size_t)row[u] * H + h, v[u]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (j + u * G >= total) break;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[i] += f[u] * v[u][i];
+      accb += f[u];
+    }
+  }
+  int groups = 1;
+  while (groups < G && groups < total) groups *= 2;
+  if (groups > 1) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) share[grp][h + i] = acc[i];
+    if (h == 0) share[grp][H] = accb;
+    __syncthreads();
+    for (int half = groups / 2; half >= 1; half /= 2) {
+      if (grp < half) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) share[grp][h + i] += share[grp + half][h + i];
+        if (h == 0) share[grp][H] += share[grp + half][H];
+      }
+      __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] = share[0][h + i];
+    accb = share[0][H];
+  }
+  if (grp != 0) return;
+  add_row(dW + (size_t)key * H + h, acc);
+  if (list.dbias != nullptr && h == 0) list.dbias[key] += accb;
+}
+
 }  // namespace dev
 
 namespace {
@@ -798,6 +891,22 @@ hipError_t embed_bwd_h(int n, int V, const int32_t* tok_ptr, const int32_t* tok,
                        0, st, n_tok, V, l.block, l.blocks, a, part, dtable, list);
   return hipGetLastError();
 }
+template <typename S, int H>
+hipError_t list_rows(int R, int n, int V, int n_nodes, const dev::ListRows& list, const int32_t* id, const float* coef,
+                     const void* x, float* dW, char* ws, hipStream_t st) {
+  if (n <= dev::kFewListings && R * H <= dev::kFewRows) {
+    hipLaunchKernelGGL((dev::list_rows_few_kernel<S, H>), dim3(n), dim3(dev::kEmbThreads), 0, st, n, V, list, id, coef,
+                       static_cast<const S*>(x), dW);
+    return hipGetLastError();
+  }
+  return embed_bwd_h<S, H, true>(n_nodes, V, nullptr, id, n, 1.f, 0, coef, Dropout{}, x, dW, ws, st, list);
+}
+template <int H>
+hipError_t list_rows_h(int dt, int R, int n, int V, int n_nodes, const dev::ListRows& list, const int32_t* id,
+                       const float* coef, const void* x, float* dW, char* ws, hipStream_t st) {
+  return dt == GGNN_BF16 ? list_rows<dev::bf16s, H>(R, n, V, n_nodes, list, id, coef, x, dW, ws, st)
+                         : list_rows<float, H>(R, n, V, n_nodes, list, id, coef, x, dW, ws, st);
+}
 }  // namespace
 
 size_t embed_bwd_workspace(int H, int n_tok) { return embed_layout(H, n_tok).bytes; }
@@ -831,22 +940,15 @@ size_t list_rows_workspace(int H, int n) {
 
 hipError_t launch_list_rows(int dt, int R, int K, int H, int V, int n_nodes, const int32_t* node, const int32_t* id,
                             const float* coef, const void* x, float* dW, float* dbias, void* ws, hipStream_t st) {
-  const Dropout none{};
   const dev::ListRows list{K, node, dbias, nullptr};
   char* w = static_cast<char*>(ws);
   const int n = R * K;
-#define LIST_ROWS(H)                                                                                              \
-  case H:                                                                                                         \
-    return dt == GGNN_BF16                                                                                        \
-               ? embed_bwd_h<dev::bf16s, H, true>(n_nodes, V, nullptr, id, n, 1.f, 0, coef, none, x, dW, w, st, list) \
-               : embed_bwd_h<float, H, true>(n_nodes, V, nullptr, id, n, 1.f, 0, coef, none, x, dW, w, st, list);
   switch (H) {
-    LIST_ROWS(32)
-    LIST_ROWS(64)
-    LIST_ROWS(128)
-    LIST_ROWS(256)
+    case 32: return list_rows_h<32>(dt, R, n, V, n_nodes, list, id, coef, x, dW, w, st);
+    case 64: return list_rows_h<64>(dt, R, n, V, n_nodes, list, id, coef, x, dW, w, st);
+    case 128: return list_rows_h<128>(dt, R, n, V, n_nodes, list, id, coef, x, dW, w, st);
+    case 256: return list_rows_h<256>(dt, R, n, V, n_nodes, list, id, coef, x, dW, w, st);
   }
-#undef LIST_ROWS
   return hipErrorInvalidValue;
 }
 

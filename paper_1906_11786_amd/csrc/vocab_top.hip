@@ -282,7 +282,16 @@ __global__ __launch_bounds__(kVocThreads) void vocab_max_few_kernel(
   const int lane = threadIdx.x % kWave, g = lane / 32, r = lane % 32;
   const int split = blockIdx.x * kVocWaves + threadIdx.x / kWave;
   const int tiles = (V + 31) / 32, t0 = split * per, t1 = min(tiles, t0 + per);
-  frag_t<S> xf[NT][H / 16];
+  // a tile's rows of W and biases are on their way while the one before is worked on, the first one's before
+  // the rows' nodes are known
+  frag_t<S> xf[NT][H / 16], next[H / 16];
+  float next_bias[16];
+  auto fetch = [&](int t) {
+    load_row<S, H>(next, W, min(t * 32 + top_entry(r), V - 1), lane);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) next_bias[j] = bias != nullptr ? bias[min(t * 32 + 16 * g + j, V - 1)] : 0.f;
+  };
+  fetch(min(t0, tiles - 1));
   RowSum sum[NT];
   const uint32_t* mrow[NT];
 #pragma unroll
@@ -293,10 +302,13 @@ __global__ __launch_bounds__(kVocThreads) void vocab_max_few_kernel(
   }
   for (int t = t0; t < t1; ++t) {
     frag_t<S> wf[H / 16];
-    load_row<S, H>(wf, W, min(t * 32 + top_entry(r), V - 1), lane);
     f32x16 b;
 #pragma unroll
-    for (int j = 0; j < 16; ++j) b[j] = entry_bias(bias, t * 32 + 16 * g + j, V);
+    for (int kk = 0; kk < H / 16; ++kk) wf[kk] = next[kk];
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+      b[j] = t * 32 + 16 * g + j >= V || next_bias[j] <= kMaskedBias ? -INFINITY : next_bias[j];
+    if (t + 1 < t1) fetch(t + 1);
 #pragma unroll
     for (int a = 0; a < NT; ++a) {
       uint32_t w = ~0u;
@@ -511,15 +523,19 @@ __device__ __forceinline__ pick_t pick_at(pick_t k, int lane) {   // lane: the s
          (uint32_t)__builtin_amdgcn_readlane((int)k, lane);
 }
 // A bound that K or more of the wave's numbers a and b reach, bit by bit: the K-th
-// largest, or any between it and the next; 0 where fewer are not 0.
+// largest, or any between it and the next; 0 where fewer are not 0.  Four bits between
+// two looks whether it is reached by just K (the call for one row over 10,007 entries:
+// 13.6 us; a look each bit 18.0, all 32 bits without one 14.9).
 __device__ __forceinline__ uint32_t kth_of(uint32_t a, uint32_t b, int K) {
   uint32_t t = 0;
 #pragma unroll 1
-  for (uint32_t bit = 1u << 31; bit != 0; bit >>= 1) {
-    const uint32_t c = t | bit;
-    const int n = __popcll(__ballot(a >= c)) + __popcll(__ballot(b >= c));
-    if (n >= K) t = c;
-    if (n == K) break;
+  for (int shift = 28; shift >= 0; shift -= 4) {
+#pragma unroll
+    for (int bit = 3; bit >= 0; --bit) {
+      const uint32_t c = t | 1u << (shift + bit);
+      if (__popcll(__ballot(a >= c)) + __popcll(__ballot(b >= c)) >= K) t = c;
+    }
+    if (__popcll(__ballot(a >= t)) + __popcll(__ballot(b >= t)) == K) break;
   }
   return t;
 }
@@ -1263,7 +1279,7 @@ hipError_t top_h(const TopArgs& a, hipStream_t st) {
     return hipGetLastError();
   }
   if (a.R <= 64)
-    hipLaunchKernelGGL((vocab_pick_kernel<S, H, 16>), dim3(a.R), dim3(16 * kWave), 0, st, c, X, W);
+    hipLaunchKernelGGL((vocab_pick_kernel<S, H, 8>), dim3(a.R), dim3(8 * kWave), 0, st, c, X, W);
   else
     hipLaunchKernelGGL((vocab_pick_kernel<S, H, 4>), dim3(a.R), dim3(4 * kWave), 0, st, c, X, W);
   return hipGetLastError();
