@@ -556,10 +556,11 @@ __global__ __launch_bounds__(kVocThreads) void vocab_distill_join_kernel(
   if (r >= (GRAD ? Rp : R)) return;   // whole waves leave together
   const int grp = lane / L, h = 4 * (lane % L);
   const int n = row_node(node, r, R, n_nodes);
+  // (loads that no branch holds back are on their way together)
+  const size_t at = (size_t)r * K + lane, some = (size_t)min(r, R - 1) * K + min(lane, K - 1);
+  const int some_id = t_id[some];
+  const float some_logit = t_logit[some];
   const f32x4 x = n >= 0 ? load4f(X + (size_t)n * H + h) : f32x4{};
-  const size_t at = (size_t)r * K + lane;
-  int id = lane < K && n >= 0 ? t_id[at] : -1;
-  float t = id >= 0 ? t_logit[at] * te.inv : -INFINITY;
   const int shares = r >= R ? 0 : splits > 0 ? splits : deal.shares(r / kVocRows);
   const size_t stride = splits > 0 ? 32 : kVocRows;
   const size_t at0 = splits > 0 ? r : (size_t)deal.slot(r / kVocRows) * kVocRows + r % kVocRows;
@@ -567,6 +568,8 @@ __global__ __launch_bounds__(kVocThreads) void vocab_distill_join_kernel(
   RowBest none;
   join_shares<kWave, false>(shares, at0, stride, lane, pm, pl, nullptr, M, sum, none);
   const float v = row_lse(M, sum, te);
+  int id = lane < K && n >= 0 ? some_id : -1;
+  const float t = id >= 0 ? some_logit * te.inv : -INFINITY;
 
   bool bad = __ballot(id >= V || !(t < INFINITY)) != 0;
   const bool any = __ballot(t > -INFINITY) != 0;
@@ -600,13 +603,9 @@ __global__ __launch_bounds__(kVocThreads) void vocab_distill_join_kernel(
       float b[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int k = k0 + u * G + grp, i = __shfl(id, k % kWave);
-        w[u] = f32x4{};
-        b[u] = 0.f;
-        if (k < K && i >= 0) {
-          w[u] = load4f(W + (size_t)i * H + h);
-          b[u] = entry_bias(bias, i, V);
-        }
+        const int i = max(__shfl(id, (k0 + u * G + grp) % kWave), 0);
+        w[u] = load4f(W + (size_t)i * H + h);
+        b[u] = entry_bias(bias, i, V);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -616,6 +615,7 @@ __global__ __launch_bounds__(kVocThreads) void vocab_distill_join_kernel(
         const float qi = __shfl(q, k % kWave), tk = __shfl(t, k % kWave);
         const bool here = k < K && i >= 0;
         const float qk = here ? qi : 0.f;
+        if (!here) w[u] = f32x4{};   // (what stands there in place of an entry may be anything)
         float z = x[0] * w[u][0] + x[1] * w[u][1] + x[2] * w[u][2] + x[3] * w[u][3];
 #pragma unroll
         for (int o = L / 2; o >= 1; o /= 2) z += __shfl_xor(z, o);

@@ -861,7 +861,17 @@ __global__ __launch_bounds__(kWave* WPR) void vocab_pick_kernel(TopRows c, const
   int n = n_blocks;
   pick_t block = 0;   // one a lane
   if (n <= kWave) {
+    // the K first of them, in order: each lane counts how many come before its own
     block = lane < n ? chosen[lane] : 0;
+    int rank = lane;
+    if (lane < n) {
+      rank = 0;
+#pragma unroll 8
+      for (int i = 0; i < n; ++i) rank += chosen[i] > block;
+    }
+    block = (pick_t)(uint32_t)__builtin_amdgcn_ds_permute(4 * rank, (int)(block >> 32)) << 32 |
+            (uint32_t)__builtin_amdgcn_ds_permute(4 * rank, (int)block);
+    n = min(n, c.K);
     __syncthreads();
   } else {
     __syncthreads();
