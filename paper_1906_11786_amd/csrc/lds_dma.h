@@ -21,11 +21,6 @@ __device__ __forceinline__ void dma16(const void* gsrc, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(gsrc)
                : "memory", "m0");
 }
-// The same from a wave-uniform address and each lane's offset in bytes.
-__device__ __forceinline__ void dma16(const void* base, uint32_t offset, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base)
-               : "memory", "m0");
-}
 #pragma clang diagnostic pop
 // Wait until at most N of this wave's vector-memory loads are outstanding
 // (vmcnt only).

@@ -55,6 +55,15 @@ constexpr int top_waves(int H) {
 __device__ __forceinline__ int top_row(int r) { return 8 * ((r >> 2) & 3) + 4 * (r >> 4) + (r & 3); }
 __device__ __forceinline__ int top_entry(int i) { return 16 * ((i >> 2) & 1) + 4 * (i >> 3) + (i & 3); }
 
+// dma16 (csrc/lds_dma.h) from a wave-uniform address and each lane's offset in bytes.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void dma16(const void* base, uint32_t offset, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base)
+               : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
 // Bit masks over the entries, one a row: index of[r] (r where of is NULL); one
 // outside [0, n) excludes nothing.
 struct RowMask {
