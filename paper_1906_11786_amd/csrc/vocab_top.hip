@@ -971,7 +971,8 @@ __global__ __launch_bounds__(kWave* WPR) void vocab_pick_kernel(TopRows c, const
 // The K best blocks of each row, one wave a row: block [R][K], -1 from where none is
 // left.
 constexpr int kReach = 2 * kWave;   // blocks that reach the bound, at most
-template <typename S>   // (the same for both types)
+// The first 512 GROUPS blocks are held in registers, the rest is read twice.
+template <typename S, int GROUPS>   // (the same for both types S)
 __global__ __launch_bounds__(kVocThreads) void vocab_blocks_kernel(int R, int nb, int nbs, int K,
                                                                    const float* __restrict__ bmax,
                                                                    int32_t* __restrict__ block) {
@@ -982,33 +983,45 @@ __global__ __launch_bounds__(kVocThreads) void vocab_blocks_kernel(int R, int nb
   if (r >= R) return;   // whole waves leave together
   const float* bm = bmax + (size_t)r * nbs;
   int32_t* out = block + (size_t)r * K;
-  auto load = [&](uint32_t (&o)[U], int b0) {
-    float m[U];   // (all on their way before the first is looked at)
+  auto load = [&](float (&m)[U], int b0) {   // (all on their way before the first is looked at)
 #pragma unroll
     for (int u = 0; u < U; ++u) m[u] = bm[min(b0 + u * kWave + lane, nb - 1)];
-#pragma unroll
-    for (int u = 0; u < U; ++u) o[u] = b0 + u * kWave + lane < nb ? order_of(m[u]) : 0u;
   };
-  uint32_t most[2] = {};
-  for (int b0 = 0; b0 < nb; b0 += U * kWave) {
-    uint32_t o[U];
-    load(o, b0);
+  auto order = [&](float m, int b) { return b < nb ? order_of(m) : 0u; };
+  float held[GROUPS][U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) most[u % 2] = max(most[u % 2], o[u]);
+  for (int g = 0; g < GROUPS; ++g) load(held[g], g * U * kWave);
+  uint32_t most[2] = {};
+#pragma unroll
+  for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+    for (int u = 0; u < U; ++u) most[u % 2] = max(most[u % 2], order(held[g][u], (g * U + u) * kWave + lane));
+  for (int b0 = GROUPS * U * kWave; b0 < nb; b0 += U * kWave) {
+    float m[U];
+    load(m, b0);
+#pragma unroll
+    for (int u = 0; u < U; ++u) most[u % 2] = max(most[u % 2], order(m[u], b0 + u * kWave + lane));
   }
   const uint32_t bound = max(kth_of(most[0], most[1], K), 1u);
   const uint64_t below = (1ull << lane) - 1;
   int n = 0;
-  for (int b0 = 0; b0 < nb; b0 += U * kWave) {
-    uint32_t o[U];
-    load(o, b0);
+  auto take = [&](float m, int b) {
+    const uint32_t o = order(m, b);
+    const uint64_t in = __ballot(o >= bound);
+    if (in == 0) return;
+    const int at = n + __popcll(in & below);
+    if (o >= bound && at < kReach) reach[wave][at] = u32x2{o, (uint32_t)b};
+    n += __popcll(in);
+  };
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const uint64_t in = __ballot(o[u] >= bound);
-      const int at = n + __popcll(in & below);
-      if (o[u] >= bound && at < kReach) reach[wave][at] = u32x2{o[u], (uint32_t)(b0 + u * kWave + lane)};
-      n += __popcll(in);
-    }
+  for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+    for (int u = 0; u < U; ++u) take(held[g][u], (g * U + u) * kWave + lane);
+  for (int b0 = GROUPS * U * kWave; b0 < nb; b0 += U * kWave) {
+    float m[U];
+    load(m, b0);
+#pragma unroll
+    for (int u = 0; u < U; ++u) take(m[u], b0 + u * kWave + lane);
   }
   if (n > kReach) {   // many equal ones
     Best best;
@@ -1287,8 +1300,14 @@ hipError_t top_h(const TopArgs& a, hipStream_t st) {
     int32_t* block = reinterpret_cast<int32_t*>(ws + p.block);
     float* z = reinterpret_cast<float*>(ws + p.z);
     const int nb = cdiv(a.V, kTopBlock), pairs = a.R * a.K;
-    hipLaunchKernelGGL(vocab_blocks_kernel<S>, dim3(cdiv(a.R, kVocWaves)), dim3(kVocThreads), 0, st, a.R, nb, p.nbs, a.K,
-                       bmax, block);
+#define BLOCKS(GROUPS)                                                                                              \
+  hipLaunchKernelGGL((vocab_blocks_kernel<S, GROUPS>), dim3(cdiv(a.R, kVocWaves)), dim3(kVocThreads), 0, st, a.R, nb, \
+                     p.nbs, a.K, bmax, block)
+    if (nb <= 512) BLOCKS(1);
+    else if (nb <= 1024) BLOCKS(2);
+    else if (nb <= 2048) BLOCKS(4);
+    else BLOCKS(7);
+#undef BLOCKS
     const void* sorted;
     const hipError_t err = launch_sort(pairs, nb, block, ws + p.sort, &sorted, st);
     if (err != hipSuccess) return err;

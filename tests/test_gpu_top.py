@@ -130,6 +130,17 @@ def test_the_same_entries(dt, H, rows, V, K):
     check_exact(dt, X, W, b if H != 64 else None, node, K, tau=2.0)
 
 
+@pytest.mark.parametrize("dt,V", [("bf16", 8000), ("bf16", 16001), ("bf16", 30011), ("bf16", 60013), ("f32", 60013)])
+def test_many_rows_over_vocabularies_of_all_sizes(dt, V):
+    """Enough pairs of rows and blocks to be sorted; block maxima that registers hold, all or a part."""
+    say(f"top dt={dt} V={V}")
+    rows = 450
+    X, W, b, node = exact_case(256, rows, V, seed=V)
+    check_exact(dt, X, W, b, node, 64, tau=2.0)
+    rng = np.random.default_rng(V)
+    check_exact(dt, X, W, None, node, 64, 1.0, random_rules(rng, rows, V, 4, 60, 9, repetition=1.25, presence=0.5))
+
+
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,V,K", [(2, 3000, 64), (70, 3000, 33), (2100, 3000, 64)])
 def test_equal_logits_go_to_the_lower_entry(dt, rows, V, K):
@@ -375,3 +386,24 @@ def test_captured_and_replayed():
         np.testing.assert_array_equal(host(logit), want[1])
         np.testing.assert_array_equal(host(lse), want[2])
     assert keep
+
+
+def test_block_maxima_past_32_bits():
+    """400,000 rows over 60,000 entries: 6 GB of block maxima; the first answers are the loss's best entries."""
+    n, V, H, K = 400000, 60000, 32, 2
+    g = torch.Generator(device="cuda").manual_seed(5)
+    X = (torch.randn((n, H), generator=g, device="cuda") * 16).round_().clamp_(-127, 127).div_(16).bfloat16()
+    W = (torch.randn((V, H), generator=g, device="cuda") * 16).round_().clamp_(-127, 127).div_(64).bfloat16()
+    need = capi.ggnn_vocab_top_workspace_bytes("bf16", H, n, V, K, 0)
+    assert need > 1 << 32
+    ws = torch.empty((need,), dtype=torch.uint8, device="cuda")
+    top, logit = torch.empty((n, K), dtype=torch.int32, device="cuda"), torch.empty((n, K), device="cuda")
+    capi.ggnn_vocab_top("bf16", n, H, n, V, X, W, None, None, None, 1.0, K, top, logit, None, ws, need)
+    best, lse = torch.empty((n,), dtype=torch.int32, device="cuda"), torch.empty((n,), device="cuda")
+    capi.ggnn_vocab_loss("bf16", n, H, n, V, X, W, None, None, None, None, lse, best, ws, need)
+    assert torch.equal(top[:, 0], best)
+    for at in (0, 123457, n - 100):   # the second ones of a few rows, the lower entry of equals
+        z = X[at:at + 100].float() @ W.float().t()
+        want = torch.sort(z, dim=1, descending=True, stable=True)
+        assert torch.equal(top[at:at + 100], want.indices[:, :2].int())
+        assert torch.equal(logit[at:at + 100], want.values[:, :2])
