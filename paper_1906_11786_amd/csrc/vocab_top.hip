@@ -106,6 +106,15 @@ struct RowSum {
 // entries in the order in which lanes read them as fragments, 1 KB a fragment, so
 // that a read's place is a constant; the copies, 32 bytes a row each, pay for that
 // order, and their addresses are constants too but in the last chunk.
+//
+// 12,001 rows over 50,021 entries at H = 256: 290 us, 1.06 PFLOP/s (a plain 8,192^3 product
+// 1.39), matrix cores 53% busy and vector issue 41% at 2.0 GHz; without the log sum 247.
+// (Products and exponentials of two tiles interleaved in one wave a SIMD, three buffers:
+// 349; rows of the tile in LDS, 64 entries a barrier: 308.)  2,999 rows at H = 128: 52,
+// 0.74 PFLOP/s, matrix cores 31%, vector issue 46%, waiting 36%; without the log sum 43.
+// 3,001 rows over 10,007 at H = 64 with masks 17.4, waiting 46%: four units a workgroup
+// (two of twice the workgroups: 1.5 us more).
+// Block maxima: 10% of these times.
 template <typename S, int H, bool LSE, bool MASK>
 __global__ __launch_bounds__(kWave* top_group<S>(H), top_waves<S>(H)) void vocab_max_kernel(
     int n_nodes, int R, int V, Deal deal, Temper te, const S* __restrict__ X, const bf16s* __restrict__ W,
@@ -282,7 +291,9 @@ __global__ __launch_bounds__(kWave* top_group<S>(H), top_waves<S>(H)) void vocab
 }
 
 // First pass for at most 32 NT rows: every wave holds the same rows and takes `per`
-// tiles of 32 entries, read straight from memory, since no other wave needs them.
+// tiles of 32 entries, read straight from memory, since no other wave needs them.  4.0 us
+// for one row over 10,007 entries at H = 64 (the launch), 9.6 over 50,021 at H = 256 (25.6
+// MB, 2.7 TB/s: one or two round trips to memory a wave).
 template <typename S, int H, int NT, bool LSE, bool MASK>
 __global__ __launch_bounds__(kVocThreads) void vocab_max_few_kernel(
     int n_nodes, int R, int V, int per, Temper te, const S* __restrict__ X, const S* __restrict__ W,
@@ -374,7 +385,9 @@ __device__ __forceinline__ void list_range(const int32_t* ptr, int n, int r, int
   hi = ptr != nullptr ? min(max(ptr[r + 1], lo), n) : 0;
 }
 
-// THREADS a row.
+// THREADS a row.  Latency: 5.5 us for one row of 24 listings, 9 us for 64 rows of 780
+// (1,024 threads; 256 threads and a hash table of half the places 21), 13 us for 3,001 rows
+// of 58.
 template <typename S, int THREADS>   // (the same for both types S)
 __global__ __launch_bounds__(THREADS) void vocab_rules_kernel(int R, int V, Listing list, RowMask rm, int words,
                                                               int table, uint32_t* __restrict__ out,
@@ -785,6 +798,10 @@ __device__ __forceinline__ void join_own(RowSum own, float& M, float& sum) {
 // the K-th largest of numbers that are maxima of disjoint parts.  What reaches it is
 // seldom much more than K, and goes to LDS as one list; where it does not fit 64
 // places (many equal ones), the waves' own lists are joined instead.
+//
+// One row over 10,007 entries: 8.3 us, of which two barriers' waits and four dependent
+// round trips to memory are most (an insertion into sorted lists in registers 15.0); 64
+// rows of 780 listings 21; 1,229 rows in float32, K = 16, 31 (161 MB gathered, 5 TB/s).
 template <typename S, int H, int WPR>
 __global__ __launch_bounds__(kWave* WPR) void vocab_pick_kernel(TopRows c, const S* __restrict__ X,
                                                                 const S* __restrict__ W) {
@@ -966,7 +983,10 @@ __global__ __launch_bounds__(kWave* WPR) void vocab_pick_kernel(TopRows c, const
 //
 // A block's 16 rows of W are 16 times a state, so where many rows pick blocks it is
 // the states that move: the picked (row, block) pairs are sorted by block, and a wave
-// forms the logits of 16 pairs, mostly of one block, as one 16 x 16 tile.
+// forms the logits of 16 pairs, mostly of one block, as one 16 x 16 tile.  12,001 rows, K =
+// 32, H = 256: blocks 43 us (150 MB of maxima), sort 35, pairs 55 (420 MB of states, rows of
+// W and logits through the L2s, 7.6 TB/s), answers 29; gathering 3.1 GB of W in one
+// launch took 415.
 
 // The K best blocks of each row, one wave a row: block [R][K], -1 from where none is
 // left.
