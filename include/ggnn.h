@@ -795,7 +795,9 @@ size_t ggnn_vocab_top_workspace_bytes(ggnn_dtype dt, int32_t H, int32_t n_rows, 
  *            entry whose z is NaN or -inf is not answered.
  *   lse      [n_rows] float (written: log sum_v exp(z_v / temperature) over the entries
  *            that are left, -inf for none), or NULL
- *   temperature  in [0.001, 1000], of lse alone
+ *   temperature  in [0.001, 1000], of lse alone.  Logits over the temperature may
+ *            have any size up to 1e38, as those of ggnn_vocab_loss
+ * The row of W of an entry that the masks of all rows take out may hold anything.
  * Logits are float32 sums, formed a second time for the entries returned: entries
  * whose exact logits differ by less than the rounding of such a sum may be returned
  * in either order, or one in place of the other.  The other arguments, and nodes

@@ -317,6 +317,47 @@ def test_a_token_seen_named_and_masked_at_once():
     assert got[16] == -0.75 and got[5] == 5 / 4 - 4 + 8 and 30 not in got and 31 not in got and 38 not in got
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,K", [(4, 9), (60, 9), (150, 9), (2100, 64)])
+def test_what_stands_in_masked_rows_does_not_matter(dt, rows, K):
+    X, W, b, node = exact_case(32, rows, 3000, seed=13)
+    rng = np.random.default_rng(3)
+    mask = rng.random((1, 3000)) < 0.6
+    mask[0, 0] = False
+    rules = dict(mask=mask, mask_of=np.zeros(rows, np.int64), seen=[[0, 5, 7, 2999]] * rows, repetition=1.25, presence=0.5)
+    want = run(dt, X, W, b, node, K, 1.0, rules)
+    for value in (np.nan, np.inf, -np.inf):
+        W2 = W.copy()
+        W2[~mask[0]] = value
+        for got, w in zip(run(dt, X, W2, b, node, K, 1.0, rules), want):
+            np.testing.assert_array_equal(got, w)
+
+
+def test_two_calls_at_once_on_two_streams():
+    X, W, b, node = exact_case(64, 700, 5000, seed=14)
+    rng = np.random.default_rng(4)
+    rules = random_rules(rng, 700, 5000, 3, 40, 8, repetition=1.25, presence=0.5)
+    want = run("bf16", X, W, b, node, 16, 1.0, rules)
+    ru, keep, listed = struct(rules, 5000)
+    args = dev(X, "bf16"), dev(W, "bf16"), dev(b), ints(node)
+    outs = []
+    torch.cuda.synchronize()
+    for s in (torch.cuda.Stream(), torch.cuda.Stream()):
+        top, logit = torch.empty((700, 16), dtype=torch.int32, device="cuda"), torch.empty((700, 16), device="cuda")
+        lse, ws = torch.empty((700,), device="cuda"), scratch(capi.ggnn_vocab_top_workspace_bytes("bf16", 64, 700, 5000, 16, listed))
+        torch.cuda.synchronize()
+        outs.append((s, top, logit, lse, ws))
+    for _ in range(5):
+        for s, top, logit, lse, ws in outs:
+            capi.ggnn_vocab_top("bf16", len(X), 64, 700, 5000, *args, ru, 1.0, 16, top, logit, lse, ws, ws.numel(), stream=s)
+    torch.cuda.synchronize()
+    for _, top, logit, lse, _ in outs:
+        np.testing.assert_array_equal(top.cpu().numpy(), want[0])
+        np.testing.assert_array_equal(host(logit), want[1])
+        np.testing.assert_array_equal(host(lse), want[2])
+    assert keep
+
+
 def test_logits_that_are_not_finite():
     """NaN and infinite biases: NaN entries are not answered and make the log sum NaN, +inf is the best."""
     for rows in (3, 100):
