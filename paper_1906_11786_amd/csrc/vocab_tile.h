@@ -244,21 +244,13 @@ __device__ __forceinline__ void join_shares(int n, size_t at0, size_t stride, in
   constexpr int U = 4;   // shares in flight per lane
   for (int s0 = q; s0 < n; s0 += L * U) {
     float m[U], l[U];
-    RowBest z[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int s = s0 + u * L;
       const size_t at = at0 + (size_t)(s < n ? s : s0) * stride;
-      m[u] = pm[at];   // (a load behind a branch each would wait for the one before)
-      l[u] = pl[at];
-      if (BEST) z[u] = pb[at];
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const bool in = s0 + u * L < n;
-      m[u] = in ? m[u] : kNoMax;
-      l[u] = in ? l[u] : 0.f;
-      if (BEST && in) take_best(best, z[u].z, z[u].v);
+      m[u] = s < n ? pm[at] : kNoMax;
+      l[u] = s < n ? pl[at] : 0.f;
+      if (BEST && s < n) take_best(best, pb[at].z, pb[at].v);
     }
     float top = M;
 #pragma unroll

@@ -834,7 +834,7 @@ __global__ __launch_bounds__(kWave* WPR) void vocab_pick_kernel(TopRows c, const
   auto load = [&](uint32_t (&o)[U], int b0) {
     float m[U];   // (all on their way before the first is looked at)
 #pragma unroll
-    for (int u = 0; u < U; ++u) m[u] = bm[min(b0 + u * WPR * kWave, nb - 1)];
+    for (int u = 0; u < U; ++u) m[u] = b0 + u * WPR * kWave < nb ? bm[b0 + u * WPR * kWave] : 0.f;
 #pragma unroll
     for (int u = 0; u < U; ++u) o[u] = b0 + u * WPR * kWave < nb ? order_of(m[u]) : 0u;
   };
