@@ -387,7 +387,7 @@ __device__ __forceinline__ void list_range(const int32_t* ptr, int n, int r, int
 
 // THREADS a row.  Latency: 5.5 us for one row of 24 listings, 9 us for 64 rows of 780
 // (1,024 threads; 256 threads and a hash table of half the places 21), 13 us for 3,001 rows
-// of 58.
+// of 58: a chain of loads, table look-ups and barriers, a few rows a compute unit.
 template <typename S, int THREADS>   // (the same for both types S)
 __global__ __launch_bounds__(THREADS) void vocab_rules_kernel(int R, int V, Listing list, RowMask rm, int words,
                                                               int table, uint32_t* __restrict__ out,
@@ -799,9 +799,9 @@ __device__ __forceinline__ void join_own(RowSum own, float& M, float& sum) {
 // seldom much more than K, and goes to LDS as one list; where it does not fit 64
 // places (many equal ones), the waves' own lists are joined instead.
 //
-// One row over 10,007 entries: 8.3 us, of which two barriers' waits and four dependent
+// One row over 10,007 entries: 7.0 us, of which two barriers' waits and four dependent
 // round trips to memory are most (an insertion into sorted lists in registers 15.0); 64
-// rows of 780 listings 21; 1,229 rows in float32, K = 16, 31 (161 MB gathered, 5 TB/s).
+// rows of 780 listings 19; 1,229 rows in float32, K = 16, 30 (161 MB gathered, 5 TB/s).
 template <typename S, int H, int WPR>
 __global__ __launch_bounds__(kWave* WPR) void vocab_pick_kernel(TopRows c, const S* __restrict__ X,
                                                                 const S* __restrict__ W) {
@@ -984,7 +984,7 @@ __global__ __launch_bounds__(kWave* WPR) void vocab_pick_kernel(TopRows c, const
 // A block's 16 rows of W are 16 times a state, so where many rows pick blocks it is
 // the states that move: the picked (row, block) pairs are sorted by block, and a wave
 // forms the logits of 16 pairs, mostly of one block, as one 16 x 16 tile.  12,001 rows, K =
-// 32, H = 256: blocks 43 us (150 MB of maxima), sort 35, pairs 55 (420 MB of states, rows of
+// 32, H = 256: blocks 42 us (150 MB of maxima), sort 35, pairs 55 (420 MB of states, rows of
 // W and logits through the L2s, 7.6 TB/s), answers 29; gathering 3.1 GB of W in one
 // launch took 415.
 
