@@ -823,10 +823,10 @@ size_t ggnn_vocab_distill_workspace_bytes(ggnn_dtype dt, int32_t H, int32_t n_ro
  *   K        entries of a list, 1 .. 64;  n_rows * K <= 2^30
  *   teacher_id     [n_rows][K] int32; a negative one: no entry (any of a row's may
  *            be).  One listed twice counts twice.  At or above V: loss NaN, no gradient.
- *   teacher_logit  [n_rows][K] float, not read where there is no entry; -inf: q_k = 0;
+ *   teacher_logit  [n_rows][K] float, not used where there is no entry; -inf: q_k = 0;
  *            a NaN or +inf one: loss NaN, no gradient
  *   teacher_lse    [n_rows] float, or NULL.  One that is not finite: loss NaN, no
- *            gradient (not read into a row without entries).
+ *            gradient (not used in a row without entries).
  *   temperature    in [0.001, 1000]
  *   loss, lse      [n_rows] float (written).  A row without entries, or whose
  *            entries all have -inf, has no loss (0) and no gradient, whatever its
