@@ -76,6 +76,11 @@ struct RowMask {
     return (unsigned)i < (unsigned)n ? bits + (size_t)i * words : nullptr;
   }
 };
+// The bits of 32 entries from e0 on that the vocabulary has.  Lanes beyond it hold the last entry's logits, which
+// the starting -inf does not cover where its row is masked and holds NaN: they are taken out whatever a mask says there.
+__device__ __forceinline__ uint32_t entry_bits(int e0, int V) {
+  return V - e0 >= 32 ? ~0u : V > e0 ? (1u << (V - e0)) - 1u : 0u;
+}
 // -inf where the entry's bit is 0; a: 16 logits, w: their bits from bit 0 on.
 __device__ __forceinline__ void take_out(f32x16& a, uint32_t w) {
 #pragma unroll
@@ -174,7 +179,7 @@ __global__ __launch_bounds__(kWave* top_group<S>(H), top_waves<S>(H)) void vocab
 #pragma unroll
         for (int a = 0; a < NT; ++a)
 #pragma unroll
-          for (int i = 0; i < SUB; ++i) word[a][i] = next_word[a][i] >> (16 * g);
+          for (int i = 0; i < SUB; ++i) word[a][i] = (next_word[a][i] & entry_bits(q * T + 32 * i, V)) >> (16 * g);
       }
       wait_copies<0>();
       __syncthreads();
@@ -332,7 +337,8 @@ __global__ __launch_bounds__(kVocThreads) void vocab_max_few_kernel(
 #pragma unroll
     for (int a = 0; a < NT; ++a) {
       uint32_t w = ~0u;
-      if (MASK && mrow[a] != nullptr) w = mrow[a][t] >> (16 * g);
+      if (MASK && mrow[a] != nullptr) w = mrow[a][t];
+      w = (w & entry_bits(32 * t, V)) >> (16 * g);
       f32x16 s = b;
 #pragma unroll
       for (int kk = 0; kk < H / 16; ++kk) mma32(s, wf[kk], xf[a][kk]);
