@@ -847,6 +847,9 @@ ggnn_status ggnn_vocab_distill(ggnn_dtype dt, int32_t n_nodes, int32_t H, int32_
  *            gradient is added to the rows of the chosen nodes and the others stay
  *            as they are (after ggnn_vocab_loss_grad on the same nodes: both losses)
  *   dX, dW, dbias, weight   as in ggnn_vocab_loss_grad
+ * dW and dbias take exp(z_v / t - lse[r]) from the log sum rounded to a float: as in
+ * ggnn_vocab_loss_grad, rows with a gradient should keep |lse| below about 1e5,
+ * which is that of z / t, at any temperature.
  * The lists' share of dW and dbias is added in list order over the entries sorted
  * by v: same inputs, same bits. */
 ggnn_status ggnn_vocab_distill_grad(ggnn_dtype dt, int32_t n_nodes, int32_t H, int32_t n_rows, int32_t V,

@@ -68,9 +68,9 @@ struct Dropout {
 };
 
 // Exponents of logits over a temperature (csrc/vocab_tile.h): factors of ordinary and of very large logits, the size at
-// which the second begins, 1 / (temperature far), 1 / temperature, and the temperature.
+// which the second begins, 1 / (temperature far), and 1 / temperature.
 struct Temper {
-  float near, far, limit, back, inv, tau;
+  float near, far, limit, back, inv;
 };
 inline Temper make_temper(float temperature) {
   Temper te;
@@ -79,7 +79,6 @@ inline Temper make_temper(float temperature) {
   te.far = exp2f(floorf(log2f(te.near)) + 1.f);
   te.limit = 536870912.f * temperature;
   te.back = te.inv / te.far;
-  te.tau = temperature;
   return te;
 }
 

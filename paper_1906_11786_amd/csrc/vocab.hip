@@ -644,7 +644,7 @@ __global__ __launch_bounds__(kVocThreads) void vocab_distill_join_kernel(
     const float f = live ? (weight != nullptr ? weight[r] : 1.f) * scale * te.inv : 0.f;
     if (grp == 0) store_planes(xg + (size_t)r * H + h, (size_t)Rp * H, live ? x : f32x4{}, S{});
     if (lane == 0) {
-      lse_w[r] = live ? v * te.tau : INFINITY;
+      lse_w[r] = live ? log_of_logits(M, sum, te) : INFINITY;
       tgt_w[r] = -1;
       fac_w[r] = live ? f * s : 0.f;   // (s of a broken list may be anything)
     }

@@ -35,6 +35,15 @@ __device__ __forceinline__ float log_of(float m, float sum, const Temper& te) {
   return fabsf(m) >= te.far * te.limit ? te.back * m + s * kLn2 : (m + s) * kLn2;
 }
 
+// The same in units of the logits, rounded once: what probabilities exp2(near (z - it)) start from.
+// (log_of times the temperature has up to five roundings, U |lse| of a probability each;
+// and from 2^29 temperatures on, where one step of it is many temperatures, a row's
+// largest logit has to come back as it was, which M / far does.)
+__device__ __forceinline__ float log_of_logits(float m, float sum, const Temper& te) {
+  const double s = __log2f(sum);
+  return (float)(fabsf(m) >= te.far * te.limit ? (double)(m / te.far) + s / te.near : (m + s) / te.near);
+}
+
 // float32 states and rows enter the matrix cores as three bf16 each (x = x0 +
 // x1 + x2, exact), with the six products of order 2^-16 and up: 24 bits at 6
 // bf16 products, where the float32 matrix instructions take 16 times a bf16

@@ -60,3 +60,56 @@ def test_what_stands_in_masked_rows_at_the_end_does_not_matter(dt, rows, K, V, l
         for padding in (0, 1):
             for got, w in zip(top(dt, X, W2, b, node, K, rules, padding), want):
                 np.testing.assert_array_equal(got, w)
+
+
+def two_rows(dt, tau, size, rng, far):
+    """Row 0 is sure of the first half of the entries and row 1 of the second, with logits of about `size` temperatures
+    that are exact in float32 in any order of their sums.  Within a half they lie at most four temperatures apart
+    (far: one entry's is twice the others')."""
+    H, V, K = 32, 70, 4
+    W = np.zeros((V, H))
+    W[:, 0] = np.where(np.arange(V) < V // 2, 200.0, -200.0)
+    c = float(round_to("bf16", np.array([size * tau / 200]))[0])
+    X = np.zeros((2, H))
+    X[:, 0] = c, -c
+    b = None
+    if far:
+        W[:, 0] /= 2
+        W[[3, V - 3], 0] *= 2
+    else:
+        step = 2.0 ** (np.ceil(np.log2(tau)) - 6)   # a 24-bit logit of up to 2^17 tau has it as a place
+        b = np.floor(rng.random(V) * 4 * tau / step) * step
+    t_id = np.stack([rng.permutation(V)[:K] for _ in range(2)])
+    return dict(n=2, X=X, W=W, b=b, node=np.arange(2), t_id=t_id, t_logit=(tau * rng.standard_normal((2, K))).astype(
+        np.float32).astype(np.float64)), abs(c)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("tau", [0.3, 0.7, 1.0, 3.0, 7.0, 50.0])
+@pytest.mark.parametrize("far", [False, True])
+def test_gradients_of_logits_of_many_temperatures(dt, tau, far):
+    """dW and dbias from probabilities exp(z / tau - lse) whose log sum is rounded once, to float: with exact logits a
+    probability is off by half a step of it, exp(U |lse|) - 1; the exponential and its argument's factor, the pair of
+    bf16 and the teacher's probabilities by 2^-15 together.  (far: one entry has all of it, and its logit is the log
+    sum.)"""
+    rng = np.random.default_rng(int(10 * tau))
+    t32 = float(np.float32(tau))   # what the call gets: at 2^29 temperatures the rest of 0.7 would be many units of z / tau
+    for i in range(12):
+        size = 2.0 ** rng.uniform(29.2, 60) if far else 2.0 ** rng.uniform(14, 16.9)
+        c, x = two_rows(dt, tau, size, rng, far)
+        t_lse = None
+        if i % 2:   # probabilities that do not add up to 1
+            t_lse = (np.log(np.exp(c["t_logit"] / tau).sum(1)) + 0.5).astype(np.float32).astype(np.float64)
+        got = D.run(dt, c, t32, t_lse, scale=0.7)
+        want = L.distill(c["X"], c["W"], c["b"], c["node"], c["t_id"], c["t_logit"], t_lse, t32, None, 0.7, dt)
+        z = (c["X"] @ c["W"].T + (0.0 if c["b"] is None else c["b"])) / t32
+        P = np.exp(z - want["lse"][:, None])
+        t = np.exp(c["t_logit"] / t32)
+        q = t / t.sum(1)[:, None] if t_lse is None else t / np.exp(t_lse)[:, None]
+        Q = np.zeros_like(P)
+        np.add.at(Q, (np.arange(2)[:, None], c["t_id"]), q)
+        off = np.zeros(2) if far else np.expm1(R.U * np.abs(want["lse"]))
+        tol = (0.7 / tau * (q.sum(1)[:, None] * P * (off[:, None] + 2.0 ** -15) + Q * 2.0 ** -15)).sum(0)
+        R.within(host(got["dW"])[:, 0], want["dW"][:, 0], tol * x)
+        if c["b"] is not None:
+            R.within(host(got["db"]), want["db"], tol)
