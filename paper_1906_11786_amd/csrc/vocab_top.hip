@@ -22,6 +22,9 @@ namespace dev {
 
 constexpr int kTopMost = 64;   // K at most: a lane holds one of a wave's best
 constexpr int kTopBlock = 16;
+// Workgroups of a launch along x, at most: a dimension takes fewer than 2^32 threads, which 2^24 rows of
+// 256 (or 2^30 pairs, four threads each) would reach.  The rest goes to a further dimension.
+constexpr int kGridX = 1 << 21;
 
 // The first pass walks the entries in units of 128, in LDS chunks of top_chunk.
 constexpr int kTopUnit = 128;
@@ -406,7 +409,8 @@ __global__ __launch_bounds__(THREADS) void vocab_rules_kernel(int R, int V, List
   extern __shared__ uint32_t lds[];
   uint32_t *key = lds, *first = lds + table, *seen = lds + 2 * table;
   float* value = reinterpret_cast<float*>(lds + 3 * table);
-  const int r = blockIdx.x;
+  const int r = blockIdx.z * kGridX + blockIdx.x;
+  if (r >= R) return;   // whole workgroups leave
   int slo, shi, alo, ahi;
   list_range(list.seen_ptr, list.n_seen, r, slo, shi);
   list_range(list.add_ptr, list.n_add, r, alo, ahi);
@@ -1080,7 +1084,8 @@ __global__ __launch_bounds__(kVocThreads) void vocab_pairs_kernel(TopRows c, con
                                                                   const S* __restrict__ X, const S* __restrict__ W,
                                                                   float* __restrict__ z) {
   const int lane = threadIdx.x % kWave, q = lane % 16, kg = lane / 16;
-  const int i = (blockIdx.x * kVocWaves + threadIdx.x / kWave) * 16 + q, nb = (c.V + kTopBlock - 1) / kTopBlock;
+  const int group = blockIdx.y * kGridX + blockIdx.x, nb = (c.V + kTopBlock - 1) / kTopBlock;
+  const int i = (group * kVocWaves + threadIdx.x / kWave) * 16 + q;   // fewer than 2^30 + 64 kGridX
   const u32x2 pair = i < n_pairs ? pairs[i] : u32x2{(uint32_t)nb, 0u};
   const int b = (int)pair[0];
   uint64_t left = __ballot(b < nb) & 0xFFFFu;
@@ -1285,7 +1290,8 @@ hipError_t top_h(const TopArgs& a, hipStream_t st) {
     const bool longer = listed / a.R > 256;
     const int table = longer ? kTable : kTable / 4;
     const int parts = cdiv(a.V, table), most = a.R < 1024 ? 1024 / a.R : 1;
-    const dim3 grid(a.R, listed > table / 2 ? (parts < most ? parts : most) : 1);
+    const dim3 grid(a.R < kGridX ? a.R : kGridX, listed > table / 2 ? (parts < most ? parts : most) : 1,
+                    cdiv(a.R, kGridX));
     const size_t lds = (size_t)table * 16;
     if (longer)
       hipLaunchKernelGGL((vocab_rules_kernel<S, 1024>), grid, dim3(1024), lds, st, a.R, a.V, c.list, c.rm, p.words, table,
@@ -1295,6 +1301,8 @@ hipError_t top_h(const TopArgs& a, hipStream_t st) {
                          id, count, add);
     c.rm = RowMask{out, nullptr, a.R, p.words};
     c.ent_id = id; c.ent_count = count; c.ent_add = add;
+    const hipError_t err = hipGetLastError();   // (the passes take entries from what this launch wrote)
+    if (err != hipSuccess) return err;
   }
   const S *X = static_cast<const S*>(a.X), *W = static_cast<const S*>(a.W);
   const bf16s* Ws = static_cast<const bf16s*>(a.W);
@@ -1337,8 +1345,9 @@ hipError_t top_h(const TopArgs& a, hipStream_t st) {
     const void* sorted;
     const hipError_t err = launch_sort(pairs, nb, block, ws + p.sort, &sorted, st);
     if (err != hipSuccess) return err;
-    hipLaunchKernelGGL((vocab_pairs_kernel<S, H>), dim3(cdiv(pairs, 16 * kVocWaves)), dim3(kVocThreads), 0, st, c,
-                       static_cast<const u32x2*>(sorted), pairs, X, W, z);
+    const int groups = cdiv(pairs, 16 * kVocWaves);
+    hipLaunchKernelGGL((vocab_pairs_kernel<S, H>), dim3(groups < kGridX ? groups : kGridX, cdiv(groups, kGridX)),
+                       dim3(kVocThreads), 0, st, c, static_cast<const u32x2*>(sorted), pairs, X, W, z);
     hipLaunchKernelGGL((vocab_answer_kernel<S, H>), dim3(cdiv(a.R, kVocWaves)), dim3(kVocThreads), 0, st, c, block, z, X, W);
     return hipGetLastError();
   }

@@ -113,3 +113,43 @@ def test_gradients_of_logits_of_many_temperatures(dt, tau, far):
         R.within(host(got["dW"])[:, 0], want["dW"][:, 0], tol * x)
         if c["b"] is not None:
             R.within(host(got["db"]), want["db"], tol)
+
+
+@pytest.mark.parametrize("K,lists", [(1, True), (64, False)])
+def test_the_most_rows(K, lists):
+    """2^24 rows, the most there may be, of 64 nodes: lists of a few rows' own, and 2^30 pairs of rows and blocks."""
+    rows, V, H = 1 << 24, 40, 32
+    free = torch.cuda.mem_get_info()[0]
+    need = capi.ggnn_vocab_top_workspace_bytes("bf16", H, rows, V, K, 3 if lists else 0)
+    if free < need + 24 * rows * K + (4 << 30):
+        pytest.skip(f"{need >> 30} GB of workspace")
+    X, W, b, _ = exact_case(H, 64, V, seed=20, n=64)
+    z, _, _, _ = L.logits(X, W, b, np.arange(64))
+    node = torch.arange(rows, dtype=torch.int32, device="cuda") % 64
+    ru, seen_ptr, seen = None, None, None
+    listed = (0, 1 << 23, rows - 1)
+    if lists:   # each of these rows has seen its best entry
+        seen_ptr = torch.zeros((rows + 1,), dtype=torch.int32, device="cuda")
+        for r in listed:
+            seen_ptr[r + 1:] += 1
+        seen = ints([int(np.argmax(z[r % 64])) for r in listed])
+        ru = capi.token_rules(seen_ptr=seen_ptr, seen=seen, n_seen=3, presence=100.0)
+    top, logit = torch.empty((rows, K), dtype=torch.int32, device="cuda"), torch.empty((rows, K), device="cuda")
+    ws = torch.empty((need,), dtype=torch.uint8, device="cuda")
+    capi.ggnn_vocab_top("bf16", 64, H, rows, V, dev(X, "bf16"), dev(W, "bf16"), dev(b), node, ru, 1.0, K, top, logit, None, ws,
+                        need)
+    ids, zk = L.best(z, K)
+    same = torch.ones((rows,), dtype=torch.bool, device="cuda")
+    if lists:
+        for r in listed:
+            same[r] = False
+            penalised = z[r % 64:r % 64 + 1].copy()
+            penalised[0, seen[listed.index(r)].item()] -= 100.0
+            want = L.best(penalised, K)
+            np.testing.assert_array_equal(top[r].cpu().numpy(), want[0][0])
+            np.testing.assert_array_equal(host(logit[r]), want[1][0])
+    view = (lambda a: a.view(-1, 64 * K))
+    wrong = (view(top) != ints(ids).view(1, -1)) | (view(logit) != dev(zk).view(1, -1))
+    assert not bool((wrong.view(rows, K).any(1) & same).any())
+    del ws, top, logit, wrong
+    torch.cuda.empty_cache()
