@@ -235,7 +235,8 @@ class NodeTokens:
         """Forward pass without dropout and, for the chosen nodes, the k best
         tokens under the rules: dict of device tensors token [R, k] (-1: no token
         is left), logit [R, k] in descending order, and lse [R], the log sum at the
-        temperature.  It is what a student's setup_training() takes as `teacher`."""
+        temperature; and that temperature, a number on the host.  It is what a
+        student's setup_training() takes as `teacher`."""
         if not 1 <= k <= MAX_LIST:
             raise ValueError(f"k={k} must be in [1, {MAX_LIST}]")
         with self._on(stream):
@@ -246,7 +247,8 @@ class NodeTokens:
                     raise ValueError(f"rules for {rules.n_rows} rows over {rules.V} tokens, {R} over {self.V} are needed")
                 rules.record_stream(t.cuda.current_stream())
             out = {"token": t.empty((R, k), dtype=t.int32, device=m.device),
-                   "logit": t.empty((R, k), device=m.device), "lse": t.empty((R,), device=m.device)}
+                   "logit": t.empty((R, k), device=m.device), "lse": t.empty((R,), device=m.device),
+                   "temperature": t.tensor(float(temperature), dtype=t.float64)}
             self.embed()
             m.forward()
             listed = 0 if rules is None else rules.n_listed
@@ -277,13 +279,15 @@ class NodeTokens:
         return here(token.clamp(min=-1), t.int32), logit, lse, taught
 
     def setup_training(self, node, target, lr: float = 0.01, momentum: float = 0.9, weight_decay: float = 0.0,
-                       nesterov: bool = False, teacher=None, temperature: float = 2.0, soft: float = 0.5):
+                       nesterov: bool = False, teacher=None, temperature: float | None = None, soft: float = 0.5):
         """The nodes whose tokens are predicted (each once) and their targets,
         and zero velocities.  (Their own tokens should not be in their lists.)
 
         teacher: a teacher's top() of the same nodes (token, logit, and lse where
         the log sums over its whole vocabulary at this temperature are to count;
-        without, each list's probabilities add up to 1).  The loss is then
+        without, each list's probabilities add up to 1).  temperature: None is the
+        one that the teacher's dict holds, 2 where it holds none; log sums at
+        another one than this are refused.  The loss is then
         (1 - soft) times the mean cross entropy and soft * temperature^2 times the
         mean distillation loss of the nodes that have a list."""
         if len(np.unique(np.asarray(node))) != len(np.asarray(node)):
@@ -298,6 +302,12 @@ class NodeTokens:
                                dtype=t.uint8, device=m.device)
         self.teacher = None
         if teacher is not None:
+            told = None if teacher.get("temperature") is None else float(teacher["temperature"])
+            if temperature is None:
+                temperature = 2.0 if told is None else told
+            elif told is not None and teacher.get("lse") is not None and np.float32(told) != np.float32(temperature):
+                raise ValueError(f"the teacher's log sums are at temperature {told:g}, not {temperature:g}: its top() at this "
+                                 "one is needed, or its lists without lse")
             if not 0.0 <= soft <= 1.0 or not 1e-3 <= temperature <= 1e3:
                 raise ValueError(f"soft={soft} must be in [0, 1] and temperature={temperature} in [0.001, 1000]")
             token, logit, lse, taught = self._teacher(teacher)

@@ -153,3 +153,18 @@ def test_the_most_rows(K, lists):
     assert not bool((wrong.view(rows, K).any(1) & same).any())
     del ws, top, logit, wrong
     torch.cuda.empty_cache()
+
+
+def test_defaults_of_answers_and_of_training_on_them_fit():
+    """top() and setup_training() as they are: the student's temperature is that of the teacher's log sums."""
+    from test_gpu_node_tokens import setup
+    _, teacher, *_, node, target, _ = setup("bf16", 64)
+    m, student, *_ = setup("bf16", 64)
+    out = teacher.top(node, 6)
+    student.setup_training(node, target, teacher=out)
+    student.gradients(1)
+    want = L.distill(host(student.XT), host(student.table), host(student.bias), node, out["token"].cpu().numpy(),
+                     host(out["logit"]), host(out["lse"]), 1.0, None, 1.0, "bf16")
+    R.within(host(student.soft_loss), want["loss"], want["loss_tol"])
+    with pytest.raises(ValueError, match="log sums are at temperature 1, not 2"):
+        student.setup_training(node, target, teacher=out, temperature=2.0)

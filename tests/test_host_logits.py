@@ -182,3 +182,29 @@ def test_rules_of_rows_refuse(kw, text):
     from paper_1906_11786_amd.tokens import TokenRules
     with pytest.raises(ValueError, match=text):
         TokenRules(6, 3, device="cpu", **kw)
+
+
+def test_a_teachers_log_sums_at_another_temperature_are_refused():
+    """top()'s dict holds its temperature: the student takes it, or is refused one that the log sums do not fit."""
+    torch = pytest.importorskip("torch")
+    from test_host_tokens import node_tokens
+    t = node_tokens()
+    lists = dict(token=torch.tensor([[3, 4], [5, -1]]), logit=torch.tensor([[2.0, 1.0], [0.5, 0.0]]))
+    out = dict(lists, lse=torch.tensor([3.0, 4.0]), temperature=torch.tensor(1.0, dtype=torch.float64))
+    for told in (out, {k: v.numpy() for k, v in out.items()}, dict(out, temperature=1.0)):
+        t.setup_training([0, 2], [1, 2], teacher=told)
+        assert t.teacher["temperature"] == 1.0 and t.teacher["scale"] == 0.5 / 2
+        t.setup_training([0, 2], [1, 2], teacher=told, temperature=1)
+        for other in (2.0, 0.999):
+            with pytest.raises(ValueError, match="log sums are at temperature 1, not"):
+                t.setup_training([0, 2], [1, 2], teacher=told, temperature=other)
+    t.setup_training([0, 2], [1, 2], teacher=dict(out, temperature=0.3), temperature=float(np.float32(0.3)))
+    t.setup_training([0, 2], [1, 2], teacher=dict(lists, temperature=1.0), temperature=2.0)   # lists alone: any
+    assert t.teacher["temperature"] == 2.0
+    for plain in (lists, dict(lists, lse=out["lse"])):   # nothing told: what is asked for, or 2
+        t.setup_training([0, 2], [1, 2], teacher=plain, temperature=3.0)
+        assert t.teacher["temperature"] == 3.0
+        t.setup_training([0, 2], [1, 2], teacher=plain)
+        assert t.teacher["temperature"] == 2.0 and t.teacher["scale"] == 0.5 * 4 / 2
+    with pytest.raises(ValueError, match="temperature"):
+        t.setup_training([0, 2], [1, 2], teacher=dict(lists, temperature=0.0))
