@@ -260,9 +260,9 @@ class NodeTokens:
 
     # ------------------------------------------------------------ training
 
-    def _teacher(self, teacher):
-        """A teacher's lists for the chosen nodes on the device: (token, logit, lse or None, rows with a token)."""
-        t, R = self.torch, self.n_rows
+    def _teacher(self, teacher, R: int):
+        """A teacher's lists for R chosen nodes on the device: (token, logit, lse or None, rows with a token)."""
+        t = self.torch
         here = (lambda x, dt: t.as_tensor(x).to(device=self.model.device, dtype=dt).contiguous())
         token, logit = t.as_tensor(teacher["token"]), here(teacher["logit"], t.float32)
         if token.ndim != 2 or token.shape[0] != R or not 1 <= token.shape[1] <= MAX_LIST or logit.shape != token.shape:
@@ -292,15 +292,9 @@ class NodeTokens:
         mean distillation loss of the nodes that have a list."""
         if len(np.unique(np.asarray(node))) != len(np.asarray(node)):
             raise ValueError("a node appears more than once among the chosen nodes")
-        self.node, self.target = self._rows(node, target)
-        m, t = self.model, self.torch
-        self.n_rows = len(self.node)
-        self.n_live = int((self.target >= 0).sum())
-        self.loss = t.empty((self.n_rows,), device=m.device)
-        self.lse = t.empty_like(self.loss)
-        self.loss_ws = t.empty((max(capi.ggnn_vocab_workspace_bytes(m.dt, m.H, self.n_rows, self.V, True), 16),),
-                               dtype=t.uint8, device=m.device)
-        self.teacher = None
+        node, target = self._rows(node, target)
+        m, t, R, soft_part = self.model, self.torch, len(node), None
+        n_live = int((target >= 0).sum())
         if teacher is not None:
             told = None if teacher.get("temperature") is None else float(teacher["temperature"])
             if temperature is None:
@@ -310,12 +304,19 @@ class NodeTokens:
                                  "one is needed, or its lists without lse")
             if not 0.0 <= soft <= 1.0 or not 1e-3 <= temperature <= 1e3:
                 raise ValueError(f"soft={soft} must be in [0, 1] and temperature={temperature} in [0.001, 1000]")
-            token, logit, lse, taught = self._teacher(teacher)
-            K = token.shape[1]
-            self.teacher = dict(K=K, token=token, logit=logit, lse=lse, temperature=temperature, soft=soft,
-                                scale=soft * temperature ** 2 / max(taught, 1))
+            token, logit, lse, taught = self._teacher(teacher, R)
+            soft_part = dict(K=token.shape[1], token=token, logit=logit, lse=lse, temperature=temperature, soft=soft,
+                             scale=soft * temperature ** 2 / max(taught, 1))
+        # (from here on nothing is refused: a refused call leaves the set-up before it as it was)
+        self.node, self.target, self.n_rows, self.teacher = node, target, R, soft_part
+        self.n_live = n_live
+        self.loss = t.empty((R,), device=m.device)
+        self.lse = t.empty_like(self.loss)
+        self.loss_ws = t.empty((max(capi.ggnn_vocab_workspace_bytes(m.dt, m.H, R, self.V, True), 16),),
+                               dtype=t.uint8, device=m.device)
+        if soft_part is not None:
             self.soft_loss, self.soft_lse = t.empty_like(self.loss), t.empty_like(self.loss)
-            need = capi.ggnn_vocab_distill_workspace_bytes(m.dt, m.H, self.n_rows, self.V, K, True)
+            need = capi.ggnn_vocab_distill_workspace_bytes(m.dt, m.H, R, self.V, soft_part["K"], True)
             self.soft_ws = t.empty((max(need, 16),), dtype=t.uint8, device=m.device)
         self.opt = dict(lr=lr, momentum=momentum, weight_decay=weight_decay, nesterov=nesterov)
         self.velocity, self.model_velocity = t.zeros_like(self.master), t.zeros_like(m.master)

@@ -208,3 +208,19 @@ def test_a_teachers_log_sums_at_another_temperature_are_refused():
         assert t.teacher["temperature"] == 2.0 and t.teacher["scale"] == 0.5 * 4 / 2
     with pytest.raises(ValueError, match="temperature"):
         t.setup_training([0, 2], [1, 2], teacher=dict(lists, temperature=0.0))
+
+
+@pytest.mark.parametrize("kw", [
+    dict(teacher=dict(token=np.full((3, 2), 20), logit=np.zeros((3, 2)))), dict(teacher=dict(token=np.zeros((2, 2), int),
+    logit=np.zeros((2, 2)))), dict(teacher=dict(token=np.zeros((3, 2), int), logit=np.zeros((3, 2)), lse=np.zeros(2))),
+    dict(teacher=dict(token=np.zeros((3, 2), int), logit=np.zeros((3, 2))), soft=2.0), dict(target=[1, 2, 20])])
+def test_a_refused_set_up_leaves_the_one_before_it(kw):
+    from test_host_tokens import node_tokens
+    t = node_tokens()
+    teacher = dict(token=np.array([[3, 4], [5, -1]]), logit=np.zeros((2, 2)))
+    t.setup_training([0, 2], [1, -1], teacher=teacher, lr=0.5)
+    t.step = 7
+    before = dict(vars(t))
+    with pytest.raises(ValueError):
+        t.setup_training(**dict(dict(node=[1, 2, 3], target=[1, 2, 3]), **kw))
+    assert vars(t).keys() == before.keys() and all(vars(t)[k] is before[k] for k in before)
