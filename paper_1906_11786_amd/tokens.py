@@ -245,6 +245,9 @@ class NodeTokens:
             if rules is not None:
                 if rules.n_rows != R or rules.V != self.V:
                     raise ValueError(f"rules for {rules.n_rows} rows over {rules.V} tokens, {R} over {self.V} are needed")
+                at = m.X[m.T].device
+                if any(x.device != at for x in rules.tensors):   # the kernels follow the addresses as they are
+                    raise ValueError(f"rules on {rules.tensors[0].device}, the model is on {at}")
                 rules.record_stream(t.cuda.current_stream())
             out = {"token": t.empty((R, k), dtype=t.int32, device=m.device),
                    "logit": t.empty((R, k), device=m.device), "lse": t.empty((R,), device=m.device),

@@ -224,3 +224,12 @@ def test_a_refused_set_up_leaves_the_one_before_it(kw):
     with pytest.raises(ValueError):
         t.setup_training(**dict(dict(node=[1, 2, 3], target=[1, 2, 3]), **kw))
     assert vars(t).keys() == before.keys() and all(vars(t)[k] is before[k] for k in before)
+
+
+def test_rules_on_another_device_are_refused():
+    from paper_1906_11786_amd.tokens import TokenRules
+    from test_host_tokens import node_tokens
+    t = node_tokens()
+    for kw in (dict(seen=[[1], [2]]), dict(bias=[{1: 2.0}, {}]), dict(allowed=np.ones((2, 20), bool))):
+        with pytest.raises(ValueError, match="rules on meta, the model is on cpu"):
+            t.top([0, 2], 3, TokenRules(20, 2, device="meta", **kw))
