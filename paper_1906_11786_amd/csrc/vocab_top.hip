@@ -52,10 +52,9 @@ constexpr int top_waves(int H) {
   return sizeof(S) == 4 ? (H >= 256 ? 1 : 2) : H >= 256 ? 2 : 4;
 }
 
-// A 32 x 32 tile of logits has entries as its rows.  Entry r of a tile is put on row
-// top_row(r), so that a lane (lanes 32 g .. 32 g + 31) holds entries 16 g .. 16 g + 15, one
-// block, in order.
-__device__ __forceinline__ int top_row(int r) { return 8 * ((r >> 2) & 3) + 4 * (r >> 4) + (r & 3); }
+// A 32 x 32 tile of logits has entries as its rows.  Row i holds entry top_entry(i) of its
+// 32, so that a lane (lanes 32 g .. 32 g + 31) holds entries 16 g .. 16 g + 15, one block, in
+// order.
 __device__ __forceinline__ int top_entry(int i) { return 16 * ((i >> 2) & 1) + 4 * (i >> 3) + (i & 3); }
 
 // dma16 (csrc/lds_dma.h) from a wave-uniform address and each lane's offset in bytes.
