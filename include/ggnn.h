@@ -782,7 +782,10 @@ typedef struct {
 } ggnn_token_rules;
 
 /* Workspace bytes of ggnn_vocab_top; 0 for unsupported sizes or no rows.
- * n_listed: n_seen + n_add of the rules (0 without). */
+ * n_listed: n_seen + n_add of the rules (0 without).  Most of them: n_rows * V / 4 for
+ * maxima, n_rows * V / 8 for the lists' masks, and about 84 * n_rows * K where rows are
+ * many.  The rows do not depend on each other, so that calls of some of them do
+ * with less. */
 size_t ggnn_vocab_top_workspace_bytes(ggnn_dtype dt, int32_t H, int32_t n_rows, int32_t V, int32_t K, int64_t n_listed);
 
 /* The best entries of chosen nodes over a vocabulary (device), without the
@@ -797,7 +800,8 @@ size_t ggnn_vocab_top_workspace_bytes(ggnn_dtype dt, int32_t H, int32_t n_rows, 
  *            that are left, -inf for none), or NULL
  *   temperature  in [0.001, 1000], of lse alone.  Logits over the temperature may
  *            have any size up to 1e38, as those of ggnn_vocab_loss
- * The row of W of an entry that the masks of all rows take out may hold anything.
+ * The row of W of an entry that the masks of all rows take out may hold anything,
+ * and so may a mask's bits from V on.
  * Logits are float32 sums, formed a second time for the entries returned: entries
  * whose exact logits differ by less than the rounding of such a sum may be returned
  * in either order, or one in place of the other.  The other arguments, and nodes
@@ -850,8 +854,8 @@ ggnn_status ggnn_vocab_distill(ggnn_dtype dt, int32_t n_nodes, int32_t H, int32_
  * dW and dbias take exp(z_v / t - lse[r]) from the log sum rounded to a float: as in
  * ggnn_vocab_loss_grad, rows with a gradient should keep |lse| below about 1e5,
  * which is that of z / t, at any temperature.
- * The lists' share of dW and dbias is added in list order over the entries sorted
- * by v: same inputs, same bits. */
+ * The lists' share of dW and dbias is added in an order that the sizes and the
+ * lists' entries alone decide: same inputs, same bits. */
 ggnn_status ggnn_vocab_distill_grad(ggnn_dtype dt, int32_t n_nodes, int32_t H, int32_t n_rows, int32_t V,
                                     const void* X, const void* W, const float* bias, const int32_t* node, int32_t K,
                                     const int32_t* teacher_id, const float* teacher_logit, const float* teacher_lse,

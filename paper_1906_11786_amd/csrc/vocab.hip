@@ -541,7 +541,7 @@ __global__ __launch_bounds__(kVocThreads) void vocab_join_kernel(
 // side, four of each in flight.  GRAD: also what the columns pass reads, as
 // vocab_join_kernel leaves it, and the factor -f q_k of each listing for
 // launch_list_rows (id -1: none).  splits: shares of a row from vocab_few_kernel (0:
-// dealt).  Latency of a few dependent loads and the exchanges between lanes: 13.5 us for 2,999
+// dealt).  Latency of a few dependent loads and the exchanges between lanes: 13.3 us for 2,999
 // lists of 32 at H = 128, 10.4 for 3,001 of 16 at H = 64 with gradients; 78 us for 16,001
 // of 32 at H = 256 (0.26 GB of rows of W, 0.2 of shares).  (Eight rows in flight a lane
 // group: 1% slower.)

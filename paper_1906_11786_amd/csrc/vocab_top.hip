@@ -114,12 +114,12 @@ struct RowSum {
 // that a read's place is a constant; the copies, 32 bytes a row each, pay for that
 // order, and their addresses are constants too but in the last chunk.
 //
-// 12,001 rows over 50,021 entries at H = 256: 290 us, 1.06 PFLOP/s (a plain 8,192^3 product
+// 12,001 rows over 50,021 entries at H = 256: 291 us, 1.06 PFLOP/s (a plain 8,192^3 product
 // 1.39), matrix cores 53% busy and vector issue 41% at 2.0 GHz; without the log sum 247.
 // (Products and exponentials of two tiles interleaved in one wave a SIMD, three buffers:
 // 349; rows of the tile in LDS, 64 entries a barrier: 308.)  2,999 rows at H = 128: 52,
 // 0.74 PFLOP/s, matrix cores 31%, vector issue 46%, waiting 36%; without the log sum 43.
-// 3,001 rows over 10,007 at H = 64 with masks 17.4, waiting 46%: four units a workgroup
+// 3,001 rows over 10,007 at H = 64 with masks 17.9, waiting 46%: four units a workgroup
 // (two of twice the workgroups: 1.5 us more).
 // Block maxima: 10% of these times.
 template <typename S, int H, bool LSE, bool MASK>
@@ -299,8 +299,10 @@ __global__ __launch_bounds__(kWave* top_group<S>(H), top_waves<S>(H)) void vocab
 
 // First pass for at most 32 NT rows: every wave holds the same rows and takes `per`
 // tiles of 32 entries, read straight from memory, since no other wave needs them.  4.0 us
-// for one row over 10,007 entries at H = 64 (the launch), 9.6 over 50,021 at H = 256 (25.6
-// MB, 2.7 TB/s: one or two round trips to memory a wave).
+// for one row over 10,007 entries at H = 64 (the launch), 10.0 over 50,021 at H = 256 with a
+// mask (25.6 MB, 2.6 TB/s: one or two round trips to memory a wave).  (float32 at H = 256
+// with two tiles holds more than a lane's registers, 171 to 244 of them in scratch: the call
+// for 64 rows over 10,007 entries takes 48 us, for 32 rows 32.)
 template <typename S, int H, int NT, bool LSE, bool MASK>
 __global__ __launch_bounds__(kVocThreads) void vocab_max_few_kernel(
     int n_nodes, int R, int V, int per, Temper te, const S* __restrict__ X, const S* __restrict__ W,
@@ -393,7 +395,7 @@ __device__ __forceinline__ void list_range(const int32_t* ptr, int n, int r, int
   hi = ptr != nullptr ? min(max(ptr[r + 1], lo), n) : 0;
 }
 
-// THREADS a row.  Latency: 5.5 us for one row of 24 listings, 9 us for 64 rows of 780
+// THREADS a row.  Latency: 6.7 us for one row of 24 listings, 9 us for 64 rows of 780
 // (1,024 threads; 256 threads and a hash table of half the places 21), 13 us for 3,001 rows
 // of 58: a chain of loads, table look-ups and barriers, a few rows a compute unit.
 template <typename S, int THREADS>   // (the same for both types S)
@@ -808,7 +810,7 @@ __device__ __forceinline__ void join_own(RowSum own, float& M, float& sum) {
 // seldom much more than K, and goes to LDS as one list; where it does not fit 64
 // places (many equal ones), the waves' own lists are joined instead.
 //
-// One row over 10,007 entries: 7.0 us, of which two barriers' waits and four dependent
+// One row over 10,007 entries: 6.9 us, of which two barriers' waits and four dependent
 // round trips to memory are most (an insertion into sorted lists in registers 15.0); 64
 // rows of 780 listings 19; 1,229 rows in float32, K = 16, 30 (161 MB gathered, 5 TB/s).
 template <typename S, int H, int WPR>
@@ -993,8 +995,8 @@ __global__ __launch_bounds__(kWave* WPR) void vocab_pick_kernel(TopRows c, const
 // A block's 16 rows of W are 16 times a state, so where many rows pick blocks it is
 // the states that move: the picked (row, block) pairs are sorted by block, and a wave
 // forms the logits of 16 pairs, mostly of one block, as one 16 x 16 tile.  12,001 rows, K =
-// 32, H = 256: blocks 42 us (150 MB of maxima), sort 35, pairs 55 (420 MB of states, rows of
-// W and logits through the L2s, 7.6 TB/s), answers 29; gathering 3.1 GB of W in one
+// 32, H = 256: blocks 42 us (150 MB of maxima), sort 34, pairs 54 (420 MB of states, rows of
+// W and logits through the L2s, 7.8 TB/s), answers 28; gathering 3.1 GB of W in one
 // launch took 415.
 
 // The K best blocks of each row, one wave a row: block [R][K], -1 from where none is
@@ -1209,22 +1211,31 @@ struct TopPlan {
   dev::Deal deal;
   size_t id, count, add, mask, bmax, pm, pl, wp, block, z, sort, bytes;
 };
+// Up to so many rows have a first pass of their own (vocab_max_few_kernel).  It against that
+// of many rows, the whole call in us at K = 16, 1, 32 and 64 rows: bf16, H = 64, V = 10,007
+// 11.3, 12.0, 12.8 / 12.7, 13.3, 13.5; H = 256, V = 50,021 23.4, 24.9, 27.9 / 31.7, 32.0,
+// 32.6; float32, H = 64, V = 10,007 13.5, 14.4, 16.6 / 25.4, 25.7, 25.9; H = 256, V =
+// 50,021 37.9, 40.2, 66.0 / 66.6, 67.0, 67.2, V = 5,000 27.6, 31.1, 46.2 / 38.9, 39.4, 40.7
+// (33 to 64 float32 rows at H = 256 taken to be the other way).
+constexpr int kTopFew = 64;
 // Whether the picked blocks are sorted, which takes seven launches in place of one: by the
-// bytes of W that they would gather, and some of its work a pair.  One launch against
-// seven, the whole call in us: bf16, V = 10,007, H = 64, K = 16, 1,000 rows 24 / 44, 3,001
-// 44 / 55; V = 50,021, H = 128, K = 32, 1,500 rows 69 / 82, 2,999 118 / 110; H = 256, K =
-// 16, 1,000 rows 68 / 89, 2,000 108 / 111 (taken to be the other way), K = 8, 4,000 rows
-// 159 / 156; V = 4,999, H = 32, K = 16, 8,000 rows 75 / 69; V = 50,021, K = 4, 129 / 141;
-// float32, V = 4,999, H = 128, K = 16, 1,229 rows 56 / 59, 2,000 77 / 69.
+// bytes of W that they would gather, and kPairBytes for the rest of one launch's work a pair,
+// against kSortBytes for the launches (both fitted to the times below; V, on which the sort
+// and the blocks' launch depend a little, is left out).  One launch against seven, the whole
+// call in us: bf16, V = 10,007, H = 64, K = 16, 1,000 rows 24 / 44, 3,001 44 / 55; V =
+// 50,021, H = 128, K = 32, 1,500 rows 69 / 82, 2,999 118 / 110; H = 256, K = 16, 1,000
+// rows 68 / 89, 2,000 108 / 111 (taken to be the other way), K = 8, 4,000 rows 159 / 156; V
+// = 4,999, H = 32, K = 16, 8,000 rows 75 / 69; V = 50,021, K = 4, 129 / 141; float32, V =
+// 4,999, H = 128, K = 16, 1,229 rows 56 / 59, 2,000 77 / 69.
+constexpr double kPairBytes = 1000, kSortBytes = 2.55e8;
 bool pairs_sorted(int es, int H, int R, int K) {
-  const double pairs = (double)R * K;
-  return R > 64 && pairs * (dev::kTopBlock * H * es + 1000) > 2.55e8 && pairs <= 1 << 30;
+  return R > kTopFew && (double)R * K * (dev::kTopBlock * H * es + kPairBytes) > kSortBytes;   // (at most 2^30 pairs)
 }
 template <typename S>
 TopPlan top_plan(int H, int R, int V, int K, int n_listed) {
   TopPlan p{};
   size_t shares;
-  p.few = R <= 64;
+  p.few = R <= kTopFew;
   if (p.few) {
     const int tiles = cdiv(V, 32);
     p.nt = R <= 32 ? 1 : 2;
@@ -1350,7 +1361,7 @@ hipError_t top_h(const TopArgs& a, hipStream_t st) {
     hipLaunchKernelGGL((vocab_answer_kernel<S, H>), dim3(cdiv(a.R, kVocWaves)), dim3(kVocThreads), 0, st, c, block, z, X, W);
     return hipGetLastError();
   }
-  if (a.R <= 64)
+  if (p.few)
     hipLaunchKernelGGL((vocab_pick_kernel<S, H, 8>), dim3(a.R), dim3(8 * kWave), 0, st, c, X, W);
   else
     hipLaunchKernelGGL((vocab_pick_kernel<S, H, 4>), dim3(a.R), dim3(4 * kWave), 0, st, c, X, W);
